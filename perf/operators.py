@@ -1,0 +1,347 @@
+"""Performance cases of the operators that run, train and judge a block of refined layers.
+
+Each case is a dict of plain values; "op" names the operator:
+
+  ffn      the gated feed-forward block y = act(x Wg^T) * (x Wu^T) in 16 bits; with
+           "train" its backward pass too (gradients of the tokens and of both weights);
+  i8       a linear layer in 8-bit integers: tokens quantized with a scale each, times
+           int8 weights with a scale for each channel, or for each group of a channel
+           (the codes minus zero points of a refined layer);
+  logprob  log probabilities of given tokens, with the entropy and the top
+           alternatives of each position; with "train" the gradient of the logits.
+
+`own` false computes a case in plain torch operations in 32 bits, rounded once at the
+end; true calls the library.  Every input comes from the seed.
+"""
+
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+_DTYPES = {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}
+
+
+def listed():
+    return [
+        # one token through the MLP of a 4096-wide block: the weights are read once
+        {"name": "ffn_token", "op": "ffn", "tokens": 1, "d": 4096, "f": 11008,
+         "dtype": "bfloat16", "act": "silu", "train": False},
+        # a small ragged batch of sequences, one token each
+        {"name": "ffn_batch", "op": "ffn", "tokens": 53, "d": 4096, "f": 14336,
+         "dtype": "float16", "act": "silu", "train": False},
+        # calibration or prefill: two sequences of 2048 through the widest block
+        {"name": "ffn_prefill", "op": "ffn", "tokens": 4096, "d": 4096, "f": 14336,
+         "dtype": "bfloat16", "act": "silu", "train": False},
+        # a training step of the block, forward and backward
+        {"name": "ffn_train", "op": "ffn", "tokens": 4096, "d": 4096, "f": 11008,
+         "dtype": "bfloat16", "act": "silu", "train": True},
+        # a small block with odd sizes, a short batch
+        {"name": "ffn_train_odd", "op": "ffn", "tokens": 611, "d": 1000, "f": 2752,
+         "dtype": "float16", "act": "gelu_tanh", "train": True},
+        # one token through an attention projection, a scale per channel
+        {"name": "i8_token", "op": "i8", "tokens": 1, "n": 4096, "k": 4096, "group": 0,
+         "dtype": "bfloat16"},
+        # a ragged batch of single tokens through an up projection from its codes
+        {"name": "i8_batch", "op": "i8", "tokens": 37, "n": 11008, "k": 4096, "group": 128,
+         "dtype": "bfloat16"},
+        # prefill through a down projection, a scale per channel
+        {"name": "i8_prefill", "op": "i8", "tokens": 8192, "n": 4096, "k": 14336, "group": 0,
+         "dtype": "bfloat16"},
+        # evaluation of a refined layer from its codes: group scales
+        {"name": "i8_codes", "op": "i8", "tokens": 2048, "n": 4096, "k": 11008, "group": 64,
+         "dtype": "float16"},
+        # the next token's alternatives in a serving step, one sequence
+        {"name": "logprob_token", "op": "logprob", "tokens": 1, "vocab": 128000, "top": 8,
+         "dtype": "bfloat16", "masked": False, "train": False},
+        # perplexity of an evaluation sequence: fp32 logits, banned and padded entries
+        {"name": "logprob_eval", "op": "logprob", "tokens": 2047, "vocab": 32001, "top": 20,
+         "dtype": "float32", "masked": True, "train": False},
+        # a training step's loss over two sequences with its gradient
+        {"name": "logprob_train", "op": "logprob", "tokens": 4096, "vocab": 128000, "top": 0,
+         "dtype": "bfloat16", "masked": False, "train": True},
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(max(lo, hi))))))
+
+
+def draw(rng):
+    op = rng.choice(["ffn", "i8", "logprob"])
+    if op == "ffn":
+        d, f = 8 * _log(rng, 16, 512), 8 * _log(rng, 16, 1792)
+        train = rng.random() < 0.5
+        most = 4096 * 4096 * 14336 // (d * f * (3 if train else 1))
+        return {"op": op, "tokens": _log(rng, 1, min(4096, most)), "d": d, "f": f,
+                "dtype": rng.choice(["bfloat16", "bfloat16", "float16"]),
+                "act": rng.choice(["silu", "silu", "gelu", "gelu_tanh"]), "train": train}
+    if op == "i8":
+        group = rng.choice([0, 0, 32, 64, 128])
+        unit = group or 32
+        k = unit * _log(rng, max(1, 128 // unit), 14336 // unit)
+        return {"op": op, "tokens": _log(rng, 1, 8192), "n": _log(rng, 16, 8192), "k": k,
+                "group": group, "dtype": rng.choice(["bfloat16", "float16", "float32"])}
+    train = rng.random() < 0.4
+    vocab = _log(rng, 1000, 128000)
+    return {"op": op, "tokens": _log(rng, 1, 4096), "vocab": vocab,
+            "top": 0 if train else rng.choice([0, 1, 5, 20]),
+            "dtype": rng.choice(["bfloat16", "float16", "float32"]) if vocab < 64000
+            else rng.choice(["bfloat16", "float16"]),
+            "masked": rng.random() < 0.5, "train": train}
+
+
+# ---- inputs ----
+
+def _gen(seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(int(seed))
+    return gen
+
+
+def _randn(gen, *shape):
+    return torch.randn(*shape, generator=gen, device="cuda", dtype=torch.float32)
+
+
+def _tokens(gen, m, cols):
+    """m hidden states: one channel in a hundred is an outlier, ten times the others."""
+    x = _randn(gen, m, cols)
+    return x * torch.where(torch.rand(cols, generator=gen, device="cuda") < 0.01, 10.0, 1.0)
+
+
+def prepare(case, seed):
+    gen = _gen(seed)
+    s = {"case": dict(case)}
+    dt = _DTYPES[case["dtype"]]
+    t = case["tokens"]
+    if case["op"] == "ffn":
+        d, f = case["d"], case["f"]
+        # pre-activations of standard deviation 1 or so, as after a norm
+        s["x"] = _tokens(gen, t, d).to(dt)
+        std = 0.3 / math.sqrt(d)
+        s["wg"], s["wu"] = (_randn(gen, f, d).mul_(std).to(dt) for _ in range(2))
+        if case["train"]:
+            s["dy"] = _randn(gen, t, f).mul_(0.05).to(dt)
+    elif case["op"] == "i8":
+        n, k, group = case["n"], case["k"], case["group"]
+        s["x"] = _tokens(gen, t, k).to(dt)
+        if group:   # 4-bit codes minus zero points, signed group scales
+            codes = torch.randint(0, 16, (n, k), generator=gen, device="cuda", dtype=torch.int16)
+            zeros = torch.randint(5, 11, (n, k // group), generator=gen, device="cuda",
+                                  dtype=torch.int16)
+            s["wq"] = (codes.view(n, k // group, group) - zeros[:, :, None]).view(n, k).to(torch.int8)
+            s["sw"] = _randn(gen, n, k // group).mul_(0.001).add_(0.005)
+        else:       # a channel's weights on 8 bits
+            s["wq"] = _randn(gen, n, k).mul_(30.0).round_().clamp_(-127, 127).to(torch.int8)
+            s["sw"] = torch.rand(n, 1, generator=gen, device="cuda").mul_(0.001).add_(0.0005)
+    else:
+        v = case["vocab"]
+        x = torch.randn(t, v, generator=gen, device="cuda",
+                        dtype=torch.float32 if dt == torch.float32 else torch.bfloat16)
+        x = x.mul_(2.5)
+        s["targets"] = torch.randint(0, v, (t,), generator=gen, device="cuda")
+        # half of the positions are predicted well: their token leads
+        lead = torch.rand(t, generator=gen, device="cuda").mul_(24.0).sub_(12.0).clamp_min_(0.0)
+        x[torch.arange(t, device="cuda"), s["targets"]] += lead.to(x.dtype)
+        if case["masked"]:   # banned entries, padding positions
+            x[:, torch.rand(v, generator=gen, device="cuda") < 0.2] = -math.inf
+            pad = torch.rand(t, generator=gen, device="cuda") < 0.1
+            s["targets"] = torch.where(pad, -1, s["targets"])
+        s["logits"] = x.to(dt)
+        if case["train"]:
+            s["d_logprob"] = torch.rand(t, generator=gen, device="cuda").add_(0.5).neg_()
+            s["d_entropy"] = _randn(gen, t).mul_(0.1)
+    return s
+
+
+# ---- one pass ----
+
+def run(state):
+    return _PATHS[state["case"]["op"]][1 if own else 0](state)
+
+
+def _act(a, act):
+    """The activation and its derivative."""
+    if act == "silu":
+        sig = 1.0 / (1.0 + torch.exp(-a))
+        return a * sig, sig * (1.0 + a * (1.0 - sig))
+    if act == "gelu":
+        cdf = 0.5 * (1.0 + torch.erf(a * math.sqrt(0.5)))
+        return a * cdf, cdf + a * torch.exp(-0.5 * a * a) * (1.0 / math.sqrt(2.0 * math.pi))
+    c = math.sqrt(2.0 / math.pi)
+    th = torch.tanh(c * (a + 0.044715 * a * a * a))
+    return (0.5 * a * (1.0 + th),
+            0.5 * (1.0 + th) + 0.5 * a * (1.0 - th * th) * c * (1.0 + 3.0 * 0.044715 * a * a))
+
+
+def _ffn_plain(s):
+    c = s["case"]
+    x, wg, wu = s["x"].float(), s["wg"].float(), s["wu"].float()
+    a, b = x @ wg.t(), x @ wu.t()
+    h, dh = _act(a, c["act"])
+    y = (h * b).to(s["x"].dtype)
+    if not c["train"]:
+        return {"y": y}
+    dy = s["dy"].float()
+    da, db = dy * b * dh, dy * h
+    return {"y": y, "dx": (da @ wg + db @ wu).to(y.dtype), "dwg": (da.t() @ x).to(y.dtype),
+            "dwu": (db.t() @ x).to(y.dtype)}
+
+
+def _ffn_own(s):
+    from paper_2609_38599_amd import binding as jb
+    c = s["case"]
+    if not c["train"]:
+        return {"y": jb.gated_forward(s["x"], s["wg"], s["wu"], act=c["act"])}
+    y, pre = jb.gated_forward(s["x"], s["wg"], s["wu"], act=c["act"], save=True)
+    dx, dwg, dwu = jb.gated_backward(s["x"], s["wg"], s["wu"], s["dy"], pre, act=c["act"])
+    return {"y": y, "dx": dx, "dwg": dwg, "dwu": dwu}
+
+
+def _i8_plain(s):
+    x, wq, sw = s["x"].float(), s["wq"], s["sw"]
+    amax = x.abs().amax(1, keepdim=True)
+    live = amax >= 2.0 ** -100
+    xq = torch.where(live, torch.round(x * (127.0 / torch.where(live, amax, 1.0))), 0.0)
+    sx = torch.where(live, amax / 127.0, 0.0)
+    n, k = wq.shape
+    w = (wq.view(n, sw.shape[1], -1).float() * sw[:, :, None]).view(n, k)
+    return {"y": ((xq @ w.t()) * sx).to(s["x"].dtype)}
+
+
+def _i8_own(s):
+    from paper_2609_38599_amd import binding as jb
+    return {"y": jb.linear_i8(s["x"], s["wq"], s["sw"])}
+
+
+def _logprob_plain(s):
+    c, t = s["case"], s["targets"]
+    x = s["logits"].float()
+    m = x.amax(1, keepdim=True).clamp_min(torch.finfo(torch.float32).min)
+    shifted = x - m
+    e = torch.exp(shifted)
+    z = e.sum(1, keepdim=True)
+    lse = (m + torch.log(z))[:, 0]
+    p = e / z
+    entropy = torch.log(z)[:, 0] - (p * shifted.clamp_min(-1000.0)).sum(1)
+    has = t >= 0
+    at = t.clamp_min(0)[:, None]
+    logprob = torch.where(has, x.gather(1, at)[:, 0] - lse, 0.0)
+    out = {"logprob": logprob, "entropy": entropy}
+    if c["top"]:
+        # a key that orders by value, then by the lowest index
+        bits = (x + 0.0).view(torch.int32)
+        order = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).long()
+        key = order * (1 << 32) + torch.arange(x.shape[1] - 1, -1, -1, device=x.device)
+        index = torch.topk(key, c["top"], dim=1).indices
+        out["top_index"] = index.int()
+        out["top_logprob"] = x.gather(1, index) - lse[:, None]
+    if c["train"]:
+        g = torch.where(has, s["d_logprob"], 0.0)[:, None]
+        logp = (x - lse[:, None]).clamp_min(-1000.0)
+        d = -p * (g + s["d_entropy"][:, None] * (logp + entropy[:, None]))
+        out["d_logits"] = d.scatter_add_(1, at, g).to(s["logits"].dtype)
+    return out
+
+
+def _logprob_own(s):
+    from paper_2609_38599_amd import binding as jb
+    c = s["case"]
+    r = jb.token_logprobs(s["logits"], s["targets"], top=c["top"])
+    out = {"logprob": r.logprob, "entropy": r.entropy}
+    if c["top"]:
+        out["top_index"], out["top_logprob"] = r.top_index, r.top_logprob
+    if c["train"]:
+        out["d_logits"] = jb.token_logprobs_backward(s["logits"], s["targets"], r,
+                                                     s["d_logprob"], s["d_entropy"])
+    return out
+
+
+_PATHS = {"ffn": (_ffn_plain, _ffn_own), "i8": (_i8_plain, _i8_own),
+          "logprob": (_logprob_plain, _logprob_own)}
+
+
+# ---- what a pass cannot do without ----
+
+def work(case):
+    e = torch.finfo(_DTYPES[case["dtype"]]).bits // 8
+    t = case["tokens"]
+    if case["op"] == "ffn":
+        d, f = case["d"], case["f"]
+        fwd = t * d + 2 * f * d + t * f
+        if not case["train"]:
+            return {"bytes": e * fwd, "flops": 4 * t * d * f}
+        return {"bytes": e * (fwd + t * f + t * d + 2 * f * d), "flops": 12 * t * d * f}
+    if case["op"] == "i8":
+        n, k = case["n"], case["k"]
+        groups = k // case["group"] if case["group"] else 1
+        return {"bytes": e * t * k + n * k + 4 * n * groups + e * t * n, "flops": 2 * t * n * k}
+    v = case["vocab"]
+    return {"bytes": t * v * e * (2 if case["train"] else 1) + t * (16 + 8 * case["top"]),
+            "flops": t * v * (10 if case["train"] else 6)}
+
+
+# ---- the definitions in 64 bits ----
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"ffn": _ffn_exact, "i8": _i8_exact, "logprob": _logprob_exact}[case["op"]](case, s)
+
+
+def _ffn_exact(case, s):
+    act = {"silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu,
+           "gelu_tanh": lambda a: torch.nn.functional.gelu(a, approximate="tanh")}[case["act"]]
+    leaves = [s[n].double().requires_grad_(case["train"]) for n in ("x", "wg", "wu")]
+    x, wg, wu = leaves
+    y = act(torch.mm(x, wg.t())) * torch.mm(x, wu.t())
+    if not case["train"]:
+        return {"y": y}
+    grads = torch.autograd.grad(y, leaves, s["dy"].double())
+    return {"y": y.detach(), "dx": grads[0], "dwg": grads[1], "dwu": grads[2]}
+
+
+def _i8_exact(case, s):
+    # the integers of a token are fixed by their definition in 32 bits
+    x = s["x"].double()
+    amax = x.abs().max(dim=1).values
+    inv = (127.0 / amax).float().double()
+    xq = (x * inv[:, None]).float().round().double()
+    n, k = case["n"], case["k"]
+    step = case["group"] or k
+    y = torch.zeros(case["tokens"], n, dtype=torch.float64, device=x.device)
+    for g in range(0, k, step):
+        y += torch.mm(xq[:, g:g + step], s["wq"][:, g:g + step].double().t()) \
+            * s["sw"][:, g // step].double()[None, :]
+    return {"y": y * (amax / 127.0)[:, None]}
+
+
+def _logprob_exact(case, s):
+    rows = max(1, (1 << 26) // case["vocab"])
+    parts = [_logprob_exact_rows(case, {k: v[i:i + rows] for k, v in s.items() if k != "case"})
+             for i in range(0, case["tokens"], rows)]
+    out = {k: torch.cat([p[k] for p in parts]) for k in parts[0]}
+    if case["top"]:
+        out["top_index"] = None   # whole numbers: compared for equality elsewhere
+    return out
+
+
+def _logprob_exact_rows(case, s):
+    x, t = s["logits"].double(), s["targets"]
+    logp = torch.log_softmax(x, dim=1)
+    p = logp.exp()
+    surprise = torch.where(p > 0, -logp, torch.zeros_like(logp))
+    entropy = (p * surprise).sum(1)
+    hot = torch.zeros_like(p)
+    hot[torch.arange(len(t), device=t.device)[t >= 0], t[t >= 0]] = 1.0
+    picked = torch.where(hot > 0, logp, torch.zeros_like(logp)).sum(1)
+    out = {"logprob": picked, "entropy": entropy}
+    if case["top"]:
+        out["top_logprob"] = torch.sort(logp, dim=1, descending=True).values[:, :case["top"]]
+    if case["train"]:
+        g = s["d_logprob"].double() * (t >= 0)
+        d = g[:, None] * (hot - p) + s["d_entropy"].double()[:, None] * p * (surprise - entropy[:, None])
+        out["d_logits"] = d
+    return out
