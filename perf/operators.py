@@ -205,7 +205,9 @@ def _i8_plain(s):
     x, wq, sw = s["x"].float(), s["wq"], s["sw"]
     amax = x.abs().amax(1, keepdim=True)
     live = amax >= 2.0 ** -100
-    xq = torch.where(live, torch.round(x * (127.0 / torch.where(live, amax, 1.0))), 0.0)
+    # (a quotient of tensors: a scalar's would be a product with the rounded reciprocal)
+    mul = torch.full_like(amax, 127.0) / torch.where(live, amax, 1.0)
+    xq = torch.where(live, torch.round(x * mul), 0.0)
     sx = torch.where(live, amax / 127.0, 0.0)
     n, k = wq.shape
     w = (wq.view(n, sw.shape[1], -1).float() * sw[:, :, None]).view(n, k)
