@@ -389,6 +389,129 @@ jarq_status jarq_permute(const jarq_params* p, const int32_t* perm, const float*
                          float* Wp, float* Hp, void* stream);
 
 /*
+ * Running, training and judging refined layers.
+ *
+ * Tokens are rows: X [tokens][d], 0 <= tokens <= 2^22 (0: nothing is read, and
+ * pointers to the tokens' arrays may be NULL).  Arrays are 16-byte aligned unless
+ * stated, outputs must not overlap inputs, and the calls are asynchronous
+ * unless stated.  Sums are held in fp32 (int32 for integers).
+ */
+
+/*
+ * The gated feed-forward block of two layers that share their input,
+ *     Y = act(X Wg^T) * (X Wu^T)   (elementwise product),
+ * for X [tokens][d], Wg and Wu [f][d] (the layers' weights as jarq_dequantize
+ * writes them), Y [tokens][f], all of dtype JARQ_F16 or JARQ_BF16; d and f are
+ * multiples of 8, from 8 to 2^20.  Y is rounded once.  pre (nullable): [2][tokens][f]
+ * fp32 receives X Wg^T and X Wu^T for the backward pass.
+ */
+#define JARQ_ACT_SILU 0        /* a / (1 + exp(-a)) */
+#define JARQ_ACT_GELU 1        /* a Phi(a), Phi the normal distribution function */
+#define JARQ_ACT_GELU_TANH 2   /* a (1 + tanh(sqrt(2/pi) (a + 0.044715 a^3))) / 2 */
+jarq_status jarq_gated_forward(int32_t dtype, int32_t act, int64_t tokens, int32_t d, int32_t f,
+                               const void* X, const void* Wg, const void* Wu, void* Y, float* pre,
+                               void* stream);
+
+/*
+ * Gradients of that block for dY [tokens][f], from pre as the forward pass left
+ * it: dX [tokens][d], dWg and dWu [f][d], of the block's dtype, each nullable (not
+ * formed) and overwritten.  The gradients of X Wg^T and X Wu^T are rounded to
+ * dtype before their products.  The workspace (256-byte aligned,
+ * jarq_gated_workspace_bytes bytes; 0 if the sizes are invalid) is used only
+ * during the call.
+ */
+size_t jarq_gated_workspace_bytes(int64_t tokens, int32_t d, int32_t f);
+jarq_status jarq_gated_backward(int32_t dtype, int32_t act, int64_t tokens, int32_t d, int32_t f,
+                                const void* X, const void* Wg, const void* Wu, const void* dY,
+                                const float* pre, void* dX, void* dWg, void* dWu, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
+ * Rows on 8 bits, symmetric, a scale each (of tokens, or of a layer's channels):
+ * for X [rows][cols] of any dtype (cols a multiple of 16, at most 131056), in fp32,
+ *     scale = amax / 127,  Q = rint(X (127 / amax)),  amax = max |X| of the row.
+ * Rows with amax < 2^-100 get zeros and scale 0; a row with an infinity or a NaN
+ * gets zeros and scale NaN, which makes what is computed from it NaN.  scale is
+ * 4-byte aligned.
+ */
+jarq_status jarq_quant_rows_i8(int32_t dtype, const void* X, int64_t rows, int32_t cols, int8_t* Q,
+                               float* scale, void* stream);
+
+/*
+ * The integers of a quantized layer: out [rows][cols] int8 = q - z.  With the
+ * layer's scales [rows][G] they are its weights, eq. (1), for the products below
+ * with group = group_size.  flag (device, 4-byte aligned) is scratch of one word.
+ * Synchronises `stream`; JARQ_EINVAL if some q - z is outside -128..127 (bits = 8,
+ * or zero points far outside the codes' range; out is then unspecified).
+ */
+jarq_status jarq_codes_i8(const jarq_params* p, const uint8_t* codes, const int32_t* zeros,
+                          int8_t* out, int32_t* flag, void* stream);
+
+/*
+ * Product of 8-bit integers with scales:
+ *     Y[t][c] = sx[t] sum_g sw[c][g] sum_{i in group g} Xq[t][i] Wq[c][i]
+ * for Xq [tokens][k] and Wq [n][k] int8, sx [tokens] and sw [n][G] fp32 (4-byte
+ * aligned), Y [tokens][n] of any dtype (aligned to its type).  group = 0: one scale a
+ * channel (G = 1); otherwise group is 32, 64 or 128 and divides k, G = k / group.
+ * k is a multiple of 16, at most 131056; 1 <= n <= 2^22.  Integer sums are
+ * exact; group sums are scaled and added in fp32, and Y is rounded once.
+ */
+jarq_status jarq_matmul_i8(int32_t dtype, int64_t tokens, int32_t n, int32_t k, int32_t group,
+                           const int8_t* Xq, const float* sx, const int8_t* Wq, const float* sw,
+                           void* Y, void* stream);
+
+/*
+ * The same linear layer for tokens X [tokens][k] of dtype: jarq_quant_rows_i8 on X,
+ * then the product, Y of the same dtype.  The workspace (256-byte aligned,
+ * jarq_linear_i8_workspace_bytes bytes; 0 if the sizes are invalid) is used only
+ * during the call.
+ */
+size_t jarq_linear_i8_workspace_bytes(int64_t tokens, int32_t k);
+jarq_status jarq_linear_i8(int32_t dtype, int64_t tokens, int32_t n, int32_t k, int32_t group,
+                           const void* X, const int8_t* Wq, const float* sw, void* Y,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log probabilities of given tokens.  For each position t, logits row t (vocab
+ * entries of any dtype from logits + t ld elements, aligned to the type; 1 <= vocab
+ * <= 2^30, ld >= vocab), with lse = log sum_v exp(x_v) and p_v = exp(x_v - lse):
+ *     logprob[t] = x_target - lse        (0 where targets[t] < 0, NaN where it is
+ *                                         not below vocab),
+ *     entropy[t] = -sum_v p_v log p_v    (nullable),
+ *     lse[t]                             (nullable; the backward pass takes it),
+ *     top_index, top_logprob [tokens][top]: the `top` most probable entries and
+ *         their log probabilities, by decreasing logit, ties by increasing index
+ *         (0 <= top <= JARQ_MAX_TOP, top <= vocab).
+ * Entries of -infinity (masked) have probability 0.  In a row of nothing else,
+ * lse and every log probability are -infinity and the entropy is 0.  A row with
+ * +infinity or NaN gives NaN, and -1 as indices.  Results do not depend on the
+ * stride or alignment.  Outputs are fp32 (int32 indices), 4-byte aligned; targets 8-byte.
+ * The workspace (256-byte aligned, jarq_token_logprobs_workspace_bytes bytes; 0 if
+ * the sizes are invalid) is used only during the call.
+ */
+#define JARQ_MAX_TOP 64
+size_t jarq_token_logprobs_workspace_bytes(int64_t tokens, int32_t vocab, int32_t top);
+jarq_status jarq_token_logprobs(int32_t dtype, const void* logits, int64_t ld, int64_t tokens,
+                                int32_t vocab, const int64_t* targets, int32_t top, float* logprob,
+                                float* entropy, float* lse, int32_t* top_index, float* top_logprob,
+                                void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradient of sum_t (d_logprob[t] logprob[t] + d_entropy[t] entropy[t]) in the
+ * logits, rounded once to their dtype:
+ *     d_logits[t][v] = g (1{v = target} - p_v) - h p_v (log p_v + entropy[t]),
+ * g = d_logprob[t] (0 without a target), h = d_entropy[t] (d_entropy nullable: 0, and
+ * entropy is not read).  lse and entropy as the forward pass left them.  Rows of
+ * nothing but -infinity get zeros.  d_logits has row stride ld_d and may be the logits
+ * themselves (ld_d = ld).
+ */
+jarq_status jarq_token_logprobs_backward(int32_t dtype, const void* logits, int64_t ld,
+                                         int64_t tokens, int32_t vocab, const int64_t* targets,
+                                         const float* lse, const float* entropy,
+                                         const float* d_logprob, const float* d_entropy,
+                                         void* d_logits, int64_t ld_d, void* stream);
+
+/*
  * Measurement aid (not part of refinement): a kernel that moves a known
  * number of bytes through the local data share (LDS), used to scale LDS
  * profiler counters to bytes and to see the rate the LDS sustains for a

@@ -7,8 +7,10 @@ fails loudly when the library has not been built.
 
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -72,7 +74,7 @@ class Stats(ctypes.Structure):
         }
 
 
-_vp = ctypes.c_void_p
+_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
 _SIGNATURES = {
     "jarq_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Params)]),
     "jarq_prepare": (ctypes.c_int, [ctypes.POINTER(Params), _vp, _vp, _vp, ctypes.c_size_t, _vp]),
@@ -111,6 +113,22 @@ _SIGNATURES = {
     "jarq_gptq_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Params)]),
     "jarq_gptq": (ctypes.c_int, [ctypes.POINTER(Params), _vp, _vp, _vp, _vp, _vp, _vp,
                                  ctypes.c_size_t, _vp]),
+    "jarq_gated_forward": (ctypes.c_int, [_i32, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                          _vp]),
+    "jarq_gated_workspace_bytes": (ctypes.c_size_t, [_i64, _i32, _i32]),
+    "jarq_gated_backward": (ctypes.c_int, [_i32, _i32, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                           _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jarq_quant_rows_i8": (ctypes.c_int, [_i32, _vp, _i64, _i32, _vp, _vp, _vp]),
+    "jarq_codes_i8": (ctypes.c_int, [ctypes.POINTER(Params), _vp, _vp, _vp, _vp, _vp]),
+    "jarq_matmul_i8": (ctypes.c_int, [_i32, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "jarq_linear_i8_workspace_bytes": (ctypes.c_size_t, [_i64, _i32]),
+    "jarq_linear_i8": (ctypes.c_int, [_i32, _i64, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                      ctypes.c_size_t, _vp]),
+    "jarq_token_logprobs_workspace_bytes": (ctypes.c_size_t, [_i64, _i32, _i32]),
+    "jarq_token_logprobs": (ctypes.c_int, [_i32, _vp, _i64, _i64, _i32, _vp, _i32, _vp, _vp, _vp,
+                                           _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jarq_token_logprobs_backward": (ctypes.c_int, [_i32, _vp, _i64, _i64, _i32, _vp, _vp, _vp,
+                                                    _vp, _vp, _vp, _i64, _vp]),
     "jarq_lds_probe": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32, _vp, _vp]),
     "jarq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "jarq_abi_version": (ctypes.c_int32, []),
@@ -472,6 +490,243 @@ def gptq(p: Params, W, H, codes=None, scales=None, zeros=None, ws=None, stream=N
                          _ptr(zeros, torch.int32, "zeros"), _ptr(ws, torch.uint8, "workspace"),
                          ws.numel(), _stream(stream)), "jarq_gptq")
     return codes, scales, zeros
+
+
+# ---- running, training and judging refined layers ----
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
+
+
+def _on(stream):
+    """Where a call's own allocations belong: the stream that it runs on."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _rows(t, name, cols=None):
+    if not isinstance(t, torch.Tensor) or t.dim() != 2 or (cols is not None and t.shape[1] != cols):
+        raise ValueError(f"{name} must be [rows, {'cols' if cols is None else cols}]")
+    return t.shape
+
+
+def _act(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}, got {act!r}")
+    return ACTIVATIONS[act]
+
+
+def _dtype(t, name):
+    if t.dtype not in DTYPES:
+        raise TypeError(f"{name} must be float32, float16 or bfloat16, got {t.dtype}")
+    return DTYPES[t.dtype]
+
+
+def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
+    """act(X Wg^T) * (X Wu^T) for X [tokens, d], Wg and Wu [f, d] in 16 bits.
+
+    With save, returns (Y, pre): pre [2, tokens, f] fp32 is for gated_backward.
+    """
+    lib = load_library()
+    T, d = _rows(X, "X")
+    f, _ = _rows(Wg, "Wg", d)
+    if _rows(Wu, "Wu", d)[0] != f:
+        raise ValueError("Wg and Wu must have the same shape")
+    pre = None
+    with _on(stream):
+        if out is None:
+            out = torch.empty(T, f, dtype=X.dtype, device=X.device)
+        elif out.shape != (T, f):
+            raise ValueError("out must be [tokens, f]")
+        if save:
+            pre = torch.empty(2, T, f, dtype=torch.float32, device=X.device)
+    dt = X.dtype
+    _check(lib.jarq_gated_forward(_dtype(X, "X"), _act(act), T, d, f, _ptr(X, dt, "X"),
+                                  _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(out, dt, "out"),
+                                  _ptr(pre, torch.float32, "pre"), _stream(stream)),
+           "jarq_gated_forward")
+    return (out, pre) if save else out
+
+
+def gated_workspace_bytes(tokens, d, f) -> int:
+    return int(load_library().jarq_gated_workspace_bytes(tokens, d, f))
+
+
+def gated_backward(X, Wg, Wu, dY, pre, act="silu", need=(True, True, True), ws=None, stream=None):
+    """(dX, dWg, dWu) of gated_forward for dY [tokens, f]; None where not needed."""
+    lib = load_library()
+    T, d = _rows(X, "X")
+    f, _ = _rows(Wg, "Wg", d)
+    if _rows(Wu, "Wu", d)[0] != f or _rows(dY, "dY", f)[0] != T or pre.shape != (2, T, f):
+        raise ValueError("Wg and Wu must be [f, d], dY [tokens, f] and pre [2, tokens, f]")
+    n = int(lib.jarq_gated_workspace_bytes(T, d, f))
+    if n == 0:
+        raise JarqError(JARQ_EINVAL, "jarq_gated_workspace_bytes")
+    dt = X.dtype
+    with _on(stream):
+        dX, dWg, dWu = (torch.empty_like(t) if wanted else None
+                        for t, wanted in zip((X, Wg, Wu), need))
+        if ws is None:
+            ws = _scratch(n, X.device)
+    _check(lib.jarq_gated_backward(_dtype(X, "X"), _act(act), T, d, f, _ptr(X, dt, "X"),
+                                   _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(dY, dt, "dY"),
+                                   _ptr(pre, torch.float32, "pre"), _ptr(dX, dt, "dX"),
+                                   _ptr(dWg, dt, "dWg"), _ptr(dWu, dt, "dWu"),
+                                   _ptr(ws, torch.uint8, "workspace"), ws.numel(),
+                                   _stream(stream)), "jarq_gated_backward")
+    return dX, dWg, dWu
+
+
+def quant_rows_i8(X, out=None, scale=None, stream=None):
+    """(Q int8, scale fp32 [rows, 1]): the rows of X on 8 bits with a scale each."""
+    lib = load_library()
+    rows, cols = _rows(X, "X")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(rows, cols, dtype=torch.int8, device=X.device)
+        if scale is None:
+            scale = torch.empty(rows, 1, dtype=torch.float32, device=X.device)
+    if out.shape != (rows, cols) or scale.numel() != rows:
+        raise ValueError("out must be [rows, cols] and scale hold one value a row")
+    _check(lib.jarq_quant_rows_i8(_dtype(X, "X"), _ptr(X, X.dtype, "X"), rows, cols,
+                                  _ptr(out, torch.int8, "out"), _ptr(scale, torch.float32, "scale"),
+                                  _stream(stream)), "jarq_quant_rows_i8")
+    return out, scale
+
+
+def codes_i8(p: Params, codes, zeros, out=None, stream=None):
+    """q - z as int8: a quantized layer's weights for matmul_i8 and linear_i8."""
+    lib = load_library()
+    with _on(stream):
+        if out is None:
+            out = torch.empty(p.rows, p.cols, dtype=torch.int8, device=codes.device)
+        flag = torch.empty(1, dtype=torch.int32, device=codes.device)
+    _check(lib.jarq_codes_i8(ctypes.byref(p), _ptr(codes, torch.uint8, "codes"),
+                             _ptr(zeros, torch.int32, "zeros"), _ptr(out, torch.int8, "out"),
+                             _ptr(flag, torch.int32, "flag"), _stream(stream)), "jarq_codes_i8")
+    return out
+
+
+def _i8_layer(Wq, sw, k):
+    """(n, group) of a layer's integers [n, k] with scales [n, 1] or [n, k / group]."""
+    n, _ = _rows(Wq, "Wq", k)
+    rows, groups = _rows(sw, "sw")
+    if rows != n or groups < 1 or k % groups != 0:
+        raise ValueError("sw must be [n, 1] or [n, k / group]")
+    return n, 0 if groups == 1 else k // groups
+
+
+def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
+    """sx (Xq Wq^T under the scales sw [n, 1] or [n, k / group]) as `dtype`."""
+    lib = load_library()
+    T, k = _rows(Xq, "Xq")
+    n, group = _i8_layer(Wq, sw, k)
+    if sx.numel() != T:
+        raise ValueError("sx must hold one scale a token")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(T, n, dtype=dtype, device=Xq.device)
+        elif out.shape != (T, n):
+            raise ValueError("out must be [tokens, n]")
+    _check(lib.jarq_matmul_i8(_dtype(out, "out"), T, n, k, group, _ptr(Xq, torch.int8, "Xq"),
+                              _ptr(sx, torch.float32, "sx"), _ptr(Wq, torch.int8, "Wq"),
+                              _ptr(sw, torch.float32, "sw"), _ptr(out, out.dtype, "out"),
+                              _stream(stream)), "jarq_matmul_i8")
+    return out
+
+
+def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
+    """X [tokens, k] through the 8-bit layer (Wq [n, k], sw [n, 1] or [n, k / group])."""
+    lib = load_library()
+    T, k = _rows(X, "X")
+    n, group = _i8_layer(Wq, sw, k)
+    need = int(lib.jarq_linear_i8_workspace_bytes(T, k))
+    if need == 0:
+        raise JarqError(JARQ_EINVAL, "jarq_linear_i8_workspace_bytes")
+    dt = X.dtype
+    with _on(stream):
+        if out is None:
+            out = torch.empty(T, n, dtype=dt, device=X.device)
+        elif out.shape != (T, n):
+            raise ValueError("out must be [tokens, n]")
+        if ws is None:
+            ws = _scratch(need, X.device)
+    _check(lib.jarq_linear_i8(_dtype(X, "X"), T, n, k, group, _ptr(X, dt, "X"),
+                              _ptr(Wq, torch.int8, "Wq"), _ptr(sw, torch.float32, "sw"),
+                              _ptr(out, dt, "out"), _ptr(ws, torch.uint8, "workspace"), ws.numel(),
+                              _stream(stream)), "jarq_linear_i8")
+    return out
+
+
+class TokenLogprobs(NamedTuple):
+    logprob: torch.Tensor                  # [tokens] fp32
+    entropy: torch.Tensor                  # [tokens] fp32
+    lse: torch.Tensor                      # [tokens] fp32: log sum exp of the row
+    top_index: Optional[torch.Tensor]      # [tokens, top] int32
+    top_logprob: Optional[torch.Tensor]    # [tokens, top] fp32
+
+
+def _logits(t, name):
+    """(tokens, vocab, row stride) of logits whose rows are dense."""
+    T, V = _rows(t, name)
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if V > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name} must have dense rows")
+    ld = t.stride(0) if T > 1 else V
+    if ld < V:
+        raise ValueError(f"{name} must not have overlapping rows")
+    return T, V, ld
+
+
+def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprobs:
+    """Log probabilities of targets [tokens] int64 (< 0: none), entropies, top alternatives."""
+    lib = load_library()
+    T, V, ld = _logits(logits, "logits")
+    if targets.shape != (T,):
+        raise ValueError("targets must be [tokens]")
+    n = int(lib.jarq_token_logprobs_workspace_bytes(T, V, top))
+    if n == 0:
+        raise JarqError(JARQ_EINVAL, "jarq_token_logprobs_workspace_bytes")
+    dev = logits.device
+    with _on(stream):
+        logprob, entropy, lse = torch.empty(3, T, dtype=torch.float32, device=dev).unbind(0)
+        index = torch.empty(T, top, dtype=torch.int32, device=dev) if top else None
+        value = torch.empty(T, top, dtype=torch.float32, device=dev) if top else None
+        if ws is None:
+            ws = _scratch(n, dev)
+    _check(lib.jarq_token_logprobs(_dtype(logits, "logits"), ctypes.c_void_p(logits.data_ptr()),
+                                   ld, T, V, _ptr(targets, torch.int64, "targets"), top,
+                                   _ptr(logprob, torch.float32, "logprob"),
+                                   _ptr(entropy, torch.float32, "entropy"),
+                                   _ptr(lse, torch.float32, "lse"),
+                                   _ptr(index, torch.int32, "top_index"),
+                                   _ptr(value, torch.float32, "top_logprob"),
+                                   _ptr(ws, torch.uint8, "workspace"), ws.numel(),
+                                   _stream(stream)), "jarq_token_logprobs")
+    return TokenLogprobs(logprob, entropy, lse, index, value)
+
+
+def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, d_entropy=None,
+                            out=None, stream=None):
+    """Gradient of the logits from those of the log probabilities and entropies [tokens]."""
+    lib = load_library()
+    T, V, ld = _logits(logits, "logits")
+    for t, name in ((targets, "targets"), (forward.lse, "lse"), (forward.entropy, "entropy"),
+                    (d_logprob, "d_logprob"), (d_entropy, "d_entropy")):
+        if t is not None and t.shape != (T,):
+            raise ValueError(f"{name} must be [tokens]")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
+    if out.shape != (T, V) or out.dtype != logits.dtype:
+        raise ValueError("out must have the logits' shape and type")
+    _, _, ld_d = _logits(out, "out")
+    _check(lib.jarq_token_logprobs_backward(
+        _dtype(logits, "logits"), ctypes.c_void_p(logits.data_ptr()), ld, T, V,
+        _ptr(targets, torch.int64, "targets"), _ptr(forward.lse, torch.float32, "lse"),
+        _ptr(forward.entropy, torch.float32, "entropy"),
+        _ptr(d_logprob, torch.float32, "d_logprob"), _ptr(d_entropy, torch.float32, "d_entropy"),
+        ctypes.c_void_p(out.data_ptr()), ld_d, _stream(stream)), "jarq_token_logprobs_backward")
+    return out
 
 
 def lds_probe(workgroups, passes, out=None, stream=None):

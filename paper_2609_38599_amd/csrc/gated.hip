@@ -1,0 +1,454 @@
+// The gated feed-forward block y = act(a) * b, a = x Wg^T, b = x Wu^T, and its
+// backward pass, for 16-bit x [T][D], Wg, Wu [F][D] (row-major).
+//
+// Forward: one kernel forms both products of a tile of y from one staging of x
+// (the tile's P rows are Wg's and Wu's of the same channels, so a lane ends up with
+// a and b of the same entry) and stores act(a) b, rounded once from fp32 sums.
+//
+// Backward: da = dy b act'(a), db = dy act(a) from the saved fp32 a and b, rounded
+// to 16 bits as the matrix cores take them (the only rounding beside the
+// outputs'); then dx = [da db] [Wg; Wu] in one product over 2 F, and
+// [dWg; dWu] = [da db]^T x in one over T.
+#include "skinny.h"
+
+namespace jarq {
+
+namespace {
+
+constexpr float kInvSqrt2 = 0.70710678118654752f;
+constexpr float kInvSqrt2Pi = 0.39894228040143268f;
+constexpr float kSqrt2OverPi = 0.79788456080286536f;
+
+// act(a), and act'(a) where `d` is given
+template <int ACT>
+__device__ __forceinline__ float activation(float a, float* d) {
+  if constexpr (ACT == 0) {          // silu
+    const float sig = 1.f / (1.f + __expf(-a));
+    if (d) *d = sig * (1.f + a * (1.f - sig));
+    return a * sig;
+  } else if constexpr (ACT == 1) {   // gelu
+    const float cdf = 0.5f * (1.f + erff(a * kInvSqrt2));
+    if (d) *d = cdf + a * kInvSqrt2Pi * __expf(-0.5f * a * a);
+    return a * cdf;
+  } else {                           // gelu, tanh form
+    const float th = tanhf(kSqrt2OverPi * (a + 0.044715f * a * a * a));
+    if (d)
+      *d = 0.5f * (1.f + th) +
+           0.5f * a * (1.f - th * th) * kSqrt2OverPi * (1.f + 3.f * 0.044715f * a * a);
+    return 0.5f * a * (1.f + th);
+  }
+}
+__device__ __forceinline__ float activation(int act, float a, float* d) {   // act is uniform
+  if (act == 0) return activation<0>(a, d);
+  if (act == 1) return activation<1>(a, d);
+  return activation<2>(a, d);
+}
+
+}  // namespace
+
+// ---- forward, many tokens ----
+// WI x WJ wavefronts, each BI blocks of 32 P rows (half Wg's, half Wu's) x BJ blocks
+// of 32 tokens.
+template <int KIND, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
+    const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
+    int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre, int ni, int nj) {
+  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  typedef KContig<TI, NW, true> LP;
+  typedef KContig<TJ, NW, false> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int f0 = ti * (TI / 2), t0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(Wg, Wu, 2 * (size_t)D, f0, F, 2 * D, wave, lane);
+  lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
+  f32x16 acc[BI][BJ] = {};
+  // block a < BI / 2: Wg, the others: Wu of the same channels
+  auto prow = [&](int a) {
+    return a < BI / 2 ? wi * 16 * BI + 32 * a : TI / 2 + wi * 16 * BI + 32 * (a - BI / 2);
+  };
+  mma_loop(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, buf0, buf1,
+           [&](const char* cur, int) __attribute__((always_inline)) {
+             mma_chunk<KIND, BI, BJ, LP, LQ>(cur, lane, prow, wj * 32 * BJ, acc);
+           });
+#pragma unroll
+  for (int b = 0; b < BJ; ++b) {
+    const int t = t0 + wj * 32 * BJ + 32 * b + (lane & 31);
+#pragma unroll
+    for (int a = 0; a < BI / 2; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int f = f0 + wi * 16 * BI + 32 * a + 8 * r + 4 * (lane >> 5);
+        if (t < T && f < F) {
+          f32x4 g, u, y;
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            g[v] = acc[a][b][4 * r + v];
+            u[v] = acc[BI / 2 + a][b][4 * r + v];
+            y[v] = activation(act, g[v], nullptr) * u[v];
+          }
+          const size_t e = (size_t)t * F + f;
+          *(u32x2*)(Y + e) = u32x2{pack16<KIND>(y[0], y[1]), pack16<KIND>(y[2], y[3])};
+          if (pre) {
+            *(f32x4*)(pre + e) = g;
+            *(f32x4*)(pre + (size_t)T * F + e) = u;
+          }
+        }
+      }
+  }
+}
+
+// ---- forward, few tokens ----
+// A work-group: 16 channels of both projections x up to 16 IB tokens (blockIdx.y),
+// eight wavefronts along k.
+template <int KIND, int IB>
+__global__ __launch_bounds__(512) void gated_skinny_kernel(
+    const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
+    int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre) {
+  constexpr int NW = 8;
+  __shared__ __attribute__((aligned(16))) float red[NW * IB * 2 * 256];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int f0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * IB;
+  const int row = lane & 15;
+  const char* p[IB];
+#pragma unroll
+  for (int a = 0; a < IB; ++a)
+    p[a] = (const char*)X + (size_t)min(t0 + 16 * a + row, T - 1) * (2 * (size_t)D);
+  const size_t wrow = (size_t)min(f0 + row, F - 1) * (2 * (size_t)D);
+  const char* const q[2] = {(const char*)Wg + wrow, (const char*)Wu + wrow};
+  f32x4 acc[IB][2] = {};
+  skinny_loop<IB, 2, (IB > 2 ? 2 : 4), NW>(
+      p, q, 2 * D, wave, lane, [](int, int) {}, [&](int, int, const u32x4(&fp)[IB], const u32x4(&fq)[2])
+                                   __attribute__((always_inline)) {
+#pragma unroll
+        for (int a = 0; a < IB; ++a)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) acc[a][b] = Mma<KIND>::mul16(fp[a], fq[b], acc[a][b]);
+      });
+#pragma unroll
+  for (int a = 0; a < IB; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      *(f32x4*)(red + ((wave * IB + a) * 2 + b) * 256 + 4 * lane) = acc[a][b];
+  __syncthreads();
+  for (int e = threadIdx.x; e < IB * 256; e += 512) {
+    const int j = e & 15, i = (e >> 4) & 15, a = e >> 8;
+    const int t = t0 + 16 * a + i, f = f0 + j;
+    if (t < T && f < F) {
+      const float g = skinny_sum<NW, 2 * IB>(red, 2 * a, i, j);
+      const float u = skinny_sum<NW, 2 * IB>(red, 2 * a + 1, i, j);
+      const size_t at = (size_t)t * F + f;
+      Y[at] = to16<KIND>(activation(act, g, nullptr) * u);
+      if (pre) {
+        pre[at] = g;
+        pre[(size_t)T * F + at] = u;
+      }
+    }
+  }
+}
+
+template <int KIND>
+static hipError_t launch_gated_forward_kind(hipStream_t st, int act, int T, int D, int F,
+                                            const void* X, const void* Wg, const void* Wu,
+                                            void* Y, float* pre) {
+  uint16_t* y = (uint16_t*)Y;
+  const dim3 wg((F + 15) / 16);
+  if (T <= 16) {
+    hipLaunchKernelGGL((gated_skinny_kernel<KIND, 1>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
+                       act, y, pre);
+  } else if (T <= 32) {
+    hipLaunchKernelGGL((gated_skinny_kernel<KIND, 2>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
+                       act, y, pre);
+  } else if (T <= 64) {
+    hipLaunchKernelGGL((gated_skinny_kernel<KIND, 4>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
+                       act, y, pre);
+  } else {
+    const int bi = (F + 127) / 128, bj = (T + 255) / 256;
+    if ((long long)bi * bj >= 192) {
+      hipLaunchKernelGGL((gated_tile_kernel<KIND, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)),
+                         dim3(512), 0, st, X, Wg, Wu, T, D, F, act, y, pre, bi, bj);
+    } else {
+      const int ni = (F + 63) / 64, nj = (T + 127) / 128;
+      hipLaunchKernelGGL((gated_tile_kernel<KIND, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
+                         dim3(256), 0, st, X, Wg, Wu, T, D, F, act, y, pre, ni, nj);
+    }
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_gated_forward(hipStream_t st, int dtype, int act, int T, int D, int F,
+                                const void* X, const void* Wg, const void* Wu, void* Y,
+                                float* pre) {
+  return dtype == kBF16
+             ? launch_gated_forward_kind<kBF16>(st, act, T, D, F, X, Wg, Wu, Y, pre)
+             : launch_gated_forward_kind<kF16>(st, act, T, D, F, X, Wg, Wu, Y, pre);
+}
+
+// ---- backward: da, db ----
+// dab [T][2 F]: da in columns 0..F-1, db behind.  Eight entries a thread.
+template <int KIND>
+__global__ __launch_bounds__(256) void gated_grad_kernel(const float* __restrict__ pre,
+                                                         const uint16_t* __restrict__ dY, int T,
+                                                         int F, int act,
+                                                         uint16_t* __restrict__ dab) {
+  const size_t n = (size_t)T * F, f8 = (size_t)(F / 8);
+  for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n / 8;
+       e += (size_t)gridDim.x * 256) {
+    const size_t t = e / f8, f = (e - t * f8) * 8;
+    const size_t at = 8 * e;
+    f32x4 g[2], u[2];
+    g[0] = *(const f32x4*)(pre + at);
+    g[1] = *(const f32x4*)(pre + at + 4);
+    u[0] = *(const f32x4*)(pre + n + at);
+    u[1] = *(const f32x4*)(pre + n + at + 4);
+    const u32x4 dy = *(const u32x4*)(dY + at);
+    u32x4 da, db;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      float ga[2], gb[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int v = 2 * w + h;
+        const float d = from16<KIND>((uint16_t)(dy[w] >> (16 * h)));
+        float slope;
+        const float s = activation(act, g[v >> 2][v & 3], &slope);
+        ga[h] = d * u[v >> 2][v & 3] * slope;
+        gb[h] = d * s;
+      }
+      da[w] = pack16<KIND>(ga[0], ga[1]);
+      db[w] = pack16<KIND>(gb[0], gb[1]);
+    }
+    uint16_t* out = dab + t * (2 * (size_t)F) + f;
+    *(u32x4*)out = da;
+    *(u32x4*)(out + F) = db;
+  }
+}
+
+// ---- backward: dx = dab [Wg; Wu] ----
+// part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.
+template <int KIND, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
+    const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
+    int D, int F, int each, uint16_t* __restrict__ dX, float* __restrict__ part, int ni, int nj) {
+  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  typedef KStrided<TI, NW> LP;
+  typedef KContig<TJ, NW, false> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int d0 = ti * TI, t0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(Wg, Wu, 2 * (size_t)D, d0, D, 2 * F, F, wave, lane);
+  lq.init(dab, dab, 4 * (size_t)F, t0, T, 4 * F, wave, lane);
+  f32x16 acc[BI][BJ] = {};
+  const int nk = (2 * F + 63) / 64;
+  const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
+  auto prow = [&](int a) { return wi * 32 * BI + 32 * a; };
+  mma_loop(lp, lq, q0, q1, buf0, buf1,
+           [&](const char* cur, int) __attribute__((always_inline)) {
+             mma_chunk<KIND, BI, BJ, LP, LQ>(cur, lane, prow, wj * 32 * BJ, acc);
+           });
+#pragma unroll
+  for (int b = 0; b < BJ; ++b) {
+    const int t = t0 + wj * 32 * BJ + 32 * b + (lane & 31);
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = d0 + prow(a) + 8 * r + 4 * (lane >> 5);
+        if (t < T && d < D) {
+          const f32x16& c = acc[a][b];
+          if (part) {
+            *(f32x4*)(part + ((size_t)blockIdx.y * T + t) * D + d) =
+                f32x4{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
+          } else {
+            *(u32x2*)(dX + (size_t)t * D + d) = u32x2{pack16<KIND>(c[4 * r], c[4 * r + 1]),
+                                                      pack16<KIND>(c[4 * r + 2], c[4 * r + 3])};
+          }
+        }
+      }
+  }
+}
+
+template <int KIND>
+__global__ __launch_bounds__(256) void gated_dx_sum_kernel(const float* __restrict__ part,
+                                                           int splits, size_t n,
+                                                           uint16_t* __restrict__ dX) {
+  for (size_t e = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x); e < n;
+       e += 4 * (size_t)gridDim.x * 256) {
+    f32x4 s = *(const f32x4*)(part + e);
+    for (int k = 1; k < splits; ++k) s += *(const f32x4*)(part + k * n + e);
+    *(u32x2*)(dX + e) = u32x2{pack16<KIND>(s[0], s[1]), pack16<KIND>(s[2], s[3])};
+  }
+}
+
+// ---- backward: [dWg; dWu] = dab^T x ----
+template <int KIND, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
+    const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,
+    uint16_t* __restrict__ dWg, uint16_t* __restrict__ dWu, int ni, int nj) {
+  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  typedef KStrided<TI, NW> LP;
+  typedef KStrided<TJ, NW> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int d0 = ti * TI, f0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(X, X, 2 * (size_t)D, d0, D, T, T, wave, lane);
+  lq.init(dab, dab, 4 * (size_t)F, f0, 2 * F, T, T, wave, lane);
+  f32x16 acc[BI][BJ] = {};
+  auto prow = [&](int a) { return wi * 32 * BI + 32 * a; };
+  mma_loop(lp, lq, 0, (T + 63) / 64, buf0, buf1,
+           [&](const char* cur, int) __attribute__((always_inline)) {
+             mma_chunk<KIND, BI, BJ, LP, LQ>(cur, lane, prow, wj * 32 * BJ, acc);
+           });
+#pragma unroll
+  for (int b = 0; b < BJ; ++b) {
+    const int f = f0 + wj * 32 * BJ + 32 * b + (lane & 31);
+    uint16_t* out = f < F ? dWg : dWu;
+    const size_t row = (size_t)(f < F ? f : f - F) * D;
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = d0 + prow(a) + 8 * r + 4 * (lane >> 5);
+        if (f < 2 * F && d < D && out) {
+          const f32x16& c = acc[a][b];
+          *(u32x2*)(out + row + d) = u32x2{pack16<KIND>(c[4 * r], c[4 * r + 1]),
+                                           pack16<KIND>(c[4 * r + 2], c[4 * r + 3])};
+        }
+      }
+  }
+}
+
+namespace {
+
+struct DxPlan {
+  bool big;
+  int ni, nj, splits, each;
+};
+// Whole 256-wide tiles where they fill the chip; otherwise 128-wide ones, with the
+// 2 F cut so that about two work-groups fall on each CU.
+DxPlan dx_plan(int T, int D, int F) {
+  DxPlan p;
+  const int nk = (2 * F + 63) / 64;
+  p.big = (long long)((D + 255) / 256) * ((T + 255) / 256) >= 192;
+  const int e = p.big ? 256 : 128;
+  p.ni = (D + e - 1) / e;
+  p.nj = (T + e - 1) / e;
+  int splits = 1;
+  if (!p.big) {
+    splits = 512 / (p.ni * p.nj);
+    splits = splits < 1 ? 1 : splits > nk / 4 ? (nk / 4 < 1 ? 1 : nk / 4) : splits;
+    if (splits > 32) splits = 32;
+  }
+  p.each = (nk + splits - 1) / splits;
+  p.splits = (nk + p.each - 1) / p.each;
+  return p;
+}
+
+size_t pad256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+}  // namespace
+
+size_t gated_workspace_bytes(int T, int D, int F) {
+  const DxPlan p = dx_plan(T, D, F);
+  return pad256(4 * (size_t)T * F) +
+         (p.splits > 1 ? pad256(4 * (size_t)p.splits * T * D) : 0);
+}
+
+// The weights' gradient of no tokens.
+__global__ __launch_bounds__(256) void gated_zero_kernel(u32x4* out, size_t n) {
+  for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256)
+    out[e] = u32x4{};
+}
+
+template <int KIND>
+static hipError_t launch_gated_backward_kind(hipStream_t st, int act, int T, int D, int F,
+                                             const void* X, const void* Wg, const void* Wu,
+                                             const void* dY, const float* pre, void* dX, void* dWg,
+                                             void* dWu, char* ws) {
+  if (T == 0) {
+    for (void* out : {dWg, dWu}) {
+      if (!out) continue;
+      hipLaunchKernelGGL(gated_zero_kernel, dim3(1024), dim3(256), 0, st, (u32x4*)out,
+                         (size_t)F * D / 8);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  }
+  uint16_t* dab = (uint16_t*)ws;
+  float* part = (float*)(ws + pad256(4 * (size_t)T * F));
+  const size_t n8 = (size_t)T * F / 8;
+  const size_t blocks = (n8 + 255) / 256 < 16384 ? (n8 + 255) / 256 : 16384;
+  hipLaunchKernelGGL((gated_grad_kernel<KIND>), dim3((unsigned)blocks), dim3(256), 0, st, pre,
+                     (const uint16_t*)dY, T, F, act, dab);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (dX) {
+    const DxPlan p = dx_plan(T, D, F);
+    float* to = p.splits > 1 ? part : nullptr;
+    const dim3 grid((unsigned)(p.ni * p.nj), (unsigned)p.splits);
+    if (p.big)
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 2, 4, 4, 2>), grid, dim3(512), 0, st, dab, Wg, Wu,
+                         T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
+    else
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 2, 2, 2, 2>), grid, dim3(256), 0, st, dab, Wg, Wu,
+                         T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (to) {
+      const size_t n = (size_t)T * D, b = (n / 4 + 255) / 256;
+      hipLaunchKernelGGL((gated_dx_sum_kernel<KIND>), dim3((unsigned)(b < 4096 ? b : 4096)),
+                         dim3(256), 0, st, part, p.splits, n, (uint16_t*)dX);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (dWg || dWu) {
+    const int bi = (D + 255) / 256, bj = (2 * F + 255) / 256;
+    if ((long long)bi * bj >= 192) {
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)),
+                         dim3(512), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, bi,
+                         bj);
+    } else {
+      const int ni = (D + 127) / 128, nj = (2 * F + 127) / 128;
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
+                         dim3(256), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, ni,
+                         nj);
+    }
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+hipError_t launch_gated_backward(hipStream_t st, int dtype, int act, int T, int D, int F,
+                                 const void* X, const void* Wg, const void* Wu, const void* dY,
+                                 const float* pre, void* dX, void* dWg, void* dWu, char* ws) {
+  return dtype == kBF16 ? launch_gated_backward_kind<kBF16>(st, act, T, D, F, X, Wg, Wu, dY, pre,
+                                                            dX, dWg, dWu, ws)
+                        : launch_gated_backward_kind<kF16>(st, act, T, D, F, X, Wg, Wu, dY, pre,
+                                                           dX, dWg, dWu, ws);
+}
+
+}  // namespace jarq

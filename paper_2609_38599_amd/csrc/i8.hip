@@ -1,0 +1,371 @@
+// Linear layers in 8-bit integers.
+//
+// quant_rows_kernel: a row's values on a symmetric grid of its own, scale = amax /
+// 127, q = rint(x (127 / amax)), all in fp32.
+//
+// The product: y[t][n] = sx_t sum_g sw[n][g] sum_{k in g} xq[t][k] wq[n][k], the
+// integer sums exact in int32 on v_mfma_i32_32x32x32_i8, a group's sum converted
+// and added in fp32.  Tokens are the P rows and channels the Q rows, so that a lane
+// holds one channel and needs one group scale.
+#include "skinny.h"
+
+namespace jarq {
+
+namespace {
+
+constexpr uint32_t kInfBits = 0x7f800000u;
+constexpr uint32_t kTinyBits = 0x0d800000u;   // 2^-100
+
+// |x| as ordered bits: NaN above infinity above every finite value
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// A row's scale and multiplier.  Rows under 2^-100 are zeros (their multiplier
+// would overflow); a row with an infinity or a NaN has a NaN scale and zeros, so that
+// what is computed from it is NaN.
+__device__ __forceinline__ void row_scale(uint32_t amax_bits, float& scale, float& mul) {
+  const float amax = __uint_as_float(amax_bits);
+  mul = 0.f;
+  if (amax_bits >= kInfBits) {
+    scale = __uint_as_float(0x7fc00000u);
+  } else if (amax_bits < kTinyBits) {
+    scale = 0.f;
+  } else {
+    scale = amax / 127.f;
+    mul = 127.f / amax;
+  }
+}
+__device__ __forceinline__ uint32_t quant(float x, float mul) {
+  // a zero multiplier gives 0 for any x
+  return mul == 0.f ? 0u : (uint32_t)(int)rintf(x * mul) & 0xffu;
+}
+
+// Eight values from element 8 v of a row.
+template <int DT>
+__device__ __forceinline__ void load8(const void* row, int v, float (&x)[8]) {
+  if constexpr (DT == 0) {
+    const f32x4 a = *((const f32x4*)row + 2 * v), b = *((const f32x4*)row + 2 * v + 1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = a[i];
+      x[4 + i] = b[i];
+    }
+  } else {
+    const u32x4 w = *((const u32x4*)row + v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = from16<DT>((uint16_t)w[i]);
+      x[2 * i + 1] = from16<DT>((uint16_t)(w[i] >> 16));
+    }
+  }
+}
+
+}  // namespace
+
+// A work-group a row; K a multiple of 16.
+template <int DT>
+__global__ __launch_bounds__(256) void quant_rows_kernel(const void* __restrict__ X, int K,
+                                                         int8_t* __restrict__ Q,
+                                                         float* __restrict__ scale) {
+  __shared__ uint32_t red[4];
+  const size_t r = blockIdx.x;
+  const char* row = (const char*)X + r * K * (DT == 0 ? 4 : 2);
+  const int nv = K / 8;
+  uint32_t m = 0;
+  for (int v = threadIdx.x; v < nv; v += 256) {
+    float x[8];
+    load8<DT>(row, v, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = max(max(red[0], red[1]), max(red[2], red[3]));
+  float s, mul;
+  row_scale(m, s, mul);
+  for (int v = threadIdx.x; v < nv; v += 256) {
+    float x[8];
+    load8<DT>(row, v, x);
+    uint32_t lo = 0, hi = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      lo |= quant(x[i], mul) << (8 * i);
+      hi |= quant(x[4 + i], mul) << (8 * i);
+    }
+    *(u32x2*)(Q + r * K + 8 * (size_t)v) = u32x2{lo, hi};
+  }
+  if (threadIdx.x == 0) scale[r] = s;
+}
+
+hipError_t launch_quant_rows(hipStream_t st, int dtype, const void* X, int rows, int K, int8_t* Q,
+                             float* scale) {
+  const dim3 g(rows), b(256);
+  if (dtype == 0) hipLaunchKernelGGL(quant_rows_kernel<0>, g, b, 0, st, X, K, Q, scale);
+  else if (dtype == 1) hipLaunchKernelGGL(quant_rows_kernel<1>, g, b, 0, st, X, K, Q, scale);
+  else hipLaunchKernelGGL(quant_rows_kernel<2>, g, b, 0, st, X, K, Q, scale);
+  return hipGetLastError();
+}
+
+// ---- codes minus zero points as int8 ----
+// Sixteen codes a thread (within a group); bad counts the values outside int8.
+__global__ __launch_bounds__(256) void codes_i8_kernel(const uint8_t* __restrict__ codes,
+                                                       const int32_t* __restrict__ zeros,
+                                                       long long n16, int g,
+                                                       int8_t* __restrict__ out,
+                                                       int32_t* __restrict__ bad) {
+  const long long e = (long long)blockIdx.x * 256 + threadIdx.x;
+  if (e >= n16) return;
+  const u32x4 q = *((const u32x4*)codes + e);
+  const int z = zeros[16 * e / g];
+  u32x4 o;
+  bool out_of_range = false;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t p = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int c = (int)((q[w] >> (8 * i)) & 0xffu) - z;
+      out_of_range |= c < -128 || c > 127;
+      p |= ((uint32_t)c & 0xffu) << (8 * i);
+    }
+    o[w] = p;
+  }
+  *((u32x4*)out + e) = o;
+  if (out_of_range) *bad = 1;
+}
+__global__ void clear_flag_kernel(int32_t* flag) { *flag = 0; }
+
+hipError_t launch_codes_i8(hipStream_t st, const uint8_t* codes, const int32_t* zeros, int rows,
+                           int cols, int g, int8_t* out, int32_t* bad) {
+  hipLaunchKernelGGL(clear_flag_kernel, dim3(1), dim3(1), 0, st, bad);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const long long n16 = (long long)rows * cols / 16;
+  hipLaunchKernelGGL(codes_i8_kernel, dim3((unsigned)((n16 + 255) / 256)), dim3(256), 0, st, codes,
+                     zeros, n16, g, out, bad);
+  return hipGetLastError();
+}
+
+// ---- products ----
+namespace {
+
+__device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) {   // dtype uniform
+  if (dtype == 0) ((float*)Y)[at] = y;
+  else if (dtype == 1) ((uint16_t*)Y)[at] = to16<kF16>(y);
+  else ((uint16_t*)Y)[at] = to16<kBF16>(y);
+}
+
+}  // namespace
+
+// Many tokens.  GROUP 0: one scale a channel, int32 sums over all of k; otherwise a
+// group's int32 sums (its k-slices of 32, within a chunk of 128) go to fp32.
+template <int GROUP, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
+    const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
+    const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y, int ni,
+    int nj) {
+  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  typedef KContig<TI, NW, false> LP;
+  typedef KContig<TJ, NW, false> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int t0 = ti * TI, n0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(Xq, Xq, K, t0, T, K, wave, lane);
+  lq.init(Wq, Wq, K, n0, N, K, wave, lane);
+  auto prow = [&](int a) { return wi * 32 * BI + 32 * a; };
+  const int nk = (K + kChunk - 1) / kChunk, qrow = wj * 32 * BJ;
+  f32x16 y[BI][BJ];
+  const int G = GROUP ? K / GROUP : 1;
+  const float* srow[BJ];
+#pragma unroll
+  for (int b = 0; b < BJ; ++b)
+    srow[b] = sw + (size_t)min(n0 + qrow + 32 * b + (lane & 31), N - 1) * G;
+  if constexpr (GROUP == 0) {
+    i32x16 acc[BI][BJ] = {};
+    mma_loop(lp, lq, 0, nk, buf0, buf1, [&](const char* cur, int) __attribute__((always_inline)) {
+      mma_chunk<kI8, BI, BJ, LP, LQ>(cur, lane, prow, qrow, acc);
+    });
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int b = 0; b < BJ; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) y[a][b][v] = (float)acc[a][b][v] * srow[b][0];
+  } else {
+    constexpr int GC = kChunk / GROUP;   // groups a chunk
+    constexpr int KG = 4 / GC;           // k-slices a group
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int b = 0; b < BJ; ++b) y[a][b] = f32x16{};
+    mma_loop(lp, lq, 0, nk, buf0, buf1,
+             [&](const char* cur, int q) __attribute__((always_inline)) {
+#pragma unroll
+      for (int g = 0; g < GC; ++g) {
+        // (a last chunk may hold fewer groups; what it stages past k is zeros)
+        float s[BJ];
+#pragma unroll
+        for (int b = 0; b < BJ; ++b) s[b] = q * GC + g < G ? srow[b][q * GC + g] : 0.f;
+        u32x4 fp[BI][KG], fq[BJ][KG];
+#pragma unroll
+        for (int k = 0; k < KG; ++k) {
+#pragma unroll
+          for (int a = 0; a < BI; ++a) fp[a][k] = LP::frag(cur, prow(a), g * KG + k, lane);
+#pragma unroll
+          for (int b = 0; b < BJ; ++b)
+            fq[b][k] = LQ::frag(cur + LP::kBytes, qrow + 32 * b, g * KG + k, lane);
+        }
+#pragma unroll
+        for (int a = 0; a < BI; ++a)
+#pragma unroll
+          for (int b = 0; b < BJ; ++b) {
+            i32x16 acc = {};
+#pragma unroll
+            for (int k = 0; k < KG; ++k) acc = Mma<kI8>::mul(fp[a][k], fq[b][k], acc);
+#pragma unroll
+            for (int v = 0; v < 16; ++v) y[a][b][v] = fmaf((float)acc[v], s[b], y[a][b][v]);
+          }
+      }
+    });
+  }
+#pragma unroll
+  for (int a = 0; a < BI; ++a)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      const int t = t0 + prow(a) + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
+      if (t < T) {
+        const float st = sx[t];
+#pragma unroll
+        for (int b = 0; b < BJ; ++b) {
+          const int n = n0 + qrow + 32 * b + (lane & 31);
+          if (n < N) store_y(Y, dtype, (size_t)t * N + n, y[a][b][v] * st);
+        }
+      }
+    }
+}
+
+// Few tokens: 16 channels x up to 16 IB tokens (blockIdx.y) a work-group.
+template <int GROUP, int IB>
+__global__ __launch_bounds__(512) void i8_skinny_kernel(
+    const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
+    const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y) {
+  constexpr int NW = 8, U = IB > 2 ? 2 : 4;
+  constexpr int GU = GROUP ? 64 * U / GROUP : 1;   // groups a unit
+  typedef typename std::conditional<GROUP == 0, int32_t, float>::type Sum;
+  typedef Sum Sum4 __attribute__((ext_vector_type(4)));
+  __shared__ __attribute__((aligned(16))) Sum red[NW * IB * 256];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * IB;
+  const int row = lane & 15;
+  const char* p[IB];
+#pragma unroll
+  for (int a = 0; a < IB; ++a)
+    p[a] = (const char*)Xq + (size_t)min(t0 + 16 * a + row, T - 1) * K;
+  const int n = min(n0 + row, N - 1);
+  const char* const q[1] = {(const char*)Wq + (size_t)n * K};
+  const int G = GROUP ? K / GROUP : 1;
+  const float* srow = sw + (size_t)n * G;
+  float s[2][GU];
+  Sum4 sum[IB] = {};
+  i32x4 acc[IB];
+  const bool low = lane < 32;
+  skinny_loop<IB, 1, U, NW>(
+      p, q, K, wave, lane,
+      [&](int u, int set) __attribute__((always_inline)) {
+        if constexpr (GROUP != 0) {
+#pragma unroll
+          for (int g = 0; g < GU; ++g) s[set][g] = u * GU + g < G ? srow[u * GU + g] : 0.f;
+        }
+      },
+      [&](int st, int set, const u32x4(&fp)[IB], const u32x4(&fq)[1])
+          __attribute__((always_inline)) {
+#pragma unroll
+        for (int a = 0; a < IB; ++a) {
+          if constexpr (GROUP == 0) {
+            sum[a] = Mma<kI8>::mul16(fp[a], fq[0], sum[a]);
+          } else if constexpr (GROUP == 32) {
+            // a step's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const u32x4 part = (h == 0) == low ? fp[a] : u32x4{};
+              const i32x4 c = Mma<kI8>::mul16(part, fq[0], i32x4{});
+#pragma unroll
+              for (int v = 0; v < 4; ++v)
+                sum[a][v] = fmaf((float)c[v], s[set][2 * st + h], sum[a][v]);
+            }
+          } else {
+            constexpr int SG = GROUP / 64;   // steps a group
+            acc[a] = Mma<kI8>::mul16(fp[a], fq[0], st % SG == 0 ? i32x4{} : acc[a]);
+            if (st % SG == SG - 1) {
+#pragma unroll
+              for (int v = 0; v < 4; ++v)
+                sum[a][v] = fmaf((float)acc[a][v], s[set][st / SG], sum[a][v]);
+            }
+          }
+        }
+      });
+#pragma unroll
+  for (int a = 0; a < IB; ++a) *(Sum4*)(red + (wave * IB + a) * 256 + 4 * lane) = sum[a];
+  __syncthreads();
+  for (int e = threadIdx.x; e < IB * 256; e += 512) {
+    const int j = e & 15, i = (e >> 4) & 15, a = e >> 8;
+    const int t = t0 + 16 * a + i, c = n0 + j;
+    if (t < T && c < N) {
+      float y = (float)skinny_sum<NW, IB>(red, a, i, j);
+      if (GROUP == 0) y *= sw[c];
+      store_y(Y, dtype, (size_t)t * N + c, y * sx[t]);
+    }
+  }
+}
+
+template <int GROUP>
+static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K, const int8_t* Xq,
+                                  const float* sx, const int8_t* Wq, const float* sw, void* Y) {
+  const dim3 wg((N + 15) / 16);
+  if (T <= 16) {
+    hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 1>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
+                       dtype, Y);
+  } else if (T <= 32) {
+    hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 2>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
+                       dtype, Y);
+  } else if (T <= 64) {
+    hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 4>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
+                       dtype, Y);
+  } else {
+    const int bi = (T + 255) / 256, bj = (N + 255) / 256;
+    if (GROUP == 0 && (long long)bi * bj >= 192) {
+      hipLaunchKernelGGL((i8_tile_kernel<GROUP, 2, 4, (GROUP ? 2 : 4), 2>),
+                         dim3((unsigned)(bi * bj)), dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
+                         dtype, Y, bi, bj);
+    } else {
+      const int ni = (T + 127) / 128, nj = (N + 127) / 128;
+      hipLaunchKernelGGL((i8_tile_kernel<GROUP, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
+                         dim3(256), 0, st, Xq, sx, Wq, sw, T, N, K, dtype, Y, ni, nj);
+    }
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_matmul_i8(hipStream_t st, int dtype, int T, int N, int K, int group,
+                            const int8_t* Xq, const float* sx, const int8_t* Wq, const float* sw,
+                            void* Y) {
+  switch (group) {
+    case 0: return launch_i8_group<0>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 32: return launch_i8_group<32>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 64: return launch_i8_group<64>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 128: return launch_i8_group<128>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace jarq

@@ -393,4 +393,35 @@ hipError_t launch_gptq(hipStream_t st, int rows, int cols, int g, int bits, cons
                        const float* H, char* ws, uint8_t* codes, float* scales, int32_t* zeros,
                        int** flag_out);
 
+// ---- running, training and judging refined layers ----
+// gated.hip.  dtype JARQ_F16 or JARQ_BF16, act JARQ_ACT_*.
+hipError_t launch_gated_forward(hipStream_t st, int dtype, int act, int T, int D, int F,
+                                const void* X, const void* Wg, const void* Wu, void* Y,
+                                float* pre);
+size_t gated_workspace_bytes(int T, int D, int F);   // of the backward pass
+hipError_t launch_gated_backward(hipStream_t st, int dtype, int act, int T, int D, int F,
+                                 const void* X, const void* Wg, const void* Wu, const void* dY,
+                                 const float* pre, void* dX, void* dWg, void* dWu, char* ws);
+
+// i8.hip
+hipError_t launch_quant_rows(hipStream_t st, int dtype, const void* X, int rows, int K, int8_t* Q,
+                             float* scale);
+// bad[0] becomes 1 if a code minus its zero point is outside int8, else 0
+hipError_t launch_codes_i8(hipStream_t st, const uint8_t* codes, const int32_t* zeros, int rows,
+                           int cols, int g, int8_t* out, int32_t* bad);
+hipError_t launch_matmul_i8(hipStream_t st, int dtype, int T, int N, int K, int group,
+                            const int8_t* Xq, const float* sx, const int8_t* Wq, const float* sw,
+                            void* Y);
+
+// logprob.hip
+size_t logprob_workspace_bytes(int T, int V, int top);
+hipError_t launch_token_logprobs(hipStream_t st, int dtype, const void* logits, size_t ld, int T,
+                                 int V, const int64_t* targets, int top, float* logprob,
+                                 float* entropy, float* lse, int32_t* top_index,
+                                 float* top_logprob, char* ws);
+hipError_t launch_token_logprobs_backward(hipStream_t st, int dtype, const void* logits, size_t ld,
+                                          int T, int V, const int64_t* targets, const float* lse,
+                                          const float* entropy, const float* dlp,
+                                          const float* dent, void* dlogits, size_t ldd);
+
 }  // namespace jarq
