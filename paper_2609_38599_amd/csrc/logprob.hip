@@ -53,11 +53,13 @@ __device__ __forceinline__ Soft no_entries() { return Soft{-FLT_MAX, 0.f, 0.f}; 
 // Keeps exp's argument within range for the weighted sum: exp is 0 there.
 constexpr float kLeast = -1000.f;
 
+// Adds entries; returns the largest.
 template <int DT, int N>
-__device__ __forceinline__ void add(Soft& s, const float (&x)[N]) {
-  float m = s.m;
+__device__ __forceinline__ float add(Soft& s, const float (&x)[N]) {
+  float most = x[0];
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+  for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+  const float m = fmaxf(s.m, most);
   if (m > s.m) {
     const float t = s.m - m, e = exp_of<DT>(t);
     s.zt = e * (s.zt + s.z * fmaxf(t, kLeast));
@@ -70,6 +72,7 @@ __device__ __forceinline__ void add(Soft& s, const float (&x)[N]) {
     s.z += e;
     s.zt = fmaf(e, fmaxf(t, kLeast), s.zt);
   }
+  return most;
 }
 __device__ __forceinline__ void join(Soft& s, const Soft& o) {
   const float m = fmaxf(s.m, o.m);
@@ -91,14 +94,111 @@ __device__ __forceinline__ float key_value(u64 k) {
 }
 __device__ __forceinline__ uint32_t key_index(u64 k) { return 0xffffffffu - (uint32_t)k; }
 
-__device__ __forceinline__ u64 wave_max(u64 k) {
+
+__device__ __forceinline__ uint32_t ordered(float x) { return (uint32_t)(top_key(x, 0) >> 32); }
+constexpr uint32_t kOrderedMinusInf = 0x007fffffu;
+
+// Entries of a wave (R a lane) that are at least `t`.
+template <int R>
+__device__ __forceinline__ int count_from(const uint32_t (&v)[R], uint32_t t) {
+  int c = 0;
 #pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) {
-    const u64 o = __shfl_xor(k, off);
-    k = o > k ? o : k;
-  }
-  return k;
+  for (int r = 0; r < R; ++r) c += __popcll(__ballot(v[r] >= t));
+  return c;
 }
+// The largest value, of `bits` leading bits and zeros behind, that at least k of a
+// wave's entries reach; 0 if there are fewer.
+template <int R>
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[R], int k, int bits) {
+  uint32_t t = 0;
+  for (int b = 31; b >= 32 - bits; --b)
+    if (count_from<R>(v, t | (1u << b)) >= k) t |= 1u << b;
+  return t;
+}
+
+// A wave's candidates for the top k: keys in LDS, cut back to the k largest when
+// more than kKeep are there.  A lane's entries are offered eight at a time.
+constexpr int kKeep = 128;
+template <int VE>
+struct TopList {
+  static constexpr int kCap = kKeep + 64 * VE;
+  u64* keys;          // of this wave
+  uint32_t* slots;    // one a wave: a value that ceil(k / 4) of its entries reach
+  int n, k, wave;
+  u64 kth;            // the k-th largest key when the list was last cut
+  float bound;        // a value that k entries of the row reach
+
+  __device__ __forceinline__ void init(u64* keys_, uint32_t* slots_, int k_, int w) {
+    keys = keys_;
+    slots = slots_;
+    k = k_;
+    wave = w;
+    n = 0;
+    kth = 0;
+    bound = -INFINITY;
+  }
+  // From the lanes' largest entries so far: the four waves' slots together name a
+  // value that k entries of the row reach (a slot read late is only lower).
+  __device__ __forceinline__ void raise(float lane_max, int lane) {
+    const uint32_t v[1] = {ordered(lane_max)};
+    // 16 bits: lower than the value by less than a bf16 step
+    const uint32_t mine = max(reached_by<1>(v, (k + 3) / 4, 16), kOrderedMinusInf);
+    if (lane == 0) ((volatile uint32_t*)slots)[wave] = mine;
+    uint32_t least = mine;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) least = min(least, ((volatile uint32_t*)slots)[w]);
+    bound = fmaxf(bound, key_value((u64)least << 32));
+  }
+  __device__ __forceinline__ void offer(const float (&x)[VE], float most, int i0, int lane) {
+    if (__ballot(most >= bound) == 0) return;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      if (__ballot(x[i] >= bound) == 0) continue;
+      const u64 key = top_key(x[i], (uint32_t)(i0 + i));
+      const bool hit = x[i] >= bound && key > kth;
+      const u64 mask = __ballot(hit);
+      if (hit) keys[n + __popcll(mask & ((1ull << lane) - 1))] = key;
+      n += __popcll(mask);
+    }
+    if (n > kKeep) cut(lane);
+  }
+  __device__ __forceinline__ void cut(int lane) {
+    constexpr int R = kCap / 64;
+    if (n <= k) return;
+    asm volatile("" ::: "memory");   // one wave: its LDS accesses complete in order
+    uint32_t hi[R], lo[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const int at = 64 * r + lane;
+      const u64 key = at < n ? keys[at] : 0;
+      hi[r] = (uint32_t)(key >> 32);
+      lo[r] = (uint32_t)key;
+    }
+    const uint32_t v = reached_by<R>(hi, k, 32);
+    // among the entries of value v, those of the lowest indices
+    int above = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      above += __popcll(__ballot(hi[r] > v));
+      if (hi[r] != v) lo[r] = hi[r] > v ? 0xffffffffu : 0u;
+    }
+    const uint32_t l = reached_by<R>(lo, k, 32);
+    int m = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool keep = hi[r] > v || (hi[r] == v && lo[r] >= l);
+      const u64 mask = __ballot(keep);
+      // (a key above v is found again from its LDS place)
+      const u64 key = keep ? keys[64 * r + lane] : 0;
+      if (keep) keys[m + __popcll(mask & ((1ull << lane) - 1))] = key;
+      m += __popcll(mask);
+    }
+    asm volatile("" ::: "memory");
+    n = m;
+    kth = ((u64)v << 32) | l;
+    bound = fmaxf(bound, key_value((u64)v << 32));
+  }
+};
 
 struct RowOut {
   float *logprob, *entropy, *lse, *top_logprob;
@@ -132,7 +232,7 @@ __device__ __forceinline__ void store_top(const RowOut& o, size_t at, u64 key, c
 
 // Work-group `id`: part id % splits (of `each` entries) of row id / splits.  With one
 // part it finishes the row; otherwise its sums and top keys go to the workspace.
-template <int DT>
+template <int DT, bool TOP>
 __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ logits, size_t ld,
                                                       int V, const int64_t* __restrict__ targets,
                                                       int splits, int each, int top, RowOut out,
@@ -140,9 +240,13 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
                                                       u64* __restrict__ pkey) {
   typedef typename Elem<DT>::T E;
   constexpr int VE = Elem<DT>::kVec;
+  typedef TopList<VE> List;
   __shared__ Soft red[4];
-  __shared__ u64 best[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ u64 keys[TOP ? 4 * List::kCap : 1];
+  __shared__ uint32_t slots[4];
+  __shared__ int counts[4];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const size_t t = blockIdx.x / (unsigned)splits;
   const int part = blockIdx.x % (unsigned)splits;
   const E* row = (const E*)logits + t * ld;
@@ -154,14 +258,44 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   const int own = tid < head ? b + tid : rest + tid - head;   // this thread's scalar, if any
   const bool has = tid < head || own < e;
   Soft s = no_entries();
-  if (has) {
-    const float x[1] = {value<DT>(row[own])};
-    add<DT>(s, x);
+  List list;
+  if constexpr (TOP) {
+    list.init(keys + wave * List::kCap, slots, top, wave);
+    if (tid < 4) slots[tid] = kOrderedMinusInf;
+    __syncthreads();
   }
-  for (int v = tid; v < nv; v += 256) {
+  // (every lane of a wave stays in the loop, for the list's votes)
+  int round = 0;
+  for (int v0 = 64 * wave; v0 < nv; v0 += 256, ++round) {
+    const int v = v0 + lane;
     float x[VE];
-    unpack<DT>(vec[v], x);
+    if (v < nv) {
+      unpack<DT>(vec[v], x);
+    } else {
+#pragma unroll
+      for (int i = 0; i < VE; ++i) x[i] = -INFINITY;
+    }
+    const float most = add<DT>(s, x);
+    if constexpr (TOP) {
+      // rounds 0, 1, 3, 7, ..: as many entries again are in
+      if ((round & (round + 1)) == 0) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
+      if (v0 + 64 > nv) {
+#pragma unroll
+        for (int i = 0; i < VE; ++i) x[i] = v < nv ? x[i] : __uint_as_float(0x7fc00000u);
+      }
+      list.offer(x, v < nv ? most : __uint_as_float(0x7fc00000u), b + head + v * VE, lane);
+    }
+  }
+  if (wave == 0) {
+    const float x[1] = {has ? value<DT>(row[own]) : -INFINITY};
     add<DT>(s, x);
+    if constexpr (TOP) {
+      float y[VE];
+      y[0] = has ? x[0] : __uint_as_float(0x7fc00000u);
+#pragma unroll
+      for (int i = 1; i < VE; ++i) y[i] = __uint_as_float(0x7fc00000u);
+      list.offer(y, y[0], own, lane);
+    }
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
@@ -172,6 +306,10 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
     join(s, o);
   }
   if (lane == 0) red[wave] = s;
+  if constexpr (TOP) {
+    if (list.n > 64) list.cut(lane);
+    if (lane == 0) counts[wave] = list.n;
+  }
   __syncthreads();
   s = red[0];
 #pragma unroll
@@ -185,44 +323,43 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
     p[1] = s.z;
     p[2] = s.zt;
   }
-  u64 last = ~0ull;
-  for (int k = 0; k < top; ++k) {
-    u64 mine = 0;
-    auto look = [&](float x, int i) {
-      const u64 key = top_key(x, (uint32_t)i);
-      if (key < last && key > mine) mine = key;
-    };
-    if (has) look(value<DT>(row[own]), own);
-    for (int v = tid; v < nv; v += 256) {
-      float x[VE];
-      unpack<DT>(vec[v], x);
-#pragma unroll
-      for (int i = 0; i < VE; ++i) look(x[i], b + head + v * VE + i);
+  if constexpr (TOP) {
+    // a key's place is the number of larger ones in the four lists
+    const u64 mine = lane < list.n ? list.keys[lane] : 0;
+    int place = 0, total = 0;
+    for (int w = 0; w < 4; ++w) {
+      const int m = counts[w];
+      total += m;
+      for (int i = 0; i < m; ++i) place += keys[w * List::kCap + i] > mine;
     }
-    mine = wave_max(mine);
-    if (lane == 0) best[wave] = mine;
-    __syncthreads();
-    last = best[0];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) last = best[w] > last ? best[w] : last;
-    __syncthreads();
-    if (tid == 0) {
-      if (splits == 1) store_top(out, t * top + k, last, s, lz);
-      else pkey[(size_t)blockIdx.x * top + k] = last;   // 0 where the part has fewer entries
+    const bool bad = s.z != s.z;
+    if (splits == 1) {
+      if (bad) {
+        if (tid < top) store_top(out, t * top + tid, 0, s, lz);
+      } else if (lane < list.n && place < top) {
+        store_top(out, t * top + place, mine, s, lz);
+      }
+    } else {
+      u64* to = pkey + (size_t)blockIdx.x * top;
+      if (lane < list.n && place < top) to[place] = mine;
+      if (tid >= total && tid < top) to[tid] = 0;   // a part of fewer entries
     }
   }
 }
 
-// A work-group a row: its parts' sums in order, the top of their keys.
+// A work-group a row: its parts' sums in order, the top of their keys (at most 256).
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_join_kernel(
     const void* __restrict__ logits, size_t ld, int V, const int64_t* __restrict__ targets,
     int splits, int top, RowOut out, const float* __restrict__ psum,
     const u64* __restrict__ pkey) {
   typedef typename Elem<DT>::T E;
-  __shared__ u64 best[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  __shared__ u64 keys[256];
+  const int tid = threadIdx.x;
   const size_t t = blockIdx.x;
+  const int n = splits * top;
+  const u64 mine = tid < n ? pkey[t * n + tid] : 0;
+  keys[tid] = mine;
   Soft s = no_entries();
   for (int p = 0; p < splits; ++p) {
     const float* q = psum + 3 * (t * splits + p);
@@ -234,23 +371,14 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
   }
   const float lz = logf(s.z);
   if (tid == 0) finish_row<DT>(s, (const E*)logits + t * ld, targets[t], V, t, lz, out);
-  u64 last = ~0ull;
-  const u64* keys = pkey + t * splits * top;
-  for (int k = 0; k < top; ++k) {
-    u64 mine = 0;
-    for (int i = tid; i < splits * top; i += 256) {
-      const u64 key = keys[i];
-      if (key < last && key > mine) mine = key;
-    }
-    mine = wave_max(mine);
-    if (lane == 0) best[wave] = mine;
-    __syncthreads();
-    last = best[0];
-#pragma unroll
-    for (int w = 1; w < 4; ++w) last = best[w] > last ? best[w] : last;
-    __syncthreads();
-    if (tid == 0) store_top(out, t * top + k, last, s, lz);
+  __syncthreads();
+  if (s.z != s.z) {
+    if (tid < top) store_top(out, t * top + tid, 0, s, lz);
+    return;
   }
+  int place = 0;
+  for (int i = 0; i < n; ++i) place += keys[i] > mine;
+  if (mine != 0 && place < top) store_top(out, t * top + place, mine, s, lz);
 }
 
 // ---- gradient ----
@@ -266,7 +394,8 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(
   typedef typename Elem<DT>::T E;
   constexpr int VE = Elem<DT>::kVec;
   const int tid = threadIdx.x;
-  const size_t t = blockIdx.x / (unsigned)splits;
+  // the last rows first: what the forward pass read last may still be cached
+  const size_t t = (gridDim.x - 1 - blockIdx.x) / (unsigned)splits;
   const int b = (int)(blockIdx.x % (unsigned)splits) * each, e = min(V, b + each);
   const E* row = (const E*)logits + t * ld;
   E* drow = (E*)dlogits + t * ldd;
@@ -316,12 +445,14 @@ namespace {
 struct LogprobPlan {
   int splits, each;
 };
-LogprobPlan logprob_plan(int T, int V) {
+LogprobPlan logprob_plan(int T, int V, int top) {
   LogprobPlan p;
   int splits = 512 / T;
   const int most = V / 4096;
   splits = splits < 1 || most < 1 ? 1 : splits > most ? most : splits;
-  if (splits > 64) splits = 64;
+  // the joining work-group takes a key a thread
+  const int cap = top > 4 ? 256 / top : 64;
+  if (splits > cap) splits = cap;
   p.each = ((V + splits - 1) / splits + 63) / 64 * 64;
   p.splits = (V + p.each - 1) / p.each;
   return p;
@@ -330,11 +461,16 @@ LogprobPlan logprob_plan(int T, int V) {
 template <int DT>
 hipError_t logprob_kind(hipStream_t st, const void* logits, size_t ld, int T, int V,
                         const int64_t* targets, int top, const RowOut& out, char* ws) {
-  const LogprobPlan p = logprob_plan(T, V);
+  const LogprobPlan p = logprob_plan(T, V, top);
   u64* pkey = (u64*)ws;
   float* psum = (float*)(ws + 8 * (size_t)T * p.splits * top);
-  hipLaunchKernelGGL((logprob_kernel<DT>), dim3((unsigned)(T * p.splits)), dim3(256), 0, st,
-                     logits, ld, V, targets, p.splits, p.each, top, out, psum, pkey);
+  const dim3 grid((unsigned)(T * p.splits));
+  if (top > 0)
+    hipLaunchKernelGGL((logprob_kernel<DT, true>), grid, dim3(256), 0, st, logits, ld, V, targets,
+                       p.splits, p.each, top, out, psum, pkey);
+  else
+    hipLaunchKernelGGL((logprob_kernel<DT, false>), grid, dim3(256), 0, st, logits, ld, V, targets,
+                       p.splits, p.each, top, out, psum, pkey);
   if (p.splits > 1) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -348,7 +484,7 @@ template <int DT>
 hipError_t logprob_grad_kind(hipStream_t st, const void* logits, size_t ld, int T, int V,
                              const int64_t* targets, const float* lse, const float* entropy,
                              const float* dlp, const float* dent, void* dlogits, size_t ldd) {
-  const LogprobPlan p = logprob_plan(T, V);
+  const LogprobPlan p = logprob_plan(T, V, 0);
   hipLaunchKernelGGL((logprob_grad_kernel<DT>), dim3((unsigned)(T * p.splits)), dim3(256), 0, st,
                      logits, ld, V, targets, lse, entropy, dlp, dent, p.splits, p.each, dlogits,
                      ldd);
@@ -358,7 +494,7 @@ hipError_t logprob_grad_kind(hipStream_t st, const void* logits, size_t ld, int 
 }  // namespace
 
 size_t logprob_workspace_bytes(int T, int V, int top) {
-  const LogprobPlan p = logprob_plan(T, V);
+  const LogprobPlan p = logprob_plan(T, V, top);
   return p.splits == 1 ? 0 : (size_t)T * p.splits * (8 * (size_t)top + 12);
 }
 
