@@ -9,6 +9,8 @@
 // to 16 bits as the matrix cores take them (the only rounding beside the
 // outputs'); then dx = [da db] [Wg; Wu] in one product over 2 F, and
 // [dWg; dWu] = [da db]^T x in one over T.
+#include <type_traits>
+
 #include "skinny.h"
 
 namespace jarq {
@@ -23,7 +25,7 @@ constexpr float kSqrt2OverPi = 0.79788456080286536f;
 template <int ACT>
 __device__ __forceinline__ float activation(float a, float* d) {
   if constexpr (ACT == 0) {          // silu
-    const float sig = 1.f / (1.f + __expf(-a));
+    const float sig = __builtin_amdgcn_rcpf(1.f + __expf(-a));   // to an ulp
     if (d) *d = sig * (1.f + a * (1.f - sig));
     return a * sig;
   } else if constexpr (ACT == 1) {   // gelu
@@ -54,11 +56,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre, int ni, int nj) {
   constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
-  typedef KContig<TI, NW, true> LP;
-  typedef KContig<TJ, NW, false> LQ;
+  typedef KContig<TI, NW, kRowHalves> LP;
+  typedef KContig<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
   __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
   __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -71,38 +75,58 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
   lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
   f32x16 acc[BI][BJ] = {};
   // block a < BI / 2: Wg, the others: Wu of the same channels
-  auto prow = [&](int a) {
-    return a < BI / 2 ? wi * 16 * BI + 32 * a : TI / 2 + wi * 16 * BI + 32 * (a - BI / 2);
-  };
-  mma_loop(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, buf0, buf1,
-           [&](const char* cur, int) __attribute__((always_inline)) {
-             mma_chunk<KIND, BI, BJ, LP, LQ>(cur, lane, prow, wj * 32 * BJ, acc);
-           });
+  mma_loop<BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 32 * BJ,
+                   buf0, buf1, buf2, buf3, [](int) {},
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                       __attribute__((always_inline)) {
+                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                       });
+  // Out through LDS, so that memory gets whole lines (8 bytes a lane straight from the
+  // registers: 75 us more of 800 at 4096 x 4096 -> 14336).  The waves of one wj share a
+  // stage of 32 BJ tokens.
+  char* const stage = wj == 0 ? buf0 : wj == 1 ? buf1 : wj == 2 ? buf2 : buf3;
+  const int row = lane & 31, tw = t0 + wj * 32 * BJ;
+  auto send = [&](auto* to, auto put) __attribute__((always_inline)) {
+    typedef typename std::remove_reference<decltype(*to)>::type E;
+    constexpr int RB = TI / 2 * sizeof(E), PIECES = RB / 16;
+    static_assert(32 * BJ * RB <= STAGE, "stage");
 #pragma unroll
-  for (int b = 0; b < BJ; ++b) {
-    const int t = t0 + wj * 32 * BJ + 32 * b + (lane & 31);
+    for (int b = 0; b < BJ; ++b)
 #pragma unroll
-    for (int a = 0; a < BI / 2; ++a)
+      for (int a = 0; a < BI / 2; ++a)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int f = f0 + wi * 16 * BI + 32 * a + 8 * r + 4 * (lane >> 5);
-        if (t < T && f < F) {
-          f32x4 g, u, y;
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            g[v] = acc[a][b][4 * r + v];
-            u[v] = acc[BI / 2 + a][b][4 * r + v];
-            y[v] = activation(act, g[v], nullptr) * u[v];
-          }
-          const size_t e = (size_t)t * F + f;
-          *(u32x2*)(Y + e) = u32x2{pack16<KIND>(y[0], y[1]), pack16<KIND>(y[2], y[3])};
-          if (pre) {
-            *(f32x4*)(pre + e) = g;
-            *(f32x4*)(pre + (size_t)T * F + e) = u;
-          }
+        for (int r = 0; r < 4; ++r) {
+          const int at = (wi * 16 * BI + 32 * a + 8 * r + 4 * (lane >> 5)) * (int)sizeof(E);
+          put(out_piece<RB>(stage, 32 * b + row, at >> 4) + (at & 15), a, b, 4 * r);
         }
-      }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 32 * BJ * PIECES / (WI * 64); ++k) {
+      const int p = (k * WI + wi) * 64 + lane;
+      const int t = p / PIECES, c = p % PIECES;
+      const u32x4 w = *(const u32x4*)out_piece<RB>(stage, t, c);
+      const int f = f0 + c * (16 / (int)sizeof(E));
+      if (tw + t < T && f < F) *(u32x4*)(to + (size_t)(tw + t) * F + f) = w;
+    }
+  };
+  if (pre) {   // uniform
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      send(pre + (size_t)half * T * F, [&](char* at, int a, int b, int v)
+                                           __attribute__((always_inline)) {
+        const f32x16& c = acc[half * BI / 2 + a][b];
+        *(f32x4*)at = f32x4{c[v], c[v + 1], c[v + 2], c[v + 3]};
+      });
+      __syncthreads();
+    }
   }
+  send(Y, [&](char* at, int a, int b, int v) __attribute__((always_inline)) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      y[i] = activation(act, acc[a][b][v + i], nullptr) * acc[BI / 2 + a][b][v + i];
+    *(u32x2*)at = u32x2{pack16<KIND>(y[0], y[1]), pack16<KIND>(y[2], y[3])};
+  });
 }
 
 // ---- forward, few tokens ----
@@ -232,6 +256,32 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const float* __restrict
   }
 }
 
+// A tile's sums as 16-bit values: store(j, i, w) gets eight of them from row j of the
+// 32 BJ that the WI waves of one wj share a stage for, columns i .. of the tile.
+template <int KIND, int WI, int BI, int BJ, class Store>
+__device__ __forceinline__ void store_tile16(const f32x16 (&acc)[BI][BJ], char* stage, int wi,
+                                             int lane, const Store& store) {
+  constexpr int RB = 2 * 32 * WI * BI, PIECES = RB / 16;
+#pragma unroll
+  for (int b = 0; b < BJ; ++b)
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int at = 2 * (wi * 32 * BI + 32 * a + 8 * r + 4 * (lane >> 5));
+        const f32x16& c = acc[a][b];
+        *(u32x2*)(out_piece<RB>(stage, 32 * b + (lane & 31), at >> 4) + (at & 15)) =
+            u32x2{pack16<KIND>(c[4 * r], c[4 * r + 1]), pack16<KIND>(c[4 * r + 2], c[4 * r + 3])};
+      }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 32 * BJ * PIECES / (WI * 64); ++k) {
+    const int p = (k * WI + wi) * 64 + lane;
+    const int j = p / PIECES, c = p % PIECES;
+    store(j, 8 * c, *(const u32x4*)out_piece<RB>(stage, j, c));
+  }
+}
+
 // ---- backward: dx = dab [Wg; Wu] ----
 // part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.
 template <int KIND, int WI, int WJ, int BI, int BJ>
@@ -239,11 +289,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
     const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int each, uint16_t* __restrict__ dX, float* __restrict__ part, int ni, int nj) {
   constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
-  typedef KStrided<TI, NW> LP;
-  typedef KContig<TJ, NW, false> LQ;
+  typedef KStrided<TI, NW, kTwoSpans> LP;
+  typedef KContig<TJ, NW, kTwoSpans> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
   __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
   __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -252,36 +304,39 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
   const int d0 = ti * TI, t0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init(Wg, Wu, 2 * (size_t)D, d0, D, 2 * F, F, wave, lane);
-  lq.init(dab, dab, 4 * (size_t)F, t0, T, 4 * F, wave, lane);
+  lp.init(Wg, Wu, 2 * (size_t)D, d0, D, F, wave, lane);
+  lq.init(dab, (const uint16_t*)dab + F, 4 * (size_t)F, t0, T, 2 * F, wave, lane);
   f32x16 acc[BI][BJ] = {};
-  const int nk = (2 * F + 63) / 64;
+  const int nk = 2 * ((2 * F + kChunk - 1) / kChunk);
   const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
-  auto prow = [&](int a) { return wi * 32 * BI + 32 * a; };
-  mma_loop(lp, lq, q0, q1, buf0, buf1,
-           [&](const char* cur, int) __attribute__((always_inline)) {
-             mma_chunk<KIND, BI, BJ, LP, LQ>(cur, lane, prow, wj * 32 * BJ, acc);
-           });
+  mma_loop<BI, BJ>(lp, lq, q0, q1, lane, wi * 32 * BI, wj * 32 * BJ, buf0, buf1, buf2, buf3,
+                   [](int) {},
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                       __attribute__((always_inline)) {
+                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                       });
+  if (part) {   // uniform
 #pragma unroll
-  for (int b = 0; b < BJ; ++b) {
-    const int t = t0 + wj * 32 * BJ + 32 * b + (lane & 31);
+    for (int b = 0; b < BJ; ++b) {
+      const int t = t0 + wj * 32 * BJ + 32 * b + (lane & 31);
 #pragma unroll
-    for (int a = 0; a < BI; ++a)
+      for (int a = 0; a < BI; ++a)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = d0 + prow(a) + 8 * r + 4 * (lane >> 5);
-        if (t < T && d < D) {
+        for (int r = 0; r < 4; ++r) {
+          const int d = d0 + wi * 32 * BI + 32 * a + 8 * r + 4 * (lane >> 5);
           const f32x16& c = acc[a][b];
-          if (part) {
+          if (t < T && d < D)
             *(f32x4*)(part + ((size_t)blockIdx.y * T + t) * D + d) =
                 f32x4{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
-          } else {
-            *(u32x2*)(dX + (size_t)t * D + d) = u32x2{pack16<KIND>(c[4 * r], c[4 * r + 1]),
-                                                      pack16<KIND>(c[4 * r + 2], c[4 * r + 3])};
-          }
         }
-      }
+    }
+    return;
   }
+  char* const stage = wj == 0 ? buf0 : wj == 1 ? buf1 : wj == 2 ? buf2 : buf3;
+  const int tw = t0 + wj * 32 * BJ;
+  store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
+    if (tw + t < T && d0 + i < D) *(u32x4*)(dX + (size_t)(tw + t) * D + d0 + i) = w;
+  });
 }
 
 template <int KIND>
@@ -302,11 +357,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
     const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,
     uint16_t* __restrict__ dWg, uint16_t* __restrict__ dWu, int ni, int nj) {
   constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
-  typedef KStrided<TI, NW> LP;
-  typedef KStrided<TJ, NW> LQ;
+  typedef KStrided<TI, NW, kOne> LP;
+  typedef KStrided<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
   __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
   __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -315,31 +372,23 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
   const int d0 = ti * TI, f0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init(X, X, 2 * (size_t)D, d0, D, T, T, wave, lane);
-  lq.init(dab, dab, 4 * (size_t)F, f0, 2 * F, T, T, wave, lane);
+  lp.init(X, X, 2 * (size_t)D, d0, D, T, wave, lane);
+  lq.init(dab, dab, 4 * (size_t)F, f0, 2 * F, T, wave, lane);
   f32x16 acc[BI][BJ] = {};
-  auto prow = [&](int a) { return wi * 32 * BI + 32 * a; };
-  mma_loop(lp, lq, 0, (T + 63) / 64, buf0, buf1,
-           [&](const char* cur, int) __attribute__((always_inline)) {
-             mma_chunk<KIND, BI, BJ, LP, LQ>(cur, lane, prow, wj * 32 * BJ, acc);
-           });
-#pragma unroll
-  for (int b = 0; b < BJ; ++b) {
-    const int f = f0 + wj * 32 * BJ + 32 * b + (lane & 31);
+  mma_loop<BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 32 * BI, wj * 32 * BJ,
+                   buf0, buf1, buf2, buf3, [](int) {},
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                       __attribute__((always_inline)) {
+                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                       });
+  char* const stage = wj == 0 ? buf0 : wj == 1 ? buf1 : wj == 2 ? buf2 : buf3;
+  const int fw = f0 + wj * 32 * BJ;
+  store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int r, int i, const u32x4& w) {
+    const int f = fw + r;
     uint16_t* out = f < F ? dWg : dWu;
-    const size_t row = (size_t)(f < F ? f : f - F) * D;
-#pragma unroll
-    for (int a = 0; a < BI; ++a)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = d0 + prow(a) + 8 * r + 4 * (lane >> 5);
-        if (f < 2 * F && d < D && out) {
-          const f32x16& c = acc[a][b];
-          *(u32x2*)(out + row + d) = u32x2{pack16<KIND>(c[4 * r], c[4 * r + 1]),
-                                           pack16<KIND>(c[4 * r + 2], c[4 * r + 3])};
-        }
-      }
-  }
+    if (f < 2 * F && d0 + i < D && out)
+      *(u32x4*)(out + (size_t)(f < F ? f : f - F) * D + d0 + i) = w;
+  });
 }
 
 namespace {
@@ -352,7 +401,7 @@ struct DxPlan {
 // 2 F cut so that about two work-groups fall on each CU.
 DxPlan dx_plan(int T, int D, int F) {
   DxPlan p;
-  const int nk = (2 * F + 63) / 64;
+  const int nk = 2 * ((2 * F + kChunk - 1) / kChunk);
   p.big = (long long)((D + 255) / 256) * ((T + 255) / 256) >= 192;
   const int e = p.big ? 256 : 128;
   p.ni = (D + e - 1) / e;
@@ -360,10 +409,10 @@ DxPlan dx_plan(int T, int D, int F) {
   int splits = 1;
   if (!p.big) {
     splits = 512 / (p.ni * p.nj);
-    splits = splits < 1 ? 1 : splits > nk / 4 ? (nk / 4 < 1 ? 1 : nk / 4) : splits;
+    splits = splits < 1 ? 1 : splits > nk / 8 ? (nk / 8 < 1 ? 1 : nk / 8) : splits;
     if (splits > 32) splits = 32;
   }
-  p.each = (nk + splits - 1) / splits;
+  p.each = ((nk + splits - 1) / splits + 3) / 4 * 4;   // whole rounds of stages
   p.splits = (nk + p.each - 1) / p.each;
   return p;
 }

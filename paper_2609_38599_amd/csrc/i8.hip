@@ -7,6 +7,8 @@
 // integer sums exact in int32 on v_mfma_i32_32x32x32_i8, a group's sum converted
 // and added in fp32.  Tokens are the P rows and channels the Q rows, so that a lane
 // holds one channel and needs one group scale.
+#include <type_traits>
+
 #include "skinny.h"
 
 namespace jarq {
@@ -159,18 +161,20 @@ __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) 
 }  // namespace
 
 // Many tokens.  GROUP 0: one scale a channel, int32 sums over all of k; otherwise a
-// group's int32 sums (its k-slices of 32, within a chunk of 128) go to fp32.
+// group's int32 sums go to fp32.
 template <int GROUP, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
     const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y, int ni,
     int nj) {
   constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
-  typedef KContig<TI, NW, false> LP;
-  typedef KContig<TJ, NW, false> LQ;
+  typedef KContig<TI, NW, kOne> LP;
+  typedef KContig<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
   __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
   __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
+  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -181,76 +185,98 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   LQ lq;
   lp.init(Xq, Xq, K, t0, T, K, wave, lane);
   lq.init(Wq, Wq, K, n0, N, K, wave, lane);
-  auto prow = [&](int a) { return wi * 32 * BI + 32 * a; };
-  const int nk = (K + kChunk - 1) / kChunk, qrow = wj * 32 * BJ;
-  f32x16 y[BI][BJ];
+  const int nk = (K + kChunk - 1) / kChunk, prow = wi * 32 * BI, qrow = wj * 32 * BJ;
+  f32x16 y[GROUP ? BI : 1][GROUP ? BJ : 1] = {};
+  i32x16 acc[BI][BJ] = {};
   const int G = GROUP ? K / GROUP : 1;
   const float* srow[BJ];
 #pragma unroll
   for (int b = 0; b < BJ; ++b)
     srow[b] = sw + (size_t)min(n0 + qrow + 32 * b + (lane & 31), N - 1) * G;
   if constexpr (GROUP == 0) {
-    i32x16 acc[BI][BJ] = {};
-    mma_loop(lp, lq, 0, nk, buf0, buf1, [&](const char* cur, int) __attribute__((always_inline)) {
-      mma_chunk<kI8, BI, BJ, LP, LQ>(cur, lane, prow, qrow, acc);
-    });
-#pragma unroll
-    for (int a = 0; a < BI; ++a)
+    mma_loop<BI, BJ>(lp, lq, 0, nk, lane, prow, qrow, buf0, buf1, buf2, buf3, [](int) {},
+                     [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                         __attribute__((always_inline)) {
+                           acc[a][b] = Mma<kI8>::mul(p, q, acc[a][b]);
+                         });
+  } else {
+    constexpr int GR = 4 * kChunk / GROUP;   // groups a round
+    constexpr int SG = GROUP / 32;           // k-slices a group
+    // the scales a round ahead of their use; past the last group 0
+    float s[GR][BJ], ahead[GR][BJ];
+    auto fetch = [&](int g0) __attribute__((always_inline)) {
 #pragma unroll
       for (int b = 0; b < BJ; ++b)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) y[a][b][v] = (float)acc[a][b][v] * srow[b][0];
-  } else {
-    constexpr int GC = kChunk / GROUP;   // groups a chunk
-    constexpr int KG = 4 / GC;           // k-slices a group
+        for (int g = 0; g < GR; ++g) ahead[g][b] = g0 + g < G ? srow[b][g0 + g] : 0.f;
+    };
+    fetch(0);
+    mma_loop<BI, BJ>(
+        lp, lq, 0, nk, lane, prow, qrow, buf0, buf1, buf2, buf3,
+        [&](int q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int a = 0; a < BI; ++a)
+          for (int g = 0; g < GR; ++g)
 #pragma unroll
-      for (int b = 0; b < BJ; ++b) y[a][b] = f32x16{};
-    mma_loop(lp, lq, 0, nk, buf0, buf1,
-             [&](const char* cur, int q) __attribute__((always_inline)) {
+            for (int b = 0; b < BJ; ++b) s[g][b] = ahead[g][b];
+          fetch((q / 4 + 1) * GR);
+        },
+        [&](const u32x4& p, const u32x4& q, int a, int b, int ks, int i)
+            __attribute__((always_inline)) {
+          const int slice = 2 * i + ks;
+          acc[a][b] = Mma<kI8>::mul(p, q, slice % SG == 0 ? i32x16{} : acc[a][b]);
+          if (slice % SG == SG - 1) {
 #pragma unroll
-      for (int g = 0; g < GC; ++g) {
-        // (a last chunk may hold fewer groups; what it stages past k is zeros)
-        float s[BJ];
-#pragma unroll
-        for (int b = 0; b < BJ; ++b) s[b] = q * GC + g < G ? srow[b][q * GC + g] : 0.f;
-        u32x4 fp[BI][KG], fq[BJ][KG];
-#pragma unroll
-        for (int k = 0; k < KG; ++k) {
-#pragma unroll
-          for (int a = 0; a < BI; ++a) fp[a][k] = LP::frag(cur, prow(a), g * KG + k, lane);
-#pragma unroll
-          for (int b = 0; b < BJ; ++b)
-            fq[b][k] = LQ::frag(cur + LP::kBytes, qrow + 32 * b, g * KG + k, lane);
-        }
-#pragma unroll
-        for (int a = 0; a < BI; ++a)
-#pragma unroll
-          for (int b = 0; b < BJ; ++b) {
-            i32x16 acc = {};
-#pragma unroll
-            for (int k = 0; k < KG; ++k) acc = Mma<kI8>::mul(fp[a][k], fq[b][k], acc);
-#pragma unroll
-            for (int v = 0; v < 16; ++v) y[a][b][v] = fmaf((float)acc[v], s[b], y[a][b][v]);
+            for (int v = 0; v < 16; ++v)
+              y[a][b][v] = fmaf((float)acc[a][b][v], s[slice / SG][b], y[a][b][v]);
           }
-      }
-    });
+        });
   }
+  // Out through LDS, 32 tokens x 32 BJ channels of a wave at a time.
+  constexpr int CH = 32 * BJ;
+  static_assert(NW / 2 * 32 * CH * 4 <= STAGE, "stage");
+  char* const mine = (wave < NW / 2 ? buf0 : buf1) + wave % (NW / 2) * 32 * CH * 4;
+  const int nw = n0 + qrow;
+  const size_t es = dtype == 0 ? 4 : 2;
+  // 16-byte stores where every row starts at a 16-byte boundary and none ends inside a piece
+  const bool wide = (uintptr_t)Y % 16 == 0 && (size_t)N * es % 16 == 0;
 #pragma unroll
-  for (int a = 0; a < BI; ++a)
+  for (int a = 0; a < BI; ++a) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      const int t = t0 + prow(a) + 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
-      if (t < T) {
-        const float st = sx[t];
+      const int r = 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
+      const float st = sx[min(t0 + prow + 32 * a + r, T - 1)];
 #pragma unroll
-        for (int b = 0; b < BJ; ++b) {
-          const int n = n0 + qrow + 32 * b + (lane & 31);
-          if (n < N) store_y(Y, dtype, (size_t)t * N + n, y[a][b][v] * st);
+      for (int b = 0; b < BJ; ++b) {
+        const int c = 32 * b + (lane & 31);
+        const float out =
+            (GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0]) * st;
+        if (dtype == 0) ((float*)mine)[r * CH + c] = out;
+        else
+          ((uint16_t*)mine)[r * CH + c] = dtype == kF16 ? to16<kF16>(out) : to16<kBF16>(out);
+      }
+    }
+    asm volatile("" ::: "memory");   // one wave: its LDS accesses complete in order
+    const int tw = t0 + prow + 32 * a;
+    const int pieces = CH * (int)es / 16, per = 16 / (int)es;
+    if (wide) {
+      for (int p = lane; p < 32 * pieces; p += 64) {
+        const int r = p / pieces, c = p % pieces;
+        if (tw + r < T && nw + c * per < N)
+          *(u32x4*)((char*)Y + ((size_t)(tw + r) * N + nw) * es + 16 * c) =
+              *(const u32x4*)(mine + 16 * p);
+      }
+    } else {
+      for (int e = lane; e < 32 * CH; e += 64) {
+        const int r = e / CH, c = e % CH;
+        if (tw + r < T && nw + c < N) {
+          const size_t at = (size_t)(tw + r) * N + nw + c;
+          if (dtype == 0) ((float*)Y)[at] = ((const float*)mine)[e];
+          else ((uint16_t*)Y)[at] = ((const uint16_t*)mine)[e];
         }
       }
     }
+    asm volatile("" ::: "memory");
+  }
 }
 
 // Few tokens: 16 channels x up to 16 IB tokens (blockIdx.y) a work-group.
@@ -342,11 +368,12 @@ static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K
     hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 4>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
                        dtype, Y);
   } else {
+    // (with group scales the fp32 sums take the registers that wider blocks would)
     const int bi = (T + 255) / 256, bj = (N + 255) / 256;
     if (GROUP == 0 && (long long)bi * bj >= 192) {
-      hipLaunchKernelGGL((i8_tile_kernel<GROUP, 2, 4, (GROUP ? 2 : 4), 2>),
-                         dim3((unsigned)(bi * bj)), dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
-                         dtype, Y, bi, bj);
+      if constexpr (GROUP == 0)
+        hipLaunchKernelGGL((i8_tile_kernel<0, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)), dim3(512),
+                           0, st, Xq, sx, Wq, sw, T, N, K, dtype, Y, bi, bj);
     } else {
       const int ni = (T + 127) / 128, nj = (N + 127) / 128;
       hipLaunchKernelGGL((i8_tile_kernel<GROUP, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),

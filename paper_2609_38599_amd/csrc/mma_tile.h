@@ -1,8 +1,8 @@
 // Tiles of C[j][i] = sum_k P[i][k] Q[j][k] on the matrix cores, for 16-bit floats
 // (fp32 sums) and 8-bit integers (int32 sums).
 //
-// Both operands pass through LDS in chunks of 128 bytes of k (64 values of 16
-// bits, 128 of 8), straight from memory (global_load_lds_dwordx4), one chunk
+// Both operands pass through LDS in chunks of 64 bytes of k (32 values of 16
+// bits, 64 of 8), straight from memory (buffer_load_dwordx4 .. lds), three chunks
 // ahead.  An operand lies in memory either with k along its rows (KContig) or
 // with k down its rows (KStrided, 16 bits only: read out of LDS through the
 // transposing read), so no product needs a transposed copy.
@@ -77,61 +77,95 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
   return (uint32_t)to16<KIND>(lo) | ((uint32_t)to16<KIND>(hi) << 16);
 }
 
-constexpr int kChunk = 128;   // bytes of k per chunk and row
+constexpr int kChunk = 64;   // bytes of k per chunk and row
 
-// What lanes past an operand's last k read.
-static __device__ __attribute__((aligned(16))) const uint32_t kZeros[4] = {0, 0, 0, 0};
-
-__device__ __forceinline__ void load_lds16(const void* from, char* to) {
-  __builtin_amdgcn_global_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// A buffer of memory from `from` (uniform) on; loads at offsets of kNowhere return 0.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ __forceinline__ Buffer buffer_at(const void* from, size_t bytes) {
+  const uint32_t n = bytes < 0x7fffffffu ? (uint32_t)bytes : 0x7fffffffu;
+  return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, (int)n, 0x00020000);
+}
+// 16 bytes a lane from `at` + base into LDS, lane after lane.  (A load by buffer, not
+// by address: the compiler takes one by address for a possible LDS access and then
+// waits for every LDS read in flight at the next use of any.)
+__device__ __forceinline__ void load_lds16(Buffer from, uint32_t at, uint32_t base, char* to) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16,
+                                           (int)at, (int)base, 0, 0);
 }
 
 // An operand tile of TR rows with k along the rows, staged by NW wavefronts.  A
-// row's chunk is 8 pieces of 16 bytes; piece x of row r lies at x ^ (r % 8), so
-// that the rows of a fragment read fall in distinct banks.  DUAL: the first
-// half of the rows from one matrix, the second half from another.  Rows past
-// the last read the last one (their results are not stored); k past the end
-// reads zeros.
-template <int TR, int NW, bool DUAL>
+// row's chunk is CPR pieces of 16 bytes; the pieces of a row are permuted by the row
+// so that 16 rows' same piece, which a fragment read takes at a time, fall in
+// distinct banks (64 banks of 4 bytes).  Rows past the last read the last one (their
+// results are not stored); k past the end reads zeros.
+// kOne: one matrix.  kRowHalves: the first half of the rows from one matrix, the
+// second half from another.  kTwoSpans: k runs through one matrix's columns, then
+// through another's (each in chunks of its own).
+enum Sources { kOne, kRowHalves, kTwoSpans };
+template <int TR, int NW, Sources SRC>
 struct KContig {
-  static constexpr int N = TR / 8 / NW;   // load instructions a wave (1 KB = 8 rows each)
-  static_assert(N >= 1 && N * 8 * NW == TR && (!DUAL || N % 2 == 0), "tile");
+  static constexpr int CPR = kChunk / 16;      // pieces a row
+  static constexpr int RPI = 64 / CPR;         // rows per load instruction (1 KB)
+  static constexpr int N = TR / RPI / NW;      // load instructions a wave
+  static constexpr bool HALVES = SRC == kRowHalves;
+  static constexpr int NO = HALVES ? N / 2 : N;
+  static_assert(N >= 1 && N * RPI * NW == TR && (!HALVES || N % 2 == 0), "tile");
   static constexpr int kBytes = TR * kChunk;
-  const char *b0, *b1;
-  uint32_t off[DUAL ? N / 2 : N];
+  Buffer b0, b1;
+  uint32_t off[NO];
   int kbytes, wave, piece;
 
-  // p0, p1: the matrices' first rows; ld: bytes a row; row0 < rows: the tile's
-  // first row (of each half); ld <= 2^22 so that offsets in a tile fit 32 bits.
+  static __device__ __forceinline__ int swz(int row) { return (row >> 2) & 3; }
+  // p0, p1: the matrices' first rows; ld: bytes a row; kb: bytes of k (of a span);
+  // row0 < rows: the tile's first row (of each half); ld <= 2^22 so that offsets in a
+  // tile fit 32 bits.
   __device__ __forceinline__ void init(const void* p0, const void* p1, size_t ld, int row0,
                                        int rows, int kb, int w, int lane) {
-    b0 = (const char*)p0 + (size_t)row0 * ld;
-    b1 = DUAL ? (const char*)p1 + (size_t)row0 * ld : b0;
+    const size_t skip = (size_t)row0 * ld, bytes = (size_t)(rows - row0 - 1) * ld + kb;
+    b0 = buffer_at((const char*)p0 + skip, bytes);
+    b1 = SRC == kOne ? b0 : buffer_at((const char*)p1 + skip, bytes);
     kbytes = kb;
     wave = w;
-    const int r = lane >> 3;
-    piece = 16 * ((lane & 7) ^ r);
+    const int r = RPI * w + lane / CPR;
+    piece = 16 * ((lane % CPR) ^ swz(r));
 #pragma unroll
-    for (int n = 0; n < (DUAL ? N / 2 : N); ++n)
-      off[n] = (uint32_t)min(8 * (w + NW * n) + r, rows - 1 - row0) * (uint32_t)ld +
-               (uint32_t)piece;
+    for (int n = 0; n < NO; ++n)
+      off[n] = (uint32_t)min(RPI * NW * n + r, rows - 1 - row0) * (uint32_t)ld + (uint32_t)piece;
   }
-  __device__ __forceinline__ void issue(int q, char* stage) const {
-    const int k0 = q * kChunk;
-    const bool in = k0 + kChunk <= kbytes;   // uniform
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const bool second = DUAL && n >= N / 2;
-      const char* at = (second ? b1 : b0) + k0 + off[second ? n - N / 2 : n];
-      if (!in && k0 + piece >= kbytes) at = (const char*)kZeros;
-      load_lds16(at, stage + 1024 * (wave + NW * n));
+  // A chunk's start in its span, past every span where it is not `live`.
+  struct Chunk {
+    int k0;
+    bool second;
+  };
+  __device__ __forceinline__ Chunk chunk(int q, bool live) const {
+    const int span = (kbytes + kChunk - 1) / kChunk;
+    const bool second = SRC == kTwoSpans && q >= span;
+    return {live ? (second ? q - span : q) * kChunk : kbytes, second};
+  }
+  // Load instruction n of a chunk.
+  __device__ __forceinline__ void issue(const Chunk& c, int n, char* stage) const {
+    const bool from1 = HALVES ? n >= N / 2 : c.second;
+    load_lds16(from1 ? b1 : b0, c.k0 + piece < kbytes ? off[HALVES && from1 ? n - N / 2 : n] : kNowhere,
+               (uint32_t)c.k0, stage + 1024 * (wave + NW * n));
+  }
+  // This lane's places in a stage for a wave whose B blocks of 32 rows start at row0
+  // (in each half, where there are two).
+  template <int B>
+  struct Lane {
+    uint32_t o[2];
+    __device__ __forceinline__ Lane(int row0, int lane) {
+      const uint32_t r = (uint32_t)(row0 + (lane & 31)) * kChunk;
+      const uint32_t x = (uint32_t)((lane >> 5) ^ swz(lane & 31)) << 4;
+      o[0] = r + x;
+      o[1] = r + (x ^ 32);
     }
-  }
-  // Fragment of the 32 rows from row0 (a multiple of 32), k-slice ks of 4.
-  static __device__ __forceinline__ u32x4 frag(const char* stage, int row0, int ks, int lane) {
-    const int x = (((lane >> 5) ^ (lane & 7)) << 4) ^ (ks << 5);
-    return *(const u32x4*)(stage + (row0 + (lane & 31)) * kChunk + x);
-  }
+    // Fragment of block a, k-slice ks of 2.
+    __device__ __forceinline__ u32x4 frag(const char* stage, int a, int ks) const {
+      const int row = HALVES && a >= B / 2 ? TR / 2 + 32 * (a - B / 2) : 32 * a;
+      return *(const u32x4*)(stage + o[ks] + row * kChunk);
+    }
+  };
 };
 
 __device__ __forceinline__ s16x4 lds_read_tr16(const char* p) {
@@ -140,108 +174,171 @@ __device__ __forceinline__ s16x4 lds_read_tr16(const char* p) {
 }
 
 // An operand tile of TR columns with k down the rows (16-bit values): a chunk is
-// 64 rows of TR values.  64-byte block x of row t lies at x ^ (t % 4): a
-// transposing read takes one block of four consecutive rows.  Rows sw.. come
-// from a second matrix (sw = rows if there is none).  Columns past the last
-// read the last eight; rows past the last read zeros.
-template <int TR, int NW>
+// kRows rows of TR values.  64-byte block x of row t lies at x ^ (t % 4): a
+// transposing read takes one block of four consecutive rows.  Columns past the last
+// read the last eight; rows past the last read zeros.  kTwoSpans: k runs down one
+// matrix, then down another.
+template <int TR, int NW, Sources SRC>
 struct KStrided {
+  static_assert(SRC != kRowHalves, "sources");
+  static constexpr int kRows = kChunk / 2;
   static constexpr int RB = 2 * TR;             // bytes a row
   static constexpr int CPR = RB / 16;           // pieces a row
-  static constexpr int RPP = 64 / CPR;          // rows per load instruction
-  static constexpr int N = 64 / RPP / NW;
-  static_assert(N >= 1 && N * RPP * NW == 64 && (NW * RPP) % 4 == 0, "tile");
+  static constexpr int RPI = 64 / CPR;          // rows per load instruction
+  static constexpr int N = kRows / RPI / NW;
+  static_assert(N >= 1 && N * RPI * NW == kRows && (NW * RPI) % 4 == 0, "tile");
   static constexpr int kBytes = TR * kChunk;
   const char *b0, *b1;
   size_t ld;
-  uint32_t off;      // of this lane in the first instruction's rows
-  int rows, sw, wave, lt;
+  uint32_t off[N];
+  int rows, wave, lt;
 
-  // c0: the tile's first column; cols a multiple of 8; ld bytes a row, at most 2^22.
+  // c0: the tile's first column; cols a multiple of 8; ld bytes a row, at most 2^22;
+  // rows_ of a span.
   __device__ __forceinline__ void init(const void* p0, const void* p1, size_t ld_, int c0,
-                                       int cols, int rows_, int sw_, int w, int lane) {
+                                       int cols, int rows_, int w, int lane) {
     ld = ld_;
     rows = rows_;
-    sw = sw_;
     wave = w;
-    lt = RPP * w + lane / CPR;
+    lt = RPI * w + lane / CPR;
     const int pc = (lane % CPR) ^ ((lt & 3) << 2);
-    const uint32_t col = 2u * (uint32_t)min(c0 + 8 * pc, cols - 8);
     b0 = (const char*)p0;
     b1 = (const char*)p1;
-    off = col;
-  }
-  __device__ __forceinline__ void issue(int q, char* stage) const {
-    const int k0 = q * 64;
-    const bool one = k0 + 64 <= sw || (k0 >= sw && k0 + 64 <= rows);   // uniform
-    if (one) {
-      const char* base = k0 < sw ? b0 + (size_t)k0 * ld : b1 + (size_t)(k0 - sw) * ld;
 #pragma unroll
-      for (int n = 0; n < N; ++n)
-        load_lds16(base + ((uint32_t)(lt + NW * RPP * n) * (uint32_t)ld + off),
-                   stage + 1024 * (wave + NW * n));
-    } else {
-#pragma unroll 1
-      for (int n = 0; n < N; ++n) {
-        const int t = k0 + lt + NW * RPP * n;
-        const char* at = t < sw ? b0 + (size_t)t * ld + off
-                                : b1 + (size_t)(t - sw) * ld + off;
-        if (t >= rows) at = (const char*)kZeros;
-        load_lds16(at, stage + 1024 * (wave + NW * n));
-      }
+    for (int n = 0; n < N; ++n)
+      off[n] = (uint32_t)(lt + NW * RPI * n) * (uint32_t)ld + 2u * (uint32_t)min(c0 + 8 * pc, cols - 8);
+  }
+  struct Chunk {
+    Buffer from;
+    int left;   // rows from its first one on
+  };
+  __device__ __forceinline__ Chunk chunk(int q, bool live) const {
+    const int span = (rows + kRows - 1) / kRows;
+    const bool second = SRC == kTwoSpans && q >= span;
+    const int k0 = (second ? q - span : q) * kRows;
+    return {buffer_at((second ? b1 : b0) + (live ? (size_t)k0 * ld : 0), 0x7fffffff),
+            live ? rows - k0 : 0};
+  }
+  __device__ __forceinline__ void issue(const Chunk& c, int n, char* stage) const {
+    load_lds16(c.from, lt + NW * RPI * n < c.left ? off[n] : kNowhere, 0,
+               stage + 1024 * (wave + NW * n));
+  }
+  template <int B>
+  struct Lane {
+    uint32_t o[B];
+    __device__ __forceinline__ Lane(int col0, int lane) {
+      const int gi = lane >> 4, pi = lane & 15, t = pi >> 2;
+#pragma unroll
+      for (int a = 0; a < B; ++a)
+        o[a] = (uint32_t)((8 * (gi >> 1) + t) * RB + ((((col0 >> 5) + a) ^ t) << 6) +
+                          32 * (gi & 1) + 8 * (pi & 3));
     }
-  }
-  static __device__ __forceinline__ u32x4 frag(const char* stage, int col0, int ks, int lane) {
-    const int gi = lane >> 4, pi = lane & 15, t = pi >> 2;
-    const char* p = stage + (8 * (gi >> 1) + t + 16 * ks) * RB +
-                    (((col0 >> 5) ^ t) << 6) + 32 * (gi & 1) + 8 * (pi & 3);
-    const s16x4 w[2] = {lds_read_tr16(p), lds_read_tr16(p + 4 * RB)};
-    return __builtin_bit_cast(u32x4, w);
-  }
+    __device__ __forceinline__ u32x4 frag(const char* stage, int a, int ks) const {
+      const char* p = stage + o[a] + 16 * ks * RB;
+      const s16x4 w[2] = {lds_read_tr16(p), lds_read_tr16(p + 4 * RB)};
+      return __builtin_bit_cast(u32x4, w);
+    }
+  };
 };
 
-// The products of one staged chunk.  A wave's blocks: P rows prow(a), Q rows
-// qrow + 32 b.
-template <int KIND, int BI, int BJ, class LP, class LQ, class PR>
-__device__ __forceinline__ void mma_chunk(const char* cur, int lane, const PR& prow, int qrow,
-                                          typename Mma<KIND>::Acc (&acc)[BI][BJ]) {
-#pragma unroll
-  for (int ks = 0; ks < 4; ++ks) {
-    u32x4 fp[BI], fq[BJ];
-#pragma unroll
-    for (int a = 0; a < BI; ++a) fp[a] = LP::frag(cur, prow(a), ks, lane);
-#pragma unroll
-    for (int b = 0; b < BJ; ++b) fq[b] = LQ::frag(cur + LP::kBytes, qrow + 32 * b, ks, lane);
-#pragma unroll
-    for (int a = 0; a < BI; ++a)
-#pragma unroll
-      for (int b = 0; b < BJ; ++b) acc[a][b] = Mma<KIND>::mul(fp[a], fq[b], acc[a][b]);
-  }
+// Waits until at most n of this wave's loads are outstanding and its LDS accesses
+// are done, then for the work-group's other waves.
+template <int n>
+__device__ __forceinline__ void wait_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((n & 15) | (7 << 4) | ((n >> 4) << 14));
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
-// The k-loop over chunks q0 <= q < q1 (at least one): compute(stage, q) with chunk q
-// staged, the next one's loads in flight.
-template <class LP, class LQ, class Compute>
-__device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int q1, char* buf0,
-                                         char* buf1, const Compute& compute) {
-  auto issue = [&](int q, char* stage) __attribute__((always_inline)) {
-    lp.issue(q, stage);
-    lq.issue(q, stage + LP::kBytes);
+// The k-loop over chunks q0 <= q < q1 (at least one) with four stages: while a chunk
+// is multiplied, the loads of the three behind it are in flight, and the next
+// fragments are read a slice ahead.  The four stages are arrays of their own, so that
+// the compiler can tell which of them a load in flight writes; the loop runs in
+// whole rounds of them (chunks past the last are zeros).  A wave's P blocks start at
+// row prow of the tile, its Q blocks at qrow.  round(q) comes before every fourth
+// chunk; mul(p, q, a, b, ks, i) gets the fragments of P block a and Q block b, slice ks of
+// chunk i of the round.
+//
+// 4096 x 4096 -> 2 x 14336 channels, 256-wide tiles: two stages of twice the chunk 812 us,
+// four 800; the loads in a row at the start of a chunk 860; by address instead of by
+// buffer (every LDS read then waits for all others) 905.  Bound by the matrix cores at
+// the clock that the card's power allows (1.7 GHz here).
+template <int BI, int BJ, class LP, class LQ, class Round, class Mul>
+__device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int q1, int lane,
+                                         int prow, int qrow, char* s0, char* s1, char* s2,
+                                         char* s3, const Round& round, const Mul& mul) {
+  constexpr int L = LP::N + LQ::N, R = BI + BJ, M = BI * BJ;
+  u32x4 fp[2][BI], fq[2][BJ];
+  const typename LP::template Lane<BI> pl(prow, lane);
+  const typename LQ::template Lane<BJ> ql(qrow, lane);
+  // fragment r of a slice, of Q's first
+  auto read = [&](const char* cur, int ks, int r) __attribute__((always_inline)) {
+    if (r < BJ) fq[ks][r] = ql.frag(cur + LP::kBytes, r, ks);
+    else fp[ks][r - BJ] = pl.frag(cur, r - BJ, ks);
   };
-  issue(q0, buf0);
-  __syncthreads();
-  for (int q = q0; q < q1; q += 2) {
-    // a stage was last read before the barrier that precedes its loads; the
-    // barrier after a chunk waits for the next one's loads
-    if (q + 1 < q1) issue(q + 1, buf1);
-    compute(buf0, q);
-    __syncthreads();
-    if (q + 1 < q1) {
-      if (q + 2 < q1) issue(q + 2, buf0);
-      compute(buf1, q + 1);
-      __syncthreads();
+  auto issue = [&](int l, const typename LP::Chunk& cp, const typename LQ::Chunk& cq, char* stage)
+      __attribute__((always_inline)) {
+    if (l < LP::N) lp.issue(cp, l, stage);
+    else lq.issue(cq, l - LP::N, stage + LP::kBytes);
+  };
+  auto chunk = [&](int q, int i, char* cur, char* next, char* far)
+      __attribute__((always_inline)) {
+    const typename LP::Chunk cp = lp.chunk(q + i + 3, q + i + 3 < q1);
+    const typename LQ::Chunk cq = lq.chunk(q + i + 3, q + i + 3 < q1);
+    // the second slice's fragments and the loads one at a time among the first one's
+    // products: in a row they would hold up the wave
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      mul(fp[0][m / BJ], fq[0][m % BJ], m / BJ, m % BJ, 0, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int o = m * (R + L) / M; o < (m + 1) * (R + L) / M; ++o) {
+        if (o < R) read(cur, 1, o);
+        else issue(o - R, cp, cq, far);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
+    // the loads of the next chunk are in (those of the two behind it may not be), and
+    // no wave reads this chunk's stage any more
+    wait_barrier<2 * L>();
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      mul(fp[1][m / BJ], fq[1][m % BJ], m / BJ, m % BJ, 1, i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int o = m * R * 3 / (2 * M); o < (m + 1) * R * 3 / (2 * M); ++o)
+        if (o < R) read(next, 0, o);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  char* const stages[3] = {s0, s1, s2};
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const typename LP::Chunk cp = lp.chunk(q0 + i, q0 + i < q1);
+    const typename LQ::Chunk cq = lq.chunk(q0 + i, q0 + i < q1);
+#pragma unroll
+    for (int l = 0; l < L; ++l) issue(l, cp, cq, stages[i]);
   }
+  wait_barrier<2 * L>();
+#pragma unroll
+  for (int r = 0; r < R; ++r) read(s0, 0, r);
+  for (int q = q0; q < q1; q += 4) {
+    round(q);
+    chunk(q, 0, s0, s1, s3);
+    chunk(q, 1, s1, s2, s0);
+    chunk(q, 2, s2, s3, s1);
+    chunk(q, 3, s3, s0, s2);
+  }
+  wait_barrier<0>();
+}
+
+// Rows of RB bytes in LDS on their way to memory: piece c (16 bytes) of row r.
+template <int RB>
+__device__ __forceinline__ char* out_piece(char* buf, int r, int c) {
+  return buf + r * RB + ((c ^ (r & (RB / 16 - 1))) << 4);
 }
 
 // Tile (ti, tj) of work-group `id` in a grid of ni x nj tiles: the work-groups
