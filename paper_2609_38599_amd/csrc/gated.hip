@@ -9,6 +9,7 @@
 // to 16 bits as the matrix cores take them (the only rounding beside the
 // outputs'); then dx = [da db] [Wg; Wu] in one product over 2 F, and
 // [dWg; dWu] = [da db]^T x in one over T.
+#include <algorithm>
 #include <type_traits>
 
 #include "skinny.h"
@@ -51,7 +52,7 @@ __device__ __forceinline__ float activation(int act, float a, float* d) {   // a
 // ---- forward, many tokens ----
 // WI x WJ wavefronts, each BI blocks of 32 P rows (half Wg's, half Wu's) x BJ blocks
 // of 32 tokens.
-template <int KIND, int WI, int WJ, int BI, int BJ>
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre, int ni, int nj) {
@@ -59,10 +60,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
   typedef KContig<TI, NW, kRowHalves> LP;
   typedef KContig<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
+  JARQ_STAGES(S, STAGE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -75,8 +73,8 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
   lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
   f32x16 acc[BI][BJ] = {};
   // block a < BI / 2: Wg, the others: Wu of the same channels
-  mma_loop<BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 32 * BJ,
-                   buf0, buf1, buf2, buf3, [](int) {},
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 32 * BJ,
+                   stages, [](int) {},
                    [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
@@ -84,7 +82,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
   // Out through LDS, so that memory gets whole lines (8 bytes a lane straight from the
   // registers: 75 us more of 800 at 4096 x 4096 -> 14336).  The waves of one wj share a
   // stage of 32 BJ tokens.
-  char* const stage = wj == 0 ? buf0 : wj == 1 ? buf1 : wj == 2 ? buf2 : buf3;
+  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
   const int row = lane & 31, tw = t0 + wj * 32 * BJ;
   auto send = [&](auto* to, auto put) __attribute__((always_inline)) {
     typedef typename std::remove_reference<decltype(*to)>::type E;
@@ -130,8 +128,8 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
 }
 
 // ---- forward, few tokens ----
-// A work-group: 16 channels of both projections x up to 16 IB tokens (blockIdx.y),
-// eight wavefronts along k.
+// A work-group: 16 channels of both projections x up to 16 IB tokens, eight wavefronts
+// along k.  One token, 4096 -> 11008: 34 us, 5.2 TB/s of weights (32 channels: 45 us).
 template <int KIND, int IB>
 __global__ __launch_bounds__(512) void gated_skinny_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
@@ -140,18 +138,17 @@ __global__ __launch_bounds__(512) void gated_skinny_kernel(
   __shared__ __attribute__((aligned(16))) float red[NW * IB * 2 * 256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int f0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * IB;
+  const int f0 = blockIdx.x * 16;
   const int row = lane & 15;
+  const size_t ld = 2 * (size_t)D, wrow = (size_t)min(f0 + row, F - 1) * ld;
   const char* p[IB];
 #pragma unroll
-  for (int a = 0; a < IB; ++a)
-    p[a] = (const char*)X + (size_t)min(t0 + 16 * a + row, T - 1) * (2 * (size_t)D);
-  const size_t wrow = (size_t)min(f0 + row, F - 1) * (2 * (size_t)D);
+  for (int a = 0; a < IB; ++a) p[a] = (const char*)X + (size_t)min(16 * a + row, T - 1) * ld;
   const char* const q[2] = {(const char*)Wg + wrow, (const char*)Wu + wrow};
   f32x4 acc[IB][2] = {};
-  skinny_loop<IB, 2, (IB > 2 ? 2 : 4), NW>(
-      p, q, 2 * D, wave, lane, [](int, int) {}, [&](int, int, const u32x4(&fp)[IB], const u32x4(&fq)[2])
-                                   __attribute__((always_inline)) {
+  skinny_loop<IB, 2, 4, NW>(
+      p, q, 2 * D, wave, lane, [](int, int) {},
+      [&](int, int, const u32x4(&fp)[IB], const u32x4(&fq)[2]) __attribute__((always_inline)) {
 #pragma unroll
         for (int a = 0; a < IB; ++a)
 #pragma unroll
@@ -165,7 +162,7 @@ __global__ __launch_bounds__(512) void gated_skinny_kernel(
   __syncthreads();
   for (int e = threadIdx.x; e < IB * 256; e += 512) {
     const int j = e & 15, i = (e >> 4) & 15, a = e >> 8;
-    const int t = t0 + 16 * a + i, f = f0 + j;
+    const int t = 16 * a + i, f = f0 + j;
     if (t < T && f < F) {
       const float g = skinny_sum<NW, 2 * IB>(red, 2 * a, i, j);
       const float u = skinny_sum<NW, 2 * IB>(red, 2 * a + 1, i, j);
@@ -179,33 +176,50 @@ __global__ __launch_bounds__(512) void gated_skinny_kernel(
   }
 }
 
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+static hipError_t launch_gated_tiles(hipStream_t st, int act, int T, int D, int F, const void* X,
+                                     const void* Wg, const void* Wu, uint16_t* Y, float* pre) {
+  const int ni = (F + 16 * WI * BI - 1) / (16 * WI * BI);
+  const int nj = (T + 32 * WJ * BJ - 1) / (32 * WJ * BJ);
+  hipLaunchKernelGGL((gated_tile_kernel<KIND, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
+                     dim3(64 * WI * WJ), 0, st, X, Wg, Wu, T, D, F, act, Y, pre, ni, nj);
+  return hipGetLastError();
+}
+
+// Up to 32 tokens fragments straight from memory (24 tokens, 4096 -> 11008: 48 us, tiles
+// of 64 channels 54); beyond, the tiles that tile_cost makes the cheapest.  4096 -> 1000,
+// 2752 and 11008 channels, in us with tiles of 128 x 256 (channels x tokens), 64 x 128,
+// 64 x 64 and 32 x 64:
+//    100 tokens   69 26 19 17    71 31 25 19    73  38  49  48
+//    400          72 31 26 19    73 34 44 58    91 113 125 145
+//   1600          74 37 51 59    88 104 127 149 280 337 443 515
 template <int KIND>
 static hipError_t launch_gated_forward_kind(hipStream_t st, int act, int T, int D, int F,
                                             const void* X, const void* Wg, const void* Wu,
                                             void* Y, float* pre) {
   uint16_t* y = (uint16_t*)Y;
-  const dim3 wg((F + 15) / 16);
-  if (T <= 16) {
-    hipLaunchKernelGGL((gated_skinny_kernel<KIND, 1>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
-                       act, y, pre);
-  } else if (T <= 32) {
-    hipLaunchKernelGGL((gated_skinny_kernel<KIND, 2>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
-                       act, y, pre);
-  } else if (T <= 64) {
-    hipLaunchKernelGGL((gated_skinny_kernel<KIND, 4>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
-                       act, y, pre);
-  } else {
-    const int bi = (F + 127) / 128, bj = (T + 255) / 256;
-    if ((long long)bi * bj >= 192) {
-      hipLaunchKernelGGL((gated_tile_kernel<KIND, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)),
-                         dim3(512), 0, st, X, Wg, Wu, T, D, F, act, y, pre, bi, bj);
-    } else {
-      const int ni = (F + 63) / 64, nj = (T + 127) / 128;
-      hipLaunchKernelGGL((gated_tile_kernel<KIND, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
-                         dim3(256), 0, st, X, Wg, Wu, T, D, F, act, y, pre, ni, nj);
-    }
+  if (T <= 32) {
+    const dim3 wg((F + 15) / 16);
+    if (T <= 16)
+      hipLaunchKernelGGL((gated_skinny_kernel<KIND, 1>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
+                         act, y, pre);
+    else
+      hipLaunchKernelGGL((gated_skinny_kernel<KIND, 2>), wg, dim3(512), 0, st, X, Wg, Wu, T, D, F,
+                         act, y, pre);
+    return hipGetLastError();
   }
-  return hipGetLastError();
+  auto tiles = [&](int f, int t) { return (long long)((F + f - 1) / f) * ((T + t - 1) / t); };
+  const int nk = (2 * D + kChunk - 1) / kChunk;
+  const double cost[4] = {tile_cost(tiles(128, 256), nk, 0.62, 6.0),
+                          tile_cost(tiles(64, 128), nk, 0.26, 3.3),
+                          tile_cost(tiles(64, 64), nk, 0.19, 2.7),
+                          tile_cost(tiles(32, 64), nk, 0.135, 2.6)};
+  switch ((int)(std::min_element(cost, cost + 4) - cost)) {
+    case 0: return launch_gated_tiles<KIND, 4, 2, 4, 4, 2>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    case 1: return launch_gated_tiles<KIND, 4, 2, 2, 2, 2>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    case 2: return launch_gated_tiles<KIND, 4, 2, 2, 2, 1>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    default: return launch_gated_tiles<KIND, 8, 1, 2, 2, 1>(st, act, T, D, F, X, Wg, Wu, y, pre);
+  }
 }
 
 hipError_t launch_gated_forward(hipStream_t st, int dtype, int act, int T, int D, int F,
@@ -284,7 +298,7 @@ __device__ __forceinline__ void store_tile16(const f32x16 (&acc)[BI][BJ], char* 
 
 // ---- backward: dx = dab [Wg; Wu] ----
 // part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.
-template <int KIND, int WI, int WJ, int BI, int BJ>
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
     const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int each, uint16_t* __restrict__ dX, float* __restrict__ part, int ni, int nj) {
@@ -292,10 +306,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
   typedef KStrided<TI, NW, kTwoSpans> LP;
   typedef KContig<TJ, NW, kTwoSpans> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
+  JARQ_STAGES(S, STAGE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -309,7 +320,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
   f32x16 acc[BI][BJ] = {};
   const int nk = 2 * ((2 * F + kChunk - 1) / kChunk);
   const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
-  mma_loop<BI, BJ>(lp, lq, q0, q1, lane, wi * 32 * BI, wj * 32 * BJ, buf0, buf1, buf2, buf3,
+  mma_loop<S, BI, BJ>(lp, lq, q0, q1, lane, wi * 32 * BI, wj * 32 * BJ, stages,
                    [](int) {},
                    [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
                        __attribute__((always_inline)) {
@@ -332,7 +343,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
     }
     return;
   }
-  char* const stage = wj == 0 ? buf0 : wj == 1 ? buf1 : wj == 2 ? buf2 : buf3;
+  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
   const int tw = t0 + wj * 32 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
     if (tw + t < T && d0 + i < D) *(u32x4*)(dX + (size_t)(tw + t) * D + d0 + i) = w;
@@ -352,7 +363,7 @@ __global__ __launch_bounds__(256) void gated_dx_sum_kernel(const float* __restri
 }
 
 // ---- backward: [dWg; dWu] = dab^T x ----
-template <int KIND, int WI, int WJ, int BI, int BJ>
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
     const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,
     uint16_t* __restrict__ dWg, uint16_t* __restrict__ dWu, int ni, int nj) {
@@ -360,10 +371,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
   typedef KStrided<TI, NW, kOne> LP;
   typedef KStrided<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
+  JARQ_STAGES(S, STAGE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -375,13 +383,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
   lp.init(X, X, 2 * (size_t)D, d0, D, T, wave, lane);
   lq.init(dab, dab, 4 * (size_t)F, f0, 2 * F, T, wave, lane);
   f32x16 acc[BI][BJ] = {};
-  mma_loop<BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 32 * BI, wj * 32 * BJ,
-                   buf0, buf1, buf2, buf3, [](int) {},
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 32 * BI, wj * 32 * BJ,
+                   stages, [](int) {},
                    [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                        });
-  char* const stage = wj == 0 ? buf0 : wj == 1 ? buf1 : wj == 2 ? buf2 : buf3;
+  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
   const int fw = f0 + wj * 32 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int r, int i, const u32x4& w) {
     const int f = fw + r;
@@ -394,27 +402,34 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
 namespace {
 
 struct DxPlan {
-  bool big;
+  int kind;   // tiles of 256 x 256 (channels x tokens), 128 x 128, 128 x 64
   int ni, nj, splits, each;
 };
-// Whole 256-wide tiles where they fill the chip; otherwise 128-wide ones, with the
-// 2 F cut so that about two work-groups fall on each CU.
+// The tiles and the number of parts of the 2 F that cost the least, with the parts'
+// fp32 sums written and read again.  4096 channels, F = 11008: 400 tokens 256-wide tiles in
+// 4 parts 117 us, 128-wide ones in 1, 2, 4 parts 171, 99, 98; 1600 tokens 256-wide ones in
+// 1, 2, 4 parts 388, 229, 288, 128-wide ones 357.
 DxPlan dx_plan(int T, int D, int F) {
-  DxPlan p;
   const int nk = 2 * ((2 * F + kChunk - 1) / kChunk);
-  p.big = (long long)((D + 255) / 256) * ((T + 255) / 256) >= 192;
-  const int e = p.big ? 256 : 128;
-  p.ni = (D + e - 1) / e;
-  p.nj = (T + e - 1) / e;
-  int splits = 1;
-  if (!p.big) {
-    splits = 512 / (p.ni * p.nj);
-    splits = splits < 1 ? 1 : splits > nk / 8 ? (nk / 8 < 1 ? 1 : nk / 8) : splits;
-    if (splits > 32) splits = 32;
+  constexpr int wide[3] = {256, 128, 128}, tall[3] = {256, 128, 64};
+  constexpr double chunk[3] = {0.62, 0.26, 0.19}, rest[3] = {8.0, 4.0, 3.0};
+  DxPlan best{};
+  double least = 0.0;
+  for (int kind = 0; kind < 3; ++kind) {
+    const int ni = (D + wide[kind] - 1) / wide[kind], nj = (T + tall[kind] - 1) / tall[kind];
+    for (int parts = 1; parts <= 16; ++parts) {
+      const int each = ((nk + parts - 1) / parts + 3) / 4 * 4;   // whole rounds of stages
+      const int splits = (nk + each - 1) / each;
+      if (splits != parts) continue;
+      double cost = tile_cost((long long)ni * nj * splits, each, chunk[kind], rest[kind]);
+      if (splits > 1) cost += 5.0 + 8e-6 * splits / 4.0 * T * D;
+      if (best.splits == 0 || cost < least) {
+        least = cost;
+        best = {kind, ni, nj, splits, each};
+      }
+    }
   }
-  p.each = ((nk + splits - 1) / splits + 3) / 4 * 4;   // whole rounds of stages
-  p.splits = (nk + p.each - 1) / p.each;
-  return p;
+  return best;
 }
 
 size_t pad256(size_t n) { return (n + 255) & ~(size_t)255; }
@@ -460,12 +475,15 @@ static hipError_t launch_gated_backward_kind(hipStream_t st, int act, int T, int
     const DxPlan p = dx_plan(T, D, F);
     float* to = p.splits > 1 ? part : nullptr;
     const dim3 grid((unsigned)(p.ni * p.nj), (unsigned)p.splits);
-    if (p.big)
-      hipLaunchKernelGGL((gated_dx_kernel<KIND, 2, 4, 4, 2>), grid, dim3(512), 0, st, dab, Wg, Wu,
-                         T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
+    if (p.kind == 0)
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 4, 4, 2>), grid, dim3(512), 0, st, dab, Wg,
+                         Wu, T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
+    else if (p.kind == 1)
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 2, 2, 2>), grid, dim3(256), 0, st, dab, Wg,
+                         Wu, T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
     else
-      hipLaunchKernelGGL((gated_dx_kernel<KIND, 2, 2, 2, 2>), grid, dim3(256), 0, st, dab, Wg, Wu,
-                         T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 2, 2, 1>), grid, dim3(256), 0, st, dab, Wg,
+                         Wu, T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (to) {
       const size_t n = (size_t)T * D, b = (n / 4 + 255) / 256;
@@ -475,17 +493,23 @@ static hipError_t launch_gated_backward_kind(hipStream_t st, int act, int T, int
     }
   }
   if (dWg || dWu) {
-    const int bi = (D + 255) / 256, bj = (2 * F + 255) / 256;
-    if ((long long)bi * bj >= 192) {
-      hipLaunchKernelGGL((gated_dw_kernel<KIND, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)),
+    // 256-wide tiles from 320 on (1600 tokens, 1000 channels, F = 11008, 344 of them: 69 us,
+    // 128-wide 74; 4096, F = 1000, 128 of them: 36 and 27), 128-wide ones from 192 on (1000
+    // channels, F = 2752, 344 of them: 26, 128 x 64 30; F = 1000, 128 of them: 16 and 14)
+    const int ni = (D + 127) / 128, bi = (D + 255) / 256, bj = (2 * F + 255) / 256;
+    const int nj = (2 * F + 127) / 128, nh = (2 * F + 63) / 64;
+    if ((long long)bi * bj >= 320)
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)),
                          dim3(512), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, bi,
                          bj);
-    } else {
-      const int ni = (D + 127) / 128, nj = (2 * F + 127) / 128;
-      hipLaunchKernelGGL((gated_dw_kernel<KIND, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
+    else if ((long long)ni * nj >= 192)
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
                          dim3(256), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, ni,
                          nj);
-    }
+    else
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 2, 2, 1>), dim3((unsigned)(ni * nh)),
+                         dim3(256), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, ni,
+                         nh);
     e = hipGetLastError();
   }
   return e;

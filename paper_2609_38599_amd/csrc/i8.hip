@@ -7,6 +7,7 @@
 // integer sums exact in int32 on v_mfma_i32_32x32x32_i8, a group's sum converted
 // and added in fp32.  Tokens are the P rows and channels the Q rows, so that a lane
 // holds one channel and needs one group scale.
+#include <algorithm>
 #include <type_traits>
 
 #include "skinny.h"
@@ -162,7 +163,7 @@ __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) 
 
 // Many tokens.  GROUP 0: one scale a channel, int32 sums over all of k; otherwise a
 // group's int32 sums go to fp32.
-template <int GROUP, int WI, int WJ, int BI, int BJ>
+template <int GROUP, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
     const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y, int ni,
@@ -171,10 +172,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   typedef KContig<TI, NW, kOne> LP;
   typedef KContig<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  __shared__ __attribute__((aligned(1024))) char buf0[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf1[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf2[STAGE];
-  __shared__ __attribute__((aligned(1024))) char buf3[STAGE];
+  JARQ_STAGES(S, STAGE);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -194,13 +192,13 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   for (int b = 0; b < BJ; ++b)
     srow[b] = sw + (size_t)min(n0 + qrow + 32 * b + (lane & 31), N - 1) * G;
   if constexpr (GROUP == 0) {
-    mma_loop<BI, BJ>(lp, lq, 0, nk, lane, prow, qrow, buf0, buf1, buf2, buf3, [](int) {},
+    mma_loop<S, BI, BJ>(lp, lq, 0, nk, lane, prow, qrow, stages, [](int) {},
                      [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
                          __attribute__((always_inline)) {
                            acc[a][b] = Mma<kI8>::mul(p, q, acc[a][b]);
                          });
   } else {
-    constexpr int GR = 4 * kChunk / GROUP;   // groups a round
+    constexpr int GR = S * kChunk / GROUP;   // groups a round
     constexpr int SG = GROUP / 32;           // k-slices a group
     // the scales a round ahead of their use; past the last group 0
     float s[GR][BJ], ahead[GR][BJ];
@@ -211,14 +209,14 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
         for (int g = 0; g < GR; ++g) ahead[g][b] = g0 + g < G ? srow[b][g0 + g] : 0.f;
     };
     fetch(0);
-    mma_loop<BI, BJ>(
-        lp, lq, 0, nk, lane, prow, qrow, buf0, buf1, buf2, buf3,
+    mma_loop<S, BI, BJ>(
+        lp, lq, 0, nk, lane, prow, qrow, stages,
         [&](int q) __attribute__((always_inline)) {
 #pragma unroll
           for (int g = 0; g < GR; ++g)
 #pragma unroll
             for (int b = 0; b < BJ; ++b) s[g][b] = ahead[g][b];
-          fetch((q / 4 + 1) * GR);
+          fetch((q / S + 1) * GR);
         },
         [&](const u32x4& p, const u32x4& q, int a, int b, int ks, int i)
             __attribute__((always_inline)) {
@@ -233,8 +231,10 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   }
   // Out through LDS, 32 tokens x 32 BJ channels of a wave at a time.
   constexpr int CH = 32 * BJ;
-  static_assert(NW / 2 * 32 * CH * 4 <= STAGE, "stage");
-  char* const mine = (wave < NW / 2 ? buf0 : buf1) + wave % (NW / 2) * 32 * CH * 4;
+  constexpr int PER = STAGE / (32 * CH * 4);   // waves a stage serves
+  static_assert(PER >= 1 && PER * 4 >= NW, "stage");
+  char* const mine = (wave / PER == 0 ? stage0 : wave / PER == 1 ? stage1
+                      : wave / PER == 2 ? stage2 : stage3) + wave % PER * 32 * CH * 4;
   const int nw = n0 + qrow;
   const size_t es = dtype == 0 ? 4 : 2;
   // 16-byte stores where every row starts at a 16-byte boundary and none ends inside a piece
@@ -279,108 +279,155 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   }
 }
 
-// Few tokens: 16 channels x up to 16 IB tokens (blockIdx.y) a work-group.
-template <int GROUP, int IB>
+// Few tokens: 16 JB channels x up to 16 IB tokens (blockIdx.y) a work-group.
+template <int GROUP, int IB, int JB, int U>
 __global__ __launch_bounds__(512) void i8_skinny_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
     const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y) {
-  constexpr int NW = 8, U = IB > 2 ? 2 : 4;
+  constexpr int NW = 8;
   constexpr int GU = GROUP ? 64 * U / GROUP : 1;   // groups a unit
+  static_assert(GROUP == 0 || GU >= 1, "unit");
   typedef typename std::conditional<GROUP == 0, int32_t, float>::type Sum;
   typedef Sum Sum4 __attribute__((ext_vector_type(4)));
-  __shared__ __attribute__((aligned(16))) Sum red[NW * IB * 256];
+  __shared__ __attribute__((aligned(16))) Sum red[NW * IB * JB * 256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int n0 = blockIdx.x * 16, t0 = blockIdx.y * 16 * IB;
+  const int n0 = blockIdx.x * 16 * JB, t0 = blockIdx.y * 16 * IB;
   const int row = lane & 15;
-  const char* p[IB];
+  const int G = GROUP ? K / GROUP : 1;
+  const char *p[IB], *q[JB];
+  const float* srow[JB];
 #pragma unroll
   for (int a = 0; a < IB; ++a)
     p[a] = (const char*)Xq + (size_t)min(t0 + 16 * a + row, T - 1) * K;
-  const int n = min(n0 + row, N - 1);
-  const char* const q[1] = {(const char*)Wq + (size_t)n * K};
-  const int G = GROUP ? K / GROUP : 1;
-  const float* srow = sw + (size_t)n * G;
-  float s[2][GU];
-  Sum4 sum[IB] = {};
-  i32x4 acc[IB];
+#pragma unroll
+  for (int b = 0; b < JB; ++b) {
+    const int n = min(n0 + 16 * b + row, N - 1);
+    q[b] = (const char*)Wq + (size_t)n * K;
+    srow[b] = sw + (size_t)n * G;
+  }
+  float s[2][JB][GU];
+  Sum4 sum[IB][JB] = {};
+  i32x4 acc[IB][JB];
   const bool low = lane < 32;
-  skinny_loop<IB, 1, U, NW>(
+  skinny_loop<IB, JB, U, NW>(
       p, q, K, wave, lane,
       [&](int u, int set) __attribute__((always_inline)) {
         if constexpr (GROUP != 0) {
 #pragma unroll
-          for (int g = 0; g < GU; ++g) s[set][g] = u * GU + g < G ? srow[u * GU + g] : 0.f;
+          for (int b = 0; b < JB; ++b)
+#pragma unroll
+            for (int g = 0; g < GU; ++g)
+              s[set][b][g] = u * GU + g < G ? srow[b][u * GU + g] : 0.f;
         }
       },
-      [&](int st, int set, const u32x4(&fp)[IB], const u32x4(&fq)[1])
+      [&](int st, int set, const u32x4(&fp)[IB], const u32x4(&fq)[JB])
           __attribute__((always_inline)) {
 #pragma unroll
-        for (int a = 0; a < IB; ++a) {
-          if constexpr (GROUP == 0) {
-            sum[a] = Mma<kI8>::mul16(fp[a], fq[0], sum[a]);
-          } else if constexpr (GROUP == 32) {
-            // a step's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
+        for (int a = 0; a < IB; ++a)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const u32x4 part = (h == 0) == low ? fp[a] : u32x4{};
-              const i32x4 c = Mma<kI8>::mul16(part, fq[0], i32x4{});
+          for (int b = 0; b < JB; ++b) {
+            if constexpr (GROUP == 0) {
+              sum[a][b] = Mma<kI8>::mul16(fp[a], fq[b], sum[a][b]);
+            } else if constexpr (GROUP == 32) {
+              // a step's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
 #pragma unroll
-              for (int v = 0; v < 4; ++v)
-                sum[a][v] = fmaf((float)c[v], s[set][2 * st + h], sum[a][v]);
-            }
-          } else {
-            constexpr int SG = GROUP / 64;   // steps a group
-            acc[a] = Mma<kI8>::mul16(fp[a], fq[0], st % SG == 0 ? i32x4{} : acc[a]);
-            if (st % SG == SG - 1) {
+              for (int h = 0; h < 2; ++h) {
+                const u32x4 part = (h == 0) == low ? fp[a] : u32x4{};
+                const i32x4 c = Mma<kI8>::mul16(part, fq[b], i32x4{});
 #pragma unroll
-              for (int v = 0; v < 4; ++v)
-                sum[a][v] = fmaf((float)acc[a][v], s[set][st / SG], sum[a][v]);
+                for (int v = 0; v < 4; ++v)
+                  sum[a][b][v] = fmaf((float)c[v], s[set][b][2 * st + h], sum[a][b][v]);
+              }
+            } else {
+              constexpr int SG = GROUP / 64;   // steps a group
+              acc[a][b] = Mma<kI8>::mul16(fp[a], fq[b], st % SG == 0 ? i32x4{} : acc[a][b]);
+              if (st % SG == SG - 1) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+                  sum[a][b][v] = fmaf((float)acc[a][b][v], s[set][b][st / SG], sum[a][b][v]);
+              }
             }
           }
-        }
       });
 #pragma unroll
-  for (int a = 0; a < IB; ++a) *(Sum4*)(red + (wave * IB + a) * 256 + 4 * lane) = sum[a];
+  for (int a = 0; a < IB; ++a)
+#pragma unroll
+    for (int b = 0; b < JB; ++b)
+      *(Sum4*)(red + ((wave * IB + a) * JB + b) * 256 + 4 * lane) = sum[a][b];
   __syncthreads();
-  for (int e = threadIdx.x; e < IB * 256; e += 512) {
-    const int j = e & 15, i = (e >> 4) & 15, a = e >> 8;
+  for (int e = threadIdx.x; e < IB * JB * 256; e += 512) {
+    const int j = e % (16 * JB), i = e / (16 * JB) % 16, a = e / (256 * JB);
     const int t = t0 + 16 * a + i, c = n0 + j;
     if (t < T && c < N) {
-      float y = (float)skinny_sum<NW, IB>(red, a, i, j);
+      float y = (float)skinny_sum<NW, IB * JB>(red, a * JB + j / 16, i, j % 16);
       if (GROUP == 0) y *= sw[c];
       store_y(Y, dtype, (size_t)t * N + c, y * sx[t]);
     }
   }
 }
 
+template <int GROUP, int IB, int JB, int U>
+static hipError_t launch_i8_skinny(hipStream_t st, int dtype, int T, int N, int K,
+                                   const int8_t* Xq, const float* sx, const int8_t* Wq,
+                                   const float* sw, void* Y) {
+  const dim3 grid((N + 16 * JB - 1) / (16 * JB), (T + 16 * IB - 1) / (16 * IB));
+  hipLaunchKernelGGL((i8_skinny_kernel<GROUP, IB, JB, U>), grid, dim3(512), 0, st, Xq, sx, Wq, sw,
+                     T, N, K, dtype, Y);
+  return hipGetLastError();
+}
+template <int GROUP, int S, int WI, int WJ, int BI, int BJ>
+static hipError_t launch_i8_tiles(hipStream_t st, int dtype, int T, int N, int K, const int8_t* Xq,
+                                  const float* sx, const int8_t* Wq, const float* sw, void* Y) {
+  const int ni = (T + 32 * WI * BI - 1) / (32 * WI * BI);
+  const int nj = (N + 32 * WJ * BJ - 1) / (32 * WJ * BJ);
+  hipLaunchKernelGGL((i8_tile_kernel<GROUP, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
+                     dim3(64 * WI * WJ), 0, st, Xq, sx, Wq, sw, T, N, K, dtype, Y, ni, nj);
+  return hipGetLastError();
+}
+
+// Up to 32 tokens, and up to 64 for layers of up to 8192 channels, fragments straight from
+// memory; channels in blocks of 16 where wider ones are too few for the chip.  k = 4096:
+// 64 tokens -> 4096 with 16, 32 channels a work-group 13, 11 us, tiles 14; 64 -> 1000 (groups
+// of 32) 10, 18, 31; 37 -> 11008 (groups of 128) 29, 27 and 21.  Beyond, the tiles that
+// tile_cost makes the cheapest; k = 4096 -> 1000, 4096 and 11008 channels, in us with tiles of
+// 256 x 256, 128 x 128 (tokens x channels), 128 x 64, 64 x 64 and 64 x 32:
+//    100 tokens   44 19 14 12 11   44 19 14 12 11     45  22  18  20  20
+//    400          45 19 14 12 11   48 23 16 18 28     50  39  50  47  60
+//   1600          48 23 17 18 29   51 44 63 60 77    112 110 147 146 192
+// Groups (of 64, 1600 tokens -> 4096): 128 x 128 77, 256 x 128 74; 800 -> 11008 119 and 137:
+// converting a group's sums takes the vector units as long as the matrix cores.
 template <int GROUP>
 static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K, const int8_t* Xq,
                                   const float* sx, const int8_t* Wq, const float* sw, void* Y) {
-  const dim3 wg((N + 15) / 16);
-  if (T <= 16) {
-    hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 1>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
-                       dtype, Y);
-  } else if (T <= 32) {
-    hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 2>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
-                       dtype, Y);
-  } else if (T <= 64) {
-    hipLaunchKernelGGL((i8_skinny_kernel<GROUP, 4>), wg, dim3(512), 0, st, Xq, sx, Wq, sw, T, N, K,
-                       dtype, Y);
-  } else {
-    // (with group scales the fp32 sums take the registers that wider blocks would)
-    const int bi = (T + 255) / 256, bj = (N + 255) / 256;
-    if (GROUP == 0 && (long long)bi * bj >= 192) {
+  auto tiles = [&](int t, int n) { return (long long)((T + t - 1) / t) * ((N + n - 1) / n); };
+  if (T <= 16 || (T <= 64 && N <= 2048))
+    return launch_i8_skinny<GROUP, 1, 1, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+  if (T <= 32) return launch_i8_skinny<GROUP, 2, 1, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+  if (T <= 64 && N <= 8192)
+    return launch_i8_skinny<GROUP, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+  const int nk = (K + kChunk - 1) / kChunk;
+  constexpr double plain[4] = {0.25, 0.17, 0.135, 0.12}, grouped[4] = {0.55, 0.43, 0.3, 0.28};
+  const double* c = GROUP ? grouped : plain;
+  const double cost[5] = {tile_cost(tiles(128, 128), nk, c[0], 3.8),
+                          tile_cost(tiles(128, 64), nk, c[1], 3.0),
+                          tile_cost(tiles(64, 64), nk, c[2], 3.0),
+                          tile_cost(tiles(64, 32), nk, c[3], 3.0),
+                          GROUP ? 1e30 : tile_cost(tiles(256, 256), nk, 0.7, 6.0)};
+  switch ((int)(std::min_element(cost, cost + 5) - cost)) {
+    case 0:
+      return launch_i8_tiles<GROUP, 4, 2, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 1:
+      return launch_i8_tiles<GROUP, 8, 2, 2, 2, 1>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 2:
+      return launch_i8_tiles<GROUP, 8, 2, 2, 1, 1>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 3:
+      return launch_i8_tiles<GROUP, 8, 2, 1, 1, 1>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    default:
       if constexpr (GROUP == 0)
-        hipLaunchKernelGGL((i8_tile_kernel<0, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)), dim3(512),
-                           0, st, Xq, sx, Wq, sw, T, N, K, dtype, Y, bi, bj);
-    } else {
-      const int ni = (T + 127) / 128, nj = (N + 127) / 128;
-      hipLaunchKernelGGL((i8_tile_kernel<GROUP, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
-                         dim3(256), 0, st, Xq, sx, Wq, sw, T, N, K, dtype, Y, ni, nj);
-    }
+        return launch_i8_tiles<0, 4, 2, 4, 4, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return hipErrorInvalidValue;
   }
-  return hipGetLastError();
 }
 
 hipError_t launch_matmul_i8(hipStream_t st, int dtype, int T, int N, int K, int group,

@@ -174,7 +174,7 @@ __device__ __forceinline__ s16x4 lds_read_tr16(const char* p) {
 }
 
 // An operand tile of TR columns with k down the rows (16-bit values): a chunk is
-// kRows rows of TR values.  64-byte block x of row t lies at x ^ (t % 4): a
+// kRows rows of TR values.  64-byte block x of row t lies at x ^ swz(t): a
 // transposing read takes one block of four consecutive rows.  Columns past the last
 // read the last eight; rows past the last read zeros.  kTwoSpans: k runs down one
 // matrix, then down another.
@@ -187,7 +187,9 @@ struct KStrided {
   static constexpr int RPI = 64 / CPR;          // rows per load instruction
   static constexpr int N = kRows / RPI / NW;
   static_assert(N >= 1 && N * RPI * NW == kRows && (NW * RPI) % 4 == 0, "tile");
+  static_assert(TR >= 64, "a row has two 64-byte blocks at least");
   static constexpr int kBytes = TR * kChunk;
+  static __device__ __forceinline__ int swz(int t) { return TR >= 128 ? t & 3 : (t >> 1) & 1; }
   const char *b0, *b1;
   size_t ld;
   uint32_t off[N];
@@ -201,7 +203,7 @@ struct KStrided {
     rows = rows_;
     wave = w;
     lt = RPI * w + lane / CPR;
-    const int pc = (lane % CPR) ^ ((lt & 3) << 2);
+    const int pc = (lane % CPR) ^ (swz(lt) << 2);
     b0 = (const char*)p0;
     b1 = (const char*)p1;
 #pragma unroll
@@ -230,7 +232,7 @@ struct KStrided {
       const int gi = lane >> 4, pi = lane & 15, t = pi >> 2;
 #pragma unroll
       for (int a = 0; a < B; ++a)
-        o[a] = (uint32_t)((8 * (gi >> 1) + t) * RB + ((((col0 >> 5) + a) ^ t) << 6) +
+        o[a] = (uint32_t)((8 * (gi >> 1) + t) * RB + ((((col0 >> 5) + a) ^ swz(t)) << 6) +
                           32 * (gi & 1) + 8 * (pi & 3));
     }
     __device__ __forceinline__ u32x4 frag(const char* stage, int a, int ks) const {
@@ -253,23 +255,31 @@ __device__ __forceinline__ void wait_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// The k-loop over chunks q0 <= q < q1 (at least one) with four stages: while a chunk
-// is multiplied, the loads of the three behind it are in flight, and the next
-// fragments are read a slice ahead.  The four stages are arrays of their own, so that
-// the compiler can tell which of them a load in flight writes; the loop runs in
-// whole rounds of them (chunks past the last are zeros).  A wave's P blocks start at
-// row prow of the tile, its Q blocks at qrow.  round(q) comes before every fourth
-// chunk; mul(p, q, a, b, ks, i) gets the fragments of P block a and Q block b, slice ks of
+// The S stages of a work-group, `bytes` each: arrays of their own, so that the
+// compiler can tell which of them a load in flight writes.
+#define JARQ_STAGES(S, bytes)                                                     \
+  __shared__ __attribute__((aligned(1024))) char stage0[bytes], stage1[bytes],    \
+      stage2[bytes], stage3[bytes];                                               \
+  __shared__ __attribute__((aligned(16))) char stage4[S > 4 ? (bytes) : 16],      \
+      stage5[S > 4 ? (bytes) : 16], stage6[S > 4 ? (bytes) : 16],                 \
+      stage7[S > 4 ? (bytes) : 16];                                               \
+  char* const stages[8] = {stage0, stage1, stage2, stage3, stage4, stage5, stage6, stage7}
+
+// The k-loop over chunks q0 <= q < q1 (at least one) with S stages: while a chunk is
+// multiplied, the loads of the S - 1 behind it are in flight, and the next fragments
+// are read a slice ahead.  The loop runs in whole rounds of the stages (chunks past the
+// last are zeros).  A wave's P blocks start at row prow of the tile, its Q blocks at
+// qrow.  round(q) comes before each round; mul(p, q, a, b, ks, i) gets the fragments of P block a and Q block b, slice ks of
 // chunk i of the round.
 //
 // 4096 x 4096 -> 2 x 14336 channels, 256-wide tiles: two stages of twice the chunk 812 us,
 // four 800; the loads in a row at the start of a chunk 860; by address instead of by
 // buffer (every LDS read then waits for all others) 905.  Bound by the matrix cores at
 // the clock that the card's power allows (1.7 GHz here).
-template <int BI, int BJ, class LP, class LQ, class Round, class Mul>
+template <int S, int BI, int BJ, class LP, class LQ, class Round, class Mul>
 __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int q1, int lane,
-                                         int prow, int qrow, char* s0, char* s1, char* s2,
-                                         char* s3, const Round& round, const Mul& mul) {
+                                         int prow, int qrow, char* const (&stages)[8],
+                                         const Round& round, const Mul& mul) {
   constexpr int L = LP::N + LQ::N, R = BI + BJ, M = BI * BJ;
   u32x4 fp[2][BI], fq[2][BJ];
   const typename LP::template Lane<BI> pl(prow, lane);
@@ -284,10 +294,12 @@ __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int
     if (l < LP::N) lp.issue(cp, l, stage);
     else lq.issue(cq, l - LP::N, stage + LP::kBytes);
   };
-  auto chunk = [&](int q, int i, char* cur, char* next, char* far)
-      __attribute__((always_inline)) {
-    const typename LP::Chunk cp = lp.chunk(q + i + 3, q + i + 3 < q1);
-    const typename LQ::Chunk cq = lq.chunk(q + i + 3, q + i + 3 < q1);
+  static_assert((S - 2) * L < 64, "loads in flight");
+  auto chunk = [&](int q, int i) __attribute__((always_inline)) {
+    char *const cur = stages[i], *const next = stages[(i + 1) % S];
+    char* const far = stages[(i + S - 1) % S];
+    const typename LP::Chunk cp = lp.chunk(q + i + S - 1, q + i + S - 1 < q1);
+    const typename LQ::Chunk cq = lq.chunk(q + i + S - 1, q + i + S - 1 < q1);
     // the second slice's fragments and the loads one at a time among the first one's
     // products: in a row they would hold up the wave
 #pragma unroll
@@ -301,9 +313,9 @@ __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int
       }
       __builtin_amdgcn_sched_barrier(0);
     }
-    // the loads of the next chunk are in (those of the two behind it may not be), and
-    // no wave reads this chunk's stage any more
-    wait_barrier<2 * L>();
+    // the loads of the next chunk are in (those behind it may not be), and no wave
+    // reads this chunk's stage any more
+    wait_barrier<(S - 2) * L>();
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       mul(fp[1][m / BJ], fq[1][m % BJ], m / BJ, m % BJ, 1, i);
@@ -314,23 +326,20 @@ __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int
       __builtin_amdgcn_sched_barrier(0);
     }
   };
-  char* const stages[3] = {s0, s1, s2};
 #pragma unroll
-  for (int i = 0; i < 3; ++i) {
+  for (int i = 0; i < S - 1; ++i) {
     const typename LP::Chunk cp = lp.chunk(q0 + i, q0 + i < q1);
     const typename LQ::Chunk cq = lq.chunk(q0 + i, q0 + i < q1);
 #pragma unroll
     for (int l = 0; l < L; ++l) issue(l, cp, cq, stages[i]);
   }
-  wait_barrier<2 * L>();
+  wait_barrier<(S - 2) * L>();
 #pragma unroll
-  for (int r = 0; r < R; ++r) read(s0, 0, r);
-  for (int q = q0; q < q1; q += 4) {
+  for (int r = 0; r < R; ++r) read(stages[0], 0, r);
+  for (int q = q0; q < q1; q += S) {
     round(q);
-    chunk(q, 0, s0, s1, s3);
-    chunk(q, 1, s1, s2, s0);
-    chunk(q, 2, s2, s3, s1);
-    chunk(q, 3, s3, s0, s2);
+#pragma unroll
+    for (int i = 0; i < S; ++i) chunk(q, i);
   }
   wait_barrier<0>();
 }
@@ -339,6 +348,13 @@ __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int
 template <int RB>
 __device__ __forceinline__ char* out_piece(char* buf, int r, int c) {
   return buf + r * RB + ((c ^ (r & (RB / 16 - 1))) << 4);
+}
+
+// What a launch takes in us if each of the 256 CUs has one of its work-groups at a time:
+// `chunk` a chunk and `rest` for the beginning and the end.  The launchers' figures
+// are of launches of one work-group a CU (K of 32 and of 128 chunks).
+inline double tile_cost(long long groups, int chunks, double chunk, double rest) {
+  return (double)((groups + 255) / 256) * (chunks * chunk + rest);
 }
 
 // Tile (ti, tj) of work-group `id` in a grid of ni x nj tiles: the work-groups
