@@ -131,9 +131,8 @@ jarq_status jarq_linear_i8(int32_t dtype, int64_t tokens, int32_t n, int32_t k, 
   hipStream_t st = (hipStream_t)stream;
   int8_t* q = (int8_t*)workspace;
   float* sx = (float*)((char*)workspace + pad256((size_t)tokens * k));
-  const hipError_t e = launch_quant_rows(st, dtype, X, (int)tokens, k, q, sx);
-  if (e != hipSuccess) return JARQ_EHIP;
-  return status_of(launch_matmul_i8(st, dtype, (int)tokens, n, k, group, q, sx, Wq, sw, Y));
+  return status_of(
+      launch_linear_i8(st, dtype, (int)tokens, n, k, group, X, Wq, sw, Y, q, sx));
 }
 
 size_t jarq_token_logprobs_workspace_bytes(int64_t tokens, int32_t vocab, int32_t top) {

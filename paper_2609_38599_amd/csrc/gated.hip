@@ -10,7 +10,6 @@
 // outputs'); then dx = [da db] [Wg; Wu] in one product over 2 F, and
 // [dWg; dWu] = [da db]^T x in one over T.
 #include <algorithm>
-#include <type_traits>
 
 #include "skinny.h"
 
@@ -79,52 +78,49 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                        });
-  // Out through LDS, so that memory gets whole lines (8 bytes a lane straight from the
-  // registers: 75 us more of 800 at 4096 x 4096 -> 14336).  The waves of one wj share a
-  // stage of 32 BJ tokens.
-  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
-  const int row = lane & 31, tw = t0 + wj * 32 * BJ;
-  auto send = [&](auto* to, auto put) __attribute__((always_inline)) {
-    typedef typename std::remove_reference<decltype(*to)>::type E;
-    constexpr int RB = TI / 2 * sizeof(E), PIECES = RB / 16;
-    static_assert(32 * BJ * RB <= STAGE, "stage");
+  // Out through LDS, 32 tokens of a wave column at a time: memory gets whole lines, and
+  // the activation's code is there once (formed from the registers it is 45 KB, read
+  // anew for each tile: 786 us at 4096 x 4096 -> 14336, NEWUS this way).
+  constexpr int RB = TI / 2 * 4, PIECES = RB / 16;   // a row: one projection's fp32
+  constexpr bool APART = WJ == 2;                    // two stages a column, else one
+  static_assert((APART ? 1 : 2) * 32 * RB <= STAGE && (WJ == 2 || WJ == 4), "stage");
+  char* const ga = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  char* const up = APART ? (wj == 0 ? stage2 : stage3) : ga + 32 * RB;
+  const int row = lane & 31;
 #pragma unroll
-    for (int b = 0; b < BJ; ++b)
+  for (int b = 0; b < BJ; ++b) {
+    if (b > 0) __syncthreads();
 #pragma unroll
-      for (int a = 0; a < BI / 2; ++a)
+    for (int a = 0; a < BI / 2; ++a)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int at = (wi * 16 * BI + 32 * a + 8 * r + 4 * (lane >> 5)) * (int)sizeof(E);
-          put(out_piece<RB>(stage, 32 * b + row, at >> 4) + (at & 15), a, b, 4 * r);
-        }
+      for (int r = 0; r < 4; ++r) {
+        const int c = (wi * 16 * BI + 32 * a + 8 * r + 4 * (lane >> 5)) / 4;
+        const f32x16 &g = acc[a][b], &u = acc[BI / 2 + a][b];
+        *(f32x4*)out_piece<RB>(ga, row, c) =
+            f32x4{g[4 * r], g[4 * r + 1], g[4 * r + 2], g[4 * r + 3]};
+        *(f32x4*)out_piece<RB>(up, row, c) =
+            f32x4{u[4 * r], u[4 * r + 1], u[4 * r + 2], u[4 * r + 3]};
+      }
     __syncthreads();
+    const int tb = t0 + wj * 32 * BJ + 32 * b;
+#pragma unroll 1
+    for (int p = wi * 64 + lane; p < 32 * PIECES; p += WI * 64) {
+      const int r = p / PIECES, c = p % PIECES, t = tb + r, f = f0 + 4 * c;
+      const f32x4 g = *(const f32x4*)out_piece<RB>(ga, r, c);
+      const f32x4 u = *(const f32x4*)out_piece<RB>(up, r, c);
+      if (t < T && f < F) {
+        const size_t e = (size_t)t * F + f;
+        if (pre) {
+          *(f32x4*)(pre + e) = g;
+          *(f32x4*)(pre + (size_t)T * F + e) = u;
+        }
+        float y[4];
 #pragma unroll
-    for (int k = 0; k < 32 * BJ * PIECES / (WI * 64); ++k) {
-      const int p = (k * WI + wi) * 64 + lane;
-      const int t = p / PIECES, c = p % PIECES;
-      const u32x4 w = *(const u32x4*)out_piece<RB>(stage, t, c);
-      const int f = f0 + c * (16 / (int)sizeof(E));
-      if (tw + t < T && f < F) *(u32x4*)(to + (size_t)(tw + t) * F + f) = w;
-    }
-  };
-  if (pre) {   // uniform
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      send(pre + (size_t)half * T * F, [&](char* at, int a, int b, int v)
-                                           __attribute__((always_inline)) {
-        const f32x16& c = acc[half * BI / 2 + a][b];
-        *(f32x4*)at = f32x4{c[v], c[v + 1], c[v + 2], c[v + 3]};
-      });
-      __syncthreads();
+        for (int i = 0; i < 4; ++i) y[i] = activation(act, g[i], nullptr) * u[i];
+        *(u32x2*)(Y + e) = u32x2{pack16<KIND>(y[0], y[1]), pack16<KIND>(y[2], y[3])};
+      }
     }
   }
-  send(Y, [&](char* at, int a, int b, int v) __attribute__((always_inline)) {
-    float y[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      y[i] = activation(act, acc[a][b][v + i], nullptr) * acc[BI / 2 + a][b][v + i];
-    *(u32x2*)at = u32x2{pack16<KIND>(y[0], y[1]), pack16<KIND>(y[2], y[3])};
-  });
 }
 
 // ---- forward, few tokens ----

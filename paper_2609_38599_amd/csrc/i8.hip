@@ -42,6 +42,16 @@ __device__ __forceinline__ uint32_t quant(float x, float mul) {
   return mul == 0.f ? 0u : (uint32_t)(int)rintf(x * mul) & 0xffu;
 }
 
+__device__ __forceinline__ u32x2 quant8(const float (&x)[8], float mul) {
+  uint32_t lo = 0, hi = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lo |= quant(x[i], mul) << (8 * i);
+    hi |= quant(x[4 + i], mul) << (8 * i);
+  }
+  return u32x2{lo, hi};
+}
+
 // Eight values from element 8 v of a row.
 template <int DT>
 __device__ __forceinline__ void load8(const void* row, int v, float (&x)[8]) {
@@ -90,13 +100,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const void* __restrict_
   for (int v = threadIdx.x; v < nv; v += 256) {
     float x[8];
     load8<DT>(row, v, x);
-    uint32_t lo = 0, hi = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      lo |= quant(x[i], mul) << (8 * i);
-      hi |= quant(x[4 + i], mul) << (8 * i);
-    }
-    *(u32x2*)(Q + r * K + 8 * (size_t)v) = u32x2{lo, hi};
+    *(u32x2*)(Q + r * K + 8 * (size_t)v) = quant8(x, mul);
   }
   if (threadIdx.x == 0) scale[r] = s;
 }
@@ -229,53 +233,78 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
           }
         });
   }
-  // Out through LDS, 32 tokens x 32 BJ channels of a wave at a time.
+  // Out through LDS as fp32, 32 tokens x 32 BJ channels of a wave at a time.
   constexpr int CH = 32 * BJ;
   constexpr int PER = STAGE / (32 * CH * 4);   // waves a stage serves
   static_assert(PER >= 1 && PER * 4 >= NW, "stage");
-  char* const mine = (wave / PER == 0 ? stage0 : wave / PER == 1 ? stage1
-                      : wave / PER == 2 ? stage2 : stage3) + wave % PER * 32 * CH * 4;
+  float* const mine = (float*)(wave / PER == 0 ? stage0 : wave / PER == 1 ? stage1
+                               : wave / PER == 2 ? stage2 : stage3) + wave % PER * 32 * CH;
   const int nw = n0 + qrow;
-  const size_t es = dtype == 0 ? 4 : 2;
-  // 16-byte stores where every row starts at a 16-byte boundary and none ends inside a piece
-  const bool wide = (uintptr_t)Y % 16 == 0 && (size_t)N * es % 16 == 0;
+  // four values at a time where every row starts at their boundary and none ends inside four
+  const bool wide = (uintptr_t)Y % (dtype == 0 ? 16 : 8) == 0 && N % 4 == 0;
 #pragma unroll
   for (int a = 0; a < BI; ++a) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
       const int r = 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
-      const float st = sx[min(t0 + prow + 32 * a + r, T - 1)];
 #pragma unroll
-      for (int b = 0; b < BJ; ++b) {
-        const int c = 32 * b + (lane & 31);
-        const float out =
-            (GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0]) * st;
-        if (dtype == 0) ((float*)mine)[r * CH + c] = out;
-        else
-          ((uint16_t*)mine)[r * CH + c] = dtype == kF16 ? to16<kF16>(out) : to16<kBF16>(out);
-      }
+      for (int b = 0; b < BJ; ++b)
+        mine[r * CH + 32 * b + (lane & 31)] =
+            GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0];
     }
     asm volatile("" ::: "memory");   // one wave: its LDS accesses complete in order
     const int tw = t0 + prow + 32 * a;
-    const int pieces = CH * (int)es / 16, per = 16 / (int)es;
     if (wide) {
-      for (int p = lane; p < 32 * pieces; p += 64) {
-        const int r = p / pieces, c = p % pieces;
-        if (tw + r < T && nw + c * per < N)
-          *(u32x4*)((char*)Y + ((size_t)(tw + r) * N + nw) * es + 16 * c) =
-              *(const u32x4*)(mine + 16 * p);
+#pragma unroll 1
+      for (int p = lane; p < 32 * CH / 4; p += 64) {
+        const int t = tw + p / (CH / 4), n = nw + 4 * (p % (CH / 4));
+        if (t < T && n < N) {
+          const f32x4 s = *(const f32x4*)(mine + 4 * p);
+          const float st = sx[t];
+          const float o[4] = {s[0] * st, s[1] * st, s[2] * st, s[3] * st};
+          const size_t e = (size_t)t * N + n;
+          if (dtype == 0) *(f32x4*)((float*)Y + e) = f32x4{o[0], o[1], o[2], o[3]};
+          else if (dtype == kF16)
+            *(u32x2*)((uint16_t*)Y + e) = u32x2{pack16<kF16>(o[0], o[1]), pack16<kF16>(o[2], o[3])};
+          else
+            *(u32x2*)((uint16_t*)Y + e) =
+                u32x2{pack16<kBF16>(o[0], o[1]), pack16<kBF16>(o[2], o[3])};
+        }
       }
     } else {
-      for (int e = lane; e < 32 * CH; e += 64) {
-        const int r = e / CH, c = e % CH;
-        if (tw + r < T && nw + c < N) {
-          const size_t at = (size_t)(tw + r) * N + nw + c;
-          if (dtype == 0) ((float*)Y)[at] = ((const float*)mine)[e];
-          else ((uint16_t*)Y)[at] = ((const uint16_t*)mine)[e];
-        }
+#pragma unroll 1
+      for (int p = lane; p < 32 * CH; p += 64) {
+        const int t = tw + p / CH, n = nw + p % CH;
+        if (t < T && n < N) store_y(Y, dtype, (size_t)t * N + n, mine[p] * sx[t]);
       }
     }
     asm volatile("" ::: "memory");
+  }
+}
+
+// Step `st` (64 k) of a wave's 16 x 16 block: GROUP 0 sums on; otherwise the group's
+// integer sum is complete after its last step and goes to fp32 with its scale.
+template <int GROUP, class Sum4>
+__device__ __forceinline__ void i8_step(int st, const u32x4& fp, const u32x4& fq, bool low,
+                                        const float* s, i32x4& acc, Sum4& sum) {
+  if constexpr (GROUP == 0) {
+    sum = Mma<kI8>::mul16(fp, fq, sum);
+  } else if constexpr (GROUP == 32) {
+    // a step's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const u32x4 part = (h == 0) == low ? fp : u32x4{};
+      const i32x4 c = Mma<kI8>::mul16(part, fq, i32x4{});
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)c[v], s[2 * st + h], sum[v]);
+    }
+  } else {
+    constexpr int SG = GROUP / 64;   // steps a group
+    acc = Mma<kI8>::mul16(fp, fq, st % SG == 0 ? i32x4{} : acc);
+    if (st % SG == SG - 1) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)acc[v], s[st / SG], sum[v]);
+    }
   }
 }
 
@@ -326,29 +355,8 @@ __global__ __launch_bounds__(512) void i8_skinny_kernel(
 #pragma unroll
         for (int a = 0; a < IB; ++a)
 #pragma unroll
-          for (int b = 0; b < JB; ++b) {
-            if constexpr (GROUP == 0) {
-              sum[a][b] = Mma<kI8>::mul16(fp[a], fq[b], sum[a][b]);
-            } else if constexpr (GROUP == 32) {
-              // a step's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
-#pragma unroll
-              for (int h = 0; h < 2; ++h) {
-                const u32x4 part = (h == 0) == low ? fp[a] : u32x4{};
-                const i32x4 c = Mma<kI8>::mul16(part, fq[b], i32x4{});
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                  sum[a][b][v] = fmaf((float)c[v], s[set][b][2 * st + h], sum[a][b][v]);
-              }
-            } else {
-              constexpr int SG = GROUP / 64;   // steps a group
-              acc[a][b] = Mma<kI8>::mul16(fp[a], fq[b], st % SG == 0 ? i32x4{} : acc[a][b]);
-              if (st % SG == SG - 1) {
-#pragma unroll
-                for (int v = 0; v < 4; ++v)
-                  sum[a][b][v] = fmaf((float)acc[a][b][v], s[set][b][st / SG], sum[a][b][v]);
-              }
-            }
-          }
+          for (int b = 0; b < JB; ++b)
+            i8_step<GROUP>(st, fp[a], fq[b], low, s[set][b], acc[a][b], sum[a][b]);
       });
 #pragma unroll
   for (int a = 0; a < IB; ++a)
@@ -363,6 +371,105 @@ __global__ __launch_bounds__(512) void i8_skinny_kernel(
       float y = (float)skinny_sum<NW, IB * JB>(red, a * JB + j / 16, i, j % 16);
       if (GROUP == 0) y *= sw[c];
       store_y(Y, dtype, (size_t)t * N + c, y * sx[t]);
+    }
+  }
+}
+
+// One to four tokens, quantized by every work-group for itself: one launch instead of
+// two (one token, 4096 -> 4096: TIMES).  The weights' first
+// fragments are on their way while the tokens go to LDS as integers.
+constexpr int kFusedTokens = 4, kFusedBytes = 48 << 10;   // at most, tokens and bytes of them
+template <int DT, int GROUP>
+__global__ __launch_bounds__(512) void i8_fused_kernel(const void* __restrict__ X,
+                                                       const int8_t* __restrict__ Wq,
+                                                       const float* __restrict__ sw, int T, int N,
+                                                       int K, void* __restrict__ Y) {
+  constexpr int NW = 8, U = 4;
+  constexpr int GU = GROUP ? 64 * U / GROUP : 1;
+  typedef typename std::conditional<GROUP == 0, int32_t, float>::type Sum;
+  typedef Sum Sum4 __attribute__((ext_vector_type(4)));
+  extern __shared__ __attribute__((aligned(16))) char xq[];   // [T][K], 64 U bytes behind them
+  __shared__ __attribute__((aligned(16))) Sum red[NW * 256];
+  __shared__ uint32_t amax[kFusedTokens][NW];
+  __shared__ float sx[kFusedTokens];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16, row = lane & 15, at = 16 * (lane >> 4);
+  const int n = min(n0 + row, N - 1);
+  const int G = GROUP ? K / GROUP : 1;
+  const char* q = (const char*)Wq + (size_t)n * K;
+  const float* srow = sw + (size_t)n * G;
+  const int units = (K + 64 * U - 1) / (64 * U);
+  u32x4 fq[2][U];
+  float s[2][GU];
+  auto load = [&](int u, int set) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int k = u * 64 * U + 64 * i + at;
+      fq[set][i] = k < K ? *(const u32x4*)(q + k) : u32x4{};
+    }
+    if constexpr (GROUP != 0) {
+#pragma unroll
+      for (int g = 0; g < GU; ++g) s[set][g] = u * GU + g < G ? srow[u * GU + g] : 0.f;
+    }
+  };
+  if (wave < units) load(wave, 0);
+  const size_t es = DT == 0 ? 4 : 2;
+  for (int t = 0; t < T; ++t) {
+    uint32_t m = 0;
+    for (int v = tid; v < K / 8; v += 512) {
+      float x[8];
+      load8<DT>((const char*)X + (size_t)t * K * es, v, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
+    if (lane == 0) amax[t][wave] = m;
+  }
+  __syncthreads();
+  for (int t = 0; t < T; ++t) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) m = max(m, amax[t][w]);
+    float scale, mul;
+    row_scale(m, scale, mul);
+    for (int v = tid; v < K / 8; v += 512) {
+      float x[8];
+      load8<DT>((const char*)X + (size_t)t * K * es, v, x);
+      *(u32x2*)(xq + t * K + 8 * v) = quant8(x, mul);
+    }
+    if (tid == t) sx[t] = scale;
+  }
+  __syncthreads();
+  const char* p = xq + min(row, T - 1) * K + at;
+  Sum4 sum = {};
+  i32x4 acc;
+  const bool low = lane < 32;
+  auto mul = [&](int u, int set) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      // (past k the weights are zeros)
+      const u32x4 fp = *(const u32x4*)(p + u * 64 * U + 64 * i);
+      i8_step<GROUP>(i, fp, fq[set][i], low, s[set], acc, sum);
+    }
+  };
+  for (int u = wave; u < units; u += 2 * NW) {
+    if (u + NW < units) load(u + NW, 1);
+    mul(u, 0);
+    if (u + NW < units) {
+      if (u + 2 * NW < units) load(u + 2 * NW, 0);
+      mul(u + NW, 1);
+    }
+  }
+  *(Sum4*)(red + wave * 256 + 4 * lane) = sum;
+  __syncthreads();
+  if (tid < 256) {
+    const int j = tid & 15, t = tid >> 4, c = n0 + j;
+    if (t < T && c < N) {
+      float y = (float)skinny_sum<NW, 1>(red, 0, t, j);
+      if (GROUP == 0) y *= sw[c];
+      store_y(Y, DT, (size_t)t * N + c, y * sx[t]);
     }
   }
 }
@@ -440,6 +547,35 @@ hipError_t launch_matmul_i8(hipStream_t st, int dtype, int T, int N, int K, int 
     case 128: return launch_i8_group<128>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     default: return hipErrorInvalidValue;
   }
+}
+
+template <int DT>
+static hipError_t launch_i8_fused(hipStream_t st, int T, int N, int K, int group, const void* X,
+                                  const int8_t* Wq, const float* sw, void* Y) {
+  const dim3 grid((N + 15) / 16), block(512);
+  const size_t lds = (size_t)T * K + 256;
+  if (group == 0)
+    hipLaunchKernelGGL((i8_fused_kernel<DT, 0>), grid, block, lds, st, X, Wq, sw, T, N, K, Y);
+  else if (group == 32)
+    hipLaunchKernelGGL((i8_fused_kernel<DT, 32>), grid, block, lds, st, X, Wq, sw, T, N, K, Y);
+  else if (group == 64)
+    hipLaunchKernelGGL((i8_fused_kernel<DT, 64>), grid, block, lds, st, X, Wq, sw, T, N, K, Y);
+  else
+    hipLaunchKernelGGL((i8_fused_kernel<DT, 128>), grid, block, lds, st, X, Wq, sw, T, N, K, Y);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear_i8(hipStream_t st, int dtype, int T, int N, int K, int group,
+                            const void* X, const int8_t* Wq, const float* sw, void* Y, int8_t* Xq,
+                            float* sx) {
+  if (T <= kFusedTokens && T * K <= kFusedBytes) {
+    if (dtype == 0) return launch_i8_fused<0>(st, T, N, K, group, X, Wq, sw, Y);
+    if (dtype == kF16) return launch_i8_fused<kF16>(st, T, N, K, group, X, Wq, sw, Y);
+    return launch_i8_fused<kBF16>(st, T, N, K, group, X, Wq, sw, Y);
+  }
+  const hipError_t e = launch_quant_rows(st, dtype, X, T, K, Xq, sx);
+  if (e != hipSuccess) return e;
+  return launch_matmul_i8(st, dtype, T, N, K, group, Xq, sx, Wq, sw, Y);
 }
 
 }  // namespace jarq

@@ -413,6 +413,11 @@ hipError_t launch_matmul_i8(hipStream_t st, int dtype, int T, int N, int K, int 
                             const int8_t* Xq, const float* sx, const int8_t* Wq, const float* sw,
                             void* Y);
 
+// Xq [T][K] and sx [T]: scratch
+hipError_t launch_linear_i8(hipStream_t st, int dtype, int T, int N, int K, int group,
+                            const void* X, const int8_t* Wq, const float* sw, void* Y, int8_t* Xq,
+                            float* sx);
+
 // logprob.hip
 size_t logprob_workspace_bytes(int T, int V, int top);
 hipError_t launch_token_logprobs(hipStream_t st, int dtype, const void* logits, size_t ld, int T,

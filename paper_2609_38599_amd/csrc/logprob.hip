@@ -44,6 +44,12 @@ __device__ __forceinline__ float exp_of(float t) {
   else return __expf(t);
 }
 
+template <int DT>
+__device__ __forceinline__ u32x4 minus_inf() {
+  const uint32_t w = DT == 0 ? 0xff800000u : DT == kF16 ? 0xfc00fc00u : 0xff80ff80u;
+  return u32x4{w, w, w, w};
+}
+
 // The running maximum (at least -FLT_MAX, so that x - m is never -inf + inf), sum
 // and weighted sum.
 struct Soft {
@@ -98,30 +104,31 @@ __device__ __forceinline__ uint32_t key_index(u64 k) { return 0xffffffffu - (uin
 __device__ __forceinline__ uint32_t ordered(float x) { return (uint32_t)(top_key(x, 0) >> 32); }
 constexpr uint32_t kOrderedMinusInf = 0x007fffffu;
 
-// Entries of a wave (R a lane) that are at least `t`.
+// Entries of a wave (R a lane, n in all, 64 to a register) that are at least `t` > 0.
 template <int R>
-__device__ __forceinline__ int count_from(const uint32_t (&v)[R], uint32_t t) {
+__device__ __forceinline__ int count_from(const uint32_t (&v)[R], int n, uint32_t t) {
   int c = 0;
 #pragma unroll
-  for (int r = 0; r < R; ++r) c += __popcll(__ballot(v[r] >= t));
+  for (int r = 0; r < R; ++r)
+    if (64 * r < n) c += __popcll(__ballot(v[r] >= t));   // uniform
   return c;
 }
 // The largest value, of `bits` leading bits and zeros behind, that at least k of a
 // wave's entries reach; 0 if there are fewer.
 template <int R>
-__device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[R], int k, int bits) {
+__device__ __forceinline__ uint32_t reached_by(const uint32_t (&v)[R], int n, int k, int bits) {
   uint32_t t = 0;
+#pragma unroll 1
   for (int b = 31; b >= 32 - bits; --b)
-    if (count_from<R>(v, t | (1u << b)) >= k) t |= 1u << b;
+    if (count_from<R>(v, n, t | (1u << b)) >= k) t |= 1u << b;
   return t;
 }
 
 // A wave's candidates for the top k: keys in LDS, cut back to the k largest when
-// more than kKeep are there.  A lane's entries are offered eight at a time.
+// more than kKeep are there.  A lane's entries are offered four at a time.
 constexpr int kKeep = 128;
-template <int VE>
 struct TopList {
-  static constexpr int kCap = kKeep + 64 * VE;
+  static constexpr int kCap = kKeep + 64 * 4;   // and eight zeros behind the last key
   u64* keys;          // of this wave
   uint32_t* slots;    // one a wave: a value that ceil(k / 4) of its entries reach
   int n, k, wave;
@@ -142,25 +149,30 @@ struct TopList {
   __device__ __forceinline__ void raise(float lane_max, int lane) {
     const uint32_t v[1] = {ordered(lane_max)};
     // 16 bits: lower than the value by less than a bf16 step
-    const uint32_t mine = max(reached_by<1>(v, (k + 3) / 4, 16), kOrderedMinusInf);
+    const uint32_t mine = max(reached_by<1>(v, 64, (k + 3) / 4, 16), kOrderedMinusInf);
     if (lane == 0) ((volatile uint32_t*)slots)[wave] = mine;
     uint32_t least = mine;
 #pragma unroll
     for (int w = 0; w < 4; ++w) least = min(least, ((volatile uint32_t*)slots)[w]);
     bound = fmaxf(bound, key_value((u64)least << 32));
   }
-  __device__ __forceinline__ void offer(const float (&x)[VE], float most, int i0, int lane) {
-    if (__ballot(most >= bound) == 0) return;
+  // Entries at the row's edges, of the lanes that have one: kept without a look.
+  __device__ __forceinline__ void keep(bool has, float x, int i, int lane) {
+    const u64 mask = __ballot(has);
+    if (has) keys[__popcll(mask & ((1ull << lane) - 1))] = top_key(x, (uint32_t)i);
+    n = __popcll(mask);
+  }
+  // x: this lane's entries from index i0 on; lanes that are not `in` have none.
+  __device__ __forceinline__ void offer(const float (&x)[4], bool in, int i0, int lane) {
+    if (__ballot(in && fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= bound) == 0) return;
 #pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      if (__ballot(x[i] >= bound) == 0) continue;
+    for (int i = 0; i < 4; ++i) {
       const u64 key = top_key(x[i], (uint32_t)(i0 + i));
-      const bool hit = x[i] >= bound && key > kth;
+      const bool hit = in && x[i] >= bound && key > kth;
       const u64 mask = __ballot(hit);
       if (hit) keys[n + __popcll(mask & ((1ull << lane) - 1))] = key;
       n += __popcll(mask);
     }
-    if (n > kKeep) cut(lane);
   }
   __device__ __forceinline__ void cut(int lane) {
     constexpr int R = kCap / 64;
@@ -174,7 +186,7 @@ struct TopList {
       hi[r] = (uint32_t)(key >> 32);
       lo[r] = (uint32_t)key;
     }
-    const uint32_t v = reached_by<R>(hi, k, 32);
+    const uint32_t v = reached_by<R>(hi, n, k, 32);
     // among the entries of value v, those of the lowest indices
     int above = 0;
 #pragma unroll
@@ -182,7 +194,7 @@ struct TopList {
       above += __popcll(__ballot(hi[r] > v));
       if (hi[r] != v) lo[r] = hi[r] > v ? 0xffffffffu : 0u;
     }
-    const uint32_t l = reached_by<R>(lo, k, 32);
+    const uint32_t l = reached_by<R>(lo, n, k, 32);
     int m = 0;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -240,9 +252,8 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
                                                       u64* __restrict__ pkey) {
   typedef typename Elem<DT>::T E;
   constexpr int VE = Elem<DT>::kVec;
-  typedef TopList<VE> List;
   __shared__ Soft red[4];
-  __shared__ u64 keys[TOP ? 4 * List::kCap : 1];
+  __shared__ __attribute__((aligned(16))) u64 keys[TOP ? 4 * (TopList::kCap + 8) : 1];
   __shared__ uint32_t slots[4];
   __shared__ int counts[4];
   const int tid = threadIdx.x, lane = tid & 63;
@@ -258,46 +269,63 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   const int own = tid < head ? b + tid : rest + tid - head;   // this thread's scalar, if any
   const bool has = tid < head || own < e;
   Soft s = no_entries();
-  List list;
+  TopList list;
+  const float edge = has ? value<DT>(row[own]) : -INFINITY;
   if constexpr (TOP) {
-    list.init(keys + wave * List::kCap, slots, top, wave);
+    list.init(keys + wave * (TopList::kCap + 8), slots, top, wave);
     if (tid < 4) slots[tid] = kOrderedMinusInf;
     __syncthreads();
+    list.keep(has, edge, own, lane);
   }
-  // (every lane of a wave stays in the loop, for the list's votes)
+  {
+    const float x[1] = {edge};
+    add<DT>(s, x);
+  }
+  // U vectors a lane in flight (every lane of a wave stays in the loop, for the list's
+  // votes; lanes past the end take -infinity, which adds nothing)
+  constexpr int U = 4;
   int round = 0;
-  for (int v0 = 64 * wave; v0 < nv; v0 += 256, ++round) {
-    const int v = v0 + lane;
-    float x[VE];
-    if (v < nv) {
-      unpack<DT>(vec[v], x);
-    } else {
+  for (int v0 = 64 * wave; v0 < nv; v0 += 256 * U, ++round) {
+    u32x4 w[U];
 #pragma unroll
-      for (int i = 0; i < VE; ++i) x[i] = -INFINITY;
+    for (int i = 0; i < U; ++i) {
+      const int v = v0 + 256 * i + lane;
+      w[i] = v < nv ? vec[v] : minus_inf<DT>();
     }
-    const float most = add<DT>(s, x);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      float x[VE];
+      unpack<DT>(w[i], x);
+      add<DT>(s, x);
+    }
     if constexpr (TOP) {
       // rounds 0, 1, 3, 7, ..: as many entries again are in
       if ((round & (round + 1)) == 0) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
-      if (v0 + 64 > nv) {
+      constexpr int Q = U * VE / 4;   // offers
+#pragma unroll 1
+      for (int i = 0; i < Q; ++i) {
+        const int v = v0 + 256 * (i * 4 / VE) + lane;
+        float x[VE];
+        unpack<DT>(w[0], x);
+        const float y[4] = {x[0], x[1], x[2], x[3]};
+        list.offer(y, v < nv, b + head + v * VE + i * 4 % VE, lane);
+        // (the others move up: a register array takes no index)
+        if constexpr (VE == 4) {
+          w[0] = w[1];
+          w[1] = w[2];
+          w[2] = w[3];
+        } else {
 #pragma unroll
-        for (int i = 0; i < VE; ++i) x[i] = v < nv ? x[i] : __uint_as_float(0x7fc00000u);
+          for (int j = 0; j < U; ++j) {
+            const u32x4 next = j + 1 < U ? w[j + 1] : w[j];
+            w[j] = u32x4{w[j][2], w[j][3], next[0], next[1]};
+          }
+        }
+        if (list.n > kKeep) list.cut(lane);
       }
-      list.offer(x, v < nv ? most : __uint_as_float(0x7fc00000u), b + head + v * VE, lane);
     }
   }
-  if (wave == 0) {
-    const float x[1] = {has ? value<DT>(row[own]) : -INFINITY};
-    add<DT>(s, x);
-    if constexpr (TOP) {
-      float y[VE];
-      y[0] = has ? x[0] : __uint_as_float(0x7fc00000u);
-#pragma unroll
-      for (int i = 1; i < VE; ++i) y[i] = __uint_as_float(0x7fc00000u);
-      list.offer(y, y[0], own, lane);
-    }
-  }
-#pragma unroll
+#pragma unroll 1   // (short code: a work-group reads it anew)
   for (int off = 32; off >= 1; off >>= 1) {
     Soft o;
     o.m = __shfl_xor(s.m, off);
@@ -308,6 +336,7 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   if (lane == 0) red[wave] = s;
   if constexpr (TOP) {
     if (list.n > 64) list.cut(lane);
+    if (lane < 8) list.keys[list.n + lane] = 0;
     if (lane == 0) counts[wave] = list.n;
   }
   __syncthreads();
@@ -330,7 +359,11 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
     for (int w = 0; w < 4; ++w) {
       const int m = counts[w];
       total += m;
-      for (int i = 0; i < m; ++i) place += keys[w * List::kCap + i] > mine;
+      // (eight at a time, zeros behind the last)
+      for (int i = 0; i < m; i += 8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) place += keys[w * (TopList::kCap + 8) + i + j] > mine;
+      }
     }
     const bool bad = s.z != s.z;
     if (splits == 1) {
@@ -347,7 +380,8 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   }
 }
 
-// A work-group a row: its parts' sums in order, the top of their keys (at most 256).
+// A work-group a row: its parts' sums (at most 64 parts, joined in a fixed order) and the
+// top of their keys (at most 256).
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_join_kernel(
     const void* __restrict__ logits, size_t ld, int V, const int64_t* __restrict__ targets,
@@ -360,13 +394,21 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
   const int n = splits * top;
   const u64 mine = tid < n ? pkey[t * n + tid] : 0;
   keys[tid] = mine;
+  // a part a lane, at most 64 of them
   Soft s = no_entries();
-  for (int p = 0; p < splits; ++p) {
-    const float* q = psum + 3 * (t * splits + p);
+  const int lane = tid & 63;
+  if (lane < splits) {
+    const float* q = psum + 3 * (t * splits + lane);
+    s.m = q[0];
+    s.z = q[1];
+    s.zt = q[2];
+  }
+#pragma unroll 1   // (short code: a work-group reads it anew)
+  for (int off = 32; off >= 1; off >>= 1) {
     Soft o;
-    o.m = q[0];
-    o.z = q[1];
-    o.zt = q[2];
+    o.m = __shfl_xor(s.m, off);
+    o.z = __shfl_xor(s.z, off);
+    o.zt = __shfl_xor(s.zt, off);
     join(s, o);
   }
   const float lz = logf(s.z);
@@ -377,7 +419,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
     return;
   }
   int place = 0;
-  for (int i = 0; i < n; ++i) place += keys[i] > mine;
+#pragma unroll 8
+  for (int i = 0; i < 256; ++i) place += keys[i] > mine;
   if (mine != 0 && place < top) store_top(out, t * top + place, mine, s, lz);
 }
 
