@@ -49,13 +49,13 @@ __device__ __forceinline__ float activation(int act, float a, float* d) {   // a
 }  // namespace
 
 // ---- forward, many tokens ----
-// WI x WJ wavefronts, each BI blocks of 32 P rows (half Wg's, half Wu's) x BJ blocks
-// of 32 tokens.
+// WI x WJ wavefronts, each BI blocks of 16 P rows (half Wg's, half Wu's) x BJ blocks
+// of 16 tokens.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre, int ni, int nj) {
-  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef KContig<TI, NW, kRowHalves> LP;
   typedef KContig<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
@@ -70,11 +70,11 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
   LQ lq;
   lp.init(Wg, Wu, 2 * (size_t)D, f0, F, 2 * D, wave, lane);
   lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
-  f32x16 acc[BI][BJ] = {};
+  f32x4 acc[BI][BJ] = {};
   // block a < BI / 2: Wg, the others: Wu of the same channels
-  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 32 * BJ,
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 8 * BI, wj * 16 * BJ,
                    stages, [](int) {},
-                   [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                        });
@@ -86,23 +86,20 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
   static_assert((APART ? 1 : 2) * 32 * RB <= STAGE && (WJ == 2 || WJ == 4), "stage");
   char* const ga = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
   char* const up = APART ? (wj == 0 ? stage2 : stage3) : ga + 32 * RB;
-  const int row = lane & 31;
 #pragma unroll
-  for (int b = 0; b < BJ; ++b) {
-    if (b > 0) __syncthreads();
+  for (int bb = 0; bb < BJ; bb += 2) {
+    if (bb > 0) __syncthreads();
 #pragma unroll
-    for (int a = 0; a < BI / 2; ++a)
+    for (int b = bb; b < bb + 2; ++b)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int c = (wi * 16 * BI + 32 * a + 8 * r + 4 * (lane >> 5)) / 4;
-        const f32x16 &g = acc[a][b], &u = acc[BI / 2 + a][b];
-        *(f32x4*)out_piece<RB>(ga, row, c) =
-            f32x4{g[4 * r], g[4 * r + 1], g[4 * r + 2], g[4 * r + 3]};
-        *(f32x4*)out_piece<RB>(up, row, c) =
-            f32x4{u[4 * r], u[4 * r + 1], u[4 * r + 2], u[4 * r + 3]};
+      for (int a = 0; a < BI / 2; ++a) {
+        const int row = 16 * (b - bb) + (lane & 15);
+        const int c = (wi * 8 * BI + 16 * a + 4 * (lane >> 4)) / 4;
+        *(f32x4*)out_piece<RB>(ga, row, c) = acc[a][b];
+        *(f32x4*)out_piece<RB>(up, row, c) = acc[BI / 2 + a][b];
       }
     __syncthreads();
-    const int tb = t0 + wj * 32 * BJ + 32 * b;
+    const int tb = t0 + wj * 16 * BJ + 16 * bb;
 #pragma unroll 1
     for (int p = wi * 64 + lane; p < 32 * PIECES; p += WI * 64) {
       const int r = p / PIECES, c = p % PIECES, t = tb + r, f = f0 + 4 * c;
@@ -148,7 +145,7 @@ __global__ __launch_bounds__(512) void gated_skinny_kernel(
 #pragma unroll
         for (int a = 0; a < IB; ++a)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) acc[a][b] = Mma<KIND>::mul16(fp[a], fq[b], acc[a][b]);
+          for (int b = 0; b < 2; ++b) acc[a][b] = Mma<KIND>::mul(fp[a], fq[b], acc[a][b]);
       });
 #pragma unroll
   for (int a = 0; a < IB; ++a)
@@ -175,8 +172,8 @@ __global__ __launch_bounds__(512) void gated_skinny_kernel(
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 static hipError_t launch_gated_tiles(hipStream_t st, int act, int T, int D, int F, const void* X,
                                      const void* Wg, const void* Wu, uint16_t* Y, float* pre) {
-  const int ni = (F + 16 * WI * BI - 1) / (16 * WI * BI);
-  const int nj = (T + 32 * WJ * BJ - 1) / (32 * WJ * BJ);
+  const int ni = (F + 8 * WI * BI - 1) / (8 * WI * BI);
+  const int nj = (T + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
   hipLaunchKernelGGL((gated_tile_kernel<KIND, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
                      dim3(64 * WI * WJ), 0, st, X, Wg, Wu, T, D, F, act, Y, pre, ni, nj);
   return hipGetLastError();
@@ -211,10 +208,10 @@ static hipError_t launch_gated_forward_kind(hipStream_t st, int act, int T, int 
                           tile_cost(tiles(64, 64), nk, 0.19, 2.7),
                           tile_cost(tiles(32, 64), nk, 0.135, 2.6)};
   switch ((int)(std::min_element(cost, cost + 4) - cost)) {
-    case 0: return launch_gated_tiles<KIND, 4, 2, 4, 4, 2>(st, act, T, D, F, X, Wg, Wu, y, pre);
-    case 1: return launch_gated_tiles<KIND, 4, 2, 2, 2, 2>(st, act, T, D, F, X, Wg, Wu, y, pre);
-    case 2: return launch_gated_tiles<KIND, 4, 2, 2, 2, 1>(st, act, T, D, F, X, Wg, Wu, y, pre);
-    default: return launch_gated_tiles<KIND, 8, 1, 2, 2, 1>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    case 0: return launch_gated_tiles<KIND, 4, 2, 4, 8, 4>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    case 1: return launch_gated_tiles<KIND, 4, 2, 2, 4, 4>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    case 2: return launch_gated_tiles<KIND, 4, 2, 2, 4, 2>(st, act, T, D, F, X, Wg, Wu, y, pre);
+    default: return launch_gated_tiles<KIND, 8, 1, 2, 4, 2>(st, act, T, D, F, X, Wg, Wu, y, pre);
   }
 }
 
@@ -267,26 +264,23 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const float* __restrict
 }
 
 // A tile's sums as 16-bit values: store(j, i, w) gets eight of them from row j of the
-// 32 BJ that the WI waves of one wj share a stage for, columns i .. of the tile.
+// 16 BJ that the WI waves of one wj share a stage for, columns i .. of the tile.
 template <int KIND, int WI, int BI, int BJ, class Store>
-__device__ __forceinline__ void store_tile16(const f32x16 (&acc)[BI][BJ], char* stage, int wi,
+__device__ __forceinline__ void store_tile16(const f32x4 (&acc)[BI][BJ], char* stage, int wi,
                                              int lane, const Store& store) {
-  constexpr int RB = 2 * 32 * WI * BI, PIECES = RB / 16;
+  constexpr int RB = 2 * 16 * WI * BI, PIECES = RB / 16;
 #pragma unroll
   for (int b = 0; b < BJ; ++b)
 #pragma unroll
-    for (int a = 0; a < BI; ++a)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int at = 2 * (wi * 32 * BI + 32 * a + 8 * r + 4 * (lane >> 5));
-        const f32x16& c = acc[a][b];
-        *(u32x2*)(out_piece<RB>(stage, 32 * b + (lane & 31), at >> 4) + (at & 15)) =
-            u32x2{pack16<KIND>(c[4 * r], c[4 * r + 1]), pack16<KIND>(c[4 * r + 2], c[4 * r + 3])};
-      }
+    for (int a = 0; a < BI; ++a) {
+      const int at = 2 * (wi * 16 * BI + 16 * a + 4 * (lane >> 4));
+      const f32x4& c = acc[a][b];
+      *(u32x2*)(out_piece<RB>(stage, 16 * b + (lane & 15), at >> 4) + (at & 15)) =
+          u32x2{pack16<KIND>(c[0], c[1]), pack16<KIND>(c[2], c[3])};
+    }
   __syncthreads();
-#pragma unroll
-  for (int k = 0; k < 32 * BJ * PIECES / (WI * 64); ++k) {
-    const int p = (k * WI + wi) * 64 + lane;
+#pragma unroll 1
+  for (int p = wi * 64 + lane; p < 16 * BJ * PIECES; p += WI * 64) {
     const int j = p / PIECES, c = p % PIECES;
     store(j, 8 * c, *(const u32x4*)out_piece<RB>(stage, j, c));
   }
@@ -298,7 +292,7 @@ template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
     const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int each, uint16_t* __restrict__ dX, float* __restrict__ part, int ni, int nj) {
-  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef KStrided<TI, NW, kTwoSpans> LP;
   typedef KContig<TJ, NW, kTwoSpans> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
@@ -313,34 +307,29 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
   LQ lq;
   lp.init(Wg, Wu, 2 * (size_t)D, d0, D, F, wave, lane);
   lq.init(dab, (const uint16_t*)dab + F, 4 * (size_t)F, t0, T, 2 * F, wave, lane);
-  f32x16 acc[BI][BJ] = {};
+  f32x4 acc[BI][BJ] = {};
   const int nk = 2 * ((2 * F + kChunk - 1) / kChunk);
   const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
-  mma_loop<S, BI, BJ>(lp, lq, q0, q1, lane, wi * 32 * BI, wj * 32 * BJ, stages,
+  mma_loop<S, BI, BJ>(lp, lq, q0, q1, lane, wi * 16 * BI, wj * 16 * BJ, stages,
                    [](int) {},
-                   [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                        });
   if (part) {   // uniform
 #pragma unroll
     for (int b = 0; b < BJ; ++b) {
-      const int t = t0 + wj * 32 * BJ + 32 * b + (lane & 31);
+      const int t = t0 + wj * 16 * BJ + 16 * b + (lane & 15);
 #pragma unroll
-      for (int a = 0; a < BI; ++a)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = d0 + wi * 32 * BI + 32 * a + 8 * r + 4 * (lane >> 5);
-          const f32x16& c = acc[a][b];
-          if (t < T && d < D)
-            *(f32x4*)(part + ((size_t)blockIdx.y * T + t) * D + d) =
-                f32x4{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
-        }
+      for (int a = 0; a < BI; ++a) {
+        const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
+        if (t < T && d < D) *(f32x4*)(part + ((size_t)blockIdx.y * T + t) * D + d) = acc[a][b];
+      }
     }
     return;
   }
   char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
-  const int tw = t0 + wj * 32 * BJ;
+  const int tw = t0 + wj * 16 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
     if (tw + t < T && d0 + i < D) *(u32x4*)(dX + (size_t)(tw + t) * D + d0 + i) = w;
   });
@@ -363,7 +352,7 @@ template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
     const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,
     uint16_t* __restrict__ dWg, uint16_t* __restrict__ dWu, int ni, int nj) {
-  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef KStrided<TI, NW, kOne> LP;
   typedef KStrided<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
@@ -378,15 +367,15 @@ __global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
   LQ lq;
   lp.init(X, X, 2 * (size_t)D, d0, D, T, wave, lane);
   lq.init(dab, dab, 4 * (size_t)F, f0, 2 * F, T, wave, lane);
-  f32x16 acc[BI][BJ] = {};
-  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 32 * BI, wj * 32 * BJ,
+  f32x4 acc[BI][BJ] = {};
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
                    stages, [](int) {},
-                   [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                        });
   char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
-  const int fw = f0 + wj * 32 * BJ;
+  const int fw = f0 + wj * 16 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int r, int i, const u32x4& w) {
     const int f = fw + r;
     uint16_t* out = f < F ? dWg : dWu;
@@ -472,13 +461,13 @@ static hipError_t launch_gated_backward_kind(hipStream_t st, int act, int T, int
     float* to = p.splits > 1 ? part : nullptr;
     const dim3 grid((unsigned)(p.ni * p.nj), (unsigned)p.splits);
     if (p.kind == 0)
-      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 4, 4, 2>), grid, dim3(512), 0, st, dab, Wg,
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 4, 8, 4>), grid, dim3(512), 0, st, dab, Wg,
                          Wu, T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
     else if (p.kind == 1)
-      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 2, 2, 2>), grid, dim3(256), 0, st, dab, Wg,
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 2, 4, 4>), grid, dim3(256), 0, st, dab, Wg,
                          Wu, T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
     else
-      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 2, 2, 1>), grid, dim3(256), 0, st, dab, Wg,
+      hipLaunchKernelGGL((gated_dx_kernel<KIND, 4, 2, 2, 4, 2>), grid, dim3(256), 0, st, dab, Wg,
                          Wu, T, D, F, p.each, (uint16_t*)dX, to, p.ni, p.nj);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     if (to) {
@@ -495,15 +484,15 @@ static hipError_t launch_gated_backward_kind(hipStream_t st, int act, int T, int
     const int ni = (D + 127) / 128, bi = (D + 255) / 256, bj = (2 * F + 255) / 256;
     const int nj = (2 * F + 127) / 128, nh = (2 * F + 63) / 64;
     if ((long long)bi * bj >= 320)
-      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 4, 4, 2>), dim3((unsigned)(bi * bj)),
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 4, 8, 4>), dim3((unsigned)(bi * bj)),
                          dim3(512), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, bi,
                          bj);
     else if ((long long)ni * nj >= 192)
-      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 2, 2, 2>), dim3((unsigned)(ni * nj)),
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 2, 4, 4>), dim3((unsigned)(ni * nj)),
                          dim3(256), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, ni,
                          nj);
     else
-      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 2, 2, 1>), dim3((unsigned)(ni * nh)),
+      hipLaunchKernelGGL((gated_dw_kernel<KIND, 4, 2, 2, 4, 2>), dim3((unsigned)(ni * nh)),
                          dim3(256), 0, st, dab, X, T, D, F, (uint16_t*)dWg, (uint16_t*)dWu, ni,
                          nh);
     e = hipGetLastError();

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
     const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y, int ni,
     int nj) {
-  constexpr int TI = 32 * WI * BI, TJ = 32 * WJ * BJ, NW = WI * WJ;
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef KContig<TI, NW, kOne> LP;
   typedef KContig<TJ, NW, kOne> LQ;
   constexpr int STAGE = LP::kBytes + LQ::kBytes;
@@ -187,25 +187,25 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   LQ lq;
   lp.init(Xq, Xq, K, t0, T, K, wave, lane);
   lq.init(Wq, Wq, K, n0, N, K, wave, lane);
-  const int nk = (K + kChunk - 1) / kChunk, prow = wi * 32 * BI, qrow = wj * 32 * BJ;
-  f32x16 y[GROUP ? BI : 1][GROUP ? BJ : 1] = {};
-  i32x16 acc[BI][BJ] = {};
+  const int nk = (K + kChunk - 1) / kChunk, prow = wi * 16 * BI, qrow = wj * 16 * BJ;
+  f32x4 y[GROUP ? BI : 1][GROUP ? BJ : 1] = {};
+  i32x4 acc[BI][BJ] = {};
   const int G = GROUP ? K / GROUP : 1;
   const float* srow[BJ];
 #pragma unroll
   for (int b = 0; b < BJ; ++b)
-    srow[b] = sw + (size_t)min(n0 + qrow + 32 * b + (lane & 31), N - 1) * G;
+    srow[b] = sw + (size_t)min(n0 + qrow + 16 * b + (lane & 15), N - 1) * G;
   if constexpr (GROUP == 0) {
     mma_loop<S, BI, BJ>(lp, lq, 0, nk, lane, prow, qrow, stages, [](int) {},
-                     [&](const u32x4& p, const u32x4& q, int a, int b, int, int)
-                         __attribute__((always_inline)) {
-                           acc[a][b] = Mma<kI8>::mul(p, q, acc[a][b]);
-                         });
+                        [&](const u32x4& p, const u32x4& q, int a, int b, int)
+                            __attribute__((always_inline)) {
+                              acc[a][b] = Mma<kI8>::mul(p, q, acc[a][b]);
+                            });
   } else {
     constexpr int GR = S * kChunk / GROUP;   // groups a round
-    constexpr int SG = GROUP / 32;           // k-slices a group
     // the scales a round ahead of their use; past the last group 0
-    float s[GR][BJ], ahead[GR][BJ];
+    float s[GR][BJ] = {}, ahead[GR][BJ];
+    float before = 0.f, before0 = 0.f;   // the last block's, of the round before
     auto fetch = [&](int g0) __attribute__((always_inline)) {
 #pragma unroll
       for (int b = 0; b < BJ; ++b)
@@ -213,28 +213,47 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
         for (int g = 0; g < GR; ++g) ahead[g][b] = g0 + g < G ? srow[b][g0 + g] : 0.f;
     };
     fetch(0);
+    auto scale = [&](int a, int b, const i32x4& c, float sc) __attribute__((always_inline)) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v) y[a][b][v] = fmaf((float)c[v], sc, y[a][b][v]);
+    };
+    const bool low = lane < 32;
     mma_loop<S, BI, BJ>(
         lp, lq, 0, nk, lane, prow, qrow, stages,
         [&](int q) __attribute__((always_inline)) {
+          before = s[GR - 1][BJ - 1];
+          before0 = GROUP == 32 ? s[GR - 2][BJ - 1] : 0.f;
 #pragma unroll
           for (int g = 0; g < GR; ++g)
 #pragma unroll
             for (int b = 0; b < BJ; ++b) s[g][b] = ahead[g][b];
           fetch((q / S + 1) * GR);
         },
-        [&](const u32x4& p, const u32x4& q, int a, int b, int ks, int i)
-            __attribute__((always_inline)) {
-          const int slice = 2 * i + ks;
-          acc[a][b] = Mma<kI8>::mul(p, q, slice % SG == 0 ? i32x16{} : acc[a][b]);
-          if (slice % SG == SG - 1) {
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-              y[a][b][v] = fmaf((float)acc[a][b][v], s[slice / SG][b], y[a][b][v]);
+        [&](const u32x4& p, const u32x4& q, int a, int b, int i) __attribute__((always_inline)) {
+          // the sums of the block before go to fp32 while the matrix cores form this one's
+          const int at = a * BJ + b, pa = at ? (at - 1) / BJ : BI - 1, pb = at ? (at - 1) % BJ : BJ - 1;
+          if constexpr (GROUP == 32) {
+            // a chunk's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
+            const u32x4 none = {};
+            const i32x4 c0 = Mma<kI8>::mul(low ? p : none, q, i32x4{});
+            const i32x4 c1 = Mma<kI8>::mul(low ? none : p, q, i32x4{});
+            scale(pa, pb, acc[0][0], at ? s[2 * i][pb] : i ? s[2 * i - 2][pb] : before0);
+            scale(pa, pb, acc[0][1], at ? s[2 * i + 1][pb] : i ? s[2 * i - 1][pb] : before);
+            acc[0][0] = c0;
+            acc[0][1] = c1;
+          } else {
+            constexpr int PER = GROUP / kChunk;   // chunks a group
+            acc[a][b] = Mma<kI8>::mul(p, q, i % PER == 0 ? i32x4{} : acc[a][b]);
+            if (at != 0 && i % PER == PER - 1) scale(pa, pb, acc[pa][pb], s[i / PER][pb]);
+            if (at == 0 && i % PER == 0)
+              scale(pa, pb, acc[pa][pb], i ? s[i / PER - 1][pb] : before);
           }
         });
+    if constexpr (GROUP == 32) scale(BI - 1, BJ - 1, acc[0][0], s[GR - 2][BJ - 1]);
+    scale(BI - 1, BJ - 1, GROUP == 32 ? acc[0][1] : acc[BI - 1][BJ - 1], s[GR - 1][BJ - 1]);
   }
-  // Out through LDS as fp32, 32 tokens x 32 BJ channels of a wave at a time.
-  constexpr int CH = 32 * BJ;
+  // Out through LDS as fp32, 32 tokens x 16 BJ channels of a wave at a time.
+  constexpr int CH = 16 * BJ;
   constexpr int PER = STAGE / (32 * CH * 4);   // waves a stage serves
   static_assert(PER >= 1 && PER * 4 >= NW, "stage");
   float* const mine = (float*)(wave / PER == 0 ? stage0 : wave / PER == 1 ? stage1
@@ -243,17 +262,17 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
   // four values at a time where every row starts at their boundary and none ends inside four
   const bool wide = (uintptr_t)Y % (dtype == 0 ? 16 : 8) == 0 && N % 4 == 0;
 #pragma unroll
-  for (int a = 0; a < BI; ++a) {
+  for (int aa = 0; aa < BI; aa += 2) {
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int r = 8 * (v / 4) + 4 * (lane >> 5) + v % 4;
+    for (int a = aa; a < aa + 2; ++a)
 #pragma unroll
       for (int b = 0; b < BJ; ++b)
-        mine[r * CH + 32 * b + (lane & 31)] =
-            GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0];
-    }
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          mine[(16 * (a - aa) + 4 * (lane >> 4) + v) * CH + 16 * b + (lane & 15)] =
+              GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0];
     asm volatile("" ::: "memory");   // one wave: its LDS accesses complete in order
-    const int tw = t0 + prow + 32 * a;
+    const int tw = t0 + prow + 16 * aa;
     if (wide) {
 #pragma unroll 1
       for (int p = lane; p < 32 * CH / 4; p += 64) {
@@ -288,19 +307,19 @@ template <int GROUP, class Sum4>
 __device__ __forceinline__ void i8_step(int st, const u32x4& fp, const u32x4& fq, bool low,
                                         const float* s, i32x4& acc, Sum4& sum) {
   if constexpr (GROUP == 0) {
-    sum = Mma<kI8>::mul16(fp, fq, sum);
+    sum = Mma<kI8>::mul(fp, fq, sum);
   } else if constexpr (GROUP == 32) {
     // a step's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 part = (h == 0) == low ? fp : u32x4{};
-      const i32x4 c = Mma<kI8>::mul16(part, fq, i32x4{});
+      const i32x4 c = Mma<kI8>::mul(part, fq, i32x4{});
 #pragma unroll
       for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)c[v], s[2 * st + h], sum[v]);
     }
   } else {
     constexpr int SG = GROUP / 64;   // steps a group
-    acc = Mma<kI8>::mul16(fp, fq, st % SG == 0 ? i32x4{} : acc);
+    acc = Mma<kI8>::mul(fp, fq, st % SG == 0 ? i32x4{} : acc);
     if (st % SG == SG - 1) {
 #pragma unroll
       for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)acc[v], s[st / SG], sum[v]);
@@ -486,8 +505,8 @@ static hipError_t launch_i8_skinny(hipStream_t st, int dtype, int T, int N, int 
 template <int GROUP, int S, int WI, int WJ, int BI, int BJ>
 static hipError_t launch_i8_tiles(hipStream_t st, int dtype, int T, int N, int K, const int8_t* Xq,
                                   const float* sx, const int8_t* Wq, const float* sw, void* Y) {
-  const int ni = (T + 32 * WI * BI - 1) / (32 * WI * BI);
-  const int nj = (N + 32 * WJ * BJ - 1) / (32 * WJ * BJ);
+  const int ni = (T + 16 * WI * BI - 1) / (16 * WI * BI);
+  const int nj = (N + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
   hipLaunchKernelGGL((i8_tile_kernel<GROUP, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
                      dim3(64 * WI * WJ), 0, st, Xq, sx, Wq, sw, T, N, K, dtype, Y, ni, nj);
   return hipGetLastError();
@@ -523,16 +542,16 @@ static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K
                           GROUP ? 1e30 : tile_cost(tiles(256, 256), nk, 0.7, 6.0)};
   switch ((int)(std::min_element(cost, cost + 5) - cost)) {
     case 0:
-      return launch_i8_tiles<GROUP, 4, 2, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return launch_i8_tiles<GROUP, 4, 2, 2, 4, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 1:
-      return launch_i8_tiles<GROUP, 8, 2, 2, 2, 1>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return launch_i8_tiles<GROUP, 8, 2, 2, 4, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 2:
-      return launch_i8_tiles<GROUP, 8, 2, 2, 1, 1>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return launch_i8_tiles<GROUP, 8, 2, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 3:
-      return launch_i8_tiles<GROUP, 8, 2, 1, 1, 1>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return launch_i8_tiles<GROUP, 8, 2, 1, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     default:
       if constexpr (GROUP == 0)
-        return launch_i8_tiles<0, 4, 2, 4, 4, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+        return launch_i8_tiles<0, 4, 2, 4, 8, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
       return hipErrorInvalidValue;
   }
 }

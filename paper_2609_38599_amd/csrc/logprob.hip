@@ -145,16 +145,16 @@ struct TopList {
     bound = -INFINITY;
   }
   // From the lanes' largest entries so far: the four waves' slots together name a
-  // value that k entries of the row reach (a slot read late is only lower).
+  // value that k entries of the row reach.  Every wave of the work-group calls it.
   __device__ __forceinline__ void raise(float lane_max, int lane) {
     const uint32_t v[1] = {ordered(lane_max)};
     // 16 bits: lower than the value by less than a bf16 step
     const uint32_t mine = max(reached_by<1>(v, 64, (k + 3) / 4, 16), kOrderedMinusInf);
-    if (lane == 0) ((volatile uint32_t*)slots)[wave] = mine;
-    uint32_t least = mine;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) least = min(least, ((volatile uint32_t*)slots)[w]);
+    if (lane == 0) slots[wave] = mine;
+    __syncthreads();
+    const uint32_t least = min(min(slots[0], slots[1]), min(slots[2], slots[3]));
     bound = fmaxf(bound, key_value((u64)least << 32));
+    __syncthreads();   // (before the next one's slots)
   }
   // Entries at the row's edges, of the lanes that have one: kept without a look.
   __device__ __forceinline__ void keep(bool has, float x, int i, int lane) {
@@ -167,12 +167,30 @@ struct TopList {
     if (__ballot(in && fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) >= bound) == 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      const bool may = in && x[i] >= bound;
+      if (__ballot(may) == 0) continue;
       const u64 key = top_key(x[i], (uint32_t)(i0 + i));
-      const bool hit = in && x[i] >= bound && key > kth;
+      const bool hit = may && key > kth;
       const u64 mask = __ballot(hit);
       if (hit) keys[n + __popcll(mask & ((1ull << lane) - 1))] = key;
       n += __popcll(mask);
     }
+  }
+  // Drops the keys that the bound has passed.
+  __device__ __forceinline__ void sift(int lane) {
+    asm volatile("" ::: "memory");   // one wave: its LDS accesses complete in order
+    const uint32_t least = ordered(bound);
+    int m = 0;
+#pragma unroll 1
+    for (int r = 0; r < n; r += 64) {
+      const u64 key = r + lane < n ? keys[r + lane] : 0;
+      const bool keep = key != 0 && (uint32_t)(key >> 32) >= least;
+      const u64 mask = __ballot(keep);
+      if (keep) keys[m + __popcll(mask & ((1ull << lane) - 1))] = key;
+      m += __popcll(mask);
+    }
+    asm volatile("" ::: "memory");
+    n = m;
   }
   __device__ __forceinline__ void cut(int lane) {
     constexpr int R = kCap / 64;
@@ -285,22 +303,24 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   // votes; lanes past the end take -infinity, which adds nothing)
   constexpr int U = 4;
   int round = 0;
-  for (int v0 = 64 * wave; v0 < nv; v0 += 256 * U, ++round) {
+  for (int v0 = 64 * wave; v0 - 64 * wave < nv; v0 += 256 * U, ++round) {   // uniform
     u32x4 w[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       const int v = v0 + 256 * i + lane;
       w[i] = v < nv ? vec[v] : minus_inf<DT>();
     }
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       float x[VE];
       unpack<DT>(w[i], x);
-      add<DT>(s, x);
+      most = fmaxf(most, add<DT>(s, x));
     }
     if constexpr (TOP) {
-      // rounds 0, 1, 3, 7, ..: as many entries again are in
-      if ((round & (round + 1)) == 0) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
+      // rounds 0, 2, 6, 14, ..: twice as many entries are in each time
+      if (((round + 1) & (round + 2)) == 0) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
+      if (__ballot(most >= list.bound) == 0) continue;
       constexpr int Q = U * VE / 4;   // offers
 #pragma unroll 1
       for (int i = 0; i < Q; ++i) {
@@ -325,6 +345,7 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
       }
     }
   }
+  if constexpr (TOP) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
 #pragma unroll 1   // (short code: a work-group reads it anew)
   for (int off = 32; off >= 1; off >>= 1) {
     Soft o;
@@ -335,6 +356,7 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   }
   if (lane == 0) red[wave] = s;
   if constexpr (TOP) {
+    list.sift(lane);
     if (list.n > 64) list.cut(lane);
     if (lane < 8) list.keys[list.n + lane] = 0;
     if (lane == 0) counts[wave] = list.n;
@@ -419,8 +441,10 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
     return;
   }
   int place = 0;
-#pragma unroll 8
-  for (int i = 0; i < 256; ++i) place += keys[i] > mine;
+  for (int i = 0; i < n; i += 8) {   // (zeros from n on)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) place += keys[i + j] > mine;
+  }
   if (mine != 0 && place < top) store_top(out, t * top + place, mine, s, lz);
 }
 
@@ -490,7 +514,7 @@ struct LogprobPlan {
 };
 LogprobPlan logprob_plan(int T, int V, int top) {
   LogprobPlan p;
-  int splits = 512 / T;
+  int splits = 2048 / T;   // eight work-groups a CU
   const int most = V / 4096;
   splits = splits < 1 || most < 1 ? 1 : splits > most ? most : splits;
   // the joining work-group takes a key a thread

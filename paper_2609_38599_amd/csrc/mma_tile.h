@@ -7,8 +7,10 @@
 // with k down its rows (KStrided, 16 bits only: read out of LDS through the
 // transposing read), so no product needs a transposed copy.
 //
-// 32 x 32 blocks per instruction.  In a result block a lane holds column
-// j = lane % 32 and rows i = 8 (v / 4) + 4 (lane / 32) + v % 4, v = 0..15.
+// 16 x 16 blocks per instruction, 64 bytes of k each (v_mfma_f32_16x16x32_bf16 and the
+// like; 32 x 32 blocks take 5 % longer, at the clock that the card's power then allows).
+// A lane's operand is 16 bytes of row lane % 16, at 16 (lane / 16); in a result block
+// it holds column j = lane % 16 and rows i = 4 (lane / 16) + v, v = 0..3.
 #pragma once
 
 #include "bf16x3.h"
@@ -19,43 +21,27 @@ enum : int { kF16 = 1, kBF16 = 2, kI8 = 3 };   // 1, 2 as JARQ_F16, JARQ_BF16
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
-typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 template <int KIND> struct Mma;
 template <> struct Mma<kBF16> {
-  typedef f32x16 Acc;
-  typedef f32x4 Acc16;
+  typedef f32x4 Acc;
   static __device__ __forceinline__ Acc mul(const u32x4& a, const u32x4& b, const Acc& c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                   __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ Acc16 mul16(const u32x4& a, const u32x4& b, const Acc16& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
                                                    __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   }
 };
 template <> struct Mma<kF16> {
-  typedef f32x16 Acc;
-  typedef f32x4 Acc16;
+  typedef f32x4 Acc;
   static __device__ __forceinline__ Acc mul(const u32x4& a, const u32x4& b, const Acc& c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
-                                                  __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ Acc16 mul16(const u32x4& a, const u32x4& b, const Acc16& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
                                                   __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
   }
 };
 template <> struct Mma<kI8> {
-  typedef i32x16 Acc;
-  typedef i32x4 Acc16;
+  typedef i32x4 Acc;
   static __device__ __forceinline__ Acc mul(const u32x4& a, const u32x4& b, const Acc& c) {
-    return __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, a),
-                                                 __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ Acc16 mul16(const u32x4& a, const u32x4& b, const Acc16& c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a),
                                                  __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
   }
@@ -149,21 +135,19 @@ struct KContig {
     load_lds16(from1 ? b1 : b0, c.k0 + piece < kbytes ? off[HALVES && from1 ? n - N / 2 : n] : kNowhere,
                (uint32_t)c.k0, stage + 1024 * (wave + NW * n));
   }
-  // This lane's places in a stage for a wave whose B blocks of 32 rows start at row0
-  // (in each half, where there are two).
+  // This lane's place in a stage for a wave whose B blocks of 16 rows start at row0 (in
+  // each half, where there are two).
   template <int B>
   struct Lane {
-    uint32_t o[2];
+    uint32_t o;
     __device__ __forceinline__ Lane(int row0, int lane) {
-      const uint32_t r = (uint32_t)(row0 + (lane & 31)) * kChunk;
-      const uint32_t x = (uint32_t)((lane >> 5) ^ swz(lane & 31)) << 4;
-      o[0] = r + x;
-      o[1] = r + (x ^ 32);
+      o = (uint32_t)(row0 + (lane & 15)) * kChunk +
+          ((uint32_t)((lane >> 4) ^ swz(lane & 15)) << 4);
     }
-    // Fragment of block a, k-slice ks of 2.
-    __device__ __forceinline__ u32x4 frag(const char* stage, int a, int ks) const {
-      const int row = HALVES && a >= B / 2 ? TR / 2 + 32 * (a - B / 2) : 32 * a;
-      return *(const u32x4*)(stage + o[ks] + row * kChunk);
+    // Fragment of block a.
+    __device__ __forceinline__ u32x4 frag(const char* stage, int a) const {
+      const int row = HALVES && a >= B / 2 ? TR / 2 + 16 * (a - B / 2) : 16 * a;
+      return *(const u32x4*)(stage + o + row * kChunk);
     }
   };
 };
@@ -174,8 +158,9 @@ __device__ __forceinline__ s16x4 lds_read_tr16(const char* p) {
 }
 
 // An operand tile of TR columns with k down the rows (16-bit values): a chunk is
-// kRows rows of TR values.  64-byte block x of row t lies at x ^ swz(t): a
-// transposing read takes one block of four consecutive rows.  Columns past the last
+// kRows rows of TR values.  64-byte block x of row t lies at x ^ swz(t), its 32-byte
+// halves exchanged in every other eight rows: the transposing reads of half a wave take 32
+// bytes of four consecutive rows and of the four rows eight further down.  Columns past the last
 // read the last eight; rows past the last read zeros.  kTwoSpans: k runs down one
 // matrix, then down another.
 template <int TR, int NW, Sources SRC>
@@ -186,7 +171,7 @@ struct KStrided {
   static constexpr int CPR = RB / 16;           // pieces a row
   static constexpr int RPI = 64 / CPR;          // rows per load instruction
   static constexpr int N = kRows / RPI / NW;
-  static_assert(N >= 1 && N * RPI * NW == kRows && (NW * RPI) % 4 == 0, "tile");
+  static_assert(N >= 1 && N * RPI * NW == kRows && (NW * RPI) % 16 == 0, "tile");
   static_assert(TR >= 64, "a row has two 64-byte blocks at least");
   static constexpr int kBytes = TR * kChunk;
   static __device__ __forceinline__ int swz(int t) { return TR >= 128 ? t & 3 : (t >> 1) & 1; }
@@ -203,7 +188,7 @@ struct KStrided {
     rows = rows_;
     wave = w;
     lt = RPI * w + lane / CPR;
-    const int pc = (lane % CPR) ^ (swz(lt) << 2);
+    const int pc = (lane % CPR) ^ (swz(lt) << 2) ^ ((lt >> 2) & 2);
     b0 = (const char*)p0;
     b1 = (const char*)p1;
 #pragma unroll
@@ -231,12 +216,14 @@ struct KStrided {
     __device__ __forceinline__ Lane(int col0, int lane) {
       const int gi = lane >> 4, pi = lane & 15, t = pi >> 2;
 #pragma unroll
-      for (int a = 0; a < B; ++a)
-        o[a] = (uint32_t)((8 * (gi >> 1) + t) * RB + ((((col0 >> 5) + a) ^ swz(t)) << 6) +
-                          32 * (gi & 1) + 8 * (pi & 3));
+      for (int a = 0; a < B; ++a) {
+        const int c = (col0 >> 4) + a;   // of 16 columns
+        o[a] = (uint32_t)((8 * gi + t) * RB + (((c >> 1) ^ swz(t)) << 6) +
+                          (((c ^ gi) & 1) << 5) + 8 * (pi & 3));
+      }
     }
-    __device__ __forceinline__ u32x4 frag(const char* stage, int a, int ks) const {
-      const char* p = stage + o[a] + 16 * ks * RB;
+    __device__ __forceinline__ u32x4 frag(const char* stage, int a) const {
+      const char* p = stage + o[a];
       const s16x4 w[2] = {lds_read_tr16(p), lds_read_tr16(p + 4 * RB)};
       return __builtin_bit_cast(u32x4, w);
     }
@@ -266,50 +253,52 @@ __device__ __forceinline__ void wait_barrier() {
   char* const stages[8] = {stage0, stage1, stage2, stage3, stage4, stage5, stage6, stage7}
 
 // The k-loop over chunks q0 <= q < q1 (at least one) with S stages: while a chunk is
-// multiplied, the loads of the S - 1 behind it are in flight, and the next fragments
-// are read a slice ahead.  The loop runs in whole rounds of the stages (chunks past the
-// last are zeros).  A wave's P blocks start at row prow of the tile, its Q blocks at
-// qrow.  round(q) comes before each round; mul(p, q, a, b, ks, i) gets the fragments of P block a and Q block b, slice ks of
-// chunk i of the round.
+// multiplied, the loads of the S - 1 behind it are in flight, and fragments are read half
+// a chunk's products ahead.  The loop runs in whole rounds of the stages (chunks past the
+// last are zeros).  A wave's BI blocks of P start at row prow of the tile, its BJ of Q
+// at qrow.  round(q) comes before each round; mul(p, q, a, b, i) gets the fragments of P block
+// a and Q block b of chunk i of the round.
 //
 // 4096 x 4096 -> 2 x 14336 channels, 256-wide tiles: two stages of twice the chunk 812 us,
 // four 800; the loads in a row at the start of a chunk 860; by address instead of by
 // buffer (every LDS read then waits for all others) 905.  Bound by the matrix cores at
-// the clock that the card's power allows (1.7 GHz here).
+// the clock that the card's power allows (1.4 to 1.7 GHz here).
 template <int S, int BI, int BJ, class LP, class LQ, class Round, class Mul>
 __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int q1, int lane,
                                          int prow, int qrow, char* const (&stages)[8],
                                          const Round& round, const Mul& mul) {
-  constexpr int L = LP::N + LQ::N, R = BI + BJ, M = BI * BJ;
-  u32x4 fp[2][BI], fq[2][BJ];
+  // the products in two halves of P blocks; what is read during the first is the
+  // second half's, during the second the next chunk's Q and first half
+  constexpr int L = LP::N + LQ::N, H = BI / 2, M = H * BJ, R = BJ + H;
+  static_assert(S % 2 == 0 && BI % 2 == 0 && (S - 2) * L < 64, "stages, blocks, loads in flight");
+  u32x4 fp[BI], fq[2][BJ];
   const typename LP::template Lane<BI> pl(prow, lane);
   const typename LQ::template Lane<BJ> ql(qrow, lane);
-  // fragment r of a slice, of Q's first
-  auto read = [&](const char* cur, int ks, int r) __attribute__((always_inline)) {
-    if (r < BJ) fq[ks][r] = ql.frag(cur + LP::kBytes, r, ks);
-    else fp[ks][r - BJ] = pl.frag(cur, r - BJ, ks);
+  // read r of a chunk's Q and first half
+  auto read = [&](const char* from, int set, int r) __attribute__((always_inline)) {
+    if (r < BJ) fq[set][r] = ql.frag(from + LP::kBytes, r);
+    else fp[r - BJ] = pl.frag(from, r - BJ);
   };
   auto issue = [&](int l, const typename LP::Chunk& cp, const typename LQ::Chunk& cq, char* stage)
       __attribute__((always_inline)) {
     if (l < LP::N) lp.issue(cp, l, stage);
     else lq.issue(cq, l - LP::N, stage + LP::kBytes);
   };
-  static_assert((S - 2) * L < 64, "loads in flight");
   auto chunk = [&](int q, int i) __attribute__((always_inline)) {
     char *const cur = stages[i], *const next = stages[(i + 1) % S];
     char* const far = stages[(i + S - 1) % S];
     const typename LP::Chunk cp = lp.chunk(q + i + S - 1, q + i + S - 1 < q1);
     const typename LQ::Chunk cq = lq.chunk(q + i + S - 1, q + i + S - 1 < q1);
-    // the second slice's fragments and the loads one at a time among the first one's
-    // products: in a row they would hold up the wave
+    // reads and loads one at a time among the products: in a row they would hold up
+    // the wave
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      mul(fp[0][m / BJ], fq[0][m % BJ], m / BJ, m % BJ, 0, i);
+      mul(fp[m / BJ], fq[i & 1][m % BJ], m / BJ, m % BJ, i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int o = m * (R + L) / M; o < (m + 1) * (R + L) / M; ++o) {
-        if (o < R) read(cur, 1, o);
-        else issue(o - R, cp, cq, far);
+      for (int o = m * (H + L) / M; o < (m + 1) * (H + L) / M; ++o) {
+        if (o < H) fp[H + o] = pl.frag(cur, H + o);
+        else issue(o - H, cp, cq, far);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -318,11 +307,11 @@ __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int
     wait_barrier<(S - 2) * L>();
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      mul(fp[1][m / BJ], fq[1][m % BJ], m / BJ, m % BJ, 1, i);
+      mul(fp[H + m / BJ], fq[i & 1][m % BJ], H + m / BJ, m % BJ, i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int o = m * R * 3 / (2 * M); o < (m + 1) * R * 3 / (2 * M); ++o)
-        if (o < R) read(next, 0, o);
+      for (int o = m * (R + R / 2) / M; o < (m + 1) * (R + R / 2) / M; ++o)
+        if (o < R) read(next, (i + 1) & 1, o);
       __builtin_amdgcn_sched_barrier(0);
     }
   };
