@@ -32,12 +32,12 @@ __device__ __forceinline__ float activation(float a, float* d) {
     const float cdf = 0.5f * (1.f + erff(a * kInvSqrt2));
     if (d) *d = cdf + a * kInvSqrt2Pi * __expf(-0.5f * a * a);
     return a * cdf;
-  } else {                           // gelu, tanh form
-    const float th = tanhf(kSqrt2OverPi * (a + 0.044715f * a * a * a));
+  } else {                           // gelu, tanh form: (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
+    const float z = kSqrt2OverPi * (a + 0.044715f * a * a * a);
+    const float sig = __builtin_amdgcn_rcpf(1.f + __expf(-2.f * z));
     if (d)
-      *d = 0.5f * (1.f + th) +
-           0.5f * a * (1.f - th * th) * kSqrt2OverPi * (1.f + 3.f * 0.044715f * a * a);
-    return 0.5f * a * (1.f + th);
+      *d = sig + 2.f * a * sig * (1.f - sig) * kSqrt2OverPi * (1.f + 3.f * 0.044715f * a * a);
+    return a * sig;
   }
 }
 __device__ __forceinline__ float activation(int act, float a, float* d) {   // act is uniform
@@ -52,7 +52,7 @@ __device__ __forceinline__ float activation(int act, float a, float* d) {   // a
 // WI x WJ wavefronts, each BI blocks of 16 P rows (half Wg's, half Wu's) x BJ blocks
 // of 16 tokens.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) void gated_tile_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
@@ -289,7 +289,7 @@ __device__ __forceinline__ void store_tile16(const f32x4 (&acc)[BI][BJ], char* s
 // ---- backward: dx = dab [Wg; Wu] ----
 // part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) void gated_dx_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_dx_kernel(
     const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int each, uint16_t* __restrict__ dX, float* __restrict__ part, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(256) void gated_dx_sum_kernel(const float* __restri
 
 // ---- backward: [dWg; dWu] = dab^T x ----
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) void gated_dw_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_dw_kernel(
     const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,
     uint16_t* __restrict__ dWg, uint16_t* __restrict__ dWu, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;

@@ -52,57 +52,76 @@ __device__ __forceinline__ u32x2 quant8(const float (&x)[8], float mul) {
   return u32x2{lo, hi};
 }
 
-// Eight values from element 8 v of a row.
+// Eight values from element 8 v of a row, as they are stored.
+template <int DT> struct Piece { u32x4 w[DT == 0 ? 2 : 1]; };
 template <int DT>
-__device__ __forceinline__ void load8(const void* row, int v, float (&x)[8]) {
-  if constexpr (DT == 0) {
-    const f32x4 a = *((const f32x4*)row + 2 * v), b = *((const f32x4*)row + 2 * v + 1);
+__device__ __forceinline__ Piece<DT> load_piece(const void* row, int v) {
+  Piece<DT> p;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
-  } else {
-    const u32x4 w = *((const u32x4*)row + v);
+  for (int i = 0; i < (DT == 0 ? 2 : 1); ++i)
+    p.w[i] = *((const u32x4*)row + (DT == 0 ? 2 : 1) * v + i);
+  return p;
+}
+template <int DT>
+__device__ __forceinline__ void unpack8(const Piece<DT>& p, float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = from16<DT>((uint16_t)w[i]);
-      x[2 * i + 1] = from16<DT>((uint16_t)(w[i] >> 16));
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (DT == 0) {
+      x[i] = __uint_as_float(p.w[0][i]);
+      x[4 + i] = __uint_as_float(p.w[DT == 0 ? 1 : 0][i]);
+    } else {
+      x[2 * i] = from16<DT>((uint16_t)p.w[0][i]);
+      x[2 * i + 1] = from16<DT>((uint16_t)(p.w[0][i] >> 16));
     }
   }
 }
 
 }  // namespace
 
-// A work-group a row; K a multiple of 16.
+// A work-group a row; K a multiple of 16.  A row of up to 16384 values stays in registers
+// between its maximum and its integers: 8192 rows of 14336 in bf16 QTIME, read
+// twice 88.
 template <int DT>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const void* __restrict__ X, int K,
                                                          int8_t* __restrict__ Q,
                                                          float* __restrict__ scale) {
+  constexpr int R = 8;   // pieces of eight values a thread holds
   __shared__ uint32_t red[4];
+  const int tid = threadIdx.x;
   const size_t r = blockIdx.x;
   const char* row = (const char*)X + r * K * (DT == 0 ? 4 : 2);
   const int nv = K / 8;
+  Piece<DT> p[R];
   uint32_t m = 0;
-  for (int v = threadIdx.x; v < nv; v += 256) {
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    p[i] = tid + 256 * i < nv ? load_piece<DT>(row, tid + 256 * i) : Piece<DT>{};
+  auto most = [&](const Piece<DT>& w) __attribute__((always_inline)) {
     float x[8];
-    load8<DT>(row, v, x);
+    unpack8<DT>(w, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
-  }
+  };
+#pragma unroll
+  for (int i = 0; i < R; ++i) most(p[i]);
+  for (int v = tid + 256 * R; v < nv; v += 256) most(load_piece<DT>(row, v));
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, off));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  if ((tid & 63) == 0) red[tid >> 6] = m;
   __syncthreads();
   m = max(max(red[0], red[1]), max(red[2], red[3]));
   float s, mul;
   row_scale(m, s, mul);
-  for (int v = threadIdx.x; v < nv; v += 256) {
+  auto put = [&](int v, const Piece<DT>& w) __attribute__((always_inline)) {
     float x[8];
-    load8<DT>(row, v, x);
+    unpack8<DT>(w, x);
     *(u32x2*)(Q + r * K + 8 * (size_t)v) = quant8(x, mul);
-  }
-  if (threadIdx.x == 0) scale[r] = s;
+  };
+#pragma unroll
+  for (int i = 0; i < R; ++i)
+    if (tid + 256 * i < nv) put(tid + 256 * i, p[i]);
+  for (int v = tid + 256 * R; v < nv; v += 256) put(v, load_piece<DT>(row, v));
+  if (tid == 0) scale[r] = s;
 }
 
 hipError_t launch_quant_rows(hipStream_t st, int dtype, const void* X, int rows, int K, int8_t* Q,
@@ -157,6 +176,17 @@ hipError_t launch_codes_i8(hipStream_t st, const uint8_t* codes, const int32_t* 
 // ---- products ----
 namespace {
 
+// A group's integer sum n (|n| <= 128 x 128 x 128 = 2^21) as fp32: it starts at the bits of
+// 1.5 x 2^23, at which integers up to 2^22 either way are consecutive floats, so the
+// result's bits are those of 1.5 x 2^23 + n.  (v_cvt_f32_i32 runs at a quarter of the
+// rate: 2048 x 11008 -> 4096 with groups of 64 235 us, this way TIMEB.)
+__device__ __forceinline__ i32x4 sum_start() {
+  return i32x4{0x4b400000, 0x4b400000, 0x4b400000, 0x4b400000};
+}
+__device__ __forceinline__ float sum_value(int32_t c) {
+  return __builtin_bit_cast(float, c) - 12582912.f;
+}
+
 __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) {   // dtype uniform
   if (dtype == 0) ((float*)Y)[at] = y;
   else if (dtype == 1) ((uint16_t*)Y)[at] = to16<kF16>(y);
@@ -168,7 +198,7 @@ __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) 
 // Many tokens.  GROUP 0: one scale a channel, int32 sums over all of k; otherwise a
 // group's int32 sums go to fp32.
 template <int GROUP, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
     const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y, int ni,
     int nj) {
@@ -203,19 +233,42 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
                             });
   } else {
     constexpr int GR = S * kChunk / GROUP;   // groups a round
-    // the scales a round ahead of their use; past the last group 0
-    float s[GR][BJ] = {}, ahead[GR][BJ];
+    constexpr int GL = GR < 4 ? 1 : GR / 4;  // loads for them
+    // the scales a round ahead of their use, as they come from memory; past the last
+    // group 0
+    float s[GR][BJ] = {};
+    u32x4 ahead[GL][BJ];
     float before = 0.f, before0 = 0.f;   // the last block's, of the round before
+    const Buffer scales = buffer_at(sw + (size_t)n0 * G, (size_t)(N - n0) * G * 4);
+    uint32_t sat[BJ];
+#pragma unroll
+    for (int b = 0; b < BJ; ++b)
+      sat[b] = (uint32_t)min(qrow + 16 * b + (lane & 15), N - 1 - n0) * (uint32_t)(4 * G);
     auto fetch = [&](int g0) __attribute__((always_inline)) {
 #pragma unroll
       for (int b = 0; b < BJ; ++b)
 #pragma unroll
-        for (int g = 0; g < GR; ++g) ahead[g][b] = g0 + g < G ? srow[b][g0 + g] : 0.f;
+        for (int l = 0; l < GL; ++l) {
+          if constexpr (GR == 2) {
+            const u32x2 w = __builtin_bit_cast(
+                u32x2, __builtin_amdgcn_raw_buffer_load_b64(scales, (int)sat[b], 4 * g0, 0));
+            ahead[l][b] = u32x4{w[0], w[1], 0u, 0u};
+          } else {
+            ahead[l][b] = __builtin_bit_cast(
+                u32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, (int)sat[b] + 16 * l,
+                                                                 4 * g0, 0));
+          }
+        }
     };
     fetch(0);
+    // (here already: behind the tiles' loads every round would wait for all of those)
+#pragma unroll
+    for (int b = 0; b < BJ; ++b)
+#pragma unroll
+      for (int l = 0; l < GL; ++l) asm volatile("" : "+v"(ahead[l][b]));
     auto scale = [&](int a, int b, const i32x4& c, float sc) __attribute__((always_inline)) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) y[a][b][v] = fmaf((float)c[v], sc, y[a][b][v]);
+      for (int v = 0; v < 4; ++v) y[a][b][v] = fmaf(sum_value(c[v]), sc, y[a][b][v]);
     };
     const bool low = lane < 32;
     mma_loop<S, BI, BJ>(
@@ -226,7 +279,8 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
 #pragma unroll
           for (int g = 0; g < GR; ++g)
 #pragma unroll
-            for (int b = 0; b < BJ; ++b) s[g][b] = ahead[g][b];
+            for (int b = 0; b < BJ; ++b)
+              s[g][b] = q / S * GR + g < G ? __uint_as_float(ahead[g / 4][b][g % 4]) : 0.f;
           fetch((q / S + 1) * GR);
         },
         [&](const u32x4& p, const u32x4& q, int a, int b, int i) __attribute__((always_inline)) {
@@ -235,15 +289,15 @@ __global__ __launch_bounds__(64 * WI * WJ) void i8_tile_kernel(
           if constexpr (GROUP == 32) {
             // a chunk's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
             const u32x4 none = {};
-            const i32x4 c0 = Mma<kI8>::mul(low ? p : none, q, i32x4{});
-            const i32x4 c1 = Mma<kI8>::mul(low ? none : p, q, i32x4{});
+            const i32x4 c0 = Mma<kI8>::mul(low ? p : none, q, sum_start());
+            const i32x4 c1 = Mma<kI8>::mul(low ? none : p, q, sum_start());
             scale(pa, pb, acc[0][0], at ? s[2 * i][pb] : i ? s[2 * i - 2][pb] : before0);
             scale(pa, pb, acc[0][1], at ? s[2 * i + 1][pb] : i ? s[2 * i - 1][pb] : before);
             acc[0][0] = c0;
             acc[0][1] = c1;
           } else {
             constexpr int PER = GROUP / kChunk;   // chunks a group
-            acc[a][b] = Mma<kI8>::mul(p, q, i % PER == 0 ? i32x4{} : acc[a][b]);
+            acc[a][b] = Mma<kI8>::mul(p, q, i % PER == 0 ? sum_start() : acc[a][b]);
             if (at != 0 && i % PER == PER - 1) scale(pa, pb, acc[pa][pb], s[i / PER][pb]);
             if (at == 0 && i % PER == 0)
               scale(pa, pb, acc[pa][pb], i ? s[i / PER - 1][pb] : before);
@@ -313,16 +367,16 @@ __device__ __forceinline__ void i8_step(int st, const u32x4& fp, const u32x4& fq
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 part = (h == 0) == low ? fp : u32x4{};
-      const i32x4 c = Mma<kI8>::mul(part, fq, i32x4{});
+      const i32x4 c = Mma<kI8>::mul(part, fq, sum_start());
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)c[v], s[2 * st + h], sum[v]);
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf(sum_value(c[v]), s[2 * st + h], sum[v]);
     }
   } else {
     constexpr int SG = GROUP / 64;   // steps a group
-    acc = Mma<kI8>::mul(fp, fq, st % SG == 0 ? i32x4{} : acc);
+    acc = Mma<kI8>::mul(fp, fq, st % SG == 0 ? sum_start() : acc);
     if (st % SG == SG - 1) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)acc[v], s[st / SG], sum[v]);
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf(sum_value(acc[v]), s[st / SG], sum[v]);
     }
   }
 }
@@ -438,7 +492,7 @@ __global__ __launch_bounds__(512) void i8_fused_kernel(const void* __restrict__ 
     uint32_t m = 0;
     for (int v = tid; v < K / 8; v += 512) {
       float x[8];
-      load8<DT>((const char*)X + (size_t)t * K * es, v, x);
+      unpack8<DT>(load_piece<DT>((const char*)X + (size_t)t * K * es, v), x);
 #pragma unroll
       for (int i = 0; i < 8; ++i) m = max(m, abs_bits(x[i]));
     }
@@ -455,7 +509,7 @@ __global__ __launch_bounds__(512) void i8_fused_kernel(const void* __restrict__ 
     row_scale(m, scale, mul);
     for (int v = tid; v < K / 8; v += 512) {
       float x[8];
-      load8<DT>((const char*)X + (size_t)t * K * es, v, x);
+      unpack8<DT>(load_piece<DT>((const char*)X + (size_t)t * K * es, v), x);
       *(u32x2*)(xq + t * K + 8 * v) = quant8(x, mul);
     }
     if (tid == t) sx[t] = scale;

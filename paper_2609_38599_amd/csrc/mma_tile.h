@@ -242,6 +242,11 @@ __device__ __forceinline__ void wait_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// At least two waves on a SIMD: a wave then has no more than 256 registers, and the
+// compiler leaves the sums where the vector units reach them (the accumulation
+// registers cost a move a value: 2048 x 11008 -> 4096, groups of 64, 251 us; without 134).
+#define JARQ_TWO_WAVES __attribute__((amdgpu_waves_per_eu(2)))
+
 // The S stages of a work-group, `bytes` each: arrays of their own, so that the
 // compiler can tell which of them a load in flight writes.
 #define JARQ_STAGES(S, bytes)                                                     \
@@ -256,8 +261,9 @@ __device__ __forceinline__ void wait_barrier() {
 // multiplied, the loads of the S - 1 behind it are in flight, and fragments are read half
 // a chunk's products ahead.  The loop runs in whole rounds of the stages (chunks past the
 // last are zeros).  A wave's BI blocks of P start at row prow of the tile, its BJ of Q
-// at qrow.  round(q) comes before each round; mul(p, q, a, b, i) gets the fragments of P block
-// a and Q block b of chunk i of the round.
+// at qrow.  round(q) comes before each round (loads of its own make the next wait stricter,
+// never laxer); mul(p, q, a, b, i) gets the fragments of P block a and Q block b of chunk i of
+// the round.
 //
 // 4096 x 4096 -> 2 x 14336 channels, 256-wide tiles: two stages of twice the chunk 812 us,
 // four 800; the loads in a row at the start of a chunk 860; by address instead of by
