@@ -78,9 +78,9 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_tile_kernel
                        __attribute__((always_inline)) {
                          acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                        });
-  // Out through LDS, 32 tokens of a wave column at a time: memory gets whole lines, and
-  // the activation's code is there once (formed from the registers it is 45 KB, read
-  // anew for each tile: 786 us at 4096 x 4096 -> 14336, NEWUS this way).
+  // Out through LDS, 32 tokens of a wave column at a time: memory gets whole lines (8
+  // bytes a lane straight from the registers took 75 us of 800), and the activation's code is
+  // there once, not once a value: 10 KB a kernel, which fits the instruction cache, not 57.
   constexpr int RB = TI / 2 * 4, PIECES = RB / 16;   // a row: one projection's fp32
   constexpr bool APART = WJ == 2;                    // two stages a column, else one
   static_assert((APART ? 1 : 2) * 32 * RB <= STAGE && (WJ == 2 || WJ == 4), "stage");

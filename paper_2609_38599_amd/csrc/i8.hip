@@ -79,8 +79,8 @@ __device__ __forceinline__ void unpack8(const Piece<DT>& p, float (&x)[8]) {
 }  // namespace
 
 // A work-group a row; K a multiple of 16.  A row of up to 16384 values stays in registers
-// between its maximum and its integers: 8192 rows of 14336 in bf16 QTIME, read
-// twice 88.
+// between its maximum and its integers: 8192 rows of 14336 in bf16 57 us, read
+// twice 88 (352 MB: 69 at the rate of a copy).
 template <int DT>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const void* __restrict__ X, int K,
                                                          int8_t* __restrict__ Q,
@@ -143,7 +143,8 @@ __global__ __launch_bounds__(256) void codes_i8_kernel(const uint8_t* __restrict
   const long long e = (long long)blockIdx.x * 256 + threadIdx.x;
   if (e >= n16) return;
   const u32x4 q = *((const u32x4*)codes + e);
-  const int z = zeros[16 * e / g];
+  // (held where q - z cannot overflow; beyond that it is out of range anyway)
+  const int z = max(-1024, min(1024, zeros[16 * e / g]));
   u32x4 o;
   bool out_of_range = false;
 #pragma unroll
@@ -175,17 +176,6 @@ hipError_t launch_codes_i8(hipStream_t st, const uint8_t* codes, const int32_t* 
 
 // ---- products ----
 namespace {
-
-// A group's integer sum n (|n| <= 128 x 128 x 128 = 2^21) as fp32: it starts at the bits of
-// 1.5 x 2^23, at which integers up to 2^22 either way are consecutive floats, so the
-// result's bits are those of 1.5 x 2^23 + n.  (v_cvt_f32_i32 runs at a quarter of the
-// rate: 2048 x 11008 -> 4096 with groups of 64 235 us, this way TIMEB.)
-__device__ __forceinline__ i32x4 sum_start() {
-  return i32x4{0x4b400000, 0x4b400000, 0x4b400000, 0x4b400000};
-}
-__device__ __forceinline__ float sum_value(int32_t c) {
-  return __builtin_bit_cast(float, c) - 12582912.f;
-}
 
 __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) {   // dtype uniform
   if (dtype == 0) ((float*)Y)[at] = y;
@@ -268,7 +258,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
       for (int l = 0; l < GL; ++l) asm volatile("" : "+v"(ahead[l][b]));
     auto scale = [&](int a, int b, const i32x4& c, float sc) __attribute__((always_inline)) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) y[a][b][v] = fmaf(sum_value(c[v]), sc, y[a][b][v]);
+      for (int v = 0; v < 4; ++v) y[a][b][v] = fmaf((float)c[v], sc, y[a][b][v]);
     };
     const bool low = lane < 32;
     mma_loop<S, BI, BJ>(
@@ -289,15 +279,15 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
           if constexpr (GROUP == 32) {
             // a chunk's 64 k are two groups: lanes 0-31 hold the first, 32-63 the second
             const u32x4 none = {};
-            const i32x4 c0 = Mma<kI8>::mul(low ? p : none, q, sum_start());
-            const i32x4 c1 = Mma<kI8>::mul(low ? none : p, q, sum_start());
+            const i32x4 c0 = Mma<kI8>::mul(low ? p : none, q, i32x4{});
+            const i32x4 c1 = Mma<kI8>::mul(low ? none : p, q, i32x4{});
             scale(pa, pb, acc[0][0], at ? s[2 * i][pb] : i ? s[2 * i - 2][pb] : before0);
             scale(pa, pb, acc[0][1], at ? s[2 * i + 1][pb] : i ? s[2 * i - 1][pb] : before);
             acc[0][0] = c0;
             acc[0][1] = c1;
           } else {
             constexpr int PER = GROUP / kChunk;   // chunks a group
-            acc[a][b] = Mma<kI8>::mul(p, q, i % PER == 0 ? sum_start() : acc[a][b]);
+            acc[a][b] = Mma<kI8>::mul(p, q, i % PER == 0 ? i32x4{} : acc[a][b]);
             if (at != 0 && i % PER == PER - 1) scale(pa, pb, acc[pa][pb], s[i / PER][pb]);
             if (at == 0 && i % PER == 0)
               scale(pa, pb, acc[pa][pb], i ? s[i / PER - 1][pb] : before);
@@ -367,16 +357,16 @@ __device__ __forceinline__ void i8_step(int st, const u32x4& fp, const u32x4& fq
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const u32x4 part = (h == 0) == low ? fp : u32x4{};
-      const i32x4 c = Mma<kI8>::mul(part, fq, sum_start());
+      const i32x4 c = Mma<kI8>::mul(part, fq, i32x4{});
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum[v] = fmaf(sum_value(c[v]), s[2 * st + h], sum[v]);
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)c[v], s[2 * st + h], sum[v]);
     }
   } else {
     constexpr int SG = GROUP / 64;   // steps a group
-    acc = Mma<kI8>::mul(fp, fq, st % SG == 0 ? sum_start() : acc);
+    acc = Mma<kI8>::mul(fp, fq, st % SG == 0 ? i32x4{} : acc);
     if (st % SG == SG - 1) {
 #pragma unroll
-      for (int v = 0; v < 4; ++v) sum[v] = fmaf(sum_value(acc[v]), s[st / SG], sum[v]);
+      for (int v = 0; v < 4; ++v) sum[v] = fmaf((float)acc[v], s[st / SG], sum[v]);
     }
   }
 }
@@ -448,10 +438,11 @@ __global__ __launch_bounds__(512) void i8_skinny_kernel(
   }
 }
 
-// One to four tokens, quantized by every work-group for itself: one launch instead of
-// two (one token, 4096 -> 4096: TIMES).  The weights' first
-// fragments are on their way while the tokens go to LDS as integers.
-constexpr int kFusedTokens = 4, kFusedBytes = 48 << 10;   // at most, tokens and bytes of them
+// One or two tokens, quantized by every work-group for itself: one launch instead of two.
+// The weights' first fragments are on their way while the tokens go to LDS as integers.
+// 4096 -> 4096, weights from memory, launches back to back: one token 7.8 us (in two
+// launches 8.2), two 8.7 (8.6), four 10.5 (8.7); a launch takes the host 3 us more.
+constexpr int kFusedTokens = 2, kFusedBytes = 48 << 10;   // at most, tokens and bytes of them
 template <int DT, int GROUP>
 __global__ __launch_bounds__(512) void i8_fused_kernel(const void* __restrict__ X,
                                                        const int8_t* __restrict__ Wq,

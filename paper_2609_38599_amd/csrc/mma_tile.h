@@ -243,8 +243,8 @@ __device__ __forceinline__ void wait_barrier() {
 }
 
 // At least two waves on a SIMD: a wave then has no more than 256 registers, and the
-// compiler leaves the sums where the vector units reach them (the accumulation
-// registers cost a move a value: 2048 x 11008 -> 4096, groups of 64, 251 us; without 134).
+// compiler leaves the sums where the vector units reach them (2048 tokens x 11008 -> 4096,
+// 8 bits, groups of 64: 153 us; by way of the accumulation registers 166).
 #define JARQ_TWO_WAVES __attribute__((amdgpu_waves_per_eu(2)))
 
 // The S stages of a work-group, `bytes` each: arrays of their own, so that the

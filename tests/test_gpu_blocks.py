@@ -448,3 +448,75 @@ def test_logprobs_no_tokens_and_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((*got, d), (*want, grad)))
+
+
+# ---- every shape of tile ----
+
+# The launchers choose tiles by the sizes; these reach each of them with a last tile, a
+# last chunk of k and a last round of stages that are not whole.
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,d,f", [(40, 264, 1000), (70, 136, 4096), (100, 1000, 2752),
+                                   (250, 72, 11008), (400, 4096, 1000), (700, 264, 6000),
+                                   (3300, 520, 2048), (2100, 8, 2104), (129, 4104, 520)])
+def test_gated_tiles(T, d, f, dt):
+    say(f"[gated tiles] tokens {T} d {d} f {f} {dt}")
+    x, wg, wu, dy = _gated_inputs(T, d, f, dt)
+    y, pre = jb.gated_forward(x, wg, wu, save=True)
+    dx, dwg, dwu = jb.gated_backward(x, wg, wu, dy, pre)
+    X, G, U, D = (t.double() for t in (x, wg, wu, dy))
+    a, b = X @ G.T, X @ U.T
+    s = 1 / (1 + torch.exp(-a))
+    da, db = D * b * s * (1 + a * (1 - s)), D * a * s
+    u = ROUND[dt][0]
+    for got, want in ((pre[0], a), (pre[1], b)):
+        # fp32 sums of d products
+        assert (got.double() - want).norm() <= (d + 2) ** 0.5 * 4 * E * want.norm()
+    for got, want in ((y, a * s * b), (dx, da @ G + db @ U), (dwg, da.T @ X), (dwu, db.T @ X)):
+        # one rounding of da and db and one of the result, of relative size u at most
+        assert (got.double() - want).norm() <= 1.5 * u * want.norm()
+
+
+@pytest.mark.parametrize("g", [0, 32, 64, 128])
+@pytest.mark.parametrize("T,n,k", [(40, 1000, 512), (40, 4096, 384), (50, 10000, 1152),
+                                   (70, 1000, 1152), (150, 4000, 384), (400, 4000, 1152),
+                                   (200, 11008, 640), (1000, 4100, 384), (3000, 4100, 384),
+                                   (33, 8200, 128), (66, 700, 2688), (130, 17, 896)])
+def test_matmul_i8_tiles(T, n, k, g):
+    say(f"[i8 tiles] tokens {T} n {n} k {k} group {g}")
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    xq, wq = (torch.randint(-128, 128, (m, k), generator=gen, device="cuda", dtype=torch.int8)
+              for m in (T, n))
+    G = k // g if g else 1
+    sx = torch.rand(T, generator=gen, device="cuda")
+    sw = torch.randn(n, G, generator=gen, device="cuda")
+    w = (wq.view(n, G, -1).double() * sw.double()[:, :, None]).view(n, k)
+    want = (xq.double() @ w.T) * sx.double()[:, None]
+    for dt in (torch.float32, torch.bfloat16):
+        y = jb.matmul_i8(xq, sx, wq, sw, dtype=dt)
+        # G + 4 roundings in fp32 and the output's
+        assert (y.double() - want).norm() <= ((G + 4) * E + 1.2 * ROUND[dt][0]) * want.norm()
+
+
+def test_matmul_i8_scales_of_other_channels_do_not_reach_a_row():
+    # the loads of a row's scales run past its last group: infinities there stay there
+    for T in (3, 40, 100, 300):
+        n, k, g = 200, 192, 64
+        xq = torch.ones(T, k, dtype=torch.int8).cuda()
+        wq = torch.ones(n, k, dtype=torch.int8).cuda()
+        sw = torch.ones(n, k // g)
+        sw[1::2] = float("inf")
+        y = jb.matmul_i8(xq, torch.ones(T).cuda(), wq, sw.cuda(), dtype=torch.float32)
+        assert bool((y[:, 0::2] == k).all()) and bool(torch.isinf(y[:, 1::2]).all())
+
+
+def test_example_runs_a_refined_block():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples",
+                        "refined_block.py")
+    spec = importlib.util.spec_from_file_location("refined_block", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    r = module.main(tokens=256, d=256, f=512, vocab=1000, sweeps=3, log=say)
+    assert all(np.isfinite(v) for v in r.values())
+    assert r["after"] < r["refined"] and r["base"] < r["refined"] + 0.05
