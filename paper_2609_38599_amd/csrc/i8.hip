@@ -335,11 +335,12 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
         }
       }
     } else {
-#pragma unroll 1
-      for (int p = lane; p < 32 * CH; p += 64) {
-        const int t = tw + p / CH, n = nw + p % CH;
-        if (t < T && n < N) store_y(Y, dtype, (size_t)t * N + n, mine[p] * sx[t]);
-      }
+      // a row (CH 64) or two (CH 32) at a time
+      const int n = nw + lane % CH;
+#pragma unroll 4
+      for (int r = lane / CH; r < 32; r += 64 / CH)
+        if (tw + r < T && n < N)
+          store_y(Y, dtype, (size_t)(tw + r) * N + n, mine[r * CH + lane % CH] * sx[tw + r]);
     }
     asm volatile("" ::: "memory");
   }
@@ -561,7 +562,8 @@ static hipError_t launch_i8_tiles(hipStream_t st, int dtype, int T, int N, int K
 // memory; channels in blocks of 16 where wider ones are too few for the chip.  k = 4096:
 // 64 tokens -> 4096 with 16, 32 channels a work-group 13, 11 us, tiles 14; 64 -> 1000 (groups
 // of 32) 10, 18, 31; 37 -> 11008 (groups of 128) 29, 27 and 21.  Beyond, the tiles that
-// tile_cost makes the cheapest; k = 4096 -> 1000, 4096 and 11008 channels, in us with tiles of
+// tile_cost makes the cheapest, or fragments from memory again for a narrow layer (whose
+// wavefronts cut k in eight); k = 4096 -> 1000, 4096 and 11008 channels, in us with tiles of
 // 256 x 256, 128 x 128 (tokens x channels), 128 x 64, 64 x 64 and 64 x 32:
 //    100 tokens   44 19 14 12 11   44 19 14 12 11     45  22  18  20  20
 //    400          45 19 14 12 11   48 23 16 18 28     50  39  50  47  60
@@ -580,12 +582,13 @@ static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K
   const int nk = (K + kChunk - 1) / kChunk;
   constexpr double plain[4] = {0.25, 0.17, 0.135, 0.12}, grouped[4] = {0.55, 0.43, 0.3, 0.28};
   const double* c = GROUP ? grouped : plain;
-  const double cost[5] = {tile_cost(tiles(128, 128), nk, c[0], 3.8),
+  const double cost[6] = {tile_cost(tiles(128, 128), nk, c[0], 3.8),
                           tile_cost(tiles(128, 64), nk, c[1], 3.0),
                           tile_cost(tiles(64, 64), nk, c[2], 3.0),
                           tile_cost(tiles(64, 32), nk, c[3], 3.0),
+                          tile_cost(tiles(16, 16), nk, 0.058, 2.5),
                           GROUP ? 1e30 : tile_cost(tiles(256, 256), nk, 0.7, 6.0)};
-  switch ((int)(std::min_element(cost, cost + 5) - cost)) {
+  switch ((int)(std::min_element(cost, cost + 6) - cost)) {
     case 0:
       return launch_i8_tiles<GROUP, 4, 2, 2, 4, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 1:
@@ -594,6 +597,7 @@ static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K
       return launch_i8_tiles<GROUP, 8, 2, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 3:
       return launch_i8_tiles<GROUP, 8, 2, 1, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+    case 4: return launch_i8_skinny<GROUP, 1, 1, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     default:
       if constexpr (GROUP == 0)
         return launch_i8_tiles<0, 4, 2, 4, 8, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
