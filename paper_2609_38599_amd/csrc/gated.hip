@@ -33,10 +33,11 @@ __device__ __forceinline__ float activation(float a, float* d) {
     if (d) *d = cdf + a * kInvSqrt2Pi * __expf(-0.5f * a * a);
     return a * cdf;
   } else {                           // gelu, tanh form: (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
-    const float z = kSqrt2OverPi * (a + 0.044715f * a * a * a);
+    const float aa = fminf(a * a, 1e30f);   // (0 times it stays 0)
+    const float z = kSqrt2OverPi * (a + 0.044715f * a * aa);
     const float sig = __builtin_amdgcn_rcpf(1.f + __expf(-2.f * z));
     if (d)
-      *d = sig + 2.f * a * sig * (1.f - sig) * kSqrt2OverPi * (1.f + 3.f * 0.044715f * a * a);
+      *d = sig + sig * (1.f - sig) * a * (2.f * kSqrt2OverPi * (1.f + 3.f * 0.044715f * aa));
     return a * sig;
   }
 }

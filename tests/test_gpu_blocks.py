@@ -520,3 +520,24 @@ def test_example_runs_a_refined_block():
     r = module.main(tokens=256, d=256, f=512, vocab=1000, sweeps=3, log=say)
     assert all(np.isfinite(v) for v in r.values())
     assert r["after"] < r["refined"] and r["base"] < r["refined"] + 0.05
+
+
+@pytest.mark.parametrize("act", sorted(jb.ACTIVATIONS))
+def test_gated_values_whose_square_overflows(act):
+    # a = +-2^70: act(a) is a or 0 and act'(a) 1 or 0; every result is a power of two
+    say(f"[gated] {act} at 2^70")
+    T, d, f = 2, 8, 8
+    x, wg, wu = torch.zeros(T, d), torch.zeros(f, d), torch.zeros(f, d)
+    x[0, 0], x[1, 0], x[:, 1] = 2.0 ** 40, -2.0 ** 40, 1.0
+    wg[:, 0], wu[:, 1] = 2.0 ** 30, 2.0 ** -3
+    x, wg, wu = (t.bfloat16().cuda() for t in (x, wg, wu))
+    y, pre = jb.gated_forward(x, wg, wu, act=act, save=True)
+    dx, dwg, dwu = jb.gated_backward(x, wg, wu, torch.ones_like(y), pre, act=act)
+    assert (y[0] == 2.0 ** 67).all() and (y[1] == 0).all()
+    want = torch.zeros(T, d)
+    want[0, 0], want[0, 1] = 2.0 ** 30, 2.0 ** 70
+    assert torch.equal(dx.float().cpu(), want)
+    for got, da in ((dwg, 2.0 ** -3), (dwu, 2.0 ** 70)):
+        want = torch.zeros(f, d)
+        want[:, 0], want[:, 1] = da * 2.0 ** 40, da
+        assert torch.equal(got.float().cpu(), want)
