@@ -4,7 +4,7 @@
 // 127, q = rint(x (127 / amax)), all in fp32.
 //
 // The product: y[t][n] = sx_t sum_g sw[n][g] sum_{k in g} xq[t][k] wq[n][k], the
-// integer sums exact in int32 on v_mfma_i32_32x32x32_i8, a group's sum converted
+// integer sums exact in int32 on v_mfma_i32_16x16x64_i8, a group's sum converted
 // and added in fp32.  Tokens are the P rows and channels the Q rows, so that a lane
 // holds one channel and needs one group scale.
 #include <algorithm>
@@ -239,14 +239,15 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
       for (int b = 0; b < BJ; ++b)
 #pragma unroll
         for (int l = 0; l < GL; ++l) {
+          // (all of the offset in the part that is compared with the buffer's end)
+          const int at = (int)sat[b] + 16 * l + 4 * g0;
           if constexpr (GR == 2) {
-            const u32x2 w = __builtin_bit_cast(
-                u32x2, __builtin_amdgcn_raw_buffer_load_b64(scales, (int)sat[b], 4 * g0, 0));
+            const u32x2 w =
+                __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(scales, at, 0, 0));
             ahead[l][b] = u32x4{w[0], w[1], 0u, 0u};
           } else {
-            ahead[l][b] = __builtin_bit_cast(
-                u32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, (int)sat[b] + 16 * l,
-                                                                 4 * g0, 0));
+            ahead[l][b] =
+                __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(scales, at, 0, 0));
           }
         }
     };

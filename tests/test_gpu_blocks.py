@@ -541,3 +541,10 @@ def test_gated_values_whose_square_overflows(act):
         want = torch.zeros(f, d)
         want[:, 0], want[:, 1] = da * 2.0 ** 40, da
         assert torch.equal(got.float().cpu(), want)
+
+
+@pytest.mark.parametrize("g", [32, 64, 128])
+@pytest.mark.parametrize("T,n,k", [(3000, 4097, 384), (700, 2049, 640), (300, 1025, 896)])
+def test_matmul_i8_last_tile_of_one_channel(T, n, k, g):
+    # the loads of its scales run past the last group of the last channel
+    test_matmul_i8_tiles(T, n, k, g)
