@@ -9,7 +9,6 @@
 // to 16 bits as the matrix cores take them (the only rounding beside the
 // outputs'); then dx = [da db] [Wg; Wu] in one product over 2 F, and
 // [dWg; dWu] = [da db]^T x in one over T.
-#include <algorithm>
 
 #include "skinny.h"
 
@@ -53,7 +52,7 @@ __device__ __forceinline__ float activation(int act, float a, float* d) {   // a
 // WI x WJ wavefronts, each BI blocks of 16 P rows (half Wg's, half Wu's) x BJ blocks
 // of 16 tokens.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_tile_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int act, uint16_t* __restrict__ Y, float* __restrict__ pre, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
@@ -204,10 +203,10 @@ static hipError_t launch_gated_forward_kind(hipStream_t st, int act, int T, int 
   }
   auto tiles = [&](int f, int t) { return (long long)((F + f - 1) / f) * ((T + t - 1) / t); };
   const int nk = (2 * D + kChunk - 1) / kChunk;
-  const double cost[4] = {tile_cost(tiles(128, 256), nk, 0.62, 6.0),
-                          tile_cost(tiles(64, 128), nk, 0.26, 3.3),
-                          tile_cost(tiles(64, 64), nk, 0.19, 2.7),
-                          tile_cost(tiles(32, 64), nk, 0.135, 2.6)};
+  const double cost[4] = {tile_cost(tiles(128, 256), nk, {6.0, 0.62, 6.0, 0.62}),
+                          tile_cost(tiles(64, 128), nk, {3.3, 0.26, 3.3, 0.26}),
+                          tile_cost(tiles(64, 64), nk, {2.7, 0.19, 2.7, 0.19}),
+                          tile_cost(tiles(32, 64), nk, {2.6, 0.135, 2.6, 0.135})};
   switch ((int)(std::min_element(cost, cost + 4) - cost)) {
     case 0: return launch_gated_tiles<KIND, 4, 2, 4, 8, 4>(st, act, T, D, F, X, Wg, Wu, y, pre);
     case 1: return launch_gated_tiles<KIND, 4, 2, 2, 4, 4>(st, act, T, D, F, X, Wg, Wu, y, pre);
@@ -290,7 +289,7 @@ __device__ __forceinline__ void store_tile16(const f32x4 (&acc)[BI][BJ], char* s
 // ---- backward: dx = dab [Wg; Wu] ----
 // part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_dx_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_dx_kernel(
     const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
     int D, int F, int each, uint16_t* __restrict__ dX, float* __restrict__ part, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
@@ -350,7 +349,7 @@ __global__ __launch_bounds__(256) void gated_dx_sum_kernel(const float* __restri
 
 // ---- backward: [dWg; dWu] = dab^T x ----
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void gated_dw_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_dw_kernel(
     const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,
     uint16_t* __restrict__ dWg, uint16_t* __restrict__ dWu, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
@@ -398,7 +397,8 @@ struct DxPlan {
 DxPlan dx_plan(int T, int D, int F) {
   const int nk = 2 * ((2 * F + kChunk - 1) / kChunk);
   constexpr int wide[3] = {256, 128, 128}, tall[3] = {256, 128, 64};
-  constexpr double chunk[3] = {0.62, 0.26, 0.19}, rest[3] = {8.0, 4.0, 3.0};
+  constexpr TileTime time[3] = {
+      {8.0, 0.62, 8.0, 0.62}, {4.0, 0.26, 4.0, 0.26}, {3.0, 0.19, 3.0, 0.19}};
   DxPlan best{};
   double least = 0.0;
   for (int kind = 0; kind < 3; ++kind) {
@@ -407,7 +407,7 @@ DxPlan dx_plan(int T, int D, int F) {
       const int each = ((nk + parts - 1) / parts + 3) / 4 * 4;   // whole rounds of stages
       const int splits = (nk + each - 1) / each;
       if (splits != parts) continue;
-      double cost = tile_cost((long long)ni * nj * splits, each, chunk[kind], rest[kind]);
+      double cost = tile_cost((long long)ni * nj * splits, each, time[kind]);
       if (splits > 1) cost += 5.0 + 8e-6 * splits / 4.0 * T * D;
       if (best.splits == 0 || cost < least) {
         least = cost;

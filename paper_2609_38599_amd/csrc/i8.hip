@@ -7,7 +7,6 @@
 // integer sums exact in int32 on v_mfma_i32_16x16x64_i8, a group's sum converted
 // and added in fp32.  Tokens are the P rows and channels the Q rows, so that a lane
 // holds one channel and needs one group scale.
-#include <algorithm>
 #include <type_traits>
 
 #include "skinny.h"
@@ -188,7 +187,7 @@ __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) 
 // Many tokens.  GROUP 0: one scale a channel, int32 sums over all of k; otherwise a
 // group's int32 sums go to fp32.
 template <int GROUP, int S, int WI, int WJ, int BI, int BJ>
-__global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(GROUP && WI * WJ == 8 ? 4 : 2) void i8_tile_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,
     const float* __restrict__ sw, int T, int N, int K, int dtype, void* __restrict__ Y, int ni,
     int nj) {
@@ -304,6 +303,14 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
   float* const mine = (float*)(wave / PER == 0 ? stage0 : wave / PER == 1 ? stage1
                                : wave / PER == 2 ? stage2 : stage3) + wave % PER * 32 * CH;
   const int nw = n0 + qrow;
+  // every token's scale before the first store: loaded row by row they cost their latency
+  // each time (1993 x 128 -> 6966 in fp32: 33 us, now 27)
+  float scale_of[BI][4];
+#pragma unroll
+  for (int a = 0; a < BI; ++a)
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+      scale_of[a][v] = sx[min(t0 + prow + 16 * a + 4 * (lane >> 4) + v, T - 1)];
   // four values at a time where every row starts at their boundary and none ends inside four
   const bool wide = (uintptr_t)Y % (dtype == 0 ? 16 : 8) == 0 && N % 4 == 0;
 #pragma unroll
@@ -315,7 +322,8 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
 #pragma unroll
         for (int v = 0; v < 4; ++v)
           mine[(16 * (a - aa) + 4 * (lane >> 4) + v) * CH + 16 * b + (lane & 15)] =
-              GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0];
+              (GROUP ? y[GROUP ? a : 0][GROUP ? b : 0][v] : (float)acc[a][b][v] * srow[b][0]) *
+              scale_of[a][v];
     asm volatile("" ::: "memory");   // one wave: its LDS accesses complete in order
     const int tw = t0 + prow + 16 * aa;
     if (wide) {
@@ -323,11 +331,9 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
       for (int p = lane; p < 32 * CH / 4; p += 64) {
         const int t = tw + p / (CH / 4), n = nw + 4 * (p % (CH / 4));
         if (t < T && n < N) {
-          const f32x4 s = *(const f32x4*)(mine + 4 * p);
-          const float st = sx[t];
-          const float o[4] = {s[0] * st, s[1] * st, s[2] * st, s[3] * st};
+          const f32x4 o = *(const f32x4*)(mine + 4 * p);
           const size_t e = (size_t)t * N + n;
-          if (dtype == 0) *(f32x4*)((float*)Y + e) = f32x4{o[0], o[1], o[2], o[3]};
+          if (dtype == 0) *(f32x4*)((float*)Y + e) = o;
           else if (dtype == kF16)
             *(u32x2*)((uint16_t*)Y + e) = u32x2{pack16<kF16>(o[0], o[1]), pack16<kF16>(o[2], o[3])};
           else
@@ -341,7 +347,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_TWO_WAVES void i8_tile_kernel(
 #pragma unroll 4
       for (int r = lane / CH; r < 32; r += 64 / CH)
         if (tw + r < T && n < N)
-          store_y(Y, dtype, (size_t)(tw + r) * N + n, mine[r * CH + lane % CH] * sx[tw + r]);
+          store_y(Y, dtype, (size_t)(tw + r) * N + n, mine[r * CH + lane % CH]);
     }
     asm volatile("" ::: "memory");
   }
@@ -564,13 +570,20 @@ static hipError_t launch_i8_tiles(hipStream_t st, int dtype, int T, int N, int K
 // 64 tokens -> 4096 with 16, 32 channels a work-group 13, 11 us, tiles 14; 64 -> 1000 (groups
 // of 32) 10, 18, 31; 37 -> 11008 (groups of 128) 29, 27 and 21.  Beyond, the tiles that
 // tile_cost makes the cheapest, or fragments from memory again for a narrow layer (whose
-// wavefronts cut k in eight); k = 4096 -> 1000, 4096 and 11008 channels, in us with tiles of
-// 256 x 256, 128 x 128 (tokens x channels), 128 x 64, 64 x 64 and 64 x 32:
-//    100 tokens   44 19 14 12 11   44 19 14 12 11     45  22  18  20  20
-//    400          45 19 14 12 11   48 23 16 18 28     50  39  50  47  60
-//   1600          48 23 17 18 29   51 44 63 60 77    112 110 147 146 192
-// Groups (of 64, 1600 tokens -> 4096): 128 x 128 77, 256 x 128 74; 800 -> 11008 119 and 137:
-// converting a group's sums takes the vector units as long as the matrix cores.
+// wavefronts cut k in eight).  k = 4096 -> 1000, 4096 and 11008 channels, in us with tiles of
+// 256 x 256, 128 x 128 (tokens x channels), 128 x 64, 64 x 64, 64 x 32 and fragments:
+//    128 tokens   43 19 14 11 10 10   43 21 16 12 10  31   44  22  18  20  21   78
+//    512          46 21 16 12 10 31   46 22 18 21 29 114   51  40  46  52  65  301
+//   2048          47 22 18 20 29 114  52 49 61 68 90 447  109 121 163 169 218 1198
+// and groups of 64:
+//    128              31 26 18 16 13       32 26 18 16  45        33  28  28  26  117
+//    512              32 26 18 16 45       33 29 28 40 169        57  60  75  86  450
+//   2048              33 29 28 39 167      66 84 97 118 669      178 212 254 293 1792
+// Four stages against eight: 128 x 64 never slower, k = 256 -> 11008, 512 tokens 9.0 us and 17
+// (three work-groups fit a CU, not one); 64 x 64 4.3 and 5.0 at k = 256, 13.6 and 12.8 at 4096.
+// Groups at 128 x 128: eight wavefronts, since converting their sums takes the vector units
+// twice as long as the matrix cores (3000 tokens, k = 2048 -> 1000, groups of 64: 20 us, four
+// wavefronts 26).
 template <int GROUP>
 static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K, const int8_t* Xq,
                                   const float* sx, const int8_t* Wq, const float* sw, void* Y) {
@@ -581,20 +594,31 @@ static hipError_t launch_i8_group(hipStream_t st, int dtype, int T, int N, int K
   if (T <= 64 && N <= 8192)
     return launch_i8_skinny<GROUP, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
   const int nk = (K + kChunk - 1) / kChunk;
-  constexpr double plain[4] = {0.25, 0.17, 0.135, 0.12}, grouped[4] = {0.55, 0.43, 0.3, 0.28};
-  const double* c = GROUP ? grouped : plain;
-  const double cost[6] = {tile_cost(tiles(128, 128), nk, c[0], 3.8),
-                          tile_cost(tiles(128, 64), nk, c[1], 3.0),
-                          tile_cost(tiles(64, 64), nk, c[2], 3.0),
-                          tile_cost(tiles(64, 32), nk, c[3], 3.0),
-                          tile_cost(tiles(16, 16), nk, 0.058, 2.5),
-                          GROUP ? 1e30 : tile_cost(tiles(256, 256), nk, 0.7, 6.0)};
+  constexpr TileTime plain[5] = {{7.0, 0.31, 2.5, 0.27},
+                                 {4.7, 0.21, 1.1, 0.21},
+                                 {3.6, 0.145, 0.6, 0.125},
+                                 {3.5, 0.108, 0.5, 0.085},
+                                 {2.4, 0.06, 0.25, 0.053}};
+  constexpr TileTime grouped[5] = {{6.0, 0.53, 1.2, 0.37},
+                                   {3.9, 0.39, 0.8, 0.30},
+                                   {3.3, 0.25, 1.0, 0.165},
+                                   {3.1, 0.205, 0.7, 0.105},
+                                   {2.2, 0.085, 0.4, 0.083}};
+  const TileTime* t = GROUP ? grouped : plain;
+  const double cost[6] = {
+      tile_cost(tiles(128, 128), nk, t[0]), tile_cost(tiles(128, 64), nk, t[1]),
+      tile_cost(tiles(64, 64), nk, t[2]),   tile_cost(tiles(64, 32), nk, t[3]),
+      tile_cost(tiles(16, 16), nk, t[4]),
+      GROUP ? 1e30 : tile_cost(tiles(256, 256), nk, {15.0, 0.65, 15.0, 0.65})};
   switch ((int)(std::min_element(cost, cost + 6) - cost)) {
     case 0:
-      return launch_i8_tiles<GROUP, 4, 2, 2, 4, 4>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return launch_i8_tiles<GROUP, 4, 2, GROUP ? 4 : 2, 4, GROUP ? 2 : 4>(st, dtype, T, N, K, Xq,
+                                                                          sx, Wq, sw, Y);
     case 1:
-      return launch_i8_tiles<GROUP, 8, 2, 2, 4, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
+      return launch_i8_tiles<GROUP, 4, 2, 2, 4, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 2:
+      if (nk <= 32)
+        return launch_i8_tiles<GROUP, 4, 2, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
       return launch_i8_tiles<GROUP, 8, 2, 2, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);
     case 3:
       return launch_i8_tiles<GROUP, 8, 2, 1, 2, 2>(st, dtype, T, N, K, Xq, sx, Wq, sw, Y);

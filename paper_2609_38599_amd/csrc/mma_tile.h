@@ -13,6 +13,8 @@
 // it holds column j = lane % 16 and rows i = 4 (lane / 16) + v, v = 0..3.
 #pragma once
 
+#include <algorithm>
+
 #include "bf16x3.h"
 
 namespace jarq {
@@ -242,10 +244,10 @@ __device__ __forceinline__ void wait_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// At least two waves on a SIMD: a wave then has no more than 256 registers, and the
+// At least n waves on a SIMD.  With two a wave has no more than 256 registers, and the
 // compiler leaves the sums where the vector units reach them (2048 tokens x 11008 -> 4096,
 // 8 bits, groups of 64: 153 us; by way of the accumulation registers 166).
-#define JARQ_TWO_WAVES __attribute__((amdgpu_waves_per_eu(2)))
+#define JARQ_WAVES(n) __attribute__((amdgpu_waves_per_eu(n)))
 
 // The S stages of a work-group, `bytes` each: arrays of their own, so that the
 // compiler can tell which of them a load in flight writes.
@@ -345,11 +347,15 @@ __device__ __forceinline__ char* out_piece(char* buf, int r, int c) {
   return buf + r * RB + ((c ^ (r & (RB / 16 - 1))) << 4);
 }
 
-// What a launch takes in us if each of the 256 CUs has one of its work-groups at a time:
-// `chunk` a chunk and `rest` for the beginning and the end.  The launchers' figures
-// are of launches of one work-group a CU (K of 32 and of 128 chunks).
-inline double tile_cost(long long groups, int chunks, double chunk, double rest) {
-  return (double)((groups + 255) / 256) * (chunks * chunk + rest);
+// A launch's time in us by its tiles: `begin` and `chunk` a chunk for the first work-group
+// on a CU, `more` and `more_chunk` a chunk for each further one (beside the others as far as
+// they fit).  The launchers' figures are of launches of one to eight work-groups a CU.
+struct TileTime {
+  double begin, chunk, more, more_chunk;
+};
+inline double tile_cost(long long groups, int chunks, const TileTime& t) {
+  const double further = (double)((groups + 255) / 256 - 1);
+  return t.begin + chunks * t.chunk + further * (t.more + chunks * t.more_chunk);
 }
 
 // Tile (ti, tj) of work-group `id` in a grid of ni x nj tiles: the work-groups

@@ -548,3 +548,11 @@ def test_gated_values_whose_square_overflows(act):
 def test_matmul_i8_last_tile_of_one_channel(T, n, k, g):
     # the loads of its scales run past the last group of the last channel
     test_matmul_i8_tiles(T, n, k, g)
+
+
+@pytest.mark.parametrize("g", [0, 32, 64, 128])
+@pytest.mark.parametrize("T,n,k", [(1993, 6966, 128), (611, 11008, 256), (2047, 1001, 2048),
+                                   (150, 11008, 2176), (1030, 1000, 4096), (260, 4096, 1024),
+                                   (150, 1000, 4096), (1100, 4096, 4096)])
+def test_matmul_i8_tiles_of_many_work_groups(T, n, k, g):
+    test_matmul_i8_tiles(T, n, k, g)
