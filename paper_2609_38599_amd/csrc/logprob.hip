@@ -99,8 +99,6 @@ __device__ __forceinline__ float key_value(u64 k) {
   return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
 }
 __device__ __forceinline__ uint32_t key_index(u64 k) { return 0xffffffffu - (uint32_t)k; }
-
-
 __device__ __forceinline__ uint32_t ordered(float x) { return (uint32_t)(top_key(x, 0) >> 32); }
 constexpr uint32_t kOrderedMinusInf = 0x007fffffu;
 
@@ -261,7 +259,9 @@ __device__ __forceinline__ void store_top(const RowOut& o, size_t at, u64 key, c
 }  // namespace
 
 // Work-group `id`: part id % splits (of `each` entries) of row id / splits.  With one
-// part it finishes the row; otherwise its sums and top keys go to the workspace.
+// part it finishes the row; otherwise its sums and top keys go to the workspace.  Bound by
+// reading the logits (4096 x 128000 in bf16, no top: 235 us, 4.5 TB/s), with a top by the
+// issue of its candidates' votes (2047 x 32001 in fp32: 50 us without, top 20 74 us).
 template <int DT, bool TOP>
 __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ logits, size_t ld,
                                                       int V, const int64_t* __restrict__ targets,
@@ -403,7 +403,8 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
 }
 
 // A work-group a row: its parts' sums (at most 64 parts, joined in a fixed order) and the
-// top of their keys (at most 256).
+// top of their keys (at most 256).  Bound by its chain's latency: 1 x 128000, 31 parts, top 8
+// 5 us.
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_join_kernel(
     const void* __restrict__ logits, size_t ld, int V, const int64_t* __restrict__ targets,
@@ -451,7 +452,8 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
 // ---- gradient ----
 // d x_v = g (onehot - p) - h p (log p + H), g and h the gradients of the log
 // probability and of the entropy.  Work-group `id`: part id % splits of a row.  A
-// thread reads each entry before it writes it: dlogits may be the logits.
+// thread reads each entry before it writes it: dlogits may be the logits.  Bound by
+// memory: 4096 x 128000 in bf16 410 us, 5.1 TB/s.
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(
     const void* logits, size_t ld, int V, const int64_t* __restrict__ targets,

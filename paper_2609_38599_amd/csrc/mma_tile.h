@@ -246,7 +246,8 @@ __device__ __forceinline__ void wait_barrier() {
 
 // At least n waves on a SIMD.  With two a wave has no more than 256 registers, and the
 // compiler leaves the sums where the vector units reach them (2048 tokens x 11008 -> 4096,
-// 8 bits, groups of 64: 153 us; by way of the accumulation registers 166).
+// 8 bits, groups of 64, four wavefronts of 64 x 64: 153 us; by way of the accumulation
+// registers 166).
 #define JARQ_WAVES(n) __attribute__((amdgpu_waves_per_eu(n)))
 
 // The S stages of a work-group, `bytes` each: arrays of their own, so that the
