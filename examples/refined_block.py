@@ -6,7 +6,7 @@ A synthetic block (gate, up and down projections) with a head over a vocabulary:
 2. the refined gate and up run as one gated block, and its output tokens are the
    calibration of down, which is refined in turn;
 3. the refined block runs with down in 8-bit integers straight from its codes, and
-   the log probabilities of the next tokens judge it against the original;
+   the log probabilities of the next tokens compare it with the original;
 4. one step of recovery: the loss's gradient goes back through the head, down and the
    gated block to the dequantized gate and up.
 

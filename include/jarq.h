@@ -389,7 +389,7 @@ jarq_status jarq_permute(const jarq_params* p, const int32_t* perm, const float*
                          float* Wp, float* Hp, void* stream);
 
 /*
- * Running, training and judging refined layers.
+ * Running, training and evaluating refined layers.
  *
  * Tokens are rows: X [tokens][d], 0 <= tokens <= 2^22 (0: nothing is read, and
  * pointers to the tokens' arrays may be NULL).  Arrays are 16-byte aligned unless

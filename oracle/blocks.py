@@ -1,4 +1,4 @@
-"""Float64 definitions of the operators that run, train and judge refined layers.
+"""Float64 definitions of the operators that run, train and evaluate refined layers.
 
 The gated feed-forward block and its gradients, linear layers in 8-bit
 integers, and log probabilities of tokens with their gradient, in NumPy, row by

@@ -3,7 +3,7 @@
 The per-layer hot path of JARQ (joint alternating refinement of a group-wise
 quantized weight matrix against a calibration Hessian) as hand-written HIP for
 gfx950 behind the C ABI of include/jarq.h, with a thin ctypes binding; and the
-operators that run, train and judge refined layers: the gated feed-forward block with its
+operators that run, train and evaluate refined layers: the gated feed-forward block with its
 gradients, linear layers in 8-bit integers, and token log probabilities.
 """
 

@@ -492,7 +492,7 @@ def gptq(p: Params, W, H, codes=None, scales=None, zeros=None, ws=None, stream=N
     return codes, scales, zeros
 
 
-# ---- running, training and judging refined layers ----
+# ---- running, training and evaluating refined layers ----
 
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 

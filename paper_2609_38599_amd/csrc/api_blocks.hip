@@ -1,4 +1,4 @@
-// C ABI of the operators that run, train and judge refined layers (declared in
+// C ABI of the operators that run, train and evaluate refined layers (declared in
 // include/jarq.h): argument checks and dispatch to the kernels' launchers.
 #include "jarq.h"
 #include "jarq_internal.h"

@@ -393,7 +393,7 @@ hipError_t launch_gptq(hipStream_t st, int rows, int cols, int g, int bits, cons
                        const float* H, char* ws, uint8_t* codes, float* scales, int32_t* zeros,
                        int** flag_out);
 
-// ---- running, training and judging refined layers ----
+// ---- running, training and evaluating refined layers ----
 // gated.hip.  dtype JARQ_F16 or JARQ_BF16, act JARQ_ACT_*.
 hipError_t launch_gated_forward(hipStream_t st, int dtype, int act, int T, int D, int F,
                                 const void* X, const void* Wg, const void* Wu, void* Y,

@@ -1,4 +1,4 @@
-"""The operators that run, train and judge refined layers: their float64 definitions
+"""The operators that run, train and evaluate refined layers: their float64 definitions
 against differences, and their entry points' argument checks (CPU only)."""
 
 import ctypes

@@ -1,4 +1,4 @@
-"""The operators that run, train and judge refined layers on the GPU against their
+"""The operators that run, train and evaluate refined layers on the GPU against their
 float64 definitions.  Tolerances are bounds from the arithmetic: u is half a unit
 in the last place of the output's type, e = 2^-24 that of fp32 sums."""
 
