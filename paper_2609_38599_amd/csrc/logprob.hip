@@ -2,8 +2,10 @@
 // logits, and the gradient of the logits.
 //
 // With m = max x, z = sum exp(x - m): lse = m + log z, log p_v = x_v - lse and
-// H = log z - sum exp(x - m) (x - m) / z, all from one pass that keeps (m, z, sum
-// exp(x - m) (x - m)) per lane and rescales when m grows.
+// H = log z - sum exp(x - m) (x - m) / z, all from one pass that keeps (m, z - 1, sum
+// exp(x - m) (x - m)) per lane and rescales when m grows.  (z - 1, the sum beside the
+// maximum's own 1: where one entry takes nearly all, z would round away what the others
+// take, which is the log probability of that entry.)
 //
 // A row in which any entry is +infinity or NaN gives NaN (and index -1); entries
 // of -infinity have probability 0; a row of nothing else has lse = -infinity.
@@ -50,42 +52,56 @@ __device__ __forceinline__ u32x4 minus_inf() {
   return u32x4{w, w, w, w};
 }
 
-// The running maximum (at least -FLT_MAX, so that x - m is never -inf + inf), sum
-// and weighted sum.
+// The running maximum (at least -FLT_MAX, so that x - m is never -inf + inf), the sum
+// beside the maximum's own 1 (-1: no entry above -infinity) and the weighted sum.
 struct Soft {
-  float m, z, zt;
+  float m, more, zt;
+  __device__ __forceinline__ bool none() const { return more == -1.f; }
+  __device__ __forceinline__ bool broken() const { return more != more; }
 };
-__device__ __forceinline__ Soft no_entries() { return Soft{-FLT_MAX, 0.f, 0.f}; }
+__device__ __forceinline__ Soft no_entries() { return Soft{-FLT_MAX, -1.f, 0.f}; }
 // Keeps exp's argument within range for the weighted sum: exp is 0 there.
 constexpr float kLeast = -1000.f;
 
 // Adds entries; returns the largest.
 template <int DT, int N>
-__device__ __forceinline__ float add(Soft& s, const float (&x)[N]) {
-  float most = x[0];
+__device__ __forceinline__ float add(Soft& s, const float (&entries)[N]) {
+  float x[N], most = entries[0];
 #pragma unroll
-  for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
+  for (int i = 0; i < N; ++i) {
+    x[i] = entries[i];
+    most = fmaxf(most, x[i]);
+  }
   const float m = fmaxf(s.m, most);
   if (m > s.m) {
-    const float t = s.m - m, e = exp_of<DT>(t);
-    s.zt = e * (s.zt + s.z * fmaxf(t, kLeast));
-    s.z *= e;
+    const float t = s.m - m, e = exp_of<DT>(t), z = 1.f + s.more;
+    s.zt = e * (s.zt + z * fmaxf(t, kLeast));
+    s.more = e * z;
     s.m = m;
+    // the maximum's own 1 stays out of the sum (+infinity stays in: it gives a NaN)
+    bool out = m == INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const bool own = !out && x[i] == m;
+      out |= own;
+      x[i] = own ? -INFINITY : x[i];
+    }
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const float t = x[i] - m, e = exp_of<DT>(t);
-    s.z += e;
+    s.more += e;
     s.zt = fmaf(e, fmaxf(t, kLeast), s.zt);
   }
   return most;
 }
 __device__ __forceinline__ void join(Soft& s, const Soft& o) {
-  const float m = fmaxf(s.m, o.m);
-  const float ta = s.m - m, tb = o.m - m, ea = expf(ta), eb = expf(tb);
-  s.zt = ea * (s.zt + s.z * fmaxf(ta, kLeast)) + eb * (o.zt + o.z * fmaxf(tb, kLeast));
-  s.z = ea * s.z + eb * o.z;
-  s.m = m;
+  const bool first = s.m >= o.m;
+  const Soft a = first ? s : o, b = first ? o : s;   // the larger maximum's, the other's
+  const float t = b.m - a.m, e = expf(t), z = 1.f + b.more;
+  s.m = a.m;
+  s.more = fmaf(e, z, a.more);
+  s.zt = a.zt + e * (b.zt + z * fmaxf(t, kLeast));
 }
 
 // Orders by value, then by the lowest index; -0 counts as 0.
@@ -235,7 +251,7 @@ struct RowOut {
 
 // log p = (x - m) - log z: closer than x - lse where one entry takes nearly all.
 __device__ __forceinline__ float log_p(float x, const Soft& s, float lz) {
-  return s.z == 0.f ? -INFINITY : (x - s.m) - lz;
+  return s.none() ? -INFINITY : (x - s.m) - lz;
 }
 
 // One thread: the row's results from its sums, lz = log z.
@@ -246,14 +262,14 @@ __device__ __forceinline__ void finish_row(const Soft& s, const void* row, int64
   if (target >= V) lp = __uint_as_float(0x7fc00000u);
   else if (target >= 0) lp = log_p(value<DT>(((const typename Elem<DT>::T*)row)[target]), s, lz);
   o.logprob[t] = lp;
-  if (o.entropy) o.entropy[t] = s.z == 0.f ? 0.f : lz - s.zt / s.z;
-  if (o.lse) o.lse[t] = s.z == 0.f ? -INFINITY : s.m + lz;
+  if (o.entropy) o.entropy[t] = s.none() ? 0.f : lz - s.zt / (1.f + s.more);
+  if (o.lse) o.lse[t] = s.none() ? -INFINITY : s.m + lz;
 }
 __device__ __forceinline__ void store_top(const RowOut& o, size_t at, u64 key, const Soft& s,
                                           float lz) {
-  const bool bad = s.z != s.z;
+  const bool bad = s.broken();
   o.top_index[at] = bad ? -1 : (int32_t)key_index(key);
-  o.top_logprob[at] = bad ? s.z : log_p(key_value(key), s, lz);
+  o.top_logprob[at] = bad ? s.more : log_p(key_value(key), s, lz);
 }
 
 }  // namespace
@@ -310,16 +326,18 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
       const int v = v0 + 256 * i + lane;
       w[i] = v < nv ? vec[v] : minus_inf<DT>();
     }
-    float most = -INFINITY;
+    float all[U * VE];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       float x[VE];
       unpack<DT>(w[i], x);
-      most = fmaxf(most, add<DT>(s, x));
+#pragma unroll
+      for (int j = 0; j < VE; ++j) all[i * VE + j] = x[j];
     }
+    const float most = add<DT>(s, all);
     if constexpr (TOP) {
       // rounds 0, 2, 6, 14, ..: twice as many entries are in each time
-      if (((round + 1) & (round + 2)) == 0) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
+      if (((round + 1) & (round + 2)) == 0) list.raise(s.more > -1.f ? s.m : -INFINITY, lane);
       if (__ballot(most >= list.bound) == 0) continue;
       constexpr int Q = U * VE / 4;   // offers
 #pragma unroll 1
@@ -345,12 +363,12 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
       }
     }
   }
-  if constexpr (TOP) list.raise(s.z > 0.f ? s.m : -INFINITY, lane);
+  if constexpr (TOP) list.raise(s.more > -1.f ? s.m : -INFINITY, lane);
 #pragma unroll 1   // (short code: a work-group reads it anew)
   for (int off = 32; off >= 1; off >>= 1) {
     Soft o;
     o.m = __shfl_xor(s.m, off);
-    o.z = __shfl_xor(s.z, off);
+    o.more = __shfl_xor(s.more, off);
     o.zt = __shfl_xor(s.zt, off);
     join(s, o);
   }
@@ -365,13 +383,13 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   s = red[0];
 #pragma unroll
   for (int w = 1; w < 4; ++w) join(s, red[w]);
-  const float lz = logf(s.z);
+  const float lz = log1pf(s.more);
   if (splits == 1) {
     if (tid == 0) finish_row<DT>(s, row, targets[t], V, t, lz, out);
   } else if (tid == 0) {
     float* p = psum + 3 * (size_t)blockIdx.x;
     p[0] = s.m;
-    p[1] = s.z;
+    p[1] = s.more;
     p[2] = s.zt;
   }
   if constexpr (TOP) {
@@ -387,7 +405,7 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
         for (int j = 0; j < 8; ++j) place += keys[w * (TopList::kCap + 8) + i + j] > mine;
       }
     }
-    const bool bad = s.z != s.z;
+    const bool bad = s.broken();
     if (splits == 1) {
       if (bad) {
         if (tid < top) store_top(out, t * top + tid, 0, s, lz);
@@ -423,21 +441,21 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
   if (lane < splits) {
     const float* q = psum + 3 * (t * splits + lane);
     s.m = q[0];
-    s.z = q[1];
+    s.more = q[1];
     s.zt = q[2];
   }
 #pragma unroll 1   // (short code: a work-group reads it anew)
   for (int off = 32; off >= 1; off >>= 1) {
     Soft o;
     o.m = __shfl_xor(s.m, off);
-    o.z = __shfl_xor(s.z, off);
+    o.more = __shfl_xor(s.more, off);
     o.zt = __shfl_xor(s.zt, off);
     join(s, o);
   }
-  const float lz = logf(s.z);
+  const float lz = log1pf(s.more);
   if (tid == 0) finish_row<DT>(s, (const E*)logits + t * ld, targets[t], V, t, lz, out);
   __syncthreads();
-  if (s.z != s.z) {
+  if (s.broken()) {
     if (tid < top) store_top(out, t * top + tid, 0, s, lz);
     return;
   }
