@@ -503,13 +503,31 @@ jarq_status jarq_token_logprobs(int32_t dtype, const void* logits, int64_t ld, i
  * g = d_logprob[t] (0 without a target), h = d_entropy[t] (d_entropy nullable: 0, and
  * entropy is not read).  lse and entropy as the forward pass left them.  Rows of
  * nothing but -infinity get zeros.  d_logits has row stride ld_d and may be the logits
- * themselves (ld_d = ld).
+ * themselves (ld_d = ld).  lse alone, rounded, would leave log p off by half an ulp of
+ * lse, so each row's sums are formed again and its logits read twice; the calls below keep them.
  */
 jarq_status jarq_token_logprobs_backward(int32_t dtype, const void* logits, int64_t ld,
                                          int64_t tokens, int32_t vocab, const int64_t* targets,
                                          const float* lse, const float* entropy,
                                          const float* d_logprob, const float* d_entropy,
                                          void* d_logits, int64_t ld_d, void* stream);
+
+/*
+ * The same pair where the forward pass keeps what its gradient takes: lse_rest [tokens]
+ * (nullable in the forward pass) is what rounding left of lse, so that
+ * log p_v = (x_v - lse) - lse_rest to fp32's precision, and the logits are read once.
+ */
+jarq_status jarq_token_logprobs_keep(int32_t dtype, const void* logits, int64_t ld, int64_t tokens,
+                                     int32_t vocab, const int64_t* targets, int32_t top,
+                                     float* logprob, float* entropy, float* lse, float* lse_rest,
+                                     int32_t* top_index, float* top_logprob, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+jarq_status jarq_token_logprobs_keep_backward(int32_t dtype, const void* logits, int64_t ld,
+                                              int64_t tokens, int32_t vocab,
+                                              const int64_t* targets, const float* lse,
+                                              const float* lse_rest, const float* entropy,
+                                              const float* d_logprob, const float* d_entropy,
+                                              void* d_logits, int64_t ld_d, void* stream);
 
 /*
  * Measurement aid (not part of refinement): a kernel that moves a known

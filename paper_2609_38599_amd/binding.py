@@ -129,6 +129,10 @@ _SIGNATURES = {
                                            _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "jarq_token_logprobs_backward": (ctypes.c_int, [_i32, _vp, _i64, _i64, _i32, _vp, _vp, _vp,
                                                     _vp, _vp, _vp, _i64, _vp]),
+    "jarq_token_logprobs_keep": (ctypes.c_int, [_i32, _vp, _i64, _i64, _i32, _vp, _i32, _vp, _vp,
+                                                _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jarq_token_logprobs_keep_backward": (ctypes.c_int, [_i32, _vp, _i64, _i64, _i32, _vp, _vp,
+                                                         _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
     "jarq_lds_probe": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32, _vp, _vp]),
     "jarq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "jarq_abi_version": (ctypes.c_int32, []),
@@ -675,12 +679,21 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
     return out
 
 
-class TokenLogprobs(NamedTuple):
+class _TokenLogprobs(NamedTuple):
     logprob: torch.Tensor                  # [tokens] fp32
     entropy: torch.Tensor                  # [tokens] fp32
     lse: torch.Tensor                      # [tokens] fp32: log sum exp of the row
     top_index: Optional[torch.Tensor]      # [tokens, top] int32
     top_logprob: Optional[torch.Tensor]    # [tokens, top] fp32
+
+
+class TokenLogprobs(_TokenLogprobs):
+    """What token_logprobs returns; lse_rest [tokens] fp32 is what rounding left of lse.
+
+    A tuple made otherwise has no lse_rest: the backward pass then reads the logits twice.
+    """
+
+    lse_rest: Optional[torch.Tensor] = None
 
 
 def _logits(t, name):
@@ -707,21 +720,20 @@ def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprob
         raise JarqError(JARQ_EINVAL, "jarq_token_logprobs_workspace_bytes")
     dev = logits.device
     with _on(stream):
-        logprob, entropy, lse = torch.empty(3, T, dtype=torch.float32, device=dev).unbind(0)
+        logprob, entropy, lse, rest = torch.empty(4, T, dtype=torch.float32, device=dev).unbind(0)
         index = torch.empty(T, top, dtype=torch.int32, device=dev) if top else None
         value = torch.empty(T, top, dtype=torch.float32, device=dev) if top else None
         if ws is None:
             ws = _work(n, logits)
-    _check(lib.jarq_token_logprobs(_dtype(logits, "logits"), ctypes.c_void_p(logits.data_ptr()),
-                                   ld, T, V, _ptr(targets, torch.int64, "targets"), top,
-                                   _ptr(logprob, torch.float32, "logprob"),
-                                   _ptr(entropy, torch.float32, "entropy"),
-                                   _ptr(lse, torch.float32, "lse"),
-                                   _ptr(index, torch.int32, "top_index"),
-                                   _ptr(value, torch.float32, "top_logprob"),
-                                   _ptr(ws, torch.uint8, "workspace"), ws.numel(),
-                                   _queue(stream, logits)), "jarq_token_logprobs")
-    return TokenLogprobs(logprob, entropy, lse, index, value)
+    _check(lib.jarq_token_logprobs_keep(
+        _dtype(logits, "logits"), logits.data_ptr(), ld, T, V,
+        _ptr(targets, torch.int64, "targets"), top, logprob.data_ptr(), entropy.data_ptr(),
+        lse.data_ptr(), rest.data_ptr(), _ptr(index, torch.int32, "top_index"),
+        _ptr(value, torch.float32, "top_logprob"), _ptr(ws, torch.uint8, "workspace"), ws.numel(),
+        _queue(stream, logits)), "jarq_token_logprobs_keep")
+    result = TokenLogprobs(logprob, entropy, lse, index, value)
+    result.lse_rest = rest
+    return result
 
 
 def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, d_entropy=None,
@@ -729,8 +741,10 @@ def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, 
     """Gradient of the logits from those of the log probabilities and entropies [tokens]."""
     lib = load_library()
     T, V, ld = _logits(logits, "logits")
-    for t, name in ((targets, "targets"), (forward.lse, "lse"), (forward.entropy, "entropy"),
-                    (d_logprob, "d_logprob"), (d_entropy, "d_entropy")):
+    rest = forward.lse_rest
+    for t, name in ((targets, "targets"), (forward.lse, "lse"), (rest, "lse_rest"),
+                    (forward.entropy, "entropy"), (d_logprob, "d_logprob"),
+                    (d_entropy, "d_entropy")):
         if t is not None and t.shape != (T,):
             raise ValueError(f"{name} must be [tokens]")
     with _on(stream):
@@ -739,12 +753,18 @@ def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, 
     if out.shape != (T, V) or out.dtype != logits.dtype:
         raise ValueError("out must have the logits' shape and type")
     _, _, ld_d = _logits(out, "out")
-    _check(lib.jarq_token_logprobs_backward(
-        _dtype(logits, "logits"), ctypes.c_void_p(logits.data_ptr()), ld, T, V,
-        _ptr(targets, torch.int64, "targets"), _ptr(forward.lse, torch.float32, "lse"),
-        _ptr(forward.entropy, torch.float32, "entropy"),
-        _ptr(d_logprob, torch.float32, "d_logprob"), _ptr(d_entropy, torch.float32, "d_entropy"),
-        ctypes.c_void_p(out.data_ptr()), ld_d, _queue(stream, logits)), "jarq_token_logprobs_backward")
+    head = (_dtype(logits, "logits"), logits.data_ptr(), ld, T, V,
+            _ptr(targets, torch.int64, "targets"), _ptr(forward.lse, torch.float32, "lse"))
+    tail = (_ptr(forward.entropy, torch.float32, "entropy"),
+            _ptr(d_logprob, torch.float32, "d_logprob"),
+            _ptr(d_entropy, torch.float32, "d_entropy"), out.data_ptr(), ld_d,
+            _queue(stream, logits))
+    if rest is None:
+        _check(lib.jarq_token_logprobs_backward(*head, *tail), "jarq_token_logprobs_backward")
+    else:
+        _check(lib.jarq_token_logprobs_keep_backward(
+            *head, _ptr(rest, torch.float32, "lse_rest"), *tail),
+            "jarq_token_logprobs_keep_backward")
     return out
 
 

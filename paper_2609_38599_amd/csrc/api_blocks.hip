@@ -142,16 +142,17 @@ size_t jarq_token_logprobs_workspace_bytes(int64_t tokens, int32_t vocab, int32_
   return tokens == 0 ? 256 : pad256(logprob_workspace_bytes((int)tokens, vocab, top) + 1);
 }
 
-jarq_status jarq_token_logprobs(int32_t dtype, const void* logits, int64_t ld, int64_t tokens,
-                                int32_t vocab, const int64_t* targets, int32_t top, float* logprob,
-                                float* entropy, float* lse, int32_t* top_index, float* top_logprob,
-                                void* workspace, size_t workspace_bytes, void* stream) {
+jarq_status jarq_token_logprobs_keep(int32_t dtype, const void* logits, int64_t ld, int64_t tokens,
+                                     int32_t vocab, const int64_t* targets, int32_t top,
+                                     float* logprob, float* entropy, float* lse, float* lse_rest,
+                                     int32_t* top_index, float* top_logprob, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
   if (!valid_logits(dtype, logits, ld, tokens, vocab) || top < 0 || top > JARQ_MAX_TOP ||
       top > vocab)
     return JARQ_EINVAL;
   if (tokens == 0) return JARQ_OK;
   if (!aligned(targets, 8) || !aligned(logprob, 4) || (entropy != nullptr && !aligned(entropy, 4)) ||
-      (lse != nullptr && !aligned(lse, 4)) ||
+      (lse != nullptr && !aligned(lse, 4)) || (lse_rest != nullptr && !aligned(lse_rest, 4)) ||
       (top > 0 && (!aligned(top_index, 4) || !aligned(top_logprob, 4))))
     return JARQ_EINVAL;
   const jarq_status s = check(workspace, workspace_bytes,
@@ -159,14 +160,23 @@ jarq_status jarq_token_logprobs(int32_t dtype, const void* logits, int64_t ld, i
   if (s != JARQ_OK) return s;
   return status_of(launch_token_logprobs((hipStream_t)stream, dtype, logits, (size_t)ld,
                                          (int)tokens, vocab, targets, top, logprob, entropy, lse,
-                                         top_index, top_logprob, (char*)workspace));
+                                         lse_rest, top_index, top_logprob, (char*)workspace));
 }
 
-jarq_status jarq_token_logprobs_backward(int32_t dtype, const void* logits, int64_t ld,
-                                         int64_t tokens, int32_t vocab, const int64_t* targets,
-                                         const float* lse, const float* entropy,
-                                         const float* d_logprob, const float* d_entropy,
-                                         void* d_logits, int64_t ld_d, void* stream) {
+jarq_status jarq_token_logprobs(int32_t dtype, const void* logits, int64_t ld, int64_t tokens,
+                                int32_t vocab, const int64_t* targets, int32_t top, float* logprob,
+                                float* entropy, float* lse, int32_t* top_index, float* top_logprob,
+                                void* workspace, size_t workspace_bytes, void* stream) {
+  return jarq_token_logprobs_keep(dtype, logits, ld, tokens, vocab, targets, top, logprob, entropy,
+                                  lse, nullptr, top_index, top_logprob, workspace, workspace_bytes,
+                                  stream);
+}
+
+static jarq_status logprobs_backward(int32_t dtype, const void* logits, int64_t ld, int64_t tokens,
+                                     int32_t vocab, const int64_t* targets, const float* lse,
+                                     const float* lse_rest, const float* entropy,
+                                     const float* d_logprob, const float* d_entropy,
+                                     void* d_logits, int64_t ld_d, void* stream) {
   if (!valid_logits(dtype, logits, ld, tokens, vocab) ||
       !valid_logits(dtype, d_logits, ld_d, tokens, vocab))
     return JARQ_EINVAL;
@@ -174,9 +184,29 @@ jarq_status jarq_token_logprobs_backward(int32_t dtype, const void* logits, int6
   if (!aligned(targets, 8) || !aligned(lse, 4) || !aligned(d_logprob, 4) ||
       (d_entropy != nullptr && (!aligned(d_entropy, 4) || !aligned(entropy, 4))))
     return JARQ_EINVAL;
-  return status_of(launch_token_logprobs_backward((hipStream_t)stream, dtype, logits, (size_t)ld,
-                                                  (int)tokens, vocab, targets, lse, entropy,
-                                                  d_logprob, d_entropy, d_logits, (size_t)ld_d));
+  return status_of(launch_token_logprobs_backward(
+      (hipStream_t)stream, dtype, logits, (size_t)ld, (int)tokens, vocab, targets, lse, lse_rest,
+      entropy, d_logprob, d_entropy, d_logits, (size_t)ld_d));
+}
+
+jarq_status jarq_token_logprobs_backward(int32_t dtype, const void* logits, int64_t ld,
+                                         int64_t tokens, int32_t vocab, const int64_t* targets,
+                                         const float* lse, const float* entropy,
+                                         const float* d_logprob, const float* d_entropy,
+                                         void* d_logits, int64_t ld_d, void* stream) {
+  return logprobs_backward(dtype, logits, ld, tokens, vocab, targets, lse, nullptr, entropy,
+                           d_logprob, d_entropy, d_logits, ld_d, stream);
+}
+
+jarq_status jarq_token_logprobs_keep_backward(int32_t dtype, const void* logits, int64_t ld,
+                                              int64_t tokens, int32_t vocab,
+                                              const int64_t* targets, const float* lse,
+                                              const float* lse_rest, const float* entropy,
+                                              const float* d_logprob, const float* d_entropy,
+                                              void* d_logits, int64_t ld_d, void* stream) {
+  if (tokens > 0 && !aligned(lse_rest, 4)) return JARQ_EINVAL;
+  return logprobs_backward(dtype, logits, ld, tokens, vocab, targets, lse, lse_rest, entropy,
+                           d_logprob, d_entropy, d_logits, ld_d, stream);
 }
 
 }  // extern "C"

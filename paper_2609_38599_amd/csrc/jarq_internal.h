@@ -422,11 +422,13 @@ hipError_t launch_linear_i8(hipStream_t st, int dtype, int T, int N, int K, int 
 size_t logprob_workspace_bytes(int T, int V, int top);
 hipError_t launch_token_logprobs(hipStream_t st, int dtype, const void* logits, size_t ld, int T,
                                  int V, const int64_t* targets, int top, float* logprob,
-                                 float* entropy, float* lse, int32_t* top_index,
+                                 float* entropy, float* lse, float* rest, int32_t* top_index,
                                  float* top_logprob, char* ws);
+// rest null: the rows' sums are formed again, lse is not read
 hipError_t launch_token_logprobs_backward(hipStream_t st, int dtype, const void* logits, size_t ld,
                                           int T, int V, const int64_t* targets, const float* lse,
-                                          const float* entropy, const float* dlp,
-                                          const float* dent, void* dlogits, size_t ldd);
+                                          const float* rest, const float* entropy,
+                                          const float* dlp, const float* dent, void* dlogits,
+                                          size_t ldd);
 
 }  // namespace jarq

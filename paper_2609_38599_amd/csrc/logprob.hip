@@ -104,6 +104,24 @@ __device__ __forceinline__ void join(Soft& s, const Soft& o) {
   s.zt = a.zt + e * (b.zt + z * fmaxf(t, kLeast));
 }
 
+__device__ __forceinline__ void join_wave(Soft& s) {
+#pragma unroll 1   // (short code: a work-group reads it anew)
+  for (int off = 32; off >= 1; off >>= 1) {
+    Soft o;
+    o.m = __shfl_xor(s.m, off);
+    o.more = __shfl_xor(s.more, off);
+    o.zt = __shfl_xor(s.zt, off);
+    join(s, o);
+  }
+}
+// log sum exp, rounded, and what the rounding left: t = (x - lse) - rest is log p to an ulp
+// or two of itself (x - lse alone would be off by an ulp of lse).
+__device__ __forceinline__ void lse_parts(const Soft& s, float lz, float& lse, float& rest) {
+  lse = s.none() ? -INFINITY : s.m + lz;
+  const float d = lse - s.m;
+  rest = s.none() ? 0.f : (s.m - (lse - d)) + (lz - d);
+}
+
 // Orders by value, then by the lowest index; -0 counts as 0.
 __device__ __forceinline__ u64 top_key(float x, uint32_t index) {
   const uint32_t b = __float_as_uint(x + 0.f);
@@ -245,7 +263,7 @@ struct TopList {
 };
 
 struct RowOut {
-  float *logprob, *entropy, *lse, *top_logprob;
+  float *logprob, *entropy, *lse, *rest, *top_logprob;
   int32_t* top_index;
 };
 
@@ -263,7 +281,10 @@ __device__ __forceinline__ void finish_row(const Soft& s, const void* row, int64
   else if (target >= 0) lp = log_p(value<DT>(((const typename Elem<DT>::T*)row)[target]), s, lz);
   o.logprob[t] = lp;
   if (o.entropy) o.entropy[t] = s.none() ? 0.f : lz - s.zt / (1.f + s.more);
-  if (o.lse) o.lse[t] = s.none() ? -INFINITY : s.m + lz;
+  float lse, rest;
+  lse_parts(s, lz, lse, rest);
+  if (o.lse) o.lse[t] = lse;
+  if (o.rest) o.rest[t] = rest;
 }
 __device__ __forceinline__ void store_top(const RowOut& o, size_t at, u64 key, const Soft& s,
                                           float lz) {
@@ -364,14 +385,7 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
     }
   }
   if constexpr (TOP) list.raise(s.more > -1.f ? s.m : -INFINITY, lane);
-#pragma unroll 1   // (short code: a work-group reads it anew)
-  for (int off = 32; off >= 1; off >>= 1) {
-    Soft o;
-    o.m = __shfl_xor(s.m, off);
-    o.more = __shfl_xor(s.more, off);
-    o.zt = __shfl_xor(s.zt, off);
-    join(s, o);
-  }
+  join_wave(s);
   if (lane == 0) red[wave] = s;
   if constexpr (TOP) {
     list.sift(lane);
@@ -444,14 +458,7 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
     s.more = q[1];
     s.zt = q[2];
   }
-#pragma unroll 1   // (short code: a work-group reads it anew)
-  for (int off = 32; off >= 1; off >>= 1) {
-    Soft o;
-    o.m = __shfl_xor(s.m, off);
-    o.more = __shfl_xor(s.more, off);
-    o.zt = __shfl_xor(s.zt, off);
-    join(s, o);
-  }
+  join_wave(s);
   const float lz = log1pf(s.more);
   if (tid == 0) finish_row<DT>(s, (const E*)logits + t * ld, targets[t], V, t, lz, out);
   __syncthreads();
@@ -469,58 +476,102 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
 
 // ---- gradient ----
 // d x_v = g (onehot - p) - h p (log p + H), g and h the gradients of the log
-// probability and of the entropy.  Work-group `id`: part id % splits of a row.  A
-// thread reads each entry before it writes it: dlogits may be the logits.  Bound by
-// memory: 4096 x 128000 in bf16 410 us, 5.1 TB/s.
-template <int DT>
+// probability and of the entropy; at the target 1 - p from log p, which p's rounding would
+// lose where it is near 1.  Work-group `id`: part id % splits of a row.  A thread reads each
+// entry before it writes it: dlogits may be the logits.  SUMS: the row's sums are not given
+// and are formed first, by the one work-group that the row then has.  Bound by memory:
+// 4096 x 128000 in bf16 410 us, 5.1 TB/s.
+template <int DT, bool SUMS>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(
     const void* logits, size_t ld, int V, const int64_t* __restrict__ targets,
-    const float* __restrict__ lse_of, const float* __restrict__ entropy,
-    const float* __restrict__ dlp, const float* __restrict__ dent, int splits, int each,
-    void* dlogits, size_t ldd) {
+    const float* __restrict__ lse_of, const float* __restrict__ rest_of,
+    const float* __restrict__ entropy, const float* __restrict__ dlp,
+    const float* __restrict__ dent, int splits, int each, void* dlogits, size_t ldd) {
   typedef typename Elem<DT>::T E;
   constexpr int VE = Elem<DT>::kVec;
+  __shared__ Soft red[SUMS ? 4 : 1];
   const int tid = threadIdx.x;
   // the last rows first: what the forward pass read last may still be cached
   const size_t t = (gridDim.x - 1 - blockIdx.x) / (unsigned)splits;
   const int b = (int)(blockIdx.x % (unsigned)splits) * each, e = min(V, b + each);
   const E* row = (const E*)logits + t * ld;
   E* drow = (E*)dlogits + t * ldd;
-  const float lse = lse_of[t];
+  const uintptr_t ax = (uintptr_t)(row + b) % 16, ad = (uintptr_t)(drow + b) % 16;
+  const int head = min(e - b, (int)((16 - ax) % 16 / sizeof(E)));
+  const int nv = (e - b - head) / VE, rest = b + head + nv * VE;
+  const int own = tid < head ? b + tid : rest + tid - head;
+  const bool has = tid < head || own < e;
+  const u32x4* vec = (const u32x4*)(row + b + head);
+  float lse, left;
+  if constexpr (SUMS) {
+    Soft s = no_entries();
+    const float edge[1] = {has ? value<DT>(row[own]) : -INFINITY};
+    add<DT>(s, edge);
+    for (int v = tid; v < nv; v += 256) {
+      float x[VE];
+      unpack<DT>(vec[v], x);
+      add<DT>(s, x);
+    }
+    join_wave(s);
+    if ((tid & 63) == 0) red[tid >> 6] = s;
+    __syncthreads();   // (and every entry is read before the first is written)
+    s = red[0];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) join(s, red[w]);
+    lse_parts(s, log1pf(s.more), lse, left);
+  } else {
+    lse = lse_of[t];
+    left = rest_of[t];
+  }
   const int64_t target = targets[t];
+  const int at = target >= 0 && target < V ? (int)target : -1;
   const float g = target < 0 ? 0.f : target >= V ? __uint_as_float(0x7fc00000u) : dlp[t];
   const float h = dent ? dent[t] : 0.f;
   const float ent = dent ? entropy[t] : 0.f;
   const bool empty = lse == -INFINITY;   // nothing but -infinity: no gradient
-  auto grad = [&](float x, int64_t v) __attribute__((always_inline)) {
-    const float t = x - lse, p = exp_of<DT>(t);
-    const float c = p * (g + h * (fmaxf(t, kLeast) + ent));
-    return empty ? 0.f : (v == target ? g - c : -c);
+  auto grad = [&](float x) __attribute__((always_inline)) {
+    const float lp = (x - lse) - left;
+    const float c = exp_of<DT>(lp) * fmaf(h, fmaxf(lp, kLeast) + ent, g);
+    return empty ? 0.f : -c;
+  };
+  auto grad_at_target = [&](float x) __attribute__((always_inline)) {
+    const float lp = (x - lse) - left;
+    const float c = exp_of<DT>(lp) * h * (fmaxf(lp, kLeast) + ent);
+    return empty ? 0.f : fmaf(g, -expm1f(lp), -c);
   };
   auto word = [](float x) __attribute__((always_inline)) -> E {
     if constexpr (DT == 0) return x;
     else return to16<DT>(x);
   };
-  const uintptr_t ax = (uintptr_t)(row + b) % 16, ad = (uintptr_t)(drow + b) % 16;
+  auto put = [&](int v) __attribute__((always_inline)) {
+    const float x = value<DT>(row[v]);
+    drow[v] = word(v == at ? grad_at_target(x) : grad(x));
+  };
   if (ax != ad) {   // uniform
-    for (int v = b + tid; v < e; v += 256) drow[v] = word(grad(value<DT>(row[v]), v));
+    for (int v = b + tid; v < e; v += 256) put(v);
     return;
   }
-  const int head = min(e - b, (int)((16 - ax) % 16 / sizeof(E)));
-  const int nv = (e - b - head) / VE, rest = b + head + nv * VE;
-  const int own = tid < head ? b + tid : rest + tid - head;
-  if (tid < head || own < e) drow[own] = word(grad(value<DT>(row[own]), own));
-  const u32x4* vec = (const u32x4*)(row + b + head);
+  if (has) put(own);
   u32x4* dvec = (u32x4*)(drow + b + head);
   for (int v = tid; v < nv; v += 256) {
-    float x[VE];
+    float x[VE], y[VE];
     unpack<DT>(vec[v], x);
-    const int v0 = b + head + v * VE;
+    const int in = at - (b + head + v * VE);   // the target's place here
+#pragma unroll
+    for (int i = 0; i < VE; ++i) y[i] = grad(x[i]);
+    if ((unsigned)in < (unsigned)VE) {
+      float its = x[0];
+#pragma unroll
+      for (int i = 1; i < VE; ++i) its = in == i ? x[i] : its;
+      its = grad_at_target(its);
+#pragma unroll
+      for (int i = 0; i < VE; ++i) y[i] = in == i ? its : y[i];
+    }
     u32x4 w;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if constexpr (DT == 0) w[i] = __float_as_uint(grad(x[i], v0 + i));
-      else w[i] = pack16<DT>(grad(x[2 * i], v0 + 2 * i), grad(x[2 * i + 1], v0 + 2 * i + 1));
+      if constexpr (DT == 0) w[i] = __float_as_uint(y[i]);
+      else w[i] = pack16<DT>(y[2 * i], y[2 * i + 1]);
     }
     dvec[v] = w;
   }
@@ -569,12 +620,18 @@ hipError_t logprob_kind(hipStream_t st, const void* logits, size_t ld, int T, in
 
 template <int DT>
 hipError_t logprob_grad_kind(hipStream_t st, const void* logits, size_t ld, int T, int V,
-                             const int64_t* targets, const float* lse, const float* entropy,
-                             const float* dlp, const float* dent, void* dlogits, size_t ldd) {
-  const LogprobPlan p = logprob_plan(T, V, 0);
-  hipLaunchKernelGGL((logprob_grad_kernel<DT>), dim3((unsigned)(T * p.splits)), dim3(256), 0, st,
-                     logits, ld, V, targets, lse, entropy, dlp, dent, p.splits, p.each, dlogits,
-                     ldd);
+                             const int64_t* targets, const float* lse, const float* rest,
+                             const float* entropy, const float* dlp, const float* dent,
+                             void* dlogits, size_t ldd) {
+  if (rest) {
+    const LogprobPlan p = logprob_plan(T, V, 0);
+    hipLaunchKernelGGL((logprob_grad_kernel<DT, false>), dim3((unsigned)(T * p.splits)), dim3(256),
+                       0, st, logits, ld, V, targets, lse, rest, entropy, dlp, dent, p.splits,
+                       p.each, dlogits, ldd);
+  } else {
+    hipLaunchKernelGGL((logprob_grad_kernel<DT, true>), dim3((unsigned)T), dim3(256), 0, st, logits,
+                       ld, V, targets, lse, rest, entropy, dlp, dent, 1, V, dlogits, ldd);
+  }
   return hipGetLastError();
 }
 
@@ -587,9 +644,9 @@ size_t logprob_workspace_bytes(int T, int V, int top) {
 
 hipError_t launch_token_logprobs(hipStream_t st, int dtype, const void* logits, size_t ld, int T,
                                  int V, const int64_t* targets, int top, float* logprob,
-                                 float* entropy, float* lse, int32_t* top_index,
+                                 float* entropy, float* lse, float* rest, int32_t* top_index,
                                  float* top_logprob, char* ws) {
-  const RowOut out{logprob, entropy, lse, top_logprob, top_index};
+  const RowOut out{logprob, entropy, lse, rest, top_logprob, top_index};
   if (dtype == 0) return logprob_kind<0>(st, logits, ld, T, V, targets, top, out, ws);
   if (dtype == kF16) return logprob_kind<kF16>(st, logits, ld, T, V, targets, top, out, ws);
   return logprob_kind<kBF16>(st, logits, ld, T, V, targets, top, out, ws);
@@ -597,16 +654,17 @@ hipError_t launch_token_logprobs(hipStream_t st, int dtype, const void* logits, 
 
 hipError_t launch_token_logprobs_backward(hipStream_t st, int dtype, const void* logits, size_t ld,
                                           int T, int V, const int64_t* targets, const float* lse,
-                                          const float* entropy, const float* dlp,
-                                          const float* dent, void* dlogits, size_t ldd) {
+                                          const float* rest, const float* entropy,
+                                          const float* dlp, const float* dent, void* dlogits,
+                                          size_t ldd) {
   if (dtype == 0)
-    return logprob_grad_kind<0>(st, logits, ld, T, V, targets, lse, entropy, dlp, dent, dlogits,
-                                ldd);
+    return logprob_grad_kind<0>(st, logits, ld, T, V, targets, lse, rest, entropy, dlp, dent,
+                                dlogits, ldd);
   if (dtype == kF16)
-    return logprob_grad_kind<kF16>(st, logits, ld, T, V, targets, lse, entropy, dlp, dent, dlogits,
-                                   ldd);
-  return logprob_grad_kind<kBF16>(st, logits, ld, T, V, targets, lse, entropy, dlp, dent, dlogits,
-                                  ldd);
+    return logprob_grad_kind<kF16>(st, logits, ld, T, V, targets, lse, rest, entropy, dlp, dent,
+                                   dlogits, ldd);
+  return logprob_grad_kind<kBF16>(st, logits, ld, T, V, targets, lse, rest, entropy, dlp, dent,
+                                  dlogits, ldd);
 }
 
 }  // namespace jarq

@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from paper_2609_38599_amd import binding as jb
+from tests import test_gpu_blocks as blocks_tests
 from tests._gpu_common import say
 
 pytestmark = [pytest.mark.gpu,
@@ -66,3 +67,91 @@ def test_logprob_of_a_leading_token(T, V, dt, lead):
         want = torch.log1p(s) - sd / (1 + s)
         off = (r.entropy.cpu().double() - want).abs() / want
         assert float(off.max()) <= 2 * _sums(V) + 8 * E
+
+
+# half a unit in the last place, and half the smallest subnormal (fp32: normal)
+ROUND = {torch.float32: (2.0 ** -24, 2.0 ** -126), torch.float16: (2.0 ** -11, 2.0 ** -25),
+         torch.bfloat16: (2.0 ** -8, 2.0 ** -126)}
+
+
+def _check_leading_gradient(x, t, r, gl, ge):
+    V, dt = x.shape[1], x.dtype
+    rows = torch.arange(len(t))
+    d, s, sd = _others(x, t)
+    g, h = gl.double(), ge.double()
+    # log p + H at the target is -sd / (1 + s): nothing cancels
+    lp, ent = -torch.log1p(s), torch.log1p(s) - sd / (1 + s)
+    z, u, tiny = _sums(V), *ROUND[dt]
+    at = g * s / (1 + s) + h * sd / (1 + s) ** 2
+    at_err = g.abs() * s / (1 + s) * (z + 8 * E) + \
+        h.abs() / (1 + s) * (lp.abs() + ent) * (2 * z + 16 * E)
+    logp = d + lp[:, None]
+    p = torch.exp(logp)
+    far = torch.where(p > 0, logp.abs(), 0.0)
+    want = -p * (g[:, None] + h[:, None] * (torch.where(p > 0, logp, 0.0) + ent[:, None]))
+    err = p * (g.abs()[:, None] + h.abs()[:, None] * (far + ent[:, None] + 1)) * \
+        (2 * z + 16 * E + 8 * E * far)
+    want[rows, t], err[rows, t] = at, at_err
+    bound = err + u * (want.abs() + err) + tiny
+    xc, tc, glc, gec = x.cuda(), t.cuda(), gl.cuda(), ge.cuda()
+    # with what the forward pass kept, without it, and in place
+    rebuilt = jb.TokenLogprobs(*r)
+    for form in (r, rebuilt):
+        got = jb.token_logprobs_backward(xc, tc, form, glc, gec)
+        over = ((got.double().cpu() - want).abs() - bound).max()
+        assert float(over) <= 0, (form is r, float(over))
+        y = xc.clone()
+        assert torch.equal(jb.token_logprobs_backward(y, tc, form, glc, gec, out=y), got)
+
+
+@pytest.mark.parametrize("lead", [8.0, 18.0, 22.0, 25.0])
+@pytest.mark.parametrize("T,V,dt", LEADS)
+def test_logit_gradient_of_a_leading_token(T, V, dt, lead):
+    # g (1 - p) at the target: off by what 1 - p is, wherever the logits lie
+    for offset in (0.0, 100.0, 1e4) if dt == torch.float32 else (0.0, 100.0):
+        say(f"[gradient lead] tokens {T} vocab {V} {dt} lead {lead} offset {offset}")
+        x, t = _leading(T, V, dt, lead, offset)
+        _check_leading_gradient(x, t, jb.token_logprobs(x.cuda(), t.cuda()),
+                                _randn(1, T), _randn(2, T))
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,V", [(3, 37), (2, 40001), (700, 1003)])
+def test_logit_gradient_of_rows_of_the_lowest_value(T, V, dt):
+    # every entry masked by the type's lowest value: p = 1 / V
+    say(f"[gradient lowest] tokens {T} vocab {V} {dt}")
+    x = torch.full((T, V), torch.finfo(dt).min, dtype=dt)
+    t = torch.arange(T) % V
+    _check_leading_gradient(x, t, jb.token_logprobs(x.cuda(), t.cuda()), _randn(1, T), _randn(2, T))
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("V", [37, 5000, 40001])
+def test_logit_gradient_without_the_kept_sums(V, dt, monkeypatch):
+    # the backward pass that forms the rows' sums itself, on masked and broken rows
+    kept = jb.token_logprobs_backward
+    forms = []
+
+    def both(x, t, r, gl, ge):
+        forms.append(jb.TokenLogprobs(*r))
+        assert r.lse_rest is not None and forms[-1].lse_rest is None
+        return kept(x, t, forms[-1], gl, ge)
+
+    monkeypatch.setattr(jb, "token_logprobs_backward", both)
+    blocks_tests.test_logprobs_of_masked_and_broken_rows(V, dt)
+    assert len(forms) == 1
+
+
+@pytest.mark.parametrize("V,ld,first", [(1000, 1003, 0), (1001, 1001, 1), (7, 9, 2)])
+def test_logit_gradient_of_unaligned_rows_without_the_kept_sums(V, ld, first):
+    T = 9
+    base = _randn(5, T * ld + 8).bfloat16().cuda()
+    x = base[first:first + T * ld].view(T, ld)[:, :V]
+    t, gl, ge = torch.arange(T).cuda() % V, _randn(1, T).cuda(), _randn(2, T).cuda()
+    r = jb.TokenLogprobs(*jb.token_logprobs(x, t))
+    d = jb.token_logprobs_backward(x, t, r, gl, ge)
+    blocks_tests._check_grad(x, t, gl, ge, d)
+    out = torch.full_like(base, 7.0)
+    rows = out[first:first + T * ld].view(T, ld)
+    jb.token_logprobs_backward(x, t, r, gl, ge, out=rows[:, :V])
+    assert torch.equal(rows[:, :V], d) and bool((rows[:, V:] == 7.0).all())
