@@ -17,9 +17,28 @@ namespace jarq {
 
 namespace {
 
-constexpr float kInvSqrt2 = 0.70710678118654752f;
 constexpr float kInvSqrt2Pi = 0.39894228040143268f;
 constexpr float kSqrt2OverPi = 0.79788456080286536f;
+
+// The normal distribution function of a, e = exp(-a^2 / 2).  Phi(-u) = e v r(v) for u >= 0,
+// v = 1 / (1 + 0.36 u): r is the polynomial of degree 8 of the least largest relative error
+// on 0 <= u <= 40 (9e-8; 4e-7 in fp32 for u < 1, then what e is off by).  The tail stays
+// right to itself where (1 + erf) / 2 cancels (4 % off at -5), and takes less than erfc: 611 x
+// 1000 -> 2752 20 us, 22.
+__device__ __forceinline__ float normal_cdf(float a, float e) {
+  const float v = __builtin_amdgcn_rcpf(fmaf(0.36f, fabsf(a), 1.f));
+  float r = -0.030238334f;
+  r = fmaf(r, v, 0.13950869f);
+  r = fmaf(r, v, -0.22360012f);
+  r = fmaf(r, v, 0.10736972f);
+  r = fmaf(r, v, -0.00038668368f);
+  r = fmaf(r, v, 0.096037455f);
+  r = fmaf(r, v, 0.12400974f);
+  r = fmaf(r, v, 0.14368188f);
+  r = fmaf(r, v, 0.14361766f);
+  const float tail = e * v * r;
+  return a < 0.f ? tail : 1.f - tail;
+}
 
 // act(a), and act'(a) where `d` is given
 template <int ACT>
@@ -29,8 +48,8 @@ __device__ __forceinline__ float activation(float a, float* d) {
     if (d) *d = sig * (1.f + a * (1.f - sig));
     return a * sig;
   } else if constexpr (ACT == 1) {   // gelu
-    const float cdf = 0.5f * (1.f + erff(a * kInvSqrt2));
-    if (d) *d = cdf + a * kInvSqrt2Pi * __expf(-0.5f * a * a);
+    const float e = __expf(-0.5f * a * a), cdf = normal_cdf(a, e);
+    if (d) *d = cdf + a * kInvSqrt2Pi * e;
     return a * cdf;
   } else {                           // gelu, tanh form: (1 + tanh z) / 2 = 1 / (1 + exp(-2 z))
     const float aa = fminf(a * a, 1e30f);   // (0 times it stays 0)

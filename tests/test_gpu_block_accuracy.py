@@ -2,7 +2,8 @@
 tails and cancellations, against float64 with bounds relative to the small result itself.
 E = 2^-24 is half a unit in the last place of fp32."""
 
-import numpy as np
+import math
+
 import pytest
 import torch
 
@@ -155,3 +156,43 @@ def test_logit_gradient_of_unaligned_rows_without_the_kept_sums(V, ld, first):
     rows = out[first:first + T * ld].view(T, ld)
     jb.token_logprobs_backward(x, t, r, gl, ge, out=rows[:, :V])
     assert torch.equal(rows[:, :V], d) and bool((rows[:, V:] == 7.0).all())
+
+
+# ---- activations in their left tail ----
+
+def _activation64(a, act):
+    """(act(a), act'(a)) of one float64 below 0, without 1 + erf or 1 + tanh."""
+    if act == "silu":
+        sig, w = 1 / (1 + math.exp(-a)), 1.0
+    elif act == "gelu":
+        cdf = 0.5 * math.erfc(-a / math.sqrt(2))
+        return a * cdf, cdf + a * math.exp(-a * a / 2) / math.sqrt(2 * math.pi)
+    else:
+        c = math.sqrt(2 / math.pi)
+        sig = 1 / (1 + math.exp(-2 * c * (a + 0.044715 * a ** 3)))
+        w = 2 * c * (1 + 3 * 0.044715 * a * a)
+    return a * sig, sig * (1 + a * (1 - sig) * w)
+
+
+@pytest.mark.parametrize("dt", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("act", sorted(jb.ACTIVATIONS))
+@pytest.mark.parametrize("T", [13, 29, 200])
+def test_gated_block_in_the_left_tail(T, act, dt):
+    say(f"[gated tail] tokens {T} {act} {dt}")
+    x, wg, wu = torch.zeros(T, 8), torch.zeros(8, 8), torch.zeros(8, 8)
+    # a is the token's first value and b is 1, exactly; dx is (act'(a), act(a)) of channel 0
+    x[:, 0], x[:, 1], wg[0, 0], wu[0, 1] = torch.linspace(-9, -3, T), 1.0, 1.0, 1.0
+    x, wg, wu = x.to(dt), wg.to(dt).cuda(), wu.to(dt).cuda()
+    y, pre = jb.gated_forward(x.cuda(), wg, wu, act=act, save=True)
+    dy = torch.zeros_like(y)
+    dy[:, 0] = 1
+    dx, _, _ = jb.gated_backward(x.cuda(), wg, wu, dy, pre, act=act)
+    u, tiny = ROUND[dt]
+    for t in range(T):
+        a = float(x[t, 0])
+        h, slope = _activation64(a, act)
+        # erfc's and exp's arguments are of order a^2 and rounded a few times, their sums of
+        # one sign or no more than halved by the other
+        rel = (64 + 12 * a * a) * E
+        for got, want, r in ((y[t, 0], h, rel), (dx[t, 1], h, rel), (dx[t, 0], slope, 2 * rel)):
+            assert abs(float(got) - want) <= abs(want) * (r + u * (1 + r)) + tiny, (a, act)
