@@ -19,8 +19,17 @@ namespace {
 
 typedef unsigned long long u64;
 
-template <int DT> struct Elem { typedef uint16_t T; static constexpr int kVec = 8; };
-template <> struct Elem<0> { typedef float T; static constexpr int kVec = 4; };
+// Any: sixteen bytes at any element.
+template <int DT> struct Elem {
+  typedef uint16_t T;
+  static constexpr int kVec = 8;
+  typedef u32x4 Any __attribute__((aligned(2)));
+};
+template <> struct Elem<0> {
+  typedef float T;
+  static constexpr int kVec = 4;
+  typedef u32x4 Any __attribute__((aligned(4)));
+};
 
 template <int DT>
 __device__ __forceinline__ float value(typename Elem<DT>::T w) {
@@ -63,23 +72,36 @@ __device__ __forceinline__ Soft no_entries() { return Soft{-FLT_MAX, -1.f, 0.f};
 // Keeps exp's argument within range for the weighted sum: exp is 0 there.
 constexpr float kLeast = -1000.f;
 
-// Adds entries; returns the largest.
+// A lane's sums under its wave's running maximum.  One entry of the maximum's value, of lane
+// `holder` (-1: none yet), is in no sum.  (A maximum a lane would grow in nearly every round
+// of some lane, and each time all would rescale.)
+struct LaneSums {
+  float m, more, zt;
+  int holder;
+};
+__device__ __forceinline__ LaneSums no_sums() { return LaneSums{-FLT_MAX, 0.f, 0.f, -1}; }
+
+// Adds entries; returns the lane's largest.  Every lane of the wave calls it.
 template <int DT, int N>
-__device__ __forceinline__ float add(Soft& s, const float (&entries)[N]) {
+__device__ __forceinline__ float add(LaneSums& s, const float (&entries)[N], int lane) {
   float x[N], most = entries[0];
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     x[i] = entries[i];
     most = fmaxf(most, x[i]);
   }
-  const float m = fmaxf(s.m, most);
-  if (m > s.m) {
-    const float t = s.m - m, e = exp_of<DT>(t), z = 1.f + s.more;
+  if (__ballot(most > s.m) != 0) {   // uniform
+    float m = fmaxf(most, s.m);
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+    m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m)));
+    const float t = s.m - m, e = exp_of<DT>(t), z = s.more + (lane == s.holder ? 1.f : 0.f);
     s.zt = e * (s.zt + z * fmaxf(t, kLeast));
     s.more = e * z;
     s.m = m;
-    // the maximum's own 1 stays out of the sum (+infinity stays in: it gives a NaN)
-    bool out = m == INFINITY;
+    // (+infinity stays in the sum: it gives a NaN)
+    s.holder = m == INFINITY ? -1 : (int)__builtin_ctzll(__ballot(most == m));
+    bool out = lane != s.holder;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const bool own = !out && x[i] == m;
@@ -89,11 +111,21 @@ __device__ __forceinline__ float add(Soft& s, const float (&entries)[N]) {
   }
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float t = x[i] - m, e = exp_of<DT>(t);
+    const float t = x[i] - s.m, e = exp_of<DT>(t);
     s.more += e;
     s.zt = fmaf(e, fmaxf(t, kLeast), s.zt);
   }
   return most;
+}
+// The wave's sums, in every lane.
+__device__ __forceinline__ Soft sums_of(const LaneSums& s) {
+  float more = s.more, zt = s.zt;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) {
+    more += __shfl_xor(more, off);
+    zt += __shfl_xor(zt, off);
+  }
+  return Soft{s.m, s.holder < 0 ? more - 1.f : more, zt};
 }
 __device__ __forceinline__ void join(Soft& s, const Soft& o) {
   const bool first = s.m >= o.m;
@@ -299,12 +331,13 @@ __device__ __forceinline__ void store_top(const RowOut& o, size_t at, u64 key, c
 // part it finishes the row; otherwise its sums and top keys go to the workspace.  Bound by
 // reading the logits (4096 x 128000 in bf16, no top: 235 us, 4.5 TB/s), with a top by the
 // issue of its candidates' votes (2047 x 32001 in fp32: 50 us without, top 20 74 us).
+// Eight waves a SIMD, which keeps the registers at 64: with 70 the top 5 of 2047 x 50257 in
+// fp16 take 73 us, 69 so.
 template <int DT, bool TOP>
-__global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ logits, size_t ld,
-                                                      int V, const int64_t* __restrict__ targets,
-                                                      int splits, int each, int top, RowOut out,
-                                                      float* __restrict__ psum,
-                                                      u64* __restrict__ pkey) {
+__global__ __launch_bounds__(256) JARQ_WAVES(8) void logprob_kernel(
+    const void* __restrict__ logits, size_t ld, int V, const int64_t* __restrict__ targets,
+    int splits, int each, int top, RowOut out, float* __restrict__ psum,
+    u64* __restrict__ pkey) {
   typedef typename Elem<DT>::T E;
   constexpr int VE = Elem<DT>::kVec;
   __shared__ Soft red[4];
@@ -323,18 +356,15 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
   const u32x4* vec = (const u32x4*)(row + b + head);
   const int own = tid < head ? b + tid : rest + tid - head;   // this thread's scalar, if any
   const bool has = tid < head || own < e;
-  Soft s = no_entries();
+  LaneSums sums = no_sums();
   TopList list;
   const float edge = has ? value<DT>(row[own]) : -INFINITY;
+  float lane_max = edge;
   if constexpr (TOP) {
     list.init(keys + wave * (TopList::kCap + 8), slots, top, wave);
     if (tid < 4) slots[tid] = kOrderedMinusInf;
     __syncthreads();
     list.keep(has, edge, own, lane);
-  }
-  {
-    const float x[1] = {edge};
-    add<DT>(s, x);
   }
   // U vectors a lane in flight (every lane of a wave stays in the loop, for the list's
   // votes; lanes past the end take -infinity, which adds nothing)
@@ -347,18 +377,17 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
       const int v = v0 + 256 * i + lane;
       w[i] = v < nv ? vec[v] : minus_inf<DT>();
     }
-    float all[U * VE];
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
       float x[VE];
       unpack<DT>(w[i], x);
-#pragma unroll
-      for (int j = 0; j < VE; ++j) all[i * VE + j] = x[j];
+      most = fmaxf(most, add<DT>(sums, x, lane));
     }
-    const float most = add<DT>(s, all);
+    lane_max = fmaxf(lane_max, most);
     if constexpr (TOP) {
       // rounds 0, 2, 6, 14, ..: twice as many entries are in each time
-      if (((round + 1) & (round + 2)) == 0) list.raise(s.more > -1.f ? s.m : -INFINITY, lane);
+      if (((round + 1) & (round + 2)) == 0) list.raise(lane_max, lane);
       if (__ballot(most >= list.bound) == 0) continue;
       constexpr int Q = U * VE / 4;   // offers
 #pragma unroll 1
@@ -384,8 +413,12 @@ __global__ __launch_bounds__(256) void logprob_kernel(const void* __restrict__ l
       }
     }
   }
-  if constexpr (TOP) list.raise(s.more > -1.f ? s.m : -INFINITY, lane);
-  join_wave(s);
+  {
+    const float x[1] = {edge};
+    add<DT>(sums, x, lane);
+  }
+  if constexpr (TOP) list.raise(lane_max, lane);
+  Soft s = sums_of(sums);
   if (lane == 0) red[wave] = s;
   if constexpr (TOP) {
     list.sift(lane);
@@ -504,16 +537,20 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(
   const u32x4* vec = (const u32x4*)(row + b + head);
   float lse, left;
   if constexpr (SUMS) {
-    Soft s = no_entries();
-    const float edge[1] = {has ? value<DT>(row[own]) : -INFINITY};
-    add<DT>(s, edge);
-    for (int v = tid; v < nv; v += 256) {
+    // (by the entries' indices alone, as in the forward pass)
+    LaneSums sums = no_sums();
+    const int n = V / VE, last = n * VE + tid, lane = tid & 63;
+    for (int v0 = tid - lane; v0 < n; v0 += 256) {   // every lane of a wave
+      const u32x4 w = v0 + lane < n ? ((const typename Elem<DT>::Any*)row)[v0 + lane]
+                                    : minus_inf<DT>();
       float x[VE];
-      unpack<DT>(vec[v], x);
-      add<DT>(s, x);
+      unpack<DT>(w, x);
+      add<DT>(sums, x, lane);
     }
-    join_wave(s);
-    if ((tid & 63) == 0) red[tid >> 6] = s;
+    const float edge[1] = {last < V ? value<DT>(row[last]) : -INFINITY};
+    add<DT>(sums, edge, lane);
+    Soft s = sums_of(sums);
+    if (lane == 0) red[tid >> 6] = s;
     __syncthreads();   // (and every entry is read before the first is written)
     s = red[0];
 #pragma unroll
