@@ -220,7 +220,7 @@ struct TopList {
     bound = fmaxf(bound, key_value((u64)least << 32));
     __syncthreads();   // (before the next one's slots)
   }
-  // Entries at the row's edges, of the lanes that have one: kept without a look.
+  // Entries at the row's end, of the lanes that have one: kept without a look.
   __device__ __forceinline__ void keep(bool has, float x, int i, int lane) {
     const u64 mask = __ballot(has);
     if (has) keys[__popcll(mask & ((1ull << lane) - 1))] = top_key(x, (uint32_t)i);
@@ -350,12 +350,13 @@ __global__ __launch_bounds__(256) JARQ_WAVES(8) void logprob_kernel(
   const int part = blockIdx.x % (unsigned)splits;
   const E* row = (const E*)logits + t * ld;
   const int b = part * each, e = min(V, b + each);
-  // scalars up to the first 16-byte boundary, vectors, scalars
-  const int head = min(e - b, (int)((16 - (uintptr_t)(row + b) % 16) % 16 / sizeof(E)));
-  const int nv = (e - b - head) / VE, rest = b + head + nv * VE;
-  const u32x4* vec = (const u32x4*)(row + b + head);
-  const int own = tid < head ? b + tid : rest + tid - head;   // this thread's scalar, if any
-  const bool has = tid < head || own < e;
+  // Vectors from the part's first entry on, wherever that lies, then scalars: what a lane sums
+  // goes by the entries' indices alone, so a row's results do not depend on its address.
+  // (rows of 32001 in fp32, most off 16 bytes, and from a 16-byte boundary on: the same time)
+  const int nv = (e - b) / VE;
+  const typename Elem<DT>::Any* vec = (const typename Elem<DT>::Any*)(row + b);
+  const int own = b + nv * VE + tid;   // this thread's scalar, if any
+  const bool has = own < e;
   LaneSums sums = no_sums();
   TopList list;
   const float edge = has ? value<DT>(row[own]) : -INFINITY;
@@ -396,7 +397,7 @@ __global__ __launch_bounds__(256) JARQ_WAVES(8) void logprob_kernel(
         float x[VE];
         unpack<DT>(w[0], x);
         const float y[4] = {x[0], x[1], x[2], x[3]};
-        list.offer(y, v < nv, b + head + v * VE + i * 4 % VE, lane);
+        list.offer(y, v < nv, b + v * VE + i * 4 % VE, lane);
         // (the others move up: a register array takes no index)
         if constexpr (VE == 4) {
           w[0] = w[1];

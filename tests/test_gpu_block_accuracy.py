@@ -196,3 +196,25 @@ def test_gated_block_in_the_left_tail(T, act, dt):
         rel = (64 + 12 * a * a) * E
         for got, want, r in ((y[t, 0], h, rel), (dx[t, 1], h, rel), (dx[t, 0], slope, 2 * rel)):
             assert abs(float(got) - want) <= abs(want) * (r + u * (1 + r)) + tiny, (a, act)
+
+
+# ---- the same row elsewhere ----
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("T,V,top", [(9, 4097, 5), (5, 32001, 20), (2, 128001, 8), (9, 7, 0),
+                                     (600, 1001, 3)])
+def test_logprobs_do_not_depend_on_stride_or_alignment(T, V, top, dt):
+    say(f"[logprob placed] tokens {T} vocab {V} top {top} {dt}")
+    base = _randn(T + V, T, V, std=2.0).to(dt).cuda()
+    t, gl, ge = torch.arange(T).cuda() % V, _randn(1, T).cuda(), _randn(2, T).cuda()
+    want = None
+    for ld, first in ((V, 0), (V + 1, 0), (V + 2, 1), (V + 3, 3), (V + 8 - V % 8, 0), (V, 5)):
+        room = torch.zeros(T * ld + 16, dtype=dt, device="cuda")
+        x = room[first:first + T * ld].view(T, ld)[:, :V]
+        x.copy_(base)
+        r = jb.token_logprobs(x, t, top=top)
+        got = [v for v in (*r, r.lse_rest) if v is not None]
+        for form in (r, jb.TokenLogprobs(*r)):
+            got.append(jb.token_logprobs_backward(x, t, form, gl, ge))
+        want = want or got
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), (ld, first)
