@@ -72,6 +72,9 @@ __device__ __forceinline__ Soft no_entries() { return Soft{-FLT_MAX, -1.f, 0.f};
 // Keeps exp's argument within range for the weighted sum: exp is 0 there.
 constexpr float kLeast = -1000.f;
 
+__device__ __forceinline__ float first_lane(float x) {
+  return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x)));
+}
 // A lane's sums under its wave's running maximum.  One entry of the maximum's value, of lane
 // `holder` (-1: none yet), is in no sum.  (A maximum a lane would grow in nearly every round
 // of some lane, and each time all would rescale.)
@@ -94,7 +97,7 @@ __device__ __forceinline__ float add(LaneSums& s, const float (&entries)[N], int
     float m = fmaxf(most, s.m);
 #pragma unroll
     for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
-    m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m)));
+    m = first_lane(m);
     const float t = s.m - m, e = exp_of<DT>(t), z = s.more + (lane == s.holder ? 1.f : 0.f);
     s.zt = e * (s.zt + z * fmaxf(t, kLeast));
     s.more = e * z;
@@ -493,6 +496,10 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
     s.zt = q[2];
   }
   join_wave(s);
+  // one lane's: where parts tie for the maximum, lanes add their sums in different orders
+  s.m = first_lane(s.m);
+  s.more = first_lane(s.more);
+  s.zt = first_lane(s.zt);
   const float lz = log1pf(s.more);
   if (tid == 0) finish_row<DT>(s, (const E*)logits + t * ld, targets[t], V, t, lz, out);
   __syncthreads();

@@ -218,3 +218,19 @@ def test_logprobs_do_not_depend_on_stride_or_alignment(T, V, top, dt):
             got.append(jb.token_logprobs_backward(x, t, form, gl, ge))
         want = want or got
         assert all(torch.equal(a, b) for a, b in zip(got, want)), (ld, first)
+
+
+@pytest.mark.parametrize("ties", [2, 3, 5])
+@pytest.mark.parametrize("T,V", [(1, 128000), (8, 65536), (40, 50257), (600, 1001)])
+def test_logprob_of_an_alternative_is_its_top_logprob(T, V, ties):
+    # a row cut into parts, some of which hold its maximum: every lane has the same sums
+    say(f"[logprob top] tokens {T} vocab {V} ties {ties}")
+    x = _randn(V + ties, T, V, std=2.0)
+    for k in range(ties):
+        x[:, (2 * k + 1) * V // (2 * ties)] = 14.0
+    x, top = x.cuda(), 7
+    first = jb.token_logprobs(x, torch.zeros(T, dtype=torch.int64).cuda(), top=top)
+    for k in range(top):
+        r = jb.token_logprobs(x, first.top_index[:, k].long(), top=top)
+        assert torch.equal(r.top_logprob, first.top_logprob)
+        assert torch.equal(r.logprob, r.top_logprob[:, k])
