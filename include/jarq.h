@@ -30,6 +30,8 @@
  *     device memory and keeps no global state.
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *     All device work is enqueued on it in order.
+ *   - Work runs on the current device (hipSetDevice): pointers and `stream` are
+ *     that device's.
  *   - W, H, scales and codes must be 16-byte aligned,
  *     the workspace 256-byte aligned.
  *   - Argument errors return JARQ_EINVAL before anything is enqueued; the

@@ -509,13 +509,47 @@ def _on(stream):
     return _INLINE if stream is None else torch.cuda.stream(stream)
 
 
-def _queue(stream, t):
-    """The handle of `stream`, by default the current one of t's device.
+def _device(t, name):
+    """The device of a call, t's.  It has to be the current one, where kernels are launched."""
+    at = t.get_device()
+    if at < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    if at != torch._C._cuda_getDevice():
+        raise ValueError(f"{name} is on cuda:{at}, but cuda:{torch._C._cuda_getDevice()} is the "
+                         "current device (torch.cuda.set_device or torch.cuda.device changes it)")
+    return at
+
+
+def _at(t, dtype, name, device):
+    """The address of a dense tensor on the call's device, None without one."""
+    if t is None:
+        return None
+    try:
+        if t.dtype == dtype and t.get_device() == device and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{name} must be a torch.Tensor") from None
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on cuda:{device}, got {t.device}")
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _own(t):
+    """The address of a tensor that the call made itself, None without one."""
+    return None if t is None else t.data_ptr()
+
+
+def _queue(stream, device):
+    """The handle of `stream`, by default the current one of the call's device.
 
     (The raw handle: a Stream object of the current stream takes 2.7 us to make.)
     """
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(t.device.index)
+        return torch._C._cuda_getCurrentRawStream(device)
+    if stream.device_index != device:
+        raise ValueError(f"stream must be of cuda:{device}, got cuda:{stream.device_index}")
     return stream.cuda_stream
 
 
@@ -551,6 +585,7 @@ def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
     lib = load_library()
     T, d = _rows(X, "X")
     f, _ = _rows(Wg, "Wg", d)
+    at = _device(X, "X")
     if _rows(Wu, "Wu", d)[0] != f:
         raise ValueError("Wg and Wu must have the same shape")
     pre = None
@@ -562,9 +597,10 @@ def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
         if save:
             pre = torch.empty(2, T, f, dtype=torch.float32, device=X.device)
     dt = X.dtype
-    _check(lib.jarq_gated_forward(_dtype(X, "X"), _act(act), T, d, f, _ptr(X, dt, "X"),
-                                  _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(out, dt, "out"),
-                                  _ptr(pre, torch.float32, "pre"), _queue(stream, X)),
+    _check(lib.jarq_gated_forward(_dtype(X, "X"), _act(act), T, d, f, _at(X, dt, "X", at),
+                                  _at(Wg, dt, "Wg", at), _at(Wu, dt, "Wu", at),
+                                  _at(out, dt, "out", at), _own(pre),
+                                  _queue(stream, at)),
            "jarq_gated_forward")
     return (out, pre) if save else out
 
@@ -578,6 +614,7 @@ def gated_backward(X, Wg, Wu, dY, pre, act="silu", need=(True, True, True), ws=N
     lib = load_library()
     T, d = _rows(X, "X")
     f, _ = _rows(Wg, "Wg", d)
+    at = _device(X, "X")
     if _rows(Wu, "Wu", d)[0] != f or _rows(dY, "dY", f)[0] != T or pre.shape != (2, T, f):
         raise ValueError("Wg and Wu must be [f, d], dY [tokens, f] and pre [2, tokens, f]")
     n = int(lib.jarq_gated_workspace_bytes(T, d, f))
@@ -589,12 +626,12 @@ def gated_backward(X, Wg, Wu, dY, pre, act="silu", need=(True, True, True), ws=N
                         for t, wanted in zip((X, Wg, Wu), need))
         if ws is None:
             ws = _work(n, X)
-    _check(lib.jarq_gated_backward(_dtype(X, "X"), _act(act), T, d, f, _ptr(X, dt, "X"),
-                                   _ptr(Wg, dt, "Wg"), _ptr(Wu, dt, "Wu"), _ptr(dY, dt, "dY"),
-                                   _ptr(pre, torch.float32, "pre"), _ptr(dX, dt, "dX"),
-                                   _ptr(dWg, dt, "dWg"), _ptr(dWu, dt, "dWu"),
-                                   _ptr(ws, torch.uint8, "workspace"), ws.numel(),
-                                   _queue(stream, X)), "jarq_gated_backward")
+    _check(lib.jarq_gated_backward(_dtype(X, "X"), _act(act), T, d, f, _at(X, dt, "X", at),
+                                   _at(Wg, dt, "Wg", at), _at(Wu, dt, "Wu", at),
+                                   _at(dY, dt, "dY", at), _at(pre, torch.float32, "pre", at),
+                                   _own(dX), _own(dWg), _own(dWu),
+                                   _at(ws, torch.uint8, "workspace", at), ws.numel(),
+                                   _queue(stream, at)), "jarq_gated_backward")
     return dX, dWg, dWu
 
 
@@ -602,6 +639,7 @@ def quant_rows_i8(X, out=None, scale=None, stream=None):
     """(Q int8, scale fp32 [rows, 1]): the rows of X on 8 bits with a scale each."""
     lib = load_library()
     rows, cols = _rows(X, "X")
+    at = _device(X, "X")
     with _on(stream):
         if out is None:
             out = torch.empty(rows, cols, dtype=torch.int8, device=X.device)
@@ -609,22 +647,25 @@ def quant_rows_i8(X, out=None, scale=None, stream=None):
             scale = torch.empty(rows, 1, dtype=torch.float32, device=X.device)
     if out.shape != (rows, cols) or scale.numel() != rows:
         raise ValueError("out must be [rows, cols] and scale hold one value a row")
-    _check(lib.jarq_quant_rows_i8(_dtype(X, "X"), _ptr(X, X.dtype, "X"), rows, cols,
-                                  _ptr(out, torch.int8, "out"), _ptr(scale, torch.float32, "scale"),
-                                  _queue(stream, X)), "jarq_quant_rows_i8")
+    _check(lib.jarq_quant_rows_i8(_dtype(X, "X"), _at(X, X.dtype, "X", at), rows, cols,
+                                  _at(out, torch.int8, "out", at),
+                                  _at(scale, torch.float32, "scale", at), _queue(stream, at)),
+           "jarq_quant_rows_i8")
     return out, scale
 
 
 def codes_i8(p: Params, codes, zeros, out=None, stream=None):
     """q - z as int8: a quantized layer's weights for matmul_i8 and linear_i8."""
     lib = load_library()
+    at = _device(codes, "codes")
     with _on(stream):
         if out is None:
             out = torch.empty(p.rows, p.cols, dtype=torch.int8, device=codes.device)
         flag = torch.empty(1, dtype=torch.int32, device=codes.device)
-    _check(lib.jarq_codes_i8(ctypes.byref(p), _ptr(codes, torch.uint8, "codes"),
-                             _ptr(zeros, torch.int32, "zeros"), _ptr(out, torch.int8, "out"),
-                             _ptr(flag, torch.int32, "flag"), _queue(stream, codes)), "jarq_codes_i8")
+    _check(lib.jarq_codes_i8(ctypes.byref(p), _at(codes, torch.uint8, "codes", at),
+                             _at(zeros, torch.int32, "zeros", at), _at(out, torch.int8, "out", at),
+                             _own(flag), _queue(stream, at)),
+           "jarq_codes_i8")
     return out
 
 
@@ -642,6 +683,7 @@ def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
     lib = load_library()
     T, k = _rows(Xq, "Xq")
     n, group = _i8_layer(Wq, sw, k)
+    at = _device(Xq, "Xq")
     if sx.numel() != T:
         raise ValueError("sx must hold one scale a token")
     with _on(stream):
@@ -649,10 +691,10 @@ def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
             out = torch.empty(T, n, dtype=dtype, device=Xq.device)
         elif out.shape != (T, n):
             raise ValueError("out must be [tokens, n]")
-    _check(lib.jarq_matmul_i8(_dtype(out, "out"), T, n, k, group, _ptr(Xq, torch.int8, "Xq"),
-                              _ptr(sx, torch.float32, "sx"), _ptr(Wq, torch.int8, "Wq"),
-                              _ptr(sw, torch.float32, "sw"), _ptr(out, out.dtype, "out"),
-                              _queue(stream, Xq)), "jarq_matmul_i8")
+    _check(lib.jarq_matmul_i8(_dtype(out, "out"), T, n, k, group, _at(Xq, torch.int8, "Xq", at),
+                              _at(sx, torch.float32, "sx", at), _at(Wq, torch.int8, "Wq", at),
+                              _at(sw, torch.float32, "sw", at), _at(out, out.dtype, "out", at),
+                              _queue(stream, at)), "jarq_matmul_i8")
     return out
 
 
@@ -661,6 +703,7 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
     lib = load_library()
     T, k = _rows(X, "X")
     n, group = _i8_layer(Wq, sw, k)
+    at = _device(X, "X")
     need = int(lib.jarq_linear_i8_workspace_bytes(T, k))
     if need == 0:
         raise JarqError(JARQ_EINVAL, "jarq_linear_i8_workspace_bytes")
@@ -672,10 +715,10 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
             raise ValueError("out must be [tokens, n]")
         if ws is None:
             ws = _work(need, X)
-    _check(lib.jarq_linear_i8(_dtype(X, "X"), T, n, k, group, _ptr(X, dt, "X"),
-                              _ptr(Wq, torch.int8, "Wq"), _ptr(sw, torch.float32, "sw"),
-                              _ptr(out, dt, "out"), _ptr(ws, torch.uint8, "workspace"), ws.numel(),
-                              _queue(stream, X)), "jarq_linear_i8")
+    _check(lib.jarq_linear_i8(_dtype(X, "X"), T, n, k, group, _at(X, dt, "X", at),
+                              _at(Wq, torch.int8, "Wq", at), _at(sw, torch.float32, "sw", at),
+                              _at(out, dt, "out", at), _at(ws, torch.uint8, "workspace", at),
+                              ws.numel(), _queue(stream, at)), "jarq_linear_i8")
     return out
 
 
@@ -699,8 +742,6 @@ class TokenLogprobs(_TokenLogprobs):
 def _logits(t, name):
     """(tokens, vocab, row stride) of logits whose rows are dense."""
     T, V = _rows(t, name)
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
     if V > 1 and t.stride(1) != 1:
         raise ValueError(f"{name} must have dense rows")
     ld = t.stride(0) if T > 1 else V
@@ -713,6 +754,7 @@ def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprob
     """Log probabilities of targets [tokens] int64 (< 0: none), entropies, top alternatives."""
     lib = load_library()
     T, V, ld = _logits(logits, "logits")
+    at = _device(logits, "logits")
     if targets.shape != (T,):
         raise ValueError("targets must be [tokens]")
     n = int(lib.jarq_token_logprobs_workspace_bytes(T, V, top))
@@ -727,10 +769,10 @@ def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprob
             ws = _work(n, logits)
     _check(lib.jarq_token_logprobs_keep(
         _dtype(logits, "logits"), logits.data_ptr(), ld, T, V,
-        _ptr(targets, torch.int64, "targets"), top, logprob.data_ptr(), entropy.data_ptr(),
-        lse.data_ptr(), rest.data_ptr(), _ptr(index, torch.int32, "top_index"),
-        _ptr(value, torch.float32, "top_logprob"), _ptr(ws, torch.uint8, "workspace"), ws.numel(),
-        _queue(stream, logits)), "jarq_token_logprobs_keep")
+        _at(targets, torch.int64, "targets", at), top, logprob.data_ptr(), entropy.data_ptr(),
+        lse.data_ptr(), rest.data_ptr(), _own(index), _own(value),
+        _at(ws, torch.uint8, "workspace", at), ws.numel(), _queue(stream, at)),
+        "jarq_token_logprobs_keep")
     result = TokenLogprobs(logprob, entropy, lse, index, value)
     result.lse_rest = rest
     return result
@@ -741,29 +783,34 @@ def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, 
     """Gradient of the logits from those of the log probabilities and entropies [tokens]."""
     lib = load_library()
     T, V, ld = _logits(logits, "logits")
+    at = _device(logits, "logits")
     rest = forward.lse_rest
     for t, name in ((targets, "targets"), (forward.lse, "lse"), (rest, "lse_rest"),
                     (forward.entropy, "entropy"), (d_logprob, "d_logprob"),
                     (d_entropy, "d_entropy")):
         if t is not None and t.shape != (T,):
             raise ValueError(f"{name} must be [tokens]")
-    with _on(stream):
-        if out is None:
+    if out is None:
+        with _on(stream):
             out = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
-    if out.shape != (T, V) or out.dtype != logits.dtype:
-        raise ValueError("out must have the logits' shape and type")
-    _, _, ld_d = _logits(out, "out")
+        ld_d = V
+    else:
+        if out.shape != (T, V) or out.dtype != logits.dtype:
+            raise ValueError("out must have the logits' shape and type")
+        if out.get_device() != at:
+            raise ValueError(f"out must be on cuda:{at}, got {out.device}")
+        _, _, ld_d = _logits(out, "out")
     head = (_dtype(logits, "logits"), logits.data_ptr(), ld, T, V,
-            _ptr(targets, torch.int64, "targets"), _ptr(forward.lse, torch.float32, "lse"))
-    tail = (_ptr(forward.entropy, torch.float32, "entropy"),
-            _ptr(d_logprob, torch.float32, "d_logprob"),
-            _ptr(d_entropy, torch.float32, "d_entropy"), out.data_ptr(), ld_d,
-            _queue(stream, logits))
+            _at(targets, torch.int64, "targets", at), _at(forward.lse, torch.float32, "lse", at))
+    tail = (_at(forward.entropy, torch.float32, "entropy", at),
+            _at(d_logprob, torch.float32, "d_logprob", at),
+            _at(d_entropy, torch.float32, "d_entropy", at), out.data_ptr(), ld_d,
+            _queue(stream, at))
     if rest is None:
         _check(lib.jarq_token_logprobs_backward(*head, *tail), "jarq_token_logprobs_backward")
     else:
         _check(lib.jarq_token_logprobs_keep_backward(
-            *head, _ptr(rest, torch.float32, "lse_rest"), *tail),
+            *head, _at(rest, torch.float32, "lse_rest", at), *tail),
             "jarq_token_logprobs_keep_backward")
     return out
 
