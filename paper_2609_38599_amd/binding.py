@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
+import warnings
 from typing import NamedTuple, Optional
 
 import torch
@@ -559,6 +560,13 @@ def _work(n, like):
     return ws if ws.data_ptr() % 256 == 0 else _scratch(n, like.device)
 
 
+def _outside(call, gradient):
+    """Says that the result of an input that requires a gradient is none of autograd's."""
+    if torch.is_grad_enabled():
+        warnings.warn(f"{call}: the result is outside autograd's graph; {gradient} "
+                      "(this is not said under torch.no_grad())", stacklevel=3)
+
+
 def _rows(t, name, cols=None):
     if not isinstance(t, torch.Tensor) or t.dim() != 2 or (cols is not None and t.shape[1] != cols):
         raise ValueError(f"{name} must be [rows, {'cols' if cols is None else cols}]")
@@ -580,7 +588,8 @@ def _dtype(t, name):
 def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
     """act(X Wg^T) * (X Wu^T) for X [tokens, d], Wg and Wu [f, d] in 16 bits.
 
-    With save, returns (Y, pre): pre [2, tokens, f] fp32 is for gated_backward.
+    With save, returns (Y, pre): pre [2, tokens, f] fp32 is for gated_backward, which gives the
+    gradients; autograd records none.
     """
     lib = load_library()
     T, d = _rows(X, "X")
@@ -589,6 +598,8 @@ def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
     if _rows(Wu, "Wu", d)[0] != f:
         raise ValueError("Wg and Wu must have the same shape")
     pre = None
+    if not save and (X.requires_grad or Wg.requires_grad or Wu.requires_grad):
+        _outside("gated_forward", "gated_backward gives its gradients, from save=True")
     with _on(stream):
         if out is None:
             out = torch.empty(T, f, dtype=X.dtype, device=X.device)
@@ -679,13 +690,15 @@ def _i8_layer(Wq, sw, k):
 
 
 def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
-    """sx (Xq Wq^T under the scales sw [n, 1] or [n, k / group]) as `dtype`."""
+    """sx (Xq Wq^T under the scales sw [n, 1] or [n, k / group]) as `dtype`.  Has no gradient."""
     lib = load_library()
     T, k = _rows(Xq, "Xq")
     n, group = _i8_layer(Wq, sw, k)
     at = _device(Xq, "Xq")
     if sx.numel() != T:
         raise ValueError("sx must hold one scale a token")
+    if sx.requires_grad or sw.requires_grad:
+        _outside("matmul_i8", "it has no gradient")
     with _on(stream):
         if out is None:
             out = torch.empty(T, n, dtype=dtype, device=Xq.device)
@@ -699,7 +712,10 @@ def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
 
 
 def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
-    """X [tokens, k] through the 8-bit layer (Wq [n, k], sw [n, 1] or [n, k / group])."""
+    """X [tokens, k] through the 8-bit layer (Wq [n, k], sw [n, 1] or [n, k / group]).
+
+    Has no gradient.
+    """
     lib = load_library()
     T, k = _rows(X, "X")
     n, group = _i8_layer(Wq, sw, k)
@@ -707,6 +723,8 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
     need = int(lib.jarq_linear_i8_workspace_bytes(T, k))
     if need == 0:
         raise JarqError(JARQ_EINVAL, "jarq_linear_i8_workspace_bytes")
+    if X.requires_grad or sw.requires_grad:
+        _outside("linear_i8", "it has no gradient")
     dt = X.dtype
     with _on(stream):
         if out is None:
@@ -751,7 +769,10 @@ def _logits(t, name):
 
 
 def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprobs:
-    """Log probabilities of targets [tokens] int64 (< 0: none), entropies, top alternatives."""
+    """Log probabilities of targets [tokens] int64 (< 0: none), entropies, top alternatives.
+
+    token_logprobs_backward gives the logits' gradient; autograd records none.
+    """
     lib = load_library()
     T, V, ld = _logits(logits, "logits")
     at = _device(logits, "logits")
@@ -760,6 +781,8 @@ def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprob
     n = int(lib.jarq_token_logprobs_workspace_bytes(T, V, top))
     if n == 0:
         raise JarqError(JARQ_EINVAL, "jarq_token_logprobs_workspace_bytes")
+    if logits.requires_grad:
+        _outside("token_logprobs", "token_logprobs_backward gives the logits' gradient")
     dev = logits.device
     with _on(stream):
         logprob, entropy, lse, rest = torch.empty(4, T, dtype=torch.float32, device=dev).unbind(0)

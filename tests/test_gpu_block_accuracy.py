@@ -3,6 +3,7 @@ tails and cancellations, against float64 with bounds relative to the small resul
 E = 2^-24 is half a unit in the last place of fp32."""
 
 import math
+import warnings
 
 import pytest
 import torch
@@ -234,3 +235,27 @@ def test_logprob_of_an_alternative_is_its_top_logprob(T, V, ties):
         r = jb.token_logprobs(x, first.top_index[:, k].long(), top=top)
         assert torch.equal(r.top_logprob, first.top_logprob)
         assert torch.equal(r.logprob, r.top_logprob[:, k])
+
+
+# ---- inputs that require gradients ----
+
+def test_results_outside_the_graph_are_said_to_be():
+    x, w = _randn(1, 4, 64).bfloat16().cuda(), _randn(2, 8, 64).bfloat16().cuda()
+    wq, sw = torch.ones(8, 64, dtype=torch.int8).cuda(), torch.ones(8, 1).cuda()
+    t = torch.zeros(4, dtype=torch.int64).cuda()
+    calls = {"gated_backward": lambda x: jb.gated_forward(x, w, w),
+             "linear_i8: .* no gradient": lambda x: jb.linear_i8(x, wq, sw),
+             "token_logprobs_backward": lambda x: jb.token_logprobs(x, t)}
+    for said, call in calls.items():
+        with pytest.warns(UserWarning, match=said):
+            call(x.clone().requires_grad_())
+    with pytest.warns(UserWarning, match="matmul_i8: .* no gradient"):
+        jb.matmul_i8(wq, sw, wq, sw.clone().requires_grad_())
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        for call in calls.values():
+            call(x)
+            with torch.no_grad():
+                call(x.clone().requires_grad_())
+        # its gradients are asked for
+        jb.gated_forward(x.clone().requires_grad_(), w, w, save=True)
