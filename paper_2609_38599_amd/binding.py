@@ -673,6 +673,9 @@ def codes_i8(p: Params, codes, zeros, out=None, stream=None):
         if out is None:
             out = torch.empty(p.rows, p.cols, dtype=torch.int8, device=codes.device)
         flag = torch.empty(1, dtype=torch.int32, device=codes.device)
+    n = p.rows * p.cols
+    if codes.numel() != n or out.numel() != n or zeros.numel() * p.group_size != n:
+        raise ValueError("codes and out must be [rows, cols], zeros [rows, cols / group_size]")
     _check(lib.jarq_codes_i8(ctypes.byref(p), _at(codes, torch.uint8, "codes", at),
                              _at(zeros, torch.int32, "zeros", at), _at(out, torch.int8, "out", at),
                              _own(flag), _queue(stream, at)),

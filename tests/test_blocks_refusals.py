@@ -112,3 +112,15 @@ def test_streams_of_another_gpu_are_refused(name, monkeypatch):
     call, tensors = next(c[1:] for c in _calls() if c[0] == name)
     with pytest.raises(ValueError, match="stream must be of cuda:0"):
         call(**tensors, stream=Stream())
+
+
+@pytest.mark.parametrize("name,shape,dtype", [("codes", (7, 64), torch.uint8),
+                                              ("zeros", (7, 1), torch.int32),
+                                              ("zeros", (8, 2), torch.int32),
+                                              ("out", (8, 63), torch.int8)])
+def test_codes_of_another_size_are_refused(name, shape, dtype, monkeypatch):
+    # the kernel's grid comes from the parameters: a smaller array would be overrun
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    call, tensors = next(c[1:] for c in _calls() if c[0] == "codes_i8")
+    with pytest.raises(ValueError, match="rows, cols"):
+        call(**{**tensors, name: _placed(0, *shape, dtype=dtype)})
