@@ -259,3 +259,74 @@ def test_results_outside_the_graph_are_said_to_be():
                 call(x.clone().requires_grad_())
         # its gradients are asked for
         jb.gated_forward(x.clone().requires_grad_(), w, w, save=True)
+
+
+# ---- every entry of every shape of tile ----
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T,d,f", [(40, 264, 1000), (70, 136, 4096), (100, 1000, 2752),
+                                   (250, 72, 11008), (400, 4096, 1000), (700, 264, 6000),
+                                   (3300, 520, 2048), (2100, 8, 2104), (129, 4104, 520),
+                                   (3600, 3592, 1800)])
+def test_gated_tiles_entry_by_entry(T, d, f, dt):
+    # the bounds of the small sizes' test, in float64 on the GPU: sums of n products are off by
+    # (n + 2) e of the sum of magnitudes, and 1.13 bounds |act'| and |act''|
+    say(f"[gated entries] tokens {T} d {d} f {f} {dt}")
+    x, wg, wu, dy = blocks_tests._gated_inputs(T, d, f, dt, seed=T)
+    y, pre = jb.gated_forward(x, wg, wu, save=True)
+    dx, dwg, dwu = jb.gated_backward(x, wg, wu, dy, pre)
+    X, G, U, D = (t.double() for t in (x, wg, wu, dy))
+    u, tiny = ROUND[dt]
+
+    def check(what, got, want, err, rounded=True):
+        bound = err + u * (want.abs() + err) + tiny if rounded else err
+        over = float(((got.double() - want).abs() - bound).max())
+        assert over <= 0, (what, over)
+
+    a, b = X @ G.T, X @ U.T
+    ea, eb = ((d + 2) * E * (X.abs() @ W.abs().T) for W in (G, U))
+    check("a", pre[0], a, ea, False)
+    check("b", pre[1], b, eb, False)
+    sig = 1 / (1 + torch.exp(-a))
+    h, slope, fn = a * sig, sig * (1 + a * (1 - sig)), 64 * E * (a.abs() + 1)
+    act = 1.13 * ea + fn
+    check("y", y, h * b, b.abs() * act + h.abs() * eb + 2 * ea * eb)
+    da, db = D * b * slope, D * h
+    eda = D.abs() * (b.abs() * act + (slope.abs() + fn) * eb + 2 * ea * eb)
+    edb = D.abs() * act
+    eda, edb = (e + u * (m.abs() + e) + tiny + 4 * E * m.abs() for e, m in ((eda, da), (edb, db)))
+    err, sums = eda @ G.abs() + edb @ U.abs(), da.abs() @ G.abs() + db.abs() @ U.abs()
+    check("dx", dx, da @ G + db @ U, err + (2 * f + 2) * E * (sums + err))
+    for what, got, m, e in (("dwg", dwg, da, eda), ("dwu", dwu, db, edb)):
+        err, sums = e.T @ X.abs(), m.abs().T @ X.abs()
+        check(what, got, m.T @ X, err + (T + 2) * E * (sums + err))
+
+
+@pytest.mark.parametrize("g", [0, 32, 64, 128])
+@pytest.mark.parametrize("T,n,k", [(40, 1000, 512), (40, 4096, 384), (50, 10000, 1152),
+                                   (150, 4000, 384), (400, 4000, 1152), (1000, 4100, 384),
+                                   (3000, 4100, 384), (66, 700, 2688), (130, 17, 896),
+                                   (3000, 4097, 384), (1993, 6966, 128), (260, 4096, 1024)])
+def test_matmul_i8_tiles_entry_by_entry(T, n, k, g):
+    say(f"[i8 entries] tokens {T} n {n} k {k} group {g}")
+    gen = torch.Generator(device="cuda").manual_seed(T + k)
+    xq, wq = (torch.randint(-128, 128, (m, k), generator=gen, device="cuda", dtype=torch.int8)
+              for m in (T, n))
+    G = k // g if g else 1
+    sx = torch.rand(T, generator=gen, device="cuda")
+    sw = torch.randn(n, G, generator=gen, device="cuda")
+    want = torch.zeros(T, n, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(want)
+    for i in range(G):
+        cut = slice(i * (k // G), (i + 1) * (k // G))
+        part = (xq[:, cut].double() @ wq[:, cut].double().T) * sw[:, i].double()
+        want += part
+        size += part.abs()
+    want, size = want * sx.double()[:, None], size * sx.double()[:, None]
+    for dt in (torch.float32, torch.float16, torch.bfloat16):
+        scale = 1.0 if dt != torch.float16 else 2.0 ** -8      # within its range
+        y = jb.matmul_i8(xq, sx * scale, wq, sw, dtype=dt)
+        u, tiny = ROUND[dt]
+        err = (G + 4) * E * size * scale
+        over = (y.double() - want * scale).abs() - err - u * ((want * scale).abs() + err) - tiny
+        assert float(over.max()) <= 0, (dt, float(over.max()))
