@@ -418,7 +418,8 @@ jarq_status jarq_gated_forward(int32_t dtype, int32_t act, int64_t tokens, int32
  * Gradients of that block for dY [tokens][f], from pre as the forward pass left
  * it: dX [tokens][d], dWg and dWu [f][d], of the block's dtype, each nullable (not
  * formed) and overwritten.  The gradients of X Wg^T and X Wu^T are rounded to
- * dtype before their products.  The workspace (256-byte aligned,
+ * dtype before their products (in float16 what passes 65504 becomes an infinity, as in any
+ * gradient of that type: scale the loss).  The workspace (256-byte aligned,
  * jarq_gated_workspace_bytes bytes; 0 if the sizes are invalid) is used only
  * during the call.
  */

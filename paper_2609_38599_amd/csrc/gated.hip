@@ -71,8 +71,9 @@ __device__ __forceinline__ float activation(int act, float a, float* d) {   // a
 // ---- forward, many tokens ----
 // WI x WJ wavefronts, each BI blocks of 16 P rows (half Wg's, half Wu's) x BJ blocks
 // of 16 tokens.  Bound by the matrix cores at the clock that the card's power allows:
-// 4096 tokens, 4096 -> 14336 in bf16 785 us, 1.23 PFLOP/s; with a and b stored as well
-// 4096 -> 11008 750 us.  53 tokens, 4096 -> 14336: 50 us, 4.7 TB/s of weights.
+// 4096 tokens, 4096 -> 14336 in bf16 780 us, 1.23 PFLOP/s; with a and b stored as well
+// 4096 -> 11008 690 us, as long as 12288 channels: five rounds of 256 tiles and a third of a
+// sixth.  53 tokens, 4096 -> 14336: 224 work-groups, 54 us, 4.4 TB/s of weights.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
@@ -144,7 +145,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_tile_kernel(
 
 // ---- forward, few tokens ----
 // A work-group: 16 channels of both projections x up to 16 IB tokens, eight wavefronts
-// along k.  One token, 4096 -> 11008: 34 us, 5.2 TB/s of weights (32 channels: 45 us).
+// along k.  One token, 4096 -> 11008: 35 us, 5.2 TB/s of weights (32 channels: 45 us).
 template <int KIND, int IB>
 __global__ __launch_bounds__(512) void gated_skinny_kernel(
     const void* __restrict__ X, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
@@ -247,7 +248,7 @@ hipError_t launch_gated_forward(hipStream_t st, int dtype, int act, int T, int D
 
 // ---- backward: da, db ----
 // dab [T][2 F]: da in columns 0..F-1, db behind.  Eight entries a thread.  Bound by
-// memory, 14 bytes an entry: 4096 x 11008 125 us, 5.0 TB/s.  (Formed inside the two products
+// memory, 14 bytes an entry: 4096 x 11008 127 us, 5.0 TB/s.  (Formed inside the two products
 // each entry's would be computed D / 256 + 2 F / 256 times.)
 template <int KIND>
 __global__ __launch_bounds__(256) void gated_grad_kernel(const float* __restrict__ pre,
@@ -313,7 +314,8 @@ __device__ __forceinline__ void store_tile16(const f32x4 (&acc)[BI][BJ], char* s
 // ---- backward: dx = dab [Wg; Wu] ----
 // part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.  Wg and Wu
 // are read as they lie (k down the rows) through the transposing LDS read.  Bound by the
-// matrix cores: 4096 tokens, 4096 channels, F = 11008 590 us, 1.25 PFLOP/s.
+// matrix cores: 4096 tokens, 4096 channels, F = 11008 550 us, 1.35 PFLOP/s: one round of 256
+// tiles.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_dx_kernel(
     const void* __restrict__ dab, const void* __restrict__ Wg, const void* __restrict__ Wu, int T,
@@ -377,7 +379,8 @@ __global__ __launch_bounds__(256) void gated_dx_sum_kernel(const float* __restri
 
 // ---- backward: [dWg; dWu] = dab^T x ----
 // Both operands have k (the tokens) down their rows.  Bound by the matrix cores: 4096
-// tokens, 4096 channels, F = 11008 630 us, 1.17 PFLOP/s (twice the transposing reads of dx).
+// tokens, 4096 channels, F = 11008 580 us, 1.27 PFLOP/s.  What it lacks to dx is its last
+// round of tiles, a third full: F = 12288, six whole rounds, 618 us, dx 629.
 template <int KIND, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void gated_dw_kernel(
     const void* __restrict__ dab, const void* __restrict__ X, int T, int D, int F,

@@ -186,10 +186,10 @@ __device__ __forceinline__ void store_y(void* Y, int dtype, size_t at, float y) 
 }  // namespace
 
 // Many tokens.  GROUP 0: one scale a channel, int32 sums over all of k, bound by the
-// matrix cores at the clock that the card's power allows (8192 x 14336 -> 4096 390 us, 2.5
-// POP/s).  Otherwise a group's int32 sums go to fp32: converting one and adding it takes two
-// vector instructions, eight to a matrix instruction of half their time, beside LDS reads of
-// as much (2048 x 11008 -> 4096, groups of 64, 160 us, 1.15 POP/s).
+// matrix cores at the clock that the card's power allows (8192 x 14336 -> 4096 375 to 400 us,
+// 2.4 POP/s and more).  Otherwise a group's int32 sums go to fp32: converting one and adding
+// it takes two vector instructions, eight to a matrix instruction of half their time, beside
+// LDS reads of as much (2048 x 11008 -> 4096, groups of 64, 163 to 178 us, 1.0 to 1.1 POP/s).
 template <int GROUP, int S, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(GROUP && WI * WJ == 8 ? 4 : 2) void i8_tile_kernel(
     const int8_t* __restrict__ Xq, const float* __restrict__ sx, const int8_t* __restrict__ Wq,

@@ -2,8 +2,8 @@
 // logits, and the gradient of the logits.
 //
 // With m = max x, z = sum exp(x - m): lse = m + log z, log p_v = x_v - lse and
-// H = log z - sum exp(x - m) (x - m) / z, all from one pass that keeps (m, z - 1, sum
-// exp(x - m) (x - m)) per lane and rescales when m grows.  (z - 1, the sum beside the
+// H = log z - sum exp(x - m) (x - m) / z, all from one pass that keeps m per wavefront and
+// (z - 1, sum exp(x - m) (x - m)) per lane and rescales when m grows.  (z - 1, the sum beside the
 // maximum's own 1: where one entry takes nearly all, z would round away what the others
 // take, which is the log probability of that entry.)
 //
@@ -332,8 +332,8 @@ __device__ __forceinline__ void store_top(const RowOut& o, size_t at, u64 key, c
 
 // Work-group `id`: part id % splits (of `each` entries) of row id / splits.  With one
 // part it finishes the row; otherwise its sums and top keys go to the workspace.  Bound by
-// reading the logits (4096 x 128000 in bf16, no top: 235 us, 4.5 TB/s), with a top by the
-// issue of its candidates' votes (2047 x 32001 in fp32: 50 us without, top 20 74 us).
+// reading the logits (4096 x 128000 in bf16, no top: 230 us, 4.6 TB/s), with a top by the
+// issue of its candidates' votes (2047 x 32001 in fp32: 53 us without, top 20 66 us).
 // Eight waves a SIMD, which keeps the registers at 64: with 70 the top 5 of 2047 x 50257 in
 // fp16 take 73 us, 69 so.
 template <int DT, bool TOP>
@@ -473,7 +473,7 @@ __global__ __launch_bounds__(256) JARQ_WAVES(8) void logprob_kernel(
 
 // A work-group a row: its parts' sums (at most 64 parts, joined in a fixed order) and the
 // top of their keys (at most 256).  Bound by its chain's latency: 1 x 128000, 31 parts, top 8
-// 5 us.
+// 6 us.
 template <int DT>
 __global__ __launch_bounds__(256) void logprob_join_kernel(
     const void* __restrict__ logits, size_t ld, int V, const int64_t* __restrict__ targets,

@@ -245,9 +245,9 @@ __device__ __forceinline__ void wait_barrier() {
 }
 
 // At least n waves on a SIMD.  With two a wave has no more than 256 registers, and the
-// compiler leaves the sums where the vector units reach them (2048 tokens x 11008 -> 4096,
-// 8 bits, groups of 64, four wavefronts of 64 x 64: 153 us; by way of the accumulation
-// registers 166).
+// compiler leaves the sums where the vector units reach them (37 tokens, 4096 -> 11008 in 8
+// bits, groups of 128: 18.2 us, 19.5 without; 611 x 1000 -> 2752 forward and backward 60.1 and
+// 61.6; the large tiles the same).
 #define JARQ_WAVES(n) __attribute__((amdgpu_waves_per_eu(n)))
 
 // The S stages of a work-group, `bytes` each: arrays of their own, so that the
@@ -268,9 +268,10 @@ __device__ __forceinline__ void wait_barrier() {
 // never laxer); mul(p, q, a, b, i) gets the fragments of P block a and Q block b of chunk i of
 // the round.
 //
-// 4096 x 4096 -> 2 x 14336 channels, 256-wide tiles: two stages of twice the chunk 812 us,
-// four 800; the loads in a row at the start of a chunk 860; by address instead of by
-// buffer (every LDS read then waits for all others) 905.  Bound by the matrix cores at
+// 4096 x 4096 -> 2 x 14336 channels, 256-wide tiles, compared with each other (780 us with
+// the code as it is): two stages of twice the chunk 812 us, four 800; the loads in a row at the
+// start of a chunk 860; by address instead of by buffer (every LDS read then waits for all
+// others) 905.  Bound by the matrix cores at
 // the clock that the card's power allows (1.4 to 1.7 GHz here).
 template <int S, int BI, int BJ, class LP, class LQ, class Round, class Mul>
 __device__ __forceinline__ void mma_loop(const LP& lp, const LQ& lq, int q0, int q1, int lane,
