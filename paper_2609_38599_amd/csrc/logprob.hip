@@ -520,8 +520,9 @@ __global__ __launch_bounds__(256) void logprob_join_kernel(
 // probability and of the entropy; at the target 1 - p from log p, which p's rounding would
 // lose where it is near 1.  Work-group `id`: part id % splits of a row.  A thread reads each
 // entry before it writes it: dlogits may be the logits.  SUMS: the row's sums are not given
-// and are formed first, by the one work-group that the row then has.  Bound by memory:
-// 4096 x 128000 in bf16 410 us, 5.1 TB/s.
+// and are formed first, by the one work-group that the row then has (calls of 4096 x 128000 in
+// bf16 644 us, 438 with the sums given; of one such row 45 and 11).  Bound by memory: 4096 x
+// 128000 in bf16 410 us, 5.1 TB/s.
 template <int DT, bool SUMS>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(
     const void* logits, size_t ld, int V, const int64_t* __restrict__ targets,
