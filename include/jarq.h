@@ -533,6 +533,150 @@ jarq_status jarq_token_logprobs_keep_backward(int32_t dtype, const void* logits,
                                               void* d_logits, int64_t ld_d, void* stream);
 
 /*
+ * Around a block in a training or serving step: its norm, the loss from its hidden states, and
+ * the step on its weights.
+ */
+
+/*
+ * The root-mean-square norm of tokens X [tokens][cols] of any dtype, with the residual's
+ * addition where `residual` is given:
+ *     H = X + residual (rounded to dtype),  r = 1 / sqrt(mean H^2 + eps),
+ *     Y[t][c] = H[t][c] r[t] gain[c]        (rounded once from fp32).
+ * Without a residual H is X and the pointer NULL.  gain [cols] is of gain_dtype: dtype or
+ * JARQ_F32.  1 <= cols <= 2^20, eps at least 2^-126 and finite.  H may be X or residual, and Y X.
+ * Arrays are aligned to their type.  Sums are in fp64, so a row's squares may pass fp32's
+ * range; a row with an infinity or a NaN gives NaN or 0.
+ */
+jarq_status jarq_rms_norm(int32_t dtype, int32_t gain_dtype, int64_t tokens, int32_t cols,
+                          const void* X, const void* residual, const void* gain, float eps,
+                          void* H, void* Y, void* stream);
+
+/*
+ * The same norm on 8 bits, for jarq_matmul_i8 (cols a multiple of 16, at most 131056; Q 16-byte
+ * aligned): with w = H gain in fp32 and amax = max |w| of the row,
+ *     Q = rint(w (127 / amax)),  scale[t] = (amax / 127) r[t],
+ * so that the integers depend on no sum.  Y itself is not rounded to dtype first.  Rows with amax <
+ * 2^-100 get zeros and scale 0, rows with an infinity or a NaN zeros and scale NaN.
+ */
+jarq_status jarq_rms_norm_i8(int32_t dtype, int32_t gain_dtype, int64_t tokens, int32_t cols,
+                             const void* X, const void* residual, const void* gain, float eps,
+                             void* H, int8_t* Q, float* scale, void* stream);
+
+/*
+ * Gradients of that norm for dY [tokens][cols], from H (X without a residual) alone, with
+ * u = dY gain:
+ *     dX = r u - H r^3 mean(u H) + dH,  dgain = sum_t dY H r.
+ * dX (of dtype) is the gradient of X and of the residual; dH (nullable) is what reaches H on
+ * other ways, the residual stream's.  dgain is of gain_dtype.  dX and dgain are nullable (not
+ * formed) and overwritten; dX may be dY or dH.  Sums over tokens are in fp32 in an order that
+ * the sizes fix.  The workspace (256-byte aligned, jarq_rms_norm_workspace_bytes bytes; 0 if the sizes
+ * are invalid) is used only during the call.
+ */
+size_t jarq_rms_norm_workspace_bytes(int64_t tokens, int32_t cols);
+jarq_status jarq_rms_norm_backward(int32_t dtype, int32_t gain_dtype, int64_t tokens,
+                                   int32_t cols, const void* H, const void* gain, const void* dY,
+                                   const void* dH, float eps, void* dX, void* dgain,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Log probabilities of given tokens from hidden states X [tokens][d] and the output layer's
+ * weights W [vocab][d], both of dtype JARQ_F16 or JARQ_BF16, without the logits l = X W^T:
+ *     lse[t] = log sum_v exp(l_tv),
+ *     logprob[t] = l_target - lse        (0 where targets[t] < 0, NaN where it is not below
+ *                                         vocab),
+ *     lse_rest[t] = what rounding left of lse (the backward pass takes it).
+ * d is a multiple of 8, from 8 to 2^20; 1 <= vocab <= 2^22.  Logits are fp32 sums.  A row with an
+ * infinite or NaN logit gives NaN (-infinity alone has probability 0).  Outputs are fp32, 4-byte
+ * aligned, targets 8-byte.  The workspace (256-byte aligned,
+ * jarq_linear_logprobs_workspace_bytes bytes; 0 if the sizes are invalid) is used only during the
+ * call.
+ */
+size_t jarq_linear_logprobs_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab);
+jarq_status jarq_linear_logprobs(int32_t dtype, int64_t tokens, int32_t d, int32_t vocab,
+                                 const void* X, const void* W, const int64_t* targets,
+                                 float* logprob, float* lse, float* lse_rest, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum_t (d_logprob[t] logprob[t] + d_lse[t] lse[t]): with g = d_logprob[t] (0
+ * without a target) and h = d_lse[t] (d_lse nullable: 0),
+ *     dl = g 1{v = target} + (h - g) exp(l - lse),  dX = dl W,  dW = dl^T X,
+ * dX [tokens][d] and dW [vocab][d] of dtype, each nullable (not formed) and overwritten.  dl is
+ * formed in pieces of the vocabulary and rounded to dtype before its products (in float16
+ * scaled by a power of two, so that nothing is lost below the range).  A token of g = h = 0 adds
+ * products with 0, so an infinity or a NaN in its X makes dW NaN.  logprob, lse and lse_rest as the forward pass
+ * left them.  The workspace (256-byte aligned, at most about 0.5 GiB up to 2^17 tokens beside 4 bytes
+ * a value of dX times the shares that its sums are cut into) is used only during the call.
+ */
+size_t jarq_linear_logprobs_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab);
+jarq_status jarq_linear_logprobs_backward(int32_t dtype, int64_t tokens, int32_t d, int32_t vocab,
+                                          const void* X, const void* W, const int64_t* targets,
+                                          const float* logprob, const float* lse,
+                                          const float* lse_rest, const float* d_logprob,
+                                          const float* d_lse, void* dX, void* dW,
+                                          void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A step of AdamW over `count` tensors at once.  With g = gradient (times grad_mul) and t = step,
+ *     m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,
+ *     p = p (1 - lr weight_decay)
+ *         - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + eps),
+ * every product and sum rounded to fp32.  Gradients and parameters are of dtype, dense, aligned
+ * to their type.  Parameters of 16 bits are the rounded ones of fp32 in `master`.
+ *
+ * The state is flat: a tensor's values begin at the sum of the lengths before it, each rounded up to
+ * a multiple of 128 (jarq_adamw_state_length is the total).  What lies between is not read, and
+ * zero or left as it was.
+ *   master [n] fp32 (NULL for fp32 parameters);
+ *   bits = 32: m, v [n] fp32;
+ *   bits = 8: m and sqrt(v) [n] in e4m3 (bias 7, no infinities), m_exp, v_exp [n / 128]: a value
+ *     stands for itself times 2^(exp - 134).  The largest of a block of 128 is put in 2^7..2^8 and
+ *     the others rounded up where the 20 bits cut off (of the value's fp32 form) and
+ *     16 (noise mod 2^16) (m), 16 floor(noise / 2^16) (sqrt(v)) pass 2^20, with
+ *         noise = mix((i mod 2^32) + (key xor mix(floor(i / 2^32)))), i the place in the state,
+ *         key = mix(mix(mix(seed mod 2^32) + floor(seed / 2^32)) + (step mod 2^32)),
+ *         mix(x): x ^= x >> 16, x *= 0x9E3779B9, x ^= x >> 15, x *= 0xBB67AE85, x ^= x >> 16
+ *     (32-bit sums and products; mix(0) = 0).  sqrt(v) > 0 gets 2^-9 at least.  Blocks with an
+ *     infinity or a NaN become NaN (0x7f, exp 255).
+ * State arrays are 16-byte aligned.
+ *
+ * `out` is `in` itself, every param_out its param (in place), or all arrays written are others
+ * (the old ones stay).  A tensor whose grad is NULL is left as it is (in place only).  Arrays that
+ * overlap otherwise give JARQ_EINVAL.
+ *
+ * Options [host]: lr, weight_decay >= 0, 0 <= beta < 1, eps >= 2^-126, step >= 1.  lr_at, step_at and
+ * grad_mul (nullable, device) stand in for lr, for step, and multiply the gradients; they are read
+ * when the kernels run, so a captured graph takes their new values.  Where grad_mul is
+ * infinite or NaN, or *step_at below 1, the step changes nothing (out gets a copy).
+ */
+typedef struct jarq_adamw_tensor {   /* [host] */
+  const void* grad;
+  const void* param;
+  void* param_out;
+  int64_t numel;
+} jarq_adamw_tensor;
+typedef struct jarq_adamw_state {    /* [host], of device pointers */
+  float* master;
+  void* m;
+  void* v;
+  uint8_t* m_exp;
+  uint8_t* v_exp;
+} jarq_adamw_state;
+typedef struct jarq_adamw_options {  /* [host] */
+  double lr, beta1, beta2, eps, weight_decay;
+  int64_t step;
+  uint64_t seed;
+  const float* lr_at;
+  const int64_t* step_at;
+  const float* grad_mul;
+} jarq_adamw_options;
+int64_t jarq_adamw_state_length(int32_t count, const int64_t* numel);   /* -1: invalid */
+jarq_status jarq_adamw_step(int32_t dtype, int32_t bits, int32_t count,
+                            const jarq_adamw_tensor* tensors, const jarq_adamw_state* in,
+                            const jarq_adamw_state* out, const jarq_adamw_options* options,
+                            void* stream);
+
+/*
  * Measurement aid (not part of refinement): a kernel that moves a known
  * number of bytes through the local data share (LDS), used to scale LDS
  * profiler counters to bytes and to see the rate the LDS sustains for a

@@ -76,6 +76,19 @@ class Stats(ctypes.Structure):
 
 
 _vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+_f32 = ctypes.c_float
+
+
+class _AdamWArrays(ctypes.Structure):
+    _fields_ = [(n, _vp) for n in ("master", "m", "v", "m_exp", "v_exp")]
+
+
+class _AdamWOptions(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("lr", "beta1", "beta2", "eps", "weight_decay")] + [
+        ("step", _i64), ("seed", ctypes.c_uint64), ("lr_at", _vp), ("step_at", _vp),
+        ("grad_mul", _vp)]
+
+
 _SIGNATURES = {
     "jarq_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(Params)]),
     "jarq_prepare": (ctypes.c_int, [ctypes.POINTER(Params), _vp, _vp, _vp, ctypes.c_size_t, _vp]),
@@ -134,6 +147,23 @@ _SIGNATURES = {
                                                 _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]),
     "jarq_token_logprobs_keep_backward": (ctypes.c_int, [_i32, _vp, _i64, _i64, _i32, _vp, _vp,
                                                          _vp, _vp, _vp, _vp, _vp, _i64, _vp]),
+    "jarq_rms_norm": (ctypes.c_int, [_i32, _i32, _i64, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp]),
+    "jarq_rms_norm_i8": (ctypes.c_int, [_i32, _i32, _i64, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _vp,
+                                        _vp]),
+    "jarq_rms_norm_workspace_bytes": (ctypes.c_size_t, [_i64, _i32]),
+    "jarq_rms_norm_backward": (ctypes.c_int, [_i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _f32,
+                                              _vp, _vp, _vp, ctypes.c_size_t, _vp]),
+    "jarq_linear_logprobs_workspace_bytes": (ctypes.c_size_t, [_i64, _i32, _i32]),
+    "jarq_linear_logprobs": (ctypes.c_int, [_i32, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp,
+                                            _vp, ctypes.c_size_t, _vp]),
+    "jarq_linear_logprobs_backward_workspace_bytes": (ctypes.c_size_t, [_i64, _i32, _i32]),
+    "jarq_linear_logprobs_backward": (ctypes.c_int, [_i32, _i64, _i32, _i32, _vp, _vp, _vp, _vp,
+                                                     _vp, _vp, _vp, _vp, _vp, _vp, _vp,
+                                                     ctypes.c_size_t, _vp]),
+    "jarq_adamw_state_length": (_i64, [_i32, _vp]),
+    "jarq_adamw_step": (ctypes.c_int, [_i32, _i32, _i32, _vp, ctypes.POINTER(_AdamWArrays),
+                                       ctypes.POINTER(_AdamWArrays),
+                                       ctypes.POINTER(_AdamWOptions), _vp]),
     "jarq_lds_probe": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32, _vp, _vp]),
     "jarq_status_string": (ctypes.c_char_p, [ctypes.c_int]),
     "jarq_abi_version": (ctypes.c_int32, []),
@@ -839,6 +869,329 @@ def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, 
             *head, _at(rest, torch.float32, "lse_rest", at), *tail),
             "jarq_token_logprobs_keep_backward")
     return out
+
+
+# ---- around a block in a training or serving step ----
+
+def _norm_args(X, gain, residual, at):
+    """(type, gain's type, addresses) of a norm's inputs, checked."""
+    T, cols = _rows(X, "X")
+    dt, gt = X.dtype, gain.dtype
+    code = _dtype(X, "X")
+    if gt != dt and gt != torch.float32:
+        raise TypeError(f"gain must be {dt} or float32, got {gt}")
+    if gain.shape != (cols,):
+        raise ValueError("gain must be [cols]")
+    if residual is not None and residual.shape != X.shape:
+        raise ValueError("residual must have the shape of X")
+    return code, DTYPES[gt], T, cols, _at(X, dt, "X", at), _at(residual, dt, "residual", at), \
+        _at(gain, gt, "gain", at)
+
+
+def _no_norm_graph(call, X, gain, residual, says):
+    if X.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad):
+        _outside(call, says)
+
+
+def _sum_out(sum_out, X, residual):
+    """Where X + residual goes, None without a residual."""
+    if residual is None:
+        if sum_out is not None:
+            raise ValueError("sum_out needs a residual")
+        return None
+    if sum_out is None:
+        return torch.empty_like(X)
+    if sum_out.shape != X.shape:
+        raise ValueError("sum_out must have the shape of X")
+    return sum_out
+
+
+def rms_norm(X, gain, residual=None, eps=1e-6, out=None, sum_out=None, stream=None):
+    """The root-mean-square norm of X [tokens, cols] times gain [cols] (X's type or float32).
+
+    With a residual the norm is of H = X + residual, rounded to X's type, and (Y, H) is returned;
+    sum_out may be X or the residual, and out X.  rms_norm_backward gives the gradients; autograd
+    records none.
+    """
+    lib = load_library()
+    at = _device(X, "X")
+    code, gcode, T, cols, x, res, g = _norm_args(X, gain, residual, at)
+    _no_norm_graph("rms_norm", X, gain, residual, "rms_norm_backward gives its gradients")
+    with _on(stream):
+        if out is None:
+            out = torch.empty_like(X)
+        elif out.shape != X.shape:
+            raise ValueError("out must have the shape of X")
+        H = _sum_out(sum_out, X, residual)
+    _check(lib.jarq_rms_norm(code, gcode, T, cols, x, res, g, eps, _at(H, X.dtype, "sum_out", at),
+                             _at(out, X.dtype, "out", at), _queue(stream, at)), "jarq_rms_norm")
+    return out if residual is None else (out, H)
+
+
+def rms_norm_i8(X, gain, residual=None, eps=1e-6, out=None, scale=None, sum_out=None, stream=None):
+    """(Q int8, scale fp32 [rows, 1]) of that norm on 8 bits, for matmul_i8.  Has no gradient.
+
+    With a residual (Q, scale, H).
+    """
+    lib = load_library()
+    at = _device(X, "X")
+    code, gcode, T, cols, x, res, g = _norm_args(X, gain, residual, at)
+    _no_norm_graph("rms_norm_i8", X, gain, residual, "it has no gradient")
+    with _on(stream):
+        if out is None:
+            out = torch.empty(T, cols, dtype=torch.int8, device=X.device)
+        if scale is None:
+            scale = torch.empty(T, 1, dtype=torch.float32, device=X.device)
+        H = _sum_out(sum_out, X, residual)
+    if out.shape != X.shape or scale.numel() != T:
+        raise ValueError("out must have the shape of X and scale hold one value a row")
+    _check(lib.jarq_rms_norm_i8(code, gcode, T, cols, x, res, g, eps,
+                                _at(H, X.dtype, "sum_out", at), _at(out, torch.int8, "out", at),
+                                _at(scale, torch.float32, "scale", at), _queue(stream, at)),
+           "jarq_rms_norm_i8")
+    return (out, scale) if residual is None else (out, scale, H)
+
+
+def rms_norm_backward(H, gain, dY, dH=None, eps=1e-6, need=(True, True), ws=None, stream=None):
+    """(dX, dgain) of rms_norm, None where not needed, from H (X where there was no residual).
+
+    dX is the gradient of X and of the residual alike; dH is what reaches H on other ways.
+    """
+    lib = load_library()
+    at = _device(H, "H")
+    T, cols = _rows(H, "H")
+    if dY.shape != H.shape or (dH is not None and dH.shape != H.shape):
+        raise ValueError("dY and dH must have the shape of H")
+    code, gcode, T, cols, h, _, g = _norm_args(H, gain, None, at)
+    n = int(lib.jarq_rms_norm_workspace_bytes(T, cols))
+    if n == 0:
+        raise JarqError(JARQ_EINVAL, "jarq_rms_norm_workspace_bytes")
+    dt = H.dtype
+    with _on(stream):
+        dX = torch.empty_like(H) if need[0] else None
+        dgain = torch.empty_like(gain) if need[1] else None
+        if ws is None:
+            ws = _work(n, H)
+    _check(lib.jarq_rms_norm_backward(code, gcode, T, cols, h, g, _at(dY, dt, "dY", at),
+                                      _at(dH, dt, "dH", at), eps, _own(dX), _own(dgain),
+                                      _at(ws, torch.uint8, "workspace", at), ws.numel(),
+                                      _queue(stream, at)), "jarq_rms_norm_backward")
+    return dX, dgain
+
+
+class LinearLogprobs(NamedTuple):
+    """What linear_logprobs returns: all [tokens] fp32."""
+
+    logprob: torch.Tensor
+    lse: torch.Tensor         # log sum exp of the logits
+    lse_rest: torch.Tensor    # what rounding left of it
+
+
+def linear_logprobs(X, W, targets, ws=None, stream=None) -> LinearLogprobs:
+    """Log probabilities of targets [tokens] int64 (< 0: none) under the logits X W^T.
+
+    X [tokens, d] and W [vocab, d] in 16 bits; the logits are not formed in memory.
+    linear_logprobs_backward gives the gradients; autograd records none.
+    """
+    lib = load_library()
+    T, d = _rows(X, "X")
+    V, _ = _rows(W, "W", d)
+    at = _device(X, "X")
+    if targets.shape != (T,):
+        raise ValueError("targets must be [tokens]")
+    n = int(lib.jarq_linear_logprobs_workspace_bytes(T, d, V))
+    if n == 0:
+        raise JarqError(JARQ_EINVAL, "jarq_linear_logprobs_workspace_bytes")
+    if X.requires_grad or W.requires_grad:
+        _outside("linear_logprobs", "linear_logprobs_backward gives its gradients")
+    dt = X.dtype
+    with _on(stream):
+        r = LinearLogprobs(*torch.empty(3, T, dtype=torch.float32, device=X.device).unbind(0))
+        if ws is None:
+            ws = _work(n, X)
+    _check(lib.jarq_linear_logprobs(_dtype(X, "X"), T, d, V, _at(X, dt, "X", at),
+                                    _at(W, dt, "W", at), _at(targets, torch.int64, "targets", at),
+                                    r.logprob.data_ptr(), r.lse.data_ptr(), r.lse_rest.data_ptr(),
+                                    _at(ws, torch.uint8, "workspace", at), ws.numel(),
+                                    _queue(stream, at)), "jarq_linear_logprobs")
+    return r
+
+
+def linear_logprobs_backward(X, W, targets, forward: LinearLogprobs, d_logprob, d_lse=None,
+                             need=(True, True), ws=None, stream=None):
+    """(dX, dW) from the gradients of the log probabilities and of lse [tokens].
+
+    None where not needed.
+    """
+    lib = load_library()
+    T, d = _rows(X, "X")
+    V, _ = _rows(W, "W", d)
+    at = _device(X, "X")
+    for t, name in ((targets, "targets"), (forward.logprob, "logprob"), (forward.lse, "lse"),
+                    (forward.lse_rest, "lse_rest"), (d_logprob, "d_logprob"), (d_lse, "d_lse")):
+        if t is not None and t.shape != (T,):
+            raise ValueError(f"{name} must be [tokens]")
+    n = int(lib.jarq_linear_logprobs_backward_workspace_bytes(T, d, V))
+    if n == 0:
+        raise JarqError(JARQ_EINVAL, "jarq_linear_logprobs_backward_workspace_bytes")
+    dt, f32 = X.dtype, torch.float32
+    with _on(stream):
+        dX, dW = (torch.empty_like(t) if wanted else None for t, wanted in zip((X, W), need))
+        if ws is None:
+            ws = _work(n, X)
+    _check(lib.jarq_linear_logprobs_backward(
+        _dtype(X, "X"), T, d, V, _at(X, dt, "X", at), _at(W, dt, "W", at),
+        _at(targets, torch.int64, "targets", at), _at(forward.logprob, f32, "logprob", at),
+        _at(forward.lse, f32, "lse", at), _at(forward.lse_rest, f32, "lse_rest", at),
+        _at(d_logprob, f32, "d_logprob", at), _at(d_lse, f32, "d_lse", at), _own(dX), _own(dW),
+        _at(ws, torch.uint8, "workspace", at), ws.numel(), _queue(stream, at)),
+        "jarq_linear_logprobs_backward")
+    return dX, dW
+
+
+class AdamWState(NamedTuple):
+    """The state of adamw_step for a list of tensors, flat: see adamw_state.
+
+    A tensor's values begin at the sum of the lengths before it, each rounded up to a multiple of
+    128.  On 8 bits m and sqrt(v) are held as value * 2^(exp - 134), an exponent a 128.
+    """
+
+    master: Optional[torch.Tensor]   # [n] fp32: the parameters of 16 bits; None for fp32 ones
+    m: torch.Tensor                  # [n] fp32, or float8_e4m3fn
+    v: torch.Tensor                  # [n] fp32: v; or float8_e4m3fn: sqrt(v)
+    m_exp: Optional[torch.Tensor]    # [n / 128] uint8 on 8 bits
+    v_exp: Optional[torch.Tensor]
+
+
+def _state_length(numels):
+    n = int(load_library().jarq_adamw_state_length(len(numels), (_i64 * len(numels))(*numels)))
+    if n < 0:
+        raise JarqError(JARQ_EINVAL, "jarq_adamw_state_length")
+    return n
+
+
+def adamw_state(params, bits=32) -> AdamWState:
+    """A new state (no moments) for parameters of one type on one device.
+
+    Parameters of 16 bits get a copy in 32, which the steps advance.
+    """
+    params = list(params)
+    if bits not in (8, 32):
+        raise ValueError(f"bits must be 8 or 32, got {bits!r}")
+    if not params:
+        raise ValueError("params must hold a tensor")
+    dt = params[0].dtype
+    _dtype(params[0], "params[0]")
+    at = _device(params[0], "params[0]")
+    for k, t in enumerate(params):
+        _at(t, dt, f"params[{k}]", at)
+    n = _state_length([t.numel() for t in params])
+    dev = params[0].device
+    master = None
+    if dt != torch.float32:
+        master = torch.zeros(n, dtype=torch.float32, device=dev)
+        first = 0
+        for t in params:
+            master[first:first + t.numel()] = t.detach().view(-1)
+            first += (t.numel() + 127) // 128 * 128
+    if bits == 32:
+        return AdamWState(master, *(torch.zeros(n, dtype=torch.float32, device=dev)
+                                    for _ in range(2)), None, None)
+    m, v = (torch.zeros(n, dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+            for _ in range(2))
+    return AdamWState(master, m, v, *(torch.zeros(n // 128, dtype=torch.uint8, device=dev)
+                                      for _ in range(2)))
+
+
+def adamw_moments(state: AdamWState):
+    """(m, v) of a state as flat fp32 tensors."""
+    if state.m_exp is None:
+        return state.m, state.v
+    m, root = (torch.where(e == 255, torch.nan, torch.ldexp(x.float().view(-1, 128),
+                                                            e.int() - 134)).view(-1)
+               for x, e in ((state.m, state.m_exp[:, None]), (state.v, state.v_exp[:, None])))
+    return m, root * root
+
+
+def _addresses(tensors, dtype, name, device, numels):
+    """The addresses of dense tensors of one type on the call's device, None where one is None."""
+    try:
+        if all(t is None or (t.dtype == dtype and t.get_device() == device and t.is_contiguous()
+                             and t.numel() == n) for t, n in zip(tensors, numels)):
+            return [0 if t is None else t.data_ptr() for t in tensors]
+    except AttributeError:
+        pass
+    for k, (t, n) in enumerate(zip(tensors, numels)):
+        _at(t, dtype, f"{name}[{k}]", device)
+        if t is not None and t.numel() != n:
+            raise ValueError(f"{name}[{k}] must have {n} values, got {t.numel()}")
+    raise ValueError(f"{name} must be tensors")
+
+
+def _state_arrays(s: AdamWState, bits, wide, n, name, device):
+    held = torch.float32 if bits == 32 else torch.float8_e4m3fn
+    want = (("master", None if wide else torch.float32, n), ("m", held, n), ("v", held, n),
+            ("m_exp", None if bits == 32 else torch.uint8, n // 128),
+            ("v_exp", None if bits == 32 else torch.uint8, n // 128))
+    found = []
+    for t, (part, dt, length) in zip(s, want):
+        if (t is None) != (dt is None):
+            raise ValueError(f"{name}.{part} must be {'None' if dt is None else 'a tensor'}")
+        if t is not None and t.shape != (length,):
+            raise ValueError(f"{name}.{part} must be [{length}]")
+        found.append(_at(t, dt, f"{name}.{part}", device))
+    return _AdamWArrays(*found)
+
+
+def _one_value(t, dtype, name, device):
+    if t is not None and t.numel() != 1:
+        raise ValueError(f"{name} must hold one value")
+    return _at(t, dtype, name, device)
+
+
+def adamw_step(params, grads, state: AdamWState, step, lr, beta1=0.9, beta2=0.999, eps=1e-8,
+               weight_decay=0.01, grad_mul=None, seed=0, out=None, stream=None):
+    """A step of AdamW on params with the gradients grads, both lists of tensors of one type.
+
+    Updates params and state in place and returns them; with out, a pair (params, state) of other
+    tensors, those get the result and the old ones stay.  step counts from 1.  step and lr are
+    numbers, or device tensors of one value (int64, float32) that are read when the step runs, as
+    in a captured graph; grad_mul, a float32 one, multiplies the gradients (an infinite or NaN
+    one: the step changes nothing).  A gradient may be None (its tensor stays; not with out).  On
+    8 bits the rounding's noise comes from seed and step.
+    """
+    lib = load_library()
+    params, grads = list(params), list(grads)
+    if len(grads) != len(params) or not params:
+        raise ValueError("params and grads must hold as many tensors, one at least")
+    dt = params[0].dtype
+    code = _dtype(params[0], "params[0]")
+    at = _device(params[0], "params[0]")
+    bits = 32 if state.m_exp is None else 8
+    numels = [t.numel() for t in params]
+    n = sum([(k + 127) // 128 * 128 for k in numels])
+    if any(t is None for t in params):
+        raise ValueError("params must be tensors")
+    old = _addresses(params, dt, "params", at, numels)
+    new_params, new_state = (params, state) if out is None else (list(out[0]), out[1])
+    if len(new_params) != len(params) or any(t is None for t in new_params):
+        raise ValueError("out must hold as many parameters")
+    new = old if out is None else _addresses(new_params, dt, "out", at, numels)
+    table = (_i64 * (4 * len(params)))()
+    table[0::4] = _addresses(grads, dt, "grads", at, numels)
+    table[1::4], table[2::4], table[3::4] = old, new, numels
+    held = _state_arrays(state, bits, dt == torch.float32, n, "state", at)
+    to = held if out is None else _state_arrays(new_state, bits, dt == torch.float32, n, "out", at)
+    step_at = lr_at = None
+    if isinstance(step, torch.Tensor):
+        step, step_at = 1, _one_value(step, torch.int64, "step", at)
+    if isinstance(lr, torch.Tensor):
+        lr, lr_at = 0.0, _one_value(lr, torch.float32, "lr", at)
+    options = _AdamWOptions(lr, beta1, beta2, eps, weight_decay, step, seed & (2 ** 64 - 1), lr_at,
+                            step_at, _one_value(grad_mul, torch.float32, "grad_mul", at))
+    _check(lib.jarq_adamw_step(code, bits, len(params), ctypes.addressof(table), held, to, options,
+                               _queue(stream, at)), "jarq_adamw_step")
+    return new_params, new_state
 
 
 def lds_probe(workgroups, passes, out=None, stream=None):

@@ -19,7 +19,8 @@ INCLUDE = os.path.join(ROOT, "include")
 OBJDIR = os.path.join(ROOT, "_build", "jarq")
 LIB = os.path.join(HERE, "libjarq.so")
 SOURCES = ["chol.hip", "split.hip", "sgemm.hip", "objective.hip", "gemm.hip", "gram.hip", "solve.hip", "babai.hip", "pupdate.hip", "misc.hip", "hessian.hip", "setup.hip", "linalg.hip", "gptq.hip", "qep.hip", "post.hip", "probe.hip", "api.hip",
-           "gated.hip", "i8.hip", "logprob.hip", "api_blocks.hip"]
+           "gated.hip", "i8.hip", "logprob.hip", "norm.hip", "linlog.hip", "adamw.hip",
+           "api_blocks.hip", "api_step.hip"]
 ARCH = "gfx950"
 
 

@@ -288,29 +288,6 @@ __global__ __launch_bounds__(256) void gated_grad_kernel(const float* __restrict
   }
 }
 
-// A tile's sums as 16-bit values: store(j, i, w) gets eight of them from row j of the
-// 16 BJ that the WI waves of one wj share a stage for, columns i .. of the tile.
-template <int KIND, int WI, int BI, int BJ, class Store>
-__device__ __forceinline__ void store_tile16(const f32x4 (&acc)[BI][BJ], char* stage, int wi,
-                                             int lane, const Store& store) {
-  constexpr int RB = 2 * 16 * WI * BI, PIECES = RB / 16;
-#pragma unroll
-  for (int b = 0; b < BJ; ++b)
-#pragma unroll
-    for (int a = 0; a < BI; ++a) {
-      const int at = 2 * (wi * 16 * BI + 16 * a + 4 * (lane >> 4));
-      const f32x4& c = acc[a][b];
-      *(u32x2*)(out_piece<RB>(stage, 16 * b + (lane & 15), at >> 4) + (at & 15)) =
-          u32x2{pack16<KIND>(c[0], c[1]), pack16<KIND>(c[2], c[3])};
-    }
-  __syncthreads();
-#pragma unroll 1
-  for (int p = wi * 64 + lane; p < 16 * BJ * PIECES; p += WI * 64) {
-    const int j = p / PIECES, c = p % PIECES;
-    store(j, 8 * c, *(const u32x4*)out_piece<RB>(stage, j, c));
-  }
-}
-
 // ---- backward: dx = dab [Wg; Wu] ----
 // part: fp32 partial sums [split][T][D] where the 2 F are cut over blockIdx.y.  Wg and Wu
 // are read as they lie (k down the rows) through the transposing LDS read.  Bound by the

@@ -8,6 +8,8 @@
 
 #include <atomic>
 
+#include "jarq.h"
+
 namespace jarq {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -430,5 +432,34 @@ hipError_t launch_token_logprobs_backward(hipStream_t st, int dtype, const void*
                                           const float* rest, const float* entropy,
                                           const float* dlp, const float* dent, void* dlogits,
                                           size_t ldd);
+
+// norm.hip.  gain of gain_dtype (dtype's or JARQ_F32); residual and H both or neither
+hipError_t launch_rms_norm(hipStream_t st, int dtype, int gain_dtype, const void* X,
+                           const void* residual, const void* gain, float eps, int T, int cols,
+                           void* H, void* Y);
+hipError_t launch_rms_norm_i8(hipStream_t st, int dtype, int gain_dtype, const void* X,
+                              const void* residual, const void* gain, float eps, int T, int cols,
+                              void* H, int8_t* Q, float* scale);
+size_t rms_norm_workspace_bytes(int T, int cols);   // of the backward pass
+hipError_t launch_rms_norm_backward(hipStream_t st, int dtype, int gain_dtype, const void* H,
+                                    const void* gain, const void* dY, const void* dH, float eps,
+                                    int T, int cols, void* dX, void* dgain, char* ws);
+
+// linlog.hip.  dtype JARQ_F16 or JARQ_BF16
+size_t linear_logprobs_workspace_bytes(int T, int D, int V);
+hipError_t launch_linear_logprobs(hipStream_t st, int dtype, int T, int D, int V, const void* X,
+                                  const void* W, const int64_t* targets, float* logprob,
+                                  float* lse, float* rest, char* ws);
+size_t linear_logprobs_backward_workspace_bytes(int T, int D, int V);
+hipError_t launch_linear_logprobs_backward(hipStream_t st, int dtype, int T, int D, int V,
+                                           const void* X, const void* W, const int64_t* targets,
+                                           const float* logprob, const float* lse,
+                                           const float* rest, const float* dlp,
+                                           const float* dlse, void* dX, void* dW, char* ws);
+
+// adamw.hip.  in and out: the same arrays or other ones
+hipError_t launch_adamw(hipStream_t st, int dtype, int bits, int count,
+                        const jarq_adamw_tensor* tensors, const jarq_adamw_state& in,
+                        const jarq_adamw_state& out, const jarq_adamw_options& o);
 
 }  // namespace jarq

@@ -1,0 +1,695 @@
+// Log probabilities of given tokens straight from hidden states x [T][D] and the output
+// layer's weights w [V][D], 16-bit both, and their gradients, without the logits.
+//
+// Forward: a tile of l = x w^T leaves its maximum and the sum of exponentials beside the
+// maximum's own 1 for each token (kept apart, as in the pass over stored logits: where one entry
+// takes nearly all, log p of it is log(1 + that sum)), and the target's logit; the tiles' are
+// joined in a fixed order.
+//
+// Backward, in pieces of the vocabulary: the piece's logits again,
+//     dl = g 1{v = target} + (h - g) exp(l - lse)
+// in 16 bits as the matrix cores take them, then dx += dl w (fp32 sums between the pieces) and
+// dw = dl^T x.  Forming the logits twice is a quarter of the work; kept, they would be T V
+// values in memory.  In fp16 dl is scaled by a power of two, the largest |g|, |h| and |h - g| to
+// 2^14, so that a probability of 2^-38 is not lost; the sums are scaled back in fp32.
+#include <float.h>
+
+#include "skinny.h"
+
+namespace jarq {
+
+namespace {
+
+// The maximum (at least -FLT_MAX) and the sum of exp(x - m) beside its own 1; -1: no entry
+// above -infinity.
+struct Part {
+  float m, more;
+};
+__device__ __forceinline__ Part no_part() { return Part{-FLT_MAX, -1.f}; }
+__device__ __forceinline__ Part join(const Part& s, const Part& o) {
+  const bool first = s.m >= o.m;
+  const Part a = first ? s : o, b = first ? o : s;
+  return Part{a.m, fmaf(__expf(b.m - a.m), 1.f + b.more, a.more)};
+}
+__device__ __forceinline__ Part of_lane(const Part& s, int off) {
+  return Part{__shfl_xor(s.m, off), __shfl_xor(s.more, off)};
+}
+// N entries; -infinity has no part, +infinity and NaN make it NaN.
+template <int N>
+__device__ __forceinline__ Part part_of(const float (&x)[N]) {
+  float m = -FLT_MAX;
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+  float more = 0.f;
+  int top = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bool is = x[i] == m;
+    more += is ? 0.f : __expf(x[i] - m);
+    top += is;
+  }
+  return Part{m, m == INFINITY ? NAN : more + (float)(top - 1)};
+}
+
+}  // namespace
+
+// ---- forward, many tokens ----
+// WI x WJ wavefronts, each BI blocks of 16 rows of w x BJ blocks of 16 tokens.
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_tile_kernel(
+    const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V,
+    const int64_t* __restrict__ targets, float* __restrict__ target_logit,
+    float2* __restrict__ part, int ni, int nj) {
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
+  typedef KContig<TI, NW, kOne> LP;
+  typedef KContig<TJ, NW, kOne> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  JARQ_STAGES(S, STAGE);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int v0 = ti * TI, t0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(W, W, 2 * (size_t)D, v0, V, 2 * D, wave, lane);
+  lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
+  f32x4 acc[BI][BJ] = {};
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
+                   stages, [](int) {},
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
+                       __attribute__((always_inline)) {
+                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                       });
+  static_assert(WI <= 2 && TJ * 8 <= STAGE, "the other wave's parts fit a stage");
+  float2* const red = (float2*)stage0;
+  const int vw = v0 + wi * 16 * BI + 4 * (lane >> 4);   // this lane's first row of w
+  const int tw = wj * 16 * BJ + (lane & 15);            // its first token in the tile
+  Part parts[BJ];
+#pragma unroll
+  for (int b = 0; b < BJ; ++b) {
+    const int t = t0 + tw + 16 * b;
+    float x[4 * BI];
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[4 * a + i] = acc[a][b][i];
+    // (rows past the last one are copies of it: only a last tile has any)
+    if (v0 + TI > V)
+#pragma unroll
+      for (int a = 0; a < BI; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (vw + 16 * a + i >= V) x[4 * a + i] = -INFINITY;
+    const int64_t at = t < T ? targets[t] - vw : -1;
+    if (__any(at >= 0 && at < 16 * BI && at < V - vw)) {   // of few tiles
+#pragma unroll
+      for (int a = 0; a < BI; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at == 16 * a + i && vw + 16 * a + i < V) target_logit[t] = x[4 * a + i];
+    }
+    Part s = part_of(x);
+    s = join(s, of_lane(s, 16));
+    parts[b] = join(s, of_lane(s, 32));
+  }
+  if constexpr (WI == 2) {
+    if (wi == 1)
+#pragma unroll
+      for (int b = 0; b < BJ; ++b)
+        if (lane < 16) red[tw + 16 * b] = make_float2(parts[b].m, parts[b].more);
+    __syncthreads();
+  }
+  if (wi == 0 && lane < 16)
+#pragma unroll
+    for (int b = 0; b < BJ; ++b) {
+      Part s = parts[b];
+      if constexpr (WI == 2) {
+        const float2 o = red[tw + 16 * b];
+        s = join(s, Part{o.x, o.y});
+      }
+      const int t = t0 + tw + 16 * b;
+      if (t < T) part[(size_t)ti * T + t] = make_float2(s.m, s.more);
+    }
+}
+
+// ---- forward, few tokens ----
+// A work-group: 32 rows of w x up to 16 IB tokens, eight wavefronts along k.
+template <int KIND, int IB>
+__global__ __launch_bounds__(512) void linlog_skinny_kernel(
+    const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V,
+    const int64_t* __restrict__ targets, float* __restrict__ target_logit,
+    float2* __restrict__ part) {
+  constexpr int NW = 8;
+  __shared__ __attribute__((aligned(16))) float red[NW * IB * 2 * 256];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int v0 = blockIdx.x * 32;
+  const int row = lane & 15;
+  const size_t ld = 2 * (size_t)D;
+  const char* p[IB];
+#pragma unroll
+  for (int a = 0; a < IB; ++a) p[a] = (const char*)X + (size_t)min(16 * a + row, T - 1) * ld;
+  const char* const q[2] = {(const char*)W + (size_t)min(v0 + row, V - 1) * ld,
+                            (const char*)W + (size_t)min(v0 + 16 + row, V - 1) * ld};
+  f32x4 acc[IB][2] = {};
+  skinny_loop<IB, 2, 4, NW>(
+      p, q, 2 * D, wave, lane, [](int, int) {},
+      [&](int, int, const u32x4(&fp)[IB], const u32x4(&fq)[2]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int a = 0; a < IB; ++a)
+#pragma unroll
+          for (int b = 0; b < 2; ++b) acc[a][b] = Mma<KIND>::mul(fp[a], fq[b], acc[a][b]);
+      });
+#pragma unroll
+  for (int a = 0; a < IB; ++a)
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+      *(f32x4*)(red + ((wave * IB + a) * 2 + b) * 256 + 4 * lane) = acc[a][b];
+  __syncthreads();
+  for (int e = threadIdx.x; e < IB * 512; e += 512) {   // 32 lanes a token
+    const int j = e & 31, t = e >> 5, v = v0 + j;
+    if (t >= T) continue;
+    const float x = skinny_sum<NW, 2 * IB>(red, 2 * (t >> 4) + (j >> 4), t & 15, j & 15);
+    Part s = no_part();
+    if (v < V) {
+      const float one[1] = {x};
+      s = part_of(one);
+      if (targets[t] == v) target_logit[t] = x;
+    }
+#pragma unroll
+    for (int off = 16; off >= 1; off >>= 1) s = join(s, of_lane(s, off));
+    if (j == 0) part[(size_t)blockIdx.x * T + t] = make_float2(s.m, s.more);
+  }
+}
+
+// A token's parts in a fixed order: `tw` tokens a work-group (a power of two), 256 / tw shares of
+// the parts each.
+__global__ __launch_bounds__(256) void linlog_join_kernel(
+    const float2* __restrict__ part, int parts, int T, int V, int tw,
+    const int64_t* __restrict__ targets, const float* __restrict__ target_logit,
+    float* __restrict__ logprob, float* __restrict__ lse, float* __restrict__ rest) {
+  __shared__ float2 red[256];
+  const int shares = 256 / tw, share = threadIdx.x / tw;
+  const int t = blockIdx.x * tw + (threadIdx.x & (tw - 1));
+  Part s = no_part();
+  if (t < T) {
+    int p = share;
+    for (; p + 3 * shares < parts; p += 4 * shares) {   // four loads in flight
+      float2 o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = part[(size_t)(p + i * shares) * T + t];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s = join(s, Part{o[i].x, o[i].y});
+    }
+    for (; p < parts; p += shares) {
+      const float2 o = part[(size_t)p * T + t];
+      s = join(s, Part{o.x, o.y});
+    }
+  }
+  red[threadIdx.x] = make_float2(s.m, s.more);
+  for (int n = 128; n >= tw; n >>= 1) {
+    __syncthreads();
+    if ((int)threadIdx.x < n) {
+      const float2 o = red[threadIdx.x + n];
+      s = join(s, Part{o.x, o.y});
+      red[threadIdx.x] = make_float2(s.m, s.more);
+    }
+  }
+  if ((int)threadIdx.x >= tw || t >= T) return;
+  const bool none = s.more == -1.f;
+  const float lz = log1pf(s.more);
+  // log sum exp, rounded, and what the rounding left
+  const float l = none ? -INFINITY : s.m + lz, d = l - s.m;
+  lse[t] = l;
+  rest[t] = none ? 0.f : (s.m - (l - d)) + (lz - d);
+  const int64_t to = targets[t];
+  float lp = 0.f;
+  if (to >= V) lp = NAN;
+  else if (to >= 0) lp = none ? -INFINITY : (target_logit[t] - s.m) - lz;
+  logprob[t] = lp;
+}
+
+// ---- backward: dl of a piece ----
+// One power of two for all tokens' gradients: scale[0], and its inverse in scale[1].
+__global__ __launch_bounds__(256) void linlog_scale_kernel(const int64_t* __restrict__ targets,
+                                                           const float* __restrict__ dlp,
+                                                           const float* __restrict__ dlse, int T,
+                                                           float* __restrict__ scale) {
+  __shared__ float red[4];
+  float m = 0.f;
+  for (int t = threadIdx.x; t < T; t += 256) {
+    const float g = targets[t] >= 0 ? dlp[t] : 0.f, h = dlse ? dlse[t] : 0.f;
+    m = fmaxf(m, fmaxf(fmaxf(fabsf(g), fabsf(h)), fabsf(h - g)));
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    const int e = (int)(__float_as_uint(m) >> 23) - 127;
+    // (the scale and its inverse are both normal)
+    const int by = m > 0.f && e < 128 ? min(max(14 - e, -126), 126) : 0;
+    scale[0] = ldexpf(1.f, by);
+    scale[1] = ldexpf(1.f, -by);
+  }
+}
+
+// dl [T][ld] of rows v0 .. v0 + n of w (ld a multiple of 8; columns n .. ld are zeros).
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
+    const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V, int v0, int n,
+    int ld, const int64_t* __restrict__ targets, const float* __restrict__ logprob,
+    const float* __restrict__ lse, const float* __restrict__ rest,
+    const float* __restrict__ dlp, const float* __restrict__ dlse,
+    const float* __restrict__ scale, uint16_t* __restrict__ dl, int ni, int nj) {
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
+  typedef KContig<TI, NW, kOne> LP;
+  typedef KContig<TJ, NW, kOne> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  JARQ_STAGES(S, STAGE);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int c0 = ti * TI, t0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init((const char*)W + (size_t)v0 * 2 * D, W, 2 * (size_t)D, c0, n, 2 * D, wave, lane);
+  lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
+  f32x4 acc[BI][BJ] = {};
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
+                   stages, [](int) {},
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
+                       __attribute__((always_inline)) {
+                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                       });
+  const float by = scale ? scale[0] : 1.f;
+  const int cw = c0 + wi * 16 * BI + 4 * (lane >> 4);   // this lane's first column of dl
+#pragma unroll
+  for (int b = 0; b < BJ; ++b) {
+    const int t = min(t0 + wj * 16 * BJ + 16 * b + (lane & 15), T - 1);
+    const int64_t to = targets[t];
+    const float g = to >= 0 ? dlp[t] * by : 0.f, h = dlse ? dlse[t] * by : 0.f, c = h - g;
+    const float l = lse[t], r = rest[t];
+    // (a target that is none of the vocabulary's: NaN, as its log probability)
+    const float c1 = to >= V ? NAN : c;
+    const bool none = l == -INFINITY;
+#pragma unroll
+    for (int a = 0; a < BI; ++a)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p = none ? 0.f : __expf((acc[a][b][i] - l) - r);
+        acc[a][b][i] = c1 * p;
+      }
+    const int64_t at = to - v0 - cw;
+    if (__any(at >= 0 && at < 16 * BI && at < n - cw)) {
+      const float lt = logprob[t], p = __expf(lt);
+      const float d = none ? 0.f : fmaf(h, p, -g * expm1f(lt));   // g (1 - p) + h p
+#pragma unroll
+      for (int a = 0; a < BI; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (at == 16 * a + i) acc[a][b][i] = d;
+    }
+    if (c0 + TI > n)
+#pragma unroll
+      for (int a = 0; a < BI; ++a)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (cw + 16 * a + i >= n) acc[a][b][i] = 0.f;
+  }
+  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  const int tw = t0 + wj * 16 * BJ;
+  store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
+    if (tw + t < T && c0 + i < ld) *(u32x4*)(dl + (size_t)(tw + t) * ld + c0 + i) = w;
+  });
+}
+
+// ---- backward: dx += dl w of a piece ----
+// part [splits][T][D] fp32: the sums so far (read where `add`), of the share blockIdx.y of the
+// piece's rows; without it dX gets the finished sums.  `last` with one share: both.
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
+    const void* __restrict__ dl, const void* __restrict__ W, int T, int D, int n, int ld, int each,
+    float* __restrict__ part, int add, const float* __restrict__ scale,
+    uint16_t* __restrict__ dX, int ni, int nj) {
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
+  typedef KStrided<TI, NW, kOne> LP;
+  typedef KContig<TJ, NW, kOne> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  JARQ_STAGES(S, STAGE);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int d0 = ti * TI, t0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(W, W, 2 * (size_t)D, d0, D, n, wave, lane);
+  lq.init(dl, dl, 2 * (size_t)ld, t0, T, 2 * ((n + 7) & ~7), wave, lane);
+  f32x4 acc[BI][BJ] = {};
+  const int nk = (2 * n + kChunk - 1) / kChunk;
+  const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
+  if (q0 < q1)   // (a short last piece has no rows for the last shares)
+    mma_loop<S, BI, BJ>(lp, lq, q0, q1, lane, wi * 16 * BI, wj * 16 * BJ, stages, [](int) {},
+                     [&](const u32x4& p, const u32x4& q, int a, int b, int)
+                         __attribute__((always_inline)) {
+                           acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                         });
+  if (part) {   // uniform
+#pragma unroll
+    for (int b = 0; b < BJ; ++b) {
+      const int t = t0 + wj * 16 * BJ + 16 * b + (lane & 15);
+#pragma unroll
+      for (int a = 0; a < BI; ++a) {
+        const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
+        if (t < T && d < D) {
+          f32x4* const at = (f32x4*)(part + ((size_t)blockIdx.y * T + t) * D + d);
+          if (add) acc[a][b] += *at;
+          if (!dX) *at = acc[a][b];
+        }
+      }
+    }
+    if (!dX) return;
+  }
+  const float by = scale ? scale[1] : 1.f;
+#pragma unroll
+  for (int a = 0; a < BI; ++a)
+#pragma unroll
+    for (int b = 0; b < BJ; ++b) acc[a][b] *= by;
+  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  const int tw = t0 + wj * 16 * BJ;
+  store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
+    if (tw + t < T && d0 + i < D) *(u32x4*)(dX + (size_t)(tw + t) * D + d0 + i) = w;
+  });
+}
+
+// The shares' sums in their order, rounded once.
+template <int KIND>
+__global__ __launch_bounds__(256) void linlog_dx_sum_kernel(const float* __restrict__ part,
+                                                            int splits, size_t n,
+                                                            const float* __restrict__ scale,
+                                                            uint16_t* __restrict__ dX) {
+  const float by = scale ? scale[1] : 1.f;
+  for (size_t e = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x); e < n;
+       e += 4 * (size_t)gridDim.x * 256) {
+    f32x4 s = *(const f32x4*)(part + e);
+    for (int k = 1; k < splits; ++k) s += *(const f32x4*)(part + k * n + e);
+    s *= by;
+    *(u32x2*)(dX + e) = u32x2{pack16<KIND>(s[0], s[1]), pack16<KIND>(s[2], s[3])};
+  }
+}
+
+// ---- backward: dw = dl^T x of a piece ----
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+__global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
+    const void* __restrict__ dl, const void* __restrict__ X, int T, int D, int n, int ld,
+    const float* __restrict__ scale, uint16_t* __restrict__ dW, int ni, int nj) {
+  constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
+  typedef KStrided<TI, NW, kOne> LP;
+  typedef KStrided<TJ, NW, kOne> LQ;
+  constexpr int STAGE = LP::kBytes + LQ::kBytes;
+  JARQ_STAGES(S, STAGE);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wi = wave / WJ, wj = wave % WJ;
+  int ti, tj;
+  xcd_tile(blockIdx.x, ni, nj, ti, tj);
+  const int d0 = ti * TI, c0 = tj * TJ;
+  LP lp;
+  LQ lq;
+  lp.init(X, X, 2 * (size_t)D, d0, D, T, wave, lane);
+  lq.init(dl, dl, 2 * (size_t)ld, c0, (n + 7) & ~7, T, wave, lane);
+  f32x4 acc[BI][BJ] = {};
+  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
+                   stages, [](int) {},
+                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
+                       __attribute__((always_inline)) {
+                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                       });
+  const float by = scale ? scale[1] : 1.f;
+#pragma unroll
+  for (int a = 0; a < BI; ++a)
+#pragma unroll
+    for (int b = 0; b < BJ; ++b) acc[a][b] *= by;
+  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  const int cw = c0 + wj * 16 * BJ;
+  store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int r, int i, const u32x4& w) {
+    if (cw + r < n && d0 + i < D) *(u32x4*)(dW + (size_t)(cw + r) * D + d0 + i) = w;
+  });
+}
+
+__global__ __launch_bounds__(256) void linlog_zero_kernel(u32x4* out, size_t n) {
+  for (size_t e = (size_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (size_t)gridDim.x * 256)
+    out[e] = u32x4{};
+}
+
+namespace {
+
+constexpr int kFewTokens = 32;       // fragments straight from memory
+constexpr int kTokensAtOnce = 16384;   // of the forward pass: bounds its parts
+
+// Tiles of l = x w^T by rows of w and tokens.
+constexpr int kWide[4] = {256, 128, 128, 64}, kTall[4] = {256, 128, 64, 64};
+int logit_tiles(int T, int D, int n) {
+  constexpr TileTime time[4] = {
+      {6.0, 0.62, 6.0, 0.62}, {3.3, 0.26, 3.3, 0.26}, {2.7, 0.19, 2.7, 0.19}, {2.6, 0.135, 2.6, 0.135}};
+  const int nk = (2 * D + kChunk - 1) / kChunk;
+  int best = 0;
+  double least = 0.0;
+  for (int k = 0; k < 4; ++k) {
+    const long long tiles = (long long)((n + kWide[k] - 1) / kWide[k]) * ((T + kTall[k] - 1) / kTall[k]);
+    const double cost = tile_cost(tiles, nk, time[k]);
+    if (k == 0 || cost < least) {
+      best = k;
+      least = cost;
+    }
+  }
+  return best;
+}
+// Parts a token in the forward pass.
+int forward_parts(int T, int D, int V) {
+  if (T <= kFewTokens) return (V + 31) / 32;
+  const int k = logit_tiles(T, D, V);
+  return (V + kWide[k] - 1) / kWide[k];
+}
+
+// Rows of w a piece: dl of a piece at most 256 MiB (at least 1024 rows).
+int piece_rows(int T, int V) {
+  const int64_t most = std::max<int64_t>(1024, ((int64_t)1 << 27) / std::max(T, 1) / 1024 * 1024);
+  return (int)std::min<int64_t>(most, V);
+}
+
+struct DxPlan {
+  int kind;   // tiles of 256 x 256 (channels x tokens), 128 x 128, 128 x 64
+  int ni, nj, splits, each;
+};
+DxPlan dx_plan(int T, int D, int rows) {
+  const int nk = (2 * rows + kChunk - 1) / kChunk;
+  constexpr int wide[3] = {256, 128, 128}, tall[3] = {256, 128, 64};
+  constexpr TileTime time[3] = {
+      {8.0, 0.62, 8.0, 0.62}, {4.0, 0.26, 4.0, 0.26}, {3.0, 0.19, 3.0, 0.19}};
+  DxPlan best{};
+  double least = 0.0;
+  for (int kind = 0; kind < 3; ++kind) {
+    const int ni = (D + wide[kind] - 1) / wide[kind], nj = (T + tall[kind] - 1) / tall[kind];
+    for (int parts = 1; parts <= 32; ++parts) {
+      const int each = ((nk + parts - 1) / parts + 3) / 4 * 4;   // whole rounds of stages
+      const int splits = (nk + each - 1) / each;
+      if (splits != parts) continue;
+      double cost = tile_cost((long long)ni * nj * splits, each, time[kind]);
+      if (splits > 1) cost += 5.0 + 8e-6 * splits / 4.0 * T * D;
+      if (best.splits == 0 || cost < least) {
+        least = cost;
+        best = {kind, ni, nj, splits, each};
+      }
+    }
+  }
+  return best;
+}
+
+size_t pad256(size_t n) { return (n + 255) & ~(size_t)255; }
+int pad8(int n) { return (n + 7) & ~7; }
+
+}  // namespace
+
+size_t linear_logprobs_workspace_bytes(int T, int D, int V) {
+  const int most = std::min(T, kTokensAtOnce);
+  // (a shorter last share of the tokens may take smaller tiles)
+  size_t parts = (size_t)forward_parts(most, D, V) * most;
+  if (T > kTokensAtOnce && T % kTokensAtOnce)
+    parts = std::max(parts, (size_t)forward_parts(T % kTokensAtOnce, D, V) * (T % kTokensAtOnce));
+  return pad256(4 * (size_t)most) + 8 * parts;
+}
+
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+static void linlog_tiles(hipStream_t st, int T, int D, int V, const void* X, const void* W,
+                         const int64_t* targets, float* logit, float2* part) {
+  const int ni = (V + 16 * WI * BI - 1) / (16 * WI * BI);
+  const int nj = (T + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
+  hipLaunchKernelGGL((linlog_tile_kernel<KIND, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
+                     dim3(64 * WI * WJ), 0, st, X, W, T, D, V, targets, logit, part, ni, nj);
+}
+
+template <int KIND>
+static hipError_t launch_linlog_kind(hipStream_t st, int T, int D, int V, const void* X,
+                                     const void* W, const int64_t* targets, float* logprob,
+                                     float* lse, float* rest, char* ws) {
+  float* logit = (float*)ws;
+  float2* part = (float2*)(ws + pad256(4 * (size_t)std::min(T, kTokensAtOnce)));
+  for (int t0 = 0; t0 < T; t0 += kTokensAtOnce) {
+    const int n = std::min(T - t0, kTokensAtOnce);
+    const void* x = (const char*)X + (size_t)t0 * 2 * D;
+    const int64_t* to = targets + t0;
+    const int parts = forward_parts(n, D, V);
+    if (n <= kFewTokens) {
+      if (n <= 16)
+        hipLaunchKernelGGL((linlog_skinny_kernel<KIND, 1>), dim3(parts), dim3(512), 0, st, x, W, n,
+                           D, V, to, logit, part);
+      else
+        hipLaunchKernelGGL((linlog_skinny_kernel<KIND, 2>), dim3(parts), dim3(512), 0, st, x, W, n,
+                           D, V, to, logit, part);
+    } else {
+      switch (logit_tiles(n, D, V)) {
+        case 0: linlog_tiles<KIND, 4, 2, 4, 8, 4>(st, n, D, V, x, W, to, logit, part); break;
+        case 1: linlog_tiles<KIND, 4, 2, 2, 4, 4>(st, n, D, V, x, W, to, logit, part); break;
+        case 2: linlog_tiles<KIND, 4, 2, 2, 4, 2>(st, n, D, V, x, W, to, logit, part); break;
+        default: linlog_tiles<KIND, 8, 1, 2, 4, 2>(st, n, D, V, x, W, to, logit, part);
+      }
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    int tw = 1;
+    while (tw < 16 && tw < n) tw *= 2;
+    hipLaunchKernelGGL(linlog_join_kernel, dim3((n + tw - 1) / tw), dim3(256), 0, st, part, parts,
+                       n, V, tw, to, logit, logprob + t0, lse + t0, rest + t0);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_linear_logprobs(hipStream_t st, int dtype, int T, int D, int V, const void* X,
+                                  const void* W, const int64_t* targets, float* logprob,
+                                  float* lse, float* rest, char* ws) {
+  return dtype == kBF16
+             ? launch_linlog_kind<kBF16>(st, T, D, V, X, W, targets, logprob, lse, rest, ws)
+             : launch_linlog_kind<kF16>(st, T, D, V, X, W, targets, logprob, lse, rest, ws);
+}
+
+size_t linear_logprobs_backward_workspace_bytes(int T, int D, int V) {
+  const int rows = piece_rows(T, V);
+  const DxPlan p = dx_plan(T, D, rows);
+  size_t n = 256 + pad256(2 * (size_t)T * pad8(rows));
+  if (p.splits > 1 || rows < V) n += 4 * (size_t)p.splits * T * D;
+  return n;
+}
+
+template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+static void linlog_dl(hipStream_t st, int T, int D, int V, int v0, int n, int ld, const void* X,
+                      const void* W, const int64_t* targets, const float* logprob,
+                      const float* lse, const float* rest, const float* dlp, const float* dlse,
+                      const float* scale, uint16_t* dl) {
+  const int ni = (n + 16 * WI * BI - 1) / (16 * WI * BI);
+  const int nj = (T + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
+  hipLaunchKernelGGL((linlog_dl_kernel<KIND, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
+                     dim3(64 * WI * WJ), 0, st, X, W, T, D, V, v0, n, ld, targets, logprob, lse,
+                     rest, dlp, dlse, scale, dl, ni, nj);
+}
+
+template <int KIND>
+static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int V, const void* X,
+                                              const void* W, const int64_t* targets,
+                                              const float* logprob, const float* lse,
+                                              const float* rest, const float* dlp,
+                                              const float* dlse, void* dX, void* dW, char* ws) {
+  if (T == 0) {
+    if (!dW) return hipSuccess;
+    hipLaunchKernelGGL(linlog_zero_kernel, dim3(1024), dim3(256), 0, st, (u32x4*)dW,
+                       (size_t)V * D / 8);
+    return hipGetLastError();
+  }
+  if (!dX && !dW) return hipSuccess;
+  const int rows = piece_rows(T, V), ld = pad8(rows);
+  const DxPlan p = dx_plan(T, D, rows);
+  float* scale = KIND == kF16 ? (float*)ws : nullptr;   // bf16 has fp32's range
+  uint16_t* dl = (uint16_t*)(ws + 256);
+  float* part = p.splits > 1 || rows < V ? (float*)(ws + 256 + pad256(2 * (size_t)T * ld)) : nullptr;
+  if (scale) {
+    hipLaunchKernelGGL(linlog_scale_kernel, dim3(1), dim3(256), 0, st, targets, dlp, dlse, T,
+                       scale);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  for (int v0 = 0; v0 < V; v0 += rows) {
+    const int n = std::min(rows, V - v0);
+#define JARQ_LINLOG_DL(...)                                                                      \
+  linlog_dl<KIND, __VA_ARGS__>(st, T, D, V, v0, n, ld, X, W, targets, logprob, lse, rest, dlp,   \
+                               dlse, scale, dl)
+    switch (logit_tiles(T, D, n)) {
+      case 0: JARQ_LINLOG_DL(4, 2, 4, 8, 4); break;
+      case 1: JARQ_LINLOG_DL(4, 2, 2, 4, 4); break;
+      case 2: JARQ_LINLOG_DL(4, 2, 2, 4, 2); break;
+      default: JARQ_LINLOG_DL(8, 1, 2, 4, 2);
+    }
+#undef JARQ_LINLOG_DL
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (dX) {
+      const void* w = (const char*)W + (size_t)v0 * 2 * D;
+      const dim3 grid((unsigned)(p.ni * p.nj), (unsigned)p.splits);
+      const bool last = v0 + n == V;
+      uint16_t* out = p.splits == 1 && last ? (uint16_t*)dX : nullptr;
+      const int add = v0 > 0;
+      if (p.kind == 0)
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 4, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl, w,
+                           T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
+      else if (p.kind == 1)
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 4, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl, w,
+                           T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
+      else
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 4, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl, w,
+                           T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (last && p.splits > 1) {
+        const size_t all = (size_t)T * D, b = (all / 4 + 255) / 256;
+        hipLaunchKernelGGL((linlog_dx_sum_kernel<KIND>), dim3((unsigned)std::min<size_t>(b, 4096)),
+                           dim3(256), 0, st, part, p.splits, all, scale, (uint16_t*)dX);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+      }
+    }
+    if (dW) {
+      uint16_t* out = (uint16_t*)dW + (size_t)v0 * D;
+      const int ni = (D + 127) / 128, bi = (D + 255) / 256, bj = (n + 255) / 256;
+      const int nj = (n + 127) / 128, nh = (n + 63) / 64;
+      if ((long long)bi * bj >= 320)
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 4, 2, 4, 8, 4>), dim3((unsigned)(bi * bj)),
+                           dim3(512), 0, st, dl, X, T, D, n, ld, scale, out, bi, bj);
+      else if ((long long)ni * nj >= 192)
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 4, 2, 2, 4, 4>), dim3((unsigned)(ni * nj)),
+                           dim3(256), 0, st, dl, X, T, D, n, ld, scale, out, ni, nj);
+      else
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 4, 2, 2, 4, 2>), dim3((unsigned)(ni * nh)),
+                           dim3(256), 0, st, dl, X, T, D, n, ld, scale, out, ni, nh);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_linear_logprobs_backward(hipStream_t st, int dtype, int T, int D, int V,
+                                           const void* X, const void* W, const int64_t* targets,
+                                           const float* logprob, const float* lse,
+                                           const float* rest, const float* dlp,
+                                           const float* dlse, void* dX, void* dW, char* ws) {
+  return dtype == kBF16 ? launch_linlog_backward_kind<kBF16>(st, T, D, V, X, W, targets, logprob,
+                                                             lse, rest, dlp, dlse, dX, dW, ws)
+                        : launch_linlog_backward_kind<kF16>(st, T, D, V, X, W, targets, logprob,
+                                                            lse, rest, dlp, dlse, dX, dW, ws);
+}
+
+}  // namespace jarq

@@ -1,0 +1,878 @@
+"""The operators around a block on the GPU against their float64 definitions.  Tolerances
+are bounds from the arithmetic: u is half a unit in the last place of the output's type,
+E = 2^-24 that of fp32."""
+
+import itertools
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import step
+from paper_2609_38599_amd import binding as jb
+from tests._gpu_common import say
+from tests.test_gpu_blocks import E, ROUND, _close, _np, _randn
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+TYPES = [F32, F16, BF16]
+
+
+def _replays(graph, outputs, expected, disturb, times=3):
+    """Replays a graph with other work between the replays; every replay is checked."""
+    for _ in range(times):
+        for t in outputs:
+            t.fill_(float("nan") if t.is_floating_point() else 99)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outputs, expected))
+        disturb()
+        torch.cuda.synchronize()
+
+
+# ---- norm ----
+
+# one column to more than the registers hold; inside a piece of eight, at its edge and past it
+NORM = [(1, 1), (3, 7), (5, 8), (2, 65), (9, 512), (130, 513), (4, 1024), (3, 1025), (7, 2048), (5, 2501),
+        (1, 4096), (33, 4096), (600, 4104), (2, 8192), (3, 8193), (2, 16384), (2, 16385), (3, 20011)]
+
+
+def _norm_inputs(T, cols, dt, gt, seed=0):
+    x, res = _randn(seed, T, cols).to(dt), _randn(seed + 1, T, cols, std=2.0).to(dt)
+    gain = (1 + _randn(seed + 2, cols, std=0.2)).to(gt)
+    dy, dh = _randn(seed + 3, T, cols).to(dt), _randn(seed + 4, T, cols).to(dt)
+    return [t.cuda() for t in (x, res, gain, dy, dh)]
+
+
+def _sum(x, res):
+    return x if res is None else (x.float() + res.float()).to(x.dtype)
+
+
+def _check_norm(x, res, gain, eps, got, h):
+    want, r = step.norm(_np(h), _np(gain), eps)
+    u, tiny = ROUND[x.dtype]
+    # r, two products
+    _close(got, want, 4 * E * np.abs(want) + u * (1 + 4 * E) * np.abs(want) + tiny, "y")
+
+
+def _check_norm_grad(h, gain, dy, dh, eps, dx, dgain):
+    H, G, D = _np(h), _np(gain), _np(dy)
+    A = None if dh is None else _np(dh)
+    T, cols = H.shape
+    wx, wg = step.norm_grad(H, G, D, A, eps)
+    r = step.norm(H, G, eps)[1]
+    uu = np.abs(D * G)
+    mean = np.mean(uu * np.abs(H), axis=1, keepdims=True)
+    # u, r, the mean's own u, its rounding, three fused products
+    e = 6 * E * (r * uu + np.abs(H) * r ** 3 * mean) + 2 * E * (0 if A is None else np.abs(A))
+    u, tiny = ROUND[h.dtype]
+    if dx is not None:
+        _close(dx, wx, e + u * (np.abs(wx) + e) + tiny, "dx")
+    u, tiny = ROUND[gain.dtype]
+    e = (T + 4) * E * np.abs(D * H * r).sum(axis=0)
+    if dgain is not None:
+        _close(dgain, wg, e + u * (np.abs(wg) + e) + tiny, "dgain")
+
+
+@pytest.mark.parametrize("dt,gt", [(F32, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F32)])
+@pytest.mark.parametrize("T,cols", NORM)
+def test_norm_and_its_gradient(T, cols, dt, gt):
+    x, res, gain, dy, dh = _norm_inputs(T, cols, dt, gt)
+    eps = 1e-5
+    say(f"[norm] tokens {T} cols {cols} {dt} gain {gt}")
+    for r, a in ((None, None), (res, dh)):
+        h = _sum(x, r)
+        if r is None:
+            y = jb.rms_norm(x, gain, eps=eps)
+        else:
+            y, got = jb.rms_norm(x, gain, residual=r, eps=eps)
+            assert torch.equal(got, h)
+        _check_norm(x, r, gain, eps, y, h)
+        dx, dgain = jb.rms_norm_backward(h, gain, dy, dH=a, eps=eps)
+        _check_norm_grad(h, gain, dy, a, eps, dx, dgain)
+        # what is not needed is not formed, and changes nothing
+        assert torch.equal(jb.rms_norm_backward(h, gain, dy, dH=a, eps=eps, need=(True, False))[0], dx)
+        none, again = jb.rms_norm_backward(h, gain, dy, dH=a, eps=eps, need=(False, True))
+        assert none is None and torch.equal(again, dgain)
+
+
+@pytest.mark.parametrize("dt,gt", [(F32, F32), (F16, F16), (BF16, F32)])
+@pytest.mark.parametrize("T,cols", [(1, 16), (3, 160), (5, 528), (70, 4096), (2, 8208), (2, 20000)])
+def test_norm_on_8_bits(T, cols, dt, gt):
+    x, res, gain, _, _ = _norm_inputs(T, cols, dt, gt, seed=5)
+    say(f"[norm i8] tokens {T} cols {cols} {dt} gain {gt}")
+    for r in (None, res):
+        h = _sum(x, r)
+        got = jb.rms_norm_i8(x, gain, residual=r, eps=1e-5)
+        Q, scale = step.norm_i8(_np(h), _np(gain), float(np.float32(1e-5)))
+        assert np.array_equal(got[0].cpu().numpy(), Q)
+        _close(got[1], scale[:, None], 4 * E * scale[:, None], "scale")
+        assert r is None or torch.equal(got[2], h)
+    # the layer that takes them
+    wq = torch.randint(-127, 128, (40, cols), dtype=torch.int8).cuda()
+    sw = (torch.rand(40, 1) * 1e-3).cuda()
+    y = jb.matmul_i8(got[0], got[1], wq, sw, dtype=F32)
+    want = (Q.astype(np.float64) @ wq.cpu().numpy().T.astype(np.float64)) * scale[:, None] * _np(sw).T
+    _close(y, want, 10 * E * np.abs(want), "product")
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("cols", [48, 1040, 20000])
+def test_norm_of_zeros_infinities_nan_and_far_values(cols, dt):
+    most = torch.finfo(dt).max / (1 if dt == F16 else 8)     # (r is a normal number)
+    x = _randn(3, 8, cols).to(dt)
+    x[0] = 0
+    x[1, 5] = float("inf")
+    x[2, cols - 1] = float("nan")
+    x[3] = most                       # squares beyond fp32
+    x[4] = most if dt == F16 else 1e30
+    x[4, ::2] = 1.0
+    x[5] = torch.finfo(dt).tiny
+    x[6] = float("-inf")
+    x, gain = x.cuda(), (1 + _randn(4, cols, std=0.1)).to(dt).cuda()
+    y = _np(jb.rms_norm(x, gain, eps=1e-6))
+    u, tiny = ROUND[dt]
+    for t in (0, 3, 4, 5, 7):
+        want = step.norm(_np(x)[t:t + 1], _np(gain), 1e-6)[0][0]
+        assert np.all(np.abs(y[t] - want) <= (u + 5 * E) * np.abs(want) + tiny), t
+    assert np.all(np.isnan(y[2])) and np.isnan(y[1, 5]) and np.all(np.isnan(y[6]))
+    q, s = jb.rms_norm_i8(x, gain, eps=1e-6)
+    assert torch.all(q[[0, 1, 2, 6]] == 0) and s[0] == 0 and torch.all(torch.isnan(s[[1, 2, 6]]))
+    fine = [3, 4, 5, 7]
+    Q, S = step.norm_i8(_np(x)[fine], _np(gain), float(np.float32(1e-6)))
+    assert np.array_equal(q.cpu().numpy()[fine], Q)
+    assert np.all(np.abs(_np(s)[fine, 0] - S) <= 4 * E * S)
+    # gradients of rows that are fine beside those that are not
+    dy = _randn(6, 8, cols).to(dt).cuda()
+    dx = jb.rms_norm_backward(x, gain, dy, eps=1e-6)[0]
+    for t in (0, 4, 7):
+        _check_norm_grad(x[t:t + 1], gain, dy[t:t + 1], None, 1e-6, dx[t:t + 1], None)
+
+
+def test_norm_gradient_against_differences():
+    T, cols, eps = 6, 50, 1e-2
+    x, _, gain, dy, _ = _norm_inputs(T, cols, F32, F32, seed=11)
+    dx, dgain = (_np(t) for t in jb.rms_norm_backward(x, gain, dy, eps=eps))
+    X, G, D = _np(x), _np(gain), _np(dy)
+    loss = lambda X, G: (step.norm(X, G, eps)[0] * D).sum()  # noqa: E731
+    rng = np.random.default_rng(0)
+    for _ in range(20):
+        a, b = rng.normal(size=X.shape), rng.normal(size=G.shape)
+        s = 1e-5
+        want = (loss(X + s * a, G + s * b) - loss(X - s * a, G - s * b)) / (2 * s)
+        got = (dx * a).sum() + (dgain * b).sum()
+        # third derivatives times s^2, and the gradients' own roundings
+        assert abs(got - want) <= 1e-5 * (np.abs(dx * a).sum() + np.abs(dgain * b).sum())
+
+
+@pytest.mark.parametrize("cols", [40, 1003, 4096, 20000])
+def test_norm_in_place(cols):
+    x, res, gain, dy, dh = _norm_inputs(9, cols, BF16, BF16, seed=3)
+    y, h = jb.rms_norm(x, gain, residual=res)
+    for over in ("x", "res"):
+        a, b = x.clone(), res.clone()
+        y2, h2 = jb.rms_norm(a, gain, residual=b, out=a if over == "res" else None,
+                             sum_out=a if over == "x" else b)
+        assert torch.equal(y2, y) and torch.equal(h2, h)
+        assert torch.equal(a if over == "x" else b, h)
+    a = x.clone()
+    assert torch.equal(jb.rms_norm(a, gain, out=a), jb.rms_norm(x, gain))
+
+
+def test_norm_rows_at_any_element():
+    # rows of an odd length, from an odd element on: neither 16- nor 4-byte aligned
+    for dt, cols, first in ((BF16, 1001, 1), (F16, 4095, 3), (F32, 77, 1), (BF16, 20001, 5)):
+        x, res, gain, dy, dh = _norm_inputs(5, cols, dt, dt, seed=8)
+        off = []
+        for t in (x, res, gain, dy, dh):
+            flat = torch.empty(t.numel() + first, dtype=dt, device="cuda")
+            flat[first:] = t.view(-1)
+            off.append(flat[first:].view(t.shape))
+        y, h = jb.rms_norm(x, gain, residual=res)
+        back = jb.rms_norm_backward(h, gain, dy, dH=dh)
+        out = torch.full((5 * cols + first + 40,), 7.0, dtype=dt, device="cuda")
+        y2, h2 = jb.rms_norm(off[0], off[2], residual=off[1], out=out[first:first + 5 * cols].view(5, cols))
+        assert torch.equal(y2, y) and torch.equal(h2, h)
+        assert torch.all(out[:first] == 7) and torch.all(out[first + 5 * cols:] == 7)
+        assert all(torch.equal(a, b) for a, b in zip(jb.rms_norm_backward(h2, off[2], off[3], dH=off[4]), back))
+
+
+def test_norm_no_tokens_many_tokens_and_independent_rows():
+    gain = torch.ones(64, dtype=BF16, device="cuda")
+    none = torch.empty(0, 64, dtype=BF16, device="cuda")
+    y, h = jb.rms_norm(none, gain, residual=none)
+    assert y.shape == h.shape == (0, 64)
+    q, s = jb.rms_norm_i8(none, gain)
+    assert q.shape == (0, 64) and s.shape == (0, 1)
+    dx, dgain = jb.rms_norm_backward(none, gain, none)
+    assert dx.shape == (0, 64) and torch.equal(dgain, torch.zeros_like(gain))
+    wide = torch.empty(0, 20000, dtype=BF16, device="cuda")
+    assert torch.all(jb.rms_norm_backward(wide, torch.ones(20000, dtype=BF16, device="cuda"), wide)[1] == 0)
+    # a row's result is the same wherever it lies
+    x, res, gain, dy, dh = _norm_inputs(5000, 264, F16, F16, seed=21)
+    y, h = jb.rms_norm(x, gain, residual=res)
+    dx = jb.rms_norm_backward(h, gain, dy, dH=dh)[0]
+    for a, b in ((0, 1), (7, 300), (4998, 5000)):
+        assert torch.equal(jb.rms_norm(x[a:b], gain, residual=res[a:b])[0], y[a:b])
+        assert torch.equal(jb.rms_norm_backward(h[a:b], gain, dy[a:b], dH=dh[a:b])[0], dx[a:b])
+
+
+def test_norm_of_more_values_than_31_bits_count():
+    T, cols = 540000, 4096
+    gain = (1 + _randn(0, cols, std=0.1)).to(BF16).cuda()
+    x = torch.empty(T, cols, dtype=BF16, device="cuda")
+    for part in x.split(60000):
+        part.normal_()
+    y = jb.rms_norm(x, gain)
+    q, s = jb.rms_norm_i8(x, gain)
+    dx, _ = jb.rms_norm_backward(x, gain, y)
+    for a in (0, 524287, T - 2):
+        b = a + 2
+        assert torch.equal(jb.rms_norm(x[a:b], gain), y[a:b])
+        assert torch.equal(jb.rms_norm_i8(x[a:b], gain)[0], q[a:b])
+        assert torch.equal(jb.rms_norm_backward(x[a:b], gain, y[a:b])[0], dx[a:b])
+    _check_norm(x[-2:], None, gain, 1e-6, y[-2:], x[-2:])
+
+
+def test_norm_on_another_stream_and_in_a_graph():
+    x, res, gain, dy, dh = _norm_inputs(300, 2504, BF16, BF16, seed=31)
+    y, h = jb.rms_norm(x, gain, residual=res)
+    back = jb.rms_norm_backward(h, gain, dy, dH=dh)
+    q = jb.rms_norm_i8(x[:, :2496].contiguous(), gain[:2496].contiguous())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    y2, h2 = jb.rms_norm(x, gain, residual=res, stream=s)
+    back2 = jb.rms_norm_backward(h2, gain, dy, dH=dh, stream=s)
+    s.synchronize()
+    assert torch.equal(y2, y) and torch.equal(h2, h) and all(torch.equal(a, b) for a, b in zip(back, back2))
+    xs, gs = x[:, :2496].contiguous(), gain[:2496].contiguous()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        gy, gh = jb.rms_norm(x, gain, residual=res)
+        gb = jb.rms_norm_backward(gh, gain, dy, dH=dh)
+        gq = jb.rms_norm_i8(xs, gs)
+    _replays(graph, [gy, gh, *gb, *gq], [y, h, *back, *q],
+             lambda: jb.rms_norm_backward(h, gain, dh, dH=dy))
+
+
+# ---- log probabilities from hidden states ----
+
+# tokens of every way through (few, the tiles, more than one), vocabularies inside a tile, at
+# its edge and past it, channels of half a chunk and of several
+LINLOG = [(1, 8, 1), (1, 72, 33), (2, 64, 7), (16, 136, 100), (17, 1000, 65), (32, 8, 300), (33, 72, 257),
+          (64, 264, 64), (65, 128, 1000), (129, 520, 513), (257, 200, 1025), (300, 64, 5003)]
+
+
+def _linlog_inputs(T, d, V, dt, seed=0, std=2.0):
+    w = _randn(seed, V, d, std=std / d ** 0.5).to(dt)
+    gen = torch.Generator().manual_seed(seed + 1)
+    targets = torch.randint(0, V, (T,), generator=gen)
+    x = _randn(seed + 2, T, d)
+    x += w.float()[targets] * (torch.rand(T, 1, generator=gen) * 4)
+    targets[torch.rand(T, generator=gen) < 0.2] = -1
+    g, h = _randn(seed + 3, T), _randn(seed + 4, T, std=0.1)
+    return [t.cuda() for t in (x.to(dt), w, targets, g, h)]
+
+
+def _linlog_bounds(X, W, targets):
+    """(logits, p, a bound on log p's error at every entry, one on lse's)."""
+    T, d = X.shape
+    logits = X @ W.T
+    el = (d + 2) * E * (np.abs(X) @ np.abs(W).T)            # d products summed in fp32
+    m = logits.max(axis=1, keepdims=True)
+    p = np.exp(logits - m)
+    p /= p.sum(axis=1, keepdims=True)
+    # exp to two ulps and its argument's rounding; joins and sums of up to 256 terms in a row
+    term = el + el.max(axis=1, keepdims=True) + (np.abs(logits - m) * 3 + 4) * E
+    lse = (p * term).sum(axis=1, keepdims=True) + 260 * E
+    return logits, p, el + lse, lse
+
+
+def _check_linlog(x, w, targets, r, back=None, g=None, h=None):
+    X, W, to = _np(x), _np(w), targets.cpu().numpy()
+    lp, lse, p = step.linear_logprobs(X, W, to)
+    logits, _, ep, elz = _linlog_bounds(X, W, to)
+    T, d = X.shape
+    at = np.clip(to, 0, len(W) - 1)
+    m = logits.max(axis=1)
+    el = np.where(to >= 0, ep[np.arange(T), at], 0)
+    _close(r.logprob, lp, el + 3 * E * (np.abs(lp) + np.abs(logits[np.arange(T), at] - m)), "logprob")
+    _close(r.lse, lse, elz[:, 0] + 3 * E * (np.abs(lse) + np.abs(m)), "lse")
+    off = np.abs(_np(r.lse) + _np(r.lse_rest) - lse)
+    assert np.all(off <= elz[:, 0] + 2 * E * np.abs(lse - m) + 1e-12)
+    if back is None:
+        return
+    G, Hh = _np(g), np.zeros(T) if h is None else _np(h)
+    dX, dW, dl = step.linear_logprobs_grad(X, W, to, G, Hh)
+    G = np.where(to >= 0, G, 0.0)
+    # p from the logits formed again, then rounded to 16 bits
+    e = (np.abs(Hh - G)[:, None] * p) * (ep + (np.abs(logits - lse[:, None]) * 3 + 8) * E)
+    e += (np.abs(G) + np.abs(Hh))[:, None] * (np.arange(len(W))[None] == to[:, None]) * (el + 8 * E)[:, None]
+    u, tiny = ROUND[x.dtype]
+    most = max(np.abs(G).max(), np.abs(Hh).max(), np.abs(Hh - G).max())
+    small = tiny if x.dtype == BF16 else 2.0 ** -25 * max(most, 1e-300) * 2.0 ** -13
+    e = e + u * (np.abs(dl) + e) + small
+
+    def product(err, size, want, n):
+        e = err + (n + 2) * E * (size + err)
+        return e + u * (np.abs(want) + e) + tiny
+
+    if back[0] is not None:
+        _close(back[0], dX, product(e @ np.abs(W), np.abs(dl) @ np.abs(W), dX, len(W)), "dX")
+    if back[1] is not None:
+        _close(back[1], dW, product(e.T @ np.abs(X), np.abs(dl).T @ np.abs(X), dW, T), "dW")
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T,d,V", LINLOG)
+def test_linear_logprobs_and_gradients(T, d, V, dt):
+    x, w, targets, g, h = _linlog_inputs(T, d, V, dt)
+    say(f"[linlog] tokens {T} d {d} vocab {V} {dt}")
+    r = jb.linear_logprobs(x, w, targets)
+    _check_linlog(x, w, targets, r)
+    back = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    _check_linlog(x, w, targets, r, back, g, h)
+    only = jb.linear_logprobs_backward(x, w, targets, r, g)
+    _check_linlog(x, w, targets, r, only, g)
+    a = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h, need=(True, False))
+    b = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h, need=(False, True))
+    assert a[1] is None and b[0] is None and torch.equal(a[0], back[0]) and torch.equal(b[1], back[1])
+    assert jb.linear_logprobs_backward(x, w, targets, r, g, need=(False, False)) == (None, None)
+
+
+def test_linear_logprobs_agree_with_those_of_stored_logits():
+    x, w, targets, g, _ = _linlog_inputs(70, 256, 3001, BF16, seed=4)
+    r = jb.linear_logprobs(x, w, targets)
+    logits = x.double() @ w.double().t()
+    s = jb.token_logprobs(logits.float(), targets)
+    X, W = _np(x), _np(w)
+    bound = _linlog_bounds(X, W, None)[2].max(axis=1) + 6 * E * np.abs(_np(logits)).max(axis=1)
+    assert np.all(np.abs(_np(r.logprob) - _np(s.logprob)) <= bound + 8 * E * np.abs(_np(s.logprob)))
+    assert np.all(np.abs(_np(r.lse) - _np(s.lse)) <= bound)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T", [2, 90])
+def test_linear_logprob_of_a_token_that_takes_nearly_all(T, dt):
+    # log p is what the others take: right to itself, where 1 - p is below fp32's half unit
+    d, V = 64, 700
+    w = _randn(0, V, d, std=0.02)
+    w[:, 0] = 0
+    w[5] = 0
+    w[5, 0] = 1
+    x = _randn(1, T, d)
+    x[:, 0] = torch.linspace(12, 30, T)
+    x, w = x.to(dt).cuda(), w.to(dt).cuda()
+    targets = torch.full((T,), 5, device="cuda")
+    r = jb.linear_logprobs(x, w, targets)
+    X, W = _np(x), _np(w)
+    logits = X @ W.T
+    other = np.exp(np.delete(logits, 5, axis=1) - logits[:, 5:6]).sum(axis=1)
+    want = -np.log1p(other)
+    el = (d + 2) * E * (np.abs(X) @ np.abs(W).T).max(axis=1)
+    rel = 2 * el + 3 * E * np.abs(logits - logits[:, 5:6]).max(axis=1) + 60 * E
+    assert np.all(np.abs(_np(r.logprob) - want) <= rel * np.abs(want))
+    g = torch.ones(T, device="cuda")
+    dx = _np(jb.linear_logprobs_backward(x, w, targets, r, g)[0])
+    p = np.exp(logits - logits[:, 5:6]) / (1 + other)[:, None]
+    dl = -p
+    dl[:, 5] = other / (1 + other)
+    u, tiny = ROUND[dt]
+    size = np.abs(dl) @ np.abs(W)
+    small = tiny if dt == BF16 else 2.0 ** -38
+    bound = (rel[:, None] + 2 * u + (V + 10) * E) * size + small * np.abs(W).sum(axis=0) + u * size + tiny
+    assert np.all(np.abs(dx - dl @ W) <= bound)
+
+
+def test_linear_logprobs_of_masked_broken_and_wrong_targets():
+    x, w, targets, g, h = _linlog_inputs(40, 64, 300, BF16, seed=9)
+    targets[:] = -1
+    r = jb.linear_logprobs(x, w, targets)
+    assert torch.all(r.logprob == 0) and torch.all(torch.isfinite(r.lse))
+    dx, dw = jb.linear_logprobs_backward(x, w, targets, r, torch.full_like(g, float("nan")))
+    assert torch.all(dx == 0) and torch.all(dw == 0)      # a gradient of no target is not read
+    for T in (3, 40):
+        to = targets[:T].clone()
+        to[0], to[1], to[2] = 300, 2 ** 40, -2 ** 60
+        r = jb.linear_logprobs(x[:T], w, to)
+        assert torch.isnan(r.logprob[0]) and torch.isnan(r.logprob[1]) and r.logprob[2] == 0
+        bad = x[:T].clone()
+        bad[0, 3] = float("nan")
+        bad[1, 4] = float("inf")
+        r = jb.linear_logprobs(bad, w, to.fill_(7))
+        assert torch.all(torch.isnan(r.logprob[:2])) and torch.all(torch.isnan(r.lse[:2]))
+        good = jb.linear_logprobs(x[:T], w, to)
+        assert torch.equal(r.logprob[2:], good.logprob[2:]) and torch.equal(r.lse[2:], good.lse[2:])
+        # the other tokens' gradients are theirs
+        dx = jb.linear_logprobs_backward(bad, w, to, r, g[:T], need=(True, False))[0]
+        want = jb.linear_logprobs_backward(x[:T], w, to, good, g[:T], need=(True, False))[0]
+        assert torch.equal(dx[2:], want[2:]) and torch.all(torch.isnan(dx[:2]))
+
+
+def test_linear_logprobs_of_tied_and_equal_logits():
+    # every logit the same: the maximum's own 1 is kept apart once, not for each tie
+    for T, V in ((1, 1), (3, 500), (80, 1000), (80, 1)):
+        x = torch.ones(T, 64, dtype=BF16, device="cuda")
+        w = torch.full((V, 64), 0.5, dtype=BF16, device="cuda")
+        to = torch.arange(T, device="cuda") % V
+        r = jb.linear_logprobs(x, w, to)
+        assert np.all(np.abs(_np(r.logprob) + np.log(V)) <= 4 * E * (1 + np.log(V)))
+        assert np.all(np.abs(_np(r.lse) - 32 - np.log(V)) <= 4 * E * 40)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T,d,V,seed", [(40, 1000, 9001, 0), (200, 520, 20011, 1), (1025, 264, 8200, 2),
+                                        (700, 1032, 33000, 3), (2100, 1032, 70001, 4)])
+def test_linear_logprobs_of_many_tiles_and_pieces(T, d, V, dt, seed):
+    # on the GPU in 64 bits; the last size takes two pieces of the vocabulary
+    x, w, targets, g, h = _linlog_inputs(T, d, V, dt, seed=seed)
+    say(f"[linlog] tokens {T} d {d} vocab {V} {dt}")
+    if dt == F16:
+        g, h = g * 1e-6, h * 1e-6       # far below the type's range without the scaling
+    r = jb.linear_logprobs(x, w, targets)
+    X, W = x.double(), w.double()
+    logits = X @ W.t()
+    lse = torch.logsumexp(logits, 1)
+    has = targets >= 0
+    lp = torch.where(has, logits.gather(1, targets.clamp_min(0)[:, None])[:, 0] - lse, 0.0)
+    el = (d + 2) * E * (X.abs().sum(1) * W.abs().max() + 20)
+    assert torch.all((r.lse - lse).abs() <= 2 * el + 300 * E + 4 * E * lse.abs())
+    assert torch.all((r.logprob - lp).abs() <= 3 * el + 300 * E + 4 * E * lp.abs())
+    dx, dw = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    again = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    assert torch.equal(dx, again[0]) and torch.equal(dw, again[1])
+    G = torch.where(has, g, 0.0).double()
+    dl = (h.double() - G)[:, None] * torch.exp(logits - lse[:, None])
+    dl.scatter_add_(1, targets.clamp_min(0)[:, None], G[:, None])
+    u, tiny = ROUND[dt]
+    for got, want, a, b in ((dx, dl @ W, dl, W), (dw, dl.t() @ X, dl.t(), X)):
+        off = (got.double() - want).abs()
+        # dl's rounding and the output's, each entry by itself; p's relative error
+        size = a.abs() @ b.abs()
+        rel = 2 * u + (el.max().item() * 4 + 400 * E) + 1e-3 * u
+        floor = 0.0 if dt == BF16 else 2.0 ** -38 * max(g.abs().max().item(), h.abs().max().item()) * 2
+        bound = rel * size + floor * b.abs().sum(0, keepdim=True) + tiny
+        assert torch.all(off <= bound), (off / bound).max()
+        # independent roundings: 1.5 times one rounding's norm
+        if dt == BF16:
+            assert off.norm() <= 1.5 * u * want.norm()
+
+
+def test_linear_logprob_gradient_against_differences():
+    T, d, V = 12, 40, 90
+    x, w, targets, g, h = _linlog_inputs(T, d, V, F16, seed=13)
+    r = jb.linear_logprobs(x, w, targets)
+    dx, dw = (_np(t) for t in jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h))
+    X, W, to, G, H = _np(x), _np(w), targets.cpu().numpy(), _np(g), _np(h)
+
+    def loss(X, W):
+        lp, lse, _ = step.linear_logprobs(X, W, to)
+        return (G * lp + H * lse).sum()
+
+    dl = np.abs(step.linear_logprobs_grad(X, W, to, G, H)[2])
+    sx, sw = dl @ np.abs(W), dl.T @ np.abs(X)
+    rng = np.random.default_rng(1)
+    for _ in range(20):
+        a, b, s = rng.normal(size=X.shape), rng.normal(size=W.shape), 1e-5
+        want = (loss(X + s * a, W + s * b) - loss(X - s * a, W - s * b)) / (2 * s)
+        got = (dx * a).sum() + (dw * b).sum()
+        # dl's rounding and the output's, a half unit each; the rest is far below a third
+        assert abs(got - want) <= 3 * 2.0 ** -11 * ((sx * np.abs(a)).sum() + (sw * np.abs(b)).sum())
+
+
+def test_linear_logprobs_no_tokens_streams_and_graphs():
+    x, w, targets, g, h = _linlog_inputs(150, 136, 2000, BF16, seed=17)
+    r = jb.linear_logprobs(x[:0], w, targets[:0])
+    assert r.logprob.shape == (0,)
+    dx, dw = jb.linear_logprobs_backward(x[:0], w, targets[:0], r, g[:0])
+    assert dx.shape == (0, 136) and torch.all(dw == 0)
+    for T in (5, 150):
+        a = (x[:T], w, targets[:T])
+        r = jb.linear_logprobs(*a)
+        back = jb.linear_logprobs_backward(*a, r, g[:T], d_lse=h[:T])
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        r2 = jb.linear_logprobs(*a, stream=s)
+        back2 = jb.linear_logprobs_backward(*a, r2, g[:T], d_lse=h[:T], stream=s)
+        s.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip((*r, *back), (*r2, *back2)))
+        torch.cuda.synchronize()
+        graph, other = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            gr = jb.linear_logprobs(*a)
+            gb = jb.linear_logprobs_backward(*a, gr, g[:T], d_lse=h[:T])
+        with torch.cuda.graph(other):
+            jb.linear_logprobs_backward(*a, r, h[:T], d_lse=g[:T])
+        _replays(graph, [*gr, *gb], [*r, *back],
+                 lambda: (other.replay(), jb.linear_logprobs(x, w, targets)))
+
+
+def test_linear_logprobs_of_weights_past_32_bits():
+    # 2^32 bytes of weights and more; the last rows are read and written
+    V, d, T = 600000, 4096, 3
+    w = torch.empty(V, d, dtype=BF16, device="cuda")
+    for part in w.split(100000):
+        part.normal_(std=0.03)
+    x = torch.randn(T, d, device="cuda").to(BF16)
+    to = torch.tensor([V - 1, 0, 530000], device="cuda")
+    r = jb.linear_logprobs(x, w, to)
+    many = jb.linear_logprobs(x.repeat(20, 1), w, to.repeat(20))
+    logits = torch.cat([x.double() @ p.double().t() for p in w.split(50000)], 1)
+    lse = torch.logsumexp(logits, 1)
+    lp = logits.gather(1, to[:, None])[:, 0] - lse
+    el = (d + 2) * E * (x.abs().double().sum(1) * w.abs().max().double())
+    for got in (r.logprob, many.logprob[:T], many.logprob[-T:]):
+        assert torch.all((got - lp).abs() <= 2 * el + 300 * E + 8 * E * lse.abs())
+    g = torch.ones(T, device="cuda")
+    dx, dw = jb.linear_logprobs_backward(x, w, to, r, g)
+    p = torch.exp(logits - lse[:, None])
+    dl = -p
+    dl.scatter_add_(1, to[:, None], g.double()[:, None])
+    want = sum(dl[:, i:i + 50000] @ w[i:i + 50000].double() for i in range(0, V, 50000))
+    assert (dx.double() - want).norm() <= 1.5 * ROUND[BF16][0] * want.norm()
+    for a in (0, 530000, V - 8):
+        rows = (dl[:, a:a + 8].t() @ x.double())
+        assert (dw[a:a + 8].double() - rows).norm() <= 1.5 * ROUND[BF16][0] * rows.norm() + 1e-30
+
+
+# ---- AdamW ----
+
+NUMELS = (1, 5, 127, 128, 129, 1000, 2047, 2048, 2049, 9000, 4096 * 3)
+OPT = dict(beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1)
+
+
+def _adamw_inputs(numels, dt, seed=0, steps=3):
+    params = [_randn(seed + 7 * k, n, std=0.1).to(dt).cuda() for k, n in enumerate(numels)]
+    grads = [[(_randn(seed + 1000 * t + k, n, std=1e-3) * torch.exp(2 * _randn(seed + k + 5000, n))).to(dt).cuda()
+              for k, n in enumerate(numels)] for t in range(1, steps + 1)]
+    return params, grads
+
+
+class _Replay:
+    """The step on the CPU: the moments bit by bit, the parameters in 64 bits."""
+
+    def __init__(self, params, state, bits):
+        self.at, self.n = step.offsets([p.numel() for p in params])
+        self.numels = [p.numel() for p in params]
+        self.bits, self.dt = bits, params[0].dtype
+        self.live = np.zeros(self.n, dtype=bool)
+        for a, k in zip(self.at, self.numels):
+            self.live[a:a + k] = True
+        self.p = self.flat(params)
+        self.s = [None if t is None else t.cpu().view(torch.uint8).numpy().copy()
+                  if t.dtype == torch.float8_e4m3fn else t.cpu().numpy().copy() for t in state]
+
+    def flat(self, tensors):
+        out = np.zeros(self.n)
+        for a, t in zip(self.at, tensors):
+            out[a:a + t.numel()] = _np(t).reshape(-1)
+        return out
+
+    def check(self, grads, t, lr, seed, params, state, mul=None):
+        """Advances by one step and compares with what the GPU has."""
+        g = self.flat(grads).astype(np.float32)
+        if mul is not None:
+            g = g * np.float32(mul)
+        m0, v0 = self.s[1], self.s[2]
+        if self.bits == 8:
+            m0 = step.decode(m0, self.s[3])
+            root = step.decode(v0, self.s[4])
+            v0 = root * root
+        m, v, root = step.moments(g, m0, v0, OPT["beta1"], OPT["beta2"])
+        if self.bits == 8:
+            low, high = step.noise(np.arange(self.n), seed, t)
+            (cm, em), (cv, ev) = step.encode(m, low, False), step.encode(root, high, True)
+            want = (cm, cv, em, ev)
+        else:
+            want = (m, v)
+        p0 = self.p if self.s[0] is None else self.s[0].astype(np.float64)
+        p = np.where(self.live, step.adamw(p0, m, v, t, lr, **OPT), 0)
+        got = [None if a is None else a.cpu() for a in state]
+        for a, w, name in zip(got[1:], want, ("m", "v", "m_exp", "v_exp")):
+            a = a.view(torch.uint8).numpy() if a.dtype == torch.float8_e4m3fn else a.numpy()
+            assert np.array_equal(a, w, equal_nan=a.dtype.kind == "f"), (name, t)
+        # the rate, the root's factor, eps, a quotient to an ulp and two products; p's own
+        move = np.abs(p - p0 * (1 - lr * OPT["weight_decay"]))
+        bound = 3 * E * np.abs(p0) + 12 * E * move + E * np.abs(p) + 1e-45
+        now = self.flat(params)
+        if self.s[0] is None:
+            off = np.abs(now - p)
+        else:
+            master = got[0].numpy().astype(np.float64)
+            off = np.abs(master - p)
+            rounded = got[0].to(self.dt).double().numpy()
+            assert np.array_equal(now, np.where(self.live, rounded, 0))
+        fine = np.isfinite(p)
+        assert np.all(off[fine] <= bound[fine]), (t, (off[fine] / bound[fine]).max())
+        assert np.all(np.isnan(now[~fine]))
+        self.p = now
+        self.s = [None if a is None else a.view(torch.uint8).numpy().copy()
+                  if a.dtype == torch.float8_e4m3fn else a.numpy().copy() for a in got]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dt", TYPES)
+def test_adamw_steps(dt, bits):
+    params, grads = _adamw_inputs(NUMELS, dt)
+    state = jb.adamw_state(params, bits=bits)
+    mine = _Replay(params, state, bits)
+    say(f"[adamw] {dt} {bits} bits")
+    for t, g in enumerate(grads, 1):
+        got = jb.adamw_step(params, g, state, t, 1e-2, seed=77, **OPT)
+        assert got[0][0] is params[0] and got[1] is state
+        mine.check(g, t, 1e-2, 77, params, state)
+    m, v = jb.adamw_moments(state)
+    if bits == 8:
+        assert np.array_equal(m.cpu().numpy(), step.decode(mine.s[1], mine.s[3]))
+        root = step.decode(mine.s[2], mine.s[4])
+        assert np.array_equal(v.cpu().numpy(), root * root)
+    else:
+        assert m is state.m and v is state.v
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_adamw_of_more_tensors_than_a_launch_takes(dt, bits):
+    # some at odd elements, some empty, some of several units
+    gen = np.random.default_rng(0)
+    numels = [int(n) for n in np.exp(gen.uniform(0, 9, 150))] + [0, 70001, 0]
+    first, grads = _adamw_inputs(numels, dt, seed=3, steps=2)
+    hold = torch.full((sum(numels) + 3 * len(numels) + 16,), 5.0, dtype=dt, device="cuda")
+    params, at, used = [], 1, torch.zeros(len(hold), dtype=torch.bool, device="cuda")
+    for p in first:
+        view = hold[at:at + p.numel()]
+        view.copy_(p)
+        used[at:at + p.numel()] = True
+        params.append(view)
+        at += p.numel() + 3
+    state = jb.adamw_state(params, bits=bits)
+    mine = _Replay(params, state, bits)
+    for t, g in enumerate(grads, 1):
+        jb.adamw_step(params, g, state, t, 1e-2, seed=-5, **OPT)
+        mine.check(g, t, 1e-2, 2 ** 64 - 5, params, state)
+    assert torch.all(hold[~used] == 5)           # nothing beside the tensors is written
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dt", [F32, F16])
+def test_adamw_into_other_tensors(dt, bits):
+    params, grads = _adamw_inputs(NUMELS, dt, seed=9)
+    state = jb.adamw_state(params, bits=bits)
+    jb.adamw_step(params, grads[0], state, 1, 1e-2, seed=1, **OPT)
+    keep = [p.clone() for p in params], [None if s is None else s.clone() for s in state]
+    to = [torch.zeros_like(p) for p in params], jb.adamw_state(params, bits=bits)
+    got = jb.adamw_step(params, grads[1], state, 2, 1e-2, seed=1, out=to, **OPT)
+    assert got[1] is to[1]
+    same = lambda a, b: a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8))  # noqa: E731
+    assert all(torch.equal(a, b) for a, b in zip(params, keep[0])) and all(map(same, state, keep[1]))
+    jb.adamw_step(params, grads[1], state, 2, 1e-2, seed=1, **OPT)
+    assert all(torch.equal(a, b) for a, b in zip(params, to[0])) and all(map(same, state, to[1]))
+    # a step that is left out gives a copy
+    nan = torch.tensor([float("nan")], device="cuda")
+    for s in to[1]:
+        if s is not None:
+            s.view(torch.uint8).fill_(3)
+    jb.adamw_step(params, grads[2], state, 3, 1e-2, grad_mul=nan, out=to, **OPT)
+    assert all(torch.equal(a, b) for a, b in zip(params, to[0]))
+    live = torch.from_numpy(_Replay(params, state, bits).live).cuda()
+    for a, b in zip(state, to[1]):
+        if a is not None:
+            assert torch.equal(a, b) if len(a) < len(live) else torch.equal(a.float()[live], b.float()[live])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_multiplied_left_out_and_missing_gradients(bits):
+    params, grads = _adamw_inputs(NUMELS, BF16, seed=12)
+    state = jb.adamw_state(params, bits=bits)
+    mine = _Replay(params, state, bits)
+    mul = torch.tensor([0.37], device="cuda")
+    jb.adamw_step(params, grads[0], state, 1, 1e-2, grad_mul=mul, seed=4, **OPT)
+    mine.check(grads[0], 1, 1e-2, 4, params, state, mul=0.37)
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        jb.adamw_step(params, grads[1], state, 2, 1e-2, grad_mul=mul.fill_(bad), seed=4, **OPT)
+        assert np.array_equal(mine.flat(params), mine.p)
+    kept = [p.clone() for p in params]
+    jb.adamw_step(params, [None if k % 3 == 0 else g for k, g in enumerate(grads[1])], state, 2, 1e-2, seed=4, **OPT)
+    assert all(torch.equal(p, q) == (k % 3 == 0) for k, (p, q) in enumerate(zip(params, kept)))
+    m, _ = jb.adamw_moments(state)
+    for k, (a, n) in enumerate(zip(mine.at, mine.numels)):
+        if k % 3 == 0 and bits == 32:
+            assert np.array_equal(m[a:a + n].cpu().numpy(), mine.s[1][a:a + n])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_adamw_of_zero_far_and_broken_gradients(bits):
+    n = 128 * 12 + 40
+    params, _ = _adamw_inputs((n,), F32, seed=20)
+    state = jb.adamw_state(params, bits=bits)
+    mine = _Replay(params, state, bits)
+    for t in range(1, 4):
+        g = _randn(t, n, std=1e-3)
+        g[128:256] = 0
+        g[256:384] = 1e15
+        g[384:512] *= 1e-36                       # moments and roots far down
+        g[512:640] *= torch.exp(torch.linspace(-40, 5, 128))
+        if t == 2:
+            g[700] = float("nan")
+            g[800] = float("inf")
+            g[1000] = 3e38                        # its square passes fp32
+        jb.adamw_step(params, [g.cuda()], state, t, 1e-2, seed=6, **OPT)
+        mine.check([g], t, 1e-2, 6, params, state)
+    assert torch.all(torch.isfinite(params[0][:640])) and torch.all(torch.isfinite(params[0][1100:]))
+
+
+def test_adamw_from_device_numbers_in_a_graph():
+    # the step's number, rate and multiplier are read when the graph runs; an eager step between
+    for dt, bits in itertools.product((F32, BF16), (32, 8)):
+        params, grads = _adamw_inputs(NUMELS, dt, seed=30, steps=4)
+        state = jb.adamw_state(params, bits=bits)
+        eager = [p.clone() for p in params], jb.adamw_state(params, bits=bits)
+        number = torch.zeros(1, dtype=torch.int64, device="cuda")
+        rate, mul = torch.zeros(1, device="cuda"), torch.ones(1, device="cuda")
+        g = [torch.zeros_like(p) for p in params]
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            jb.adamw_step(params, g, state, number, rate, grad_mul=mul, seed=8, **OPT)
+        graph.replay()                            # step 0: nothing
+        assert all(torch.equal(a, b) for a, b in zip(params, eager[0]))
+        for t, now in enumerate(grads, 1):
+            lr = float(np.float32(0.01 / t))
+            number.fill_(t)
+            rate.fill_(lr)
+            mul.fill_(1.0 / t)
+            for a, b in zip(g, now):
+                a.copy_(b)
+            graph.replay()
+            jb.adamw_step(eager[0], now, eager[1], t, lr, grad_mul=mul, seed=8, **OPT)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(params, eager[0]))
+            assert all(a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+                       for a, b in zip(state, eager[1]))
+
+
+def test_adamw_on_another_stream():
+    params, grads = _adamw_inputs(NUMELS, BF16, seed=40)
+    other = [p.clone() for p in params]
+    a, b = (jb.adamw_state(params, bits=8) for _ in range(2))
+    jb.adamw_step(params, grads[0], a, 1, 1e-2, **OPT)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    jb.adamw_step(other, grads[0], b, 1, 1e-2, stream=s, **OPT)
+    s.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(params, other))
+
+
+def test_adamw_refuses_a_tensor_twice():
+    p = torch.zeros(500, device="cuda")
+    g = torch.ones(500, device="cuda")
+    state = jb.adamw_state([p, p])
+    with pytest.raises(jb.JarqError):
+        jb.adamw_step([p, p], [g, g], state, 1, 1e-2)
+    half = jb.adamw_state([p[:300], p[200:]])
+    with pytest.raises(jb.JarqError):
+        jb.adamw_step([p[:300], p[200:]], [g[:300], g[200:]], half, 1, 1e-2)
+    with pytest.raises(jb.JarqError):
+        jb.adamw_step([p], [p], jb.adamw_state([p]), 1, 1e-2)
+    assert torch.all(p == 0)
+
+
+def test_adamw_of_a_tensor_past_32_bits():
+    n = 2 ** 32 + 2 ** 12 + 40
+    p = torch.zeros(n, dtype=BF16, device="cuda")
+    g = torch.zeros(n, dtype=BF16, device="cuda")
+    spans = [(0, 256), (2 ** 31, 256), (2 ** 32 - 128, 256), (n - 168, 168)]
+    for k, (a, m) in enumerate(spans):
+        p[a:a + m] = _randn(k, m, std=0.1).to(BF16).cuda()
+        g[a:a + m] = _randn(k + 9, m, std=1e-3).to(BF16).cuda()
+    state = jb.adamw_state([p], bits=8)
+    before = [_np(state.master[a:a + m]) for a, m in spans]
+    jb.adamw_step([p], [g], state, 1, 1e-2, seed=3, **OPT)
+    for (a, m), p0 in zip(spans, before):
+        whole = m // 128 * 128
+        G = _np(g[a:a + whole]).astype(np.float32)
+        mo, v, root = step.moments(G, np.zeros(whole), np.zeros(whole), OPT["beta1"], OPT["beta2"])
+        low, high = step.noise(np.arange(a, a + whole), 3, 1)
+        for x, dither, codes, exps, pos in ((mo, low, state.m, state.m_exp, False),
+                                            (root, high, state.v, state.v_exp, True)):
+            c, e = step.encode(x, dither, pos)
+            assert np.array_equal(codes[a:a + whole].view(torch.uint8).cpu().numpy(), c)
+            assert np.array_equal(exps[a // 128:(a + whole) // 128].cpu().numpy(), e)
+        want = step.adamw(p0[:whole], mo, v, 1, 1e-2, **OPT)
+        assert np.all(np.abs(_np(state.master[a:a + whole]) - want) <= 16 * E * (np.abs(want) + 0.02))
+        assert torch.equal(state.master[a:a + m].to(BF16), p[a:a + m])
+
+
+# ---- together ----
+
+def test_results_outside_the_graph_are_said_to_be():
+    x = torch.randn(4, 64, device="cuda").to(BF16).requires_grad_()
+    w, gain = torch.randn(9, 64, device="cuda").to(BF16), torch.ones(64, dtype=BF16, device="cuda")
+    to = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for call in (lambda: jb.rms_norm(x, gain), lambda: jb.rms_norm_i8(x, gain),
+                 lambda: jb.linear_logprobs(x, w, to)):
+        with pytest.warns(UserWarning, match="autograd"):
+            call()
+
+
+def test_a_training_step_of_a_block():
+    """Norm, gated block, norm, loss and back, then the step on all weights: against autograd in
+    64 bits, whose roundings are none."""
+    T, d, f, V, dt = 96, 128, 264, 777, BF16
+    gen = lambda seed, *s, std=1.0: _randn(seed, *s, std=std).to(dt).cuda()  # noqa: E731
+    x = gen(0, T, d)
+    g1, g2 = ((1 + _randn(k, d, std=0.1)).to(dt).cuda() for k in (1, 2))
+    wg, wu, wd = gen(3, f, d, std=d ** -0.5), gen(4, f, d, std=d ** -0.5), gen(5, d, f, std=f ** -0.5)
+    head = gen(6, V, d, std=2 * d ** -0.5)
+    targets = torch.randint(0, V, (T,), generator=torch.Generator().manual_seed(7)).cuda()
+    g = torch.full((T,), -1.0 / T, device="cuda")
+
+    n1 = jb.rms_norm(x, g1)
+    h, pre = jb.gated_forward(n1, wg, wu, save=True)
+    n2, s2 = jb.rms_norm(h @ wd.t(), g2, residual=x)
+    r = jb.linear_logprobs(n2, head, targets)
+    dn2, dhead = jb.linear_logprobs_backward(n2, head, targets, r, g)
+    ds, dg2 = jb.rms_norm_backward(s2, g2, dn2)
+    dwd = ds.t().contiguous() @ h
+    dn1, dwg, dwu = jb.gated_backward(n1, wg, wu, ds @ wd, pre)
+    dx, dg1 = jb.rms_norm_backward(x, g1, dn1, dH=ds)
+
+    leaves = [t.detach().cpu().double().requires_grad_() for t in (x, g1, wg, wu, wd, g2, head)]
+    X, G1, Wg, Wu, Wd, G2, Head = leaves
+    rms = lambda a, w: a / (a.square().mean(1, keepdim=True) + 1e-6).sqrt() * w  # noqa: E731
+    N1 = rms(X, G1)
+    S2 = X + torch.nn.functional.silu(N1 @ Wg.t()) * (N1 @ Wu.t()) @ Wd.t()
+    L = torch.log_softmax(rms(S2, G2) @ Head.t(), 1)
+    loss = -L[torch.arange(T), targets.cpu()].mean()
+    want = torch.autograd.grad(loss, leaves)
+    # six roundings to bf16 on the way, amplified by less than ten in a block of this depth
+    assert abs(-r.logprob.mean().item() - loss.item()) <= 6 * 2.0 ** -8
+    for got, ref in zip((dx, dg1, dwg, dwu, dwd, dg2, dhead), want):
+        assert (got.cpu().double() - ref).norm() <= 10 * 2.0 ** -8 * ref.norm()
+
+    params, grads = [g1, wg, wu, wd, g2, head], [dg1, dwg, dwu, dwd, dg2, dhead]
+    for bits in (32, 8):
+        now = [p.clone() for p in params]
+        state = jb.adamw_state(now, bits=bits)
+        mine = _Replay(now, state, bits)
+        jb.adamw_step(now, grads, state, 1, 1e-3, seed=2, **OPT)
+        mine.check(grads, 1, 1e-3, 2, now, state)
+
+    # the same block served in integers
+    q, sc = jb.rms_norm_i8(x, g1)
+    wq, sw = jb.quant_rows_i8(wg)
+    y = jb.matmul_i8(q, sc, wq, sw, dtype=F32)
+    full = (N1 @ Wg.t()).detach()
+    # half a step of either operand in each of d products
+    bound = 0.5 * (sc.cpu().double() * Wg.abs().sum(1) + (N1.abs().sum(1, keepdim=True) * sw.cpu().double().view(-1)))
+    bound = bound + 0.25 * d * sc.cpu().double() * sw.cpu().double().view(-1)
+    assert torch.all((y.cpu().double() - full).abs() <= 1.001 * bound)
+
+
+def test_example_runs_a_training_step():
+    from examples import recovery_step
+    found = recovery_step.main(tokens=64, d=128, f=256, vocab=500, steps=2, log=lambda *a: None)
+    assert all(np.isfinite(v) for v in found["losses"]) and len(found["losses"]) == 3
