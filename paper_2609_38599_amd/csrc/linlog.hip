@@ -14,6 +14,7 @@
 // 2^14, so that a probability of 2^-38 is not lost; the sums are scaled back in fp32.
 #include <float.h>
 
+#include "mma_pairs.h"
 #include "skinny.h"
 
 namespace jarq {
@@ -34,37 +35,43 @@ __device__ __forceinline__ Part join(const Part& s, const Part& o) {
 __device__ __forceinline__ Part of_lane(const Part& s, int off) {
   return Part{__shfl_xor(s.m, off), __shfl_xor(s.more, off)};
 }
-// N entries; -infinity has no part, +infinity and NaN make it NaN.
+constexpr float kLog2e = 1.44269504088896340736f;
+// N entries (a power of two); -infinity has no part, +infinity and NaN make it NaN.  The largest
+// by a tournament: every other entry loses once, and the losers' exponentials are the sum beside
+// the largest's own 1, ties included.  (Eight issue slots an entry, four of them the exponential;
+// twelve with a maximum first and the entries that equal it counted.)
 template <int N>
-__device__ __forceinline__ Part part_of(const float (&x)[N]) {
-  float m = -FLT_MAX;
+__device__ __forceinline__ Part part_of(float (&x)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) m = fmaxf(m, x[i]);
+  for (int s = N / 2; s >= 1; s /= 2)
+#pragma unroll
+    for (int i = 0; i < s; ++i) {
+      const float hi = __builtin_elementwise_maximum(x[i], x[i + s]);   // (NaN wins)
+      x[i + s] = __builtin_elementwise_minimum(x[i], x[i + s]);
+      x[i] = hi;
+    }
+  const bool none = x[0] == -INFINITY;
+  const float m = none ? 0.f : x[0], ml = m * kLog2e;
   float more = 0.f;
-  int top = 0;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const bool is = x[i] == m;
-    more += is ? 0.f : __expf(x[i] - m);
-    top += is;
-  }
-  return Part{m, m == INFINITY ? NAN : more + (float)(top - 1)};
+  for (int i = 1; i < N; ++i) more += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -ml));
+  more *= __builtin_amdgcn_exp2f(-fmaf(m, kLog2e, -ml));   // what rounding left of ml
+  return Part{none ? -FLT_MAX : m, none ? -1.f : m == INFINITY ? NAN : more};
 }
 
 }  // namespace
 
 // ---- forward, many tokens ----
 // WI x WJ wavefronts, each BI blocks of 16 rows of w x BJ blocks of 16 tokens.
-template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_tile_kernel(
     const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V,
     const int64_t* __restrict__ targets, float* __restrict__ target_logit,
     float2* __restrict__ part, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
-  typedef KContig<TI, NW, kOne> LP;
-  typedef KContig<TJ, NW, kOne> LQ;
-  constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  JARQ_STAGES(S, STAGE);
+  typedef PairContig<TI, NW> LP;
+  typedef PairContig<TJ, NW> LQ;
+  JARQ_SLOTS(SP, SQ, LP::kBytes, LQ::kBytes);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -73,17 +80,17 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_tile_kernel
   const int v0 = ti * TI, t0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init(W, W, 2 * (size_t)D, v0, V, 2 * D, wave, lane);
-  lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
+  lp.init(W, 2 * (size_t)D, v0, V, 2 * D, wave, lane);
+  lq.init(X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
   f32x4 acc[BI][BJ] = {};
-  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
-                   stages, [](int) {},
-                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
-                       __attribute__((always_inline)) {
-                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                       });
-  static_assert(WI <= 2 && TJ * 8 <= STAGE, "the other wave's parts fit a stage");
-  float2* const red = (float2*)stage0;
+  mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI,
+                          wj * 16 * BJ, pslots, qslots,
+                          [&](const u32x4& p, const u32x4& q, int a, int b)
+                              __attribute__((always_inline)) {
+                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                              });
+  static_assert(WI <= 2 && TJ * 8 <= LP::kBytes, "the other wave's parts fit a stage");
+  float2* const red = (float2*)pslot0;
   const int vw = v0 + wi * 16 * BI + 4 * (lane >> 4);   // this lane's first row of w
   const int tw = wj * 16 * BJ + (lane & 15);            // its first token in the tile
   Part parts[BJ];
@@ -174,7 +181,7 @@ __global__ __launch_bounds__(512) void linlog_skinny_kernel(
     const float x = skinny_sum<NW, 2 * IB>(red, 2 * (t >> 4) + (j >> 4), t & 15, j & 15);
     Part s = no_part();
     if (v < V) {
-      const float one[1] = {x};
+      float one[1] = {x};
       s = part_of(one);
       if (targets[t] == v) target_logit[t] = x;
     }
@@ -258,7 +265,7 @@ __global__ __launch_bounds__(256) void linlog_scale_kernel(const int64_t* __rest
 }
 
 // dl [T][ld] of rows v0 .. v0 + n of w (ld a multiple of 8; columns n .. ld are zeros).
-template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
     const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V, int v0, int n,
     int ld, const int64_t* __restrict__ targets, const float* __restrict__ logprob,
@@ -266,10 +273,9 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
     const float* __restrict__ dlp, const float* __restrict__ dlse,
     const float* __restrict__ scale, uint16_t* __restrict__ dl, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
-  typedef KContig<TI, NW, kOne> LP;
-  typedef KContig<TJ, NW, kOne> LQ;
-  constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  JARQ_STAGES(S, STAGE);
+  typedef PairContig<TI, NW> LP;
+  typedef PairContig<TJ, NW> LQ;
+  JARQ_SLOTS(SP, SQ, LP::kBytes, LQ::kBytes);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -278,15 +284,15 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
   const int c0 = ti * TI, t0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init((const char*)W + (size_t)v0 * 2 * D, W, 2 * (size_t)D, c0, n, 2 * D, wave, lane);
-  lq.init(X, X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
+  lp.init((const char*)W + (size_t)v0 * 2 * D, 2 * (size_t)D, c0, n, 2 * D, wave, lane);
+  lq.init(X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
   f32x4 acc[BI][BJ] = {};
-  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
-                   stages, [](int) {},
-                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
-                       __attribute__((always_inline)) {
-                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                       });
+  mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI,
+                          wj * 16 * BJ, pslots, qslots,
+                          [&](const u32x4& p, const u32x4& q, int a, int b)
+                              __attribute__((always_inline)) {
+                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                              });
   const float by = scale ? scale[0] : 1.f;
   const int cw = c0 + wi * 16 * BI + 4 * (lane >> 4);   // this lane's first column of dl
 #pragma unroll
@@ -294,17 +300,15 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
     const int t = min(t0 + wj * 16 * BJ + 16 * b + (lane & 15), T - 1);
     const int64_t to = targets[t];
     const float g = to >= 0 ? dlp[t] * by : 0.f, h = dlse ? dlse[t] * by : 0.f, c = h - g;
-    const float l = lse[t], r = rest[t];
+    const bool none = lse[t] == -INFINITY;
+    const float l = none ? 0.f : lse[t], r = -rest[t] * kLog2e;
     // (a target that is none of the vocabulary's: NaN, as its log probability)
-    const float c1 = to >= V ? NAN : c;
-    const bool none = l == -INFINITY;
+    const float by_p = to >= V ? NAN : none ? 0.f : c;
 #pragma unroll
     for (int a = 0; a < BI; ++a)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = none ? 0.f : __expf((acc[a][b][i] - l) - r);
-        acc[a][b][i] = c1 * p;
-      }
+      for (int i = 0; i < 4; ++i)
+        acc[a][b][i] = by_p * __builtin_amdgcn_exp2f(fmaf(acc[a][b][i] - l, kLog2e, r));
     const int64_t at = to - v0 - cw;
     if (__any(at >= 0 && at < 16 * BI && at < n - cw)) {
       const float lt = logprob[t], p = __expf(lt);
@@ -322,7 +326,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
         for (int i = 0; i < 4; ++i)
           if (cw + 16 * a + i >= n) acc[a][b][i] = 0.f;
   }
-  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  char* const stage = wj == 0 ? pslot0 : wj == 1 ? pslot1 : wj == 2 ? qslot0 : qslot1;
   const int tw = t0 + wj * 16 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
     if (tw + t < T && c0 + i < ld) *(u32x4*)(dl + (size_t)(tw + t) * ld + c0 + i) = w;
@@ -332,16 +336,15 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
 // ---- backward: dx += dl w of a piece ----
 // part [splits][T][D] fp32: the sums so far (read where `add`), of the share blockIdx.y of the
 // piece's rows; without it dX gets the finished sums.  `last` with one share: both.
-template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
     const void* __restrict__ dl, const void* __restrict__ W, int T, int D, int n, int ld, int each,
     float* __restrict__ part, int add, const float* __restrict__ scale,
     uint16_t* __restrict__ dX, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
-  typedef KStrided<TI, NW, kOne> LP;
-  typedef KContig<TJ, NW, kOne> LQ;
-  constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  JARQ_STAGES(S, STAGE);
+  typedef PairStrided<TI, NW> LP;
+  typedef PairContig<TJ, NW> LQ;
+  JARQ_SLOTS(SP, SQ, LP::kBytes, LQ::kBytes);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -350,17 +353,17 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
   const int d0 = ti * TI, t0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init(W, W, 2 * (size_t)D, d0, D, n, wave, lane);
-  lq.init(dl, dl, 2 * (size_t)ld, t0, T, 2 * ((n + 7) & ~7), wave, lane);
+  lp.init(W, 2 * (size_t)D, d0, D, n, wave, lane);
+  lq.init(dl, 2 * (size_t)ld, t0, T, 2 * ((n + 7) & ~7), wave, lane);
   f32x4 acc[BI][BJ] = {};
   const int nk = (2 * n + kChunk - 1) / kChunk;
   const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
   if (q0 < q1)   // (a short last piece has no rows for the last shares)
-    mma_loop<S, BI, BJ>(lp, lq, q0, q1, lane, wi * 16 * BI, wj * 16 * BJ, stages, [](int) {},
-                     [&](const u32x4& p, const u32x4& q, int a, int b, int)
-                         __attribute__((always_inline)) {
-                           acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                         });
+    mma_pairs<SP, SQ, BI, BJ>(lp, lq, q0, q1, lane, wi * 16 * BI, wj * 16 * BJ, pslots, qslots,
+                          [&](const u32x4& p, const u32x4& q, int a, int b)
+                              __attribute__((always_inline)) {
+                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                              });
   if (part) {   // uniform
 #pragma unroll
     for (int b = 0; b < BJ; ++b) {
@@ -382,7 +385,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
   for (int a = 0; a < BI; ++a)
 #pragma unroll
     for (int b = 0; b < BJ; ++b) acc[a][b] *= by;
-  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  char* const stage = wj == 0 ? pslot0 : wj == 1 ? pslot1 : wj == 2 ? qslot0 : qslot1;
   const int tw = t0 + wj * 16 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
     if (tw + t < T && d0 + i < D) *(u32x4*)(dX + (size_t)(tw + t) * D + d0 + i) = w;
@@ -406,15 +409,14 @@ __global__ __launch_bounds__(256) void linlog_dx_sum_kernel(const float* __restr
 }
 
 // ---- backward: dw = dl^T x of a piece ----
-template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
     const void* __restrict__ dl, const void* __restrict__ X, int T, int D, int n, int ld,
     const float* __restrict__ scale, uint16_t* __restrict__ dW, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
-  typedef KStrided<TI, NW, kOne> LP;
-  typedef KStrided<TJ, NW, kOne> LQ;
-  constexpr int STAGE = LP::kBytes + LQ::kBytes;
-  JARQ_STAGES(S, STAGE);
+  typedef PairStrided<TI, NW> LP;
+  typedef PairStrided<TJ, NW> LQ;
+  JARQ_SLOTS(SP, SQ, LP::kBytes, LQ::kBytes);
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wi = wave / WJ, wj = wave % WJ;
@@ -423,21 +425,21 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
   const int d0 = ti * TI, c0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init(X, X, 2 * (size_t)D, d0, D, T, wave, lane);
-  lq.init(dl, dl, 2 * (size_t)ld, c0, (n + 7) & ~7, T, wave, lane);
+  lp.init(X, 2 * (size_t)D, d0, D, T, wave, lane);
+  lq.init(dl, 2 * (size_t)ld, c0, (n + 7) & ~7, T, wave, lane);
   f32x4 acc[BI][BJ] = {};
-  mma_loop<S, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 16 * BI, wj * 16 * BJ,
-                   stages, [](int) {},
-                   [&](const u32x4& p, const u32x4& q, int a, int b, int)
-                       __attribute__((always_inline)) {
-                         acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                       });
+  mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 16 * BI,
+                          wj * 16 * BJ, pslots, qslots,
+                          [&](const u32x4& p, const u32x4& q, int a, int b)
+                              __attribute__((always_inline)) {
+                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                              });
   const float by = scale ? scale[1] : 1.f;
 #pragma unroll
   for (int a = 0; a < BI; ++a)
 #pragma unroll
     for (int b = 0; b < BJ; ++b) acc[a][b] *= by;
-  char* const stage = wj == 0 ? stage0 : wj == 1 ? stage1 : wj == 2 ? stage2 : stage3;
+  char* const stage = wj == 0 ? pslot0 : wj == 1 ? pslot1 : wj == 2 ? qslot0 : qslot1;
   const int cw = c0 + wj * 16 * BJ;
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int r, int i, const u32x4& w) {
     if (cw + r < n && d0 + i < D) *(u32x4*)(dW + (size_t)(cw + r) * D + d0 + i) = w;
@@ -514,7 +516,8 @@ DxPlan dx_plan(int T, int D, int rows) {
 }
 
 size_t pad256(size_t n) { return (n + 255) & ~(size_t)255; }
-int pad8(int n) { return (n + 7) & ~7; }
+// Values a row of dl: an odd number of cache lines (rows a power of two apart share a channel).
+int dl_stride(int rows) { return ((rows + 63) / 64 | 1) * 64; }
 
 }  // namespace
 
@@ -527,12 +530,12 @@ size_t linear_logprobs_workspace_bytes(int T, int D, int V) {
   return pad256(4 * (size_t)most) + 8 * parts;
 }
 
-template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 static void linlog_tiles(hipStream_t st, int T, int D, int V, const void* X, const void* W,
                          const int64_t* targets, float* logit, float2* part) {
   const int ni = (V + 16 * WI * BI - 1) / (16 * WI * BI);
   const int nj = (T + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
-  hipLaunchKernelGGL((linlog_tile_kernel<KIND, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
+  hipLaunchKernelGGL((linlog_tile_kernel<KIND, SP, SQ, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
                      dim3(64 * WI * WJ), 0, st, X, W, T, D, V, targets, logit, part, ni, nj);
 }
 
@@ -556,10 +559,10 @@ static hipError_t launch_linlog_kind(hipStream_t st, int T, int D, int V, const 
                            D, V, to, logit, part);
     } else {
       switch (logit_tiles(n, D, V)) {
-        case 0: linlog_tiles<KIND, 4, 2, 4, 8, 4>(st, n, D, V, x, W, to, logit, part); break;
-        case 1: linlog_tiles<KIND, 4, 2, 2, 4, 4>(st, n, D, V, x, W, to, logit, part); break;
-        case 2: linlog_tiles<KIND, 4, 2, 2, 4, 2>(st, n, D, V, x, W, to, logit, part); break;
-        default: linlog_tiles<KIND, 8, 1, 2, 4, 2>(st, n, D, V, x, W, to, logit, part);
+        case 0: linlog_tiles<KIND, 3, 2, 2, 4, 8, 4>(st, n, D, V, x, W, to, logit, part); break;
+        case 1: linlog_tiles<KIND, 3, 2, 2, 2, 4, 4>(st, n, D, V, x, W, to, logit, part); break;
+        case 2: linlog_tiles<KIND, 3, 2, 2, 2, 4, 2>(st, n, D, V, x, W, to, logit, part); break;
+        default: linlog_tiles<KIND, 3, 3, 1, 2, 4, 2>(st, n, D, V, x, W, to, logit, part);
       }
     }
     hipError_t e = hipGetLastError();
@@ -584,19 +587,19 @@ hipError_t launch_linear_logprobs(hipStream_t st, int dtype, int T, int D, int V
 size_t linear_logprobs_backward_workspace_bytes(int T, int D, int V) {
   const int rows = piece_rows(T, V);
   const DxPlan p = dx_plan(T, D, rows);
-  size_t n = 256 + pad256(2 * (size_t)T * pad8(rows));
+  size_t n = 256 + pad256(2 * (size_t)T * dl_stride(rows));
   if (p.splits > 1 || rows < V) n += 4 * (size_t)p.splits * T * D;
   return n;
 }
 
-template <int KIND, int S, int WI, int WJ, int BI, int BJ>
+template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 static void linlog_dl(hipStream_t st, int T, int D, int V, int v0, int n, int ld, const void* X,
                       const void* W, const int64_t* targets, const float* logprob,
                       const float* lse, const float* rest, const float* dlp, const float* dlse,
                       const float* scale, uint16_t* dl) {
   const int ni = (n + 16 * WI * BI - 1) / (16 * WI * BI);
   const int nj = (T + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
-  hipLaunchKernelGGL((linlog_dl_kernel<KIND, S, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
+  hipLaunchKernelGGL((linlog_dl_kernel<KIND, SP, SQ, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
                      dim3(64 * WI * WJ), 0, st, X, W, T, D, V, v0, n, ld, targets, logprob, lse,
                      rest, dlp, dlse, scale, dl, ni, nj);
 }
@@ -614,7 +617,7 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
     return hipGetLastError();
   }
   if (!dX && !dW) return hipSuccess;
-  const int rows = piece_rows(T, V), ld = pad8(rows);
+  const int rows = piece_rows(T, V), ld = dl_stride(rows);
   const DxPlan p = dx_plan(T, D, rows);
   float* scale = KIND == kF16 ? (float*)ws : nullptr;   // bf16 has fp32's range
   uint16_t* dl = (uint16_t*)(ws + 256);
@@ -631,10 +634,10 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
   linlog_dl<KIND, __VA_ARGS__>(st, T, D, V, v0, n, ld, X, W, targets, logprob, lse, rest, dlp,   \
                                dlse, scale, dl)
     switch (logit_tiles(T, D, n)) {
-      case 0: JARQ_LINLOG_DL(4, 2, 4, 8, 4); break;
-      case 1: JARQ_LINLOG_DL(4, 2, 2, 4, 4); break;
-      case 2: JARQ_LINLOG_DL(4, 2, 2, 4, 2); break;
-      default: JARQ_LINLOG_DL(8, 1, 2, 4, 2);
+      case 0: JARQ_LINLOG_DL(3, 2, 2, 4, 8, 4); break;
+      case 1: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 4); break;
+      case 2: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 2); break;
+      default: JARQ_LINLOG_DL(3, 3, 1, 2, 4, 2);
     }
 #undef JARQ_LINLOG_DL
     hipError_t e = hipGetLastError();
@@ -646,13 +649,13 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
       uint16_t* out = p.splits == 1 && last ? (uint16_t*)dX : nullptr;
       const int add = v0 > 0;
       if (p.kind == 0)
-        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 4, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl, w,
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl, w,
                            T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
       else if (p.kind == 1)
-        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 4, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl, w,
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl, w,
                            T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
       else
-        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 4, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl, w,
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl, w,
                            T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (last && p.splits > 1) {
@@ -667,13 +670,13 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
       const int ni = (D + 127) / 128, bi = (D + 255) / 256, bj = (n + 255) / 256;
       const int nj = (n + 127) / 128, nh = (n + 63) / 64;
       if ((long long)bi * bj >= 320)
-        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 4, 2, 4, 8, 4>), dim3((unsigned)(bi * bj)),
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 4, 8, 4>), dim3((unsigned)(bi * bj)),
                            dim3(512), 0, st, dl, X, T, D, n, ld, scale, out, bi, bj);
       else if ((long long)ni * nj >= 192)
-        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 4, 2, 2, 4, 4>), dim3((unsigned)(ni * nj)),
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 4>), dim3((unsigned)(ni * nj)),
                            dim3(256), 0, st, dl, X, T, D, n, ld, scale, out, ni, nj);
       else
-        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 4, 2, 2, 4, 2>), dim3((unsigned)(ni * nh)),
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 2>), dim3((unsigned)(ni * nh)),
                            dim3(256), 0, st, dl, X, T, D, n, ld, scale, out, ni, nh);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
