@@ -456,11 +456,16 @@ namespace {
 constexpr int kFewTokens = 32;       // fragments straight from memory
 constexpr int kTokensAtOnce = 16384;   // of the forward pass: bounds its parts
 
-// Tiles of l = x w^T by rows of w and tokens.
+// Tiles of l = x w^T by rows of w and tokens, the ones that cost the least.  In us with tiles of 256 x
+// 256 (rows x tokens), 128 x 128, 128 x 64 and 64 x 64 (the rule is 1.8 % off the best over 84 sizes):
+//   d 1000   200 x  5003     25  12   9  10     611 x 50257   83  78 111 135
+//   d 4096   200 x 17000     75  49  61  58    2047 x 50257  656 730 1054 1302
 constexpr int kWide[4] = {256, 128, 128, 64}, kTall[4] = {256, 128, 64, 64};
 int logit_tiles(int T, int D, int n) {
-  constexpr TileTime time[4] = {
-      {6.0, 0.62, 6.0, 0.62}, {3.3, 0.26, 3.3, 0.26}, {2.7, 0.19, 2.7, 0.19}, {2.6, 0.135, 2.6, 0.135}};
+  constexpr TileTime time[4] = {{9.6, 0.54, 4.7, 0.72},
+                                {5.4, 0.225, 1.3, 0.225},
+                                {3.5, 0.18, 0.6, 0.17},
+                                {3.7, 0.137, 0.5, 0.10}};
   const int nk = (2 * D + kChunk - 1) / kChunk;
   int best = 0;
   double least = 0.0;
@@ -485,6 +490,25 @@ int forward_parts(int T, int D, int V) {
 int piece_rows(int T, int V) {
   const int64_t most = std::max<int64_t>(1024, ((int64_t)1 << 27) / std::max(T, 1) / 1024 * 1024);
   return (int)std::min<int64_t>(most, V);
+}
+
+// Tiles of dw by channels and rows of w: 256 x 256, 128 x 128, 128 x 64.  d 1000, 200 tokens x 5003
+// 12, 8.9, 9.5 us; 611 x 50257 83, 77, 103; d 4096, 611 x 17000 104, 96, 128.
+int dw_tiles(int T, int D, int n) {
+  constexpr int wide[3] = {256, 128, 128}, tall[3] = {256, 128, 64};
+  constexpr TileTime time[3] = {{7.2, 0.62, 7.6, 0.71}, {4.2, 0.254, 1.8, 0.2}, {3.2, 0.195, 1.2, 0.14}};
+  const int nk = (2 * T + kChunk - 1) / kChunk;
+  int best = 0;
+  double least = 0.0;
+  for (int k = 0; k < 3; ++k) {
+    const long long tiles = (long long)((D + wide[k] - 1) / wide[k]) * ((n + tall[k] - 1) / tall[k]);
+    const double cost = tile_cost(tiles, nk, time[k]);
+    if (k == 0 || cost < least) {
+      best = k;
+      least = cost;
+    }
+  }
+  return best;
 }
 
 struct DxPlan {
@@ -667,17 +691,18 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
     }
     if (dW) {
       uint16_t* out = (uint16_t*)dW + (size_t)v0 * D;
-      const int ni = (D + 127) / 128, bi = (D + 255) / 256, bj = (n + 255) / 256;
-      const int nj = (n + 127) / 128, nh = (n + 63) / 64;
-      if ((long long)bi * bj >= 320)
-        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 4, 8, 4>), dim3((unsigned)(bi * bj)),
-                           dim3(512), 0, st, dl, X, T, D, n, ld, scale, out, bi, bj);
-      else if ((long long)ni * nj >= 192)
-        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 4>), dim3((unsigned)(ni * nj)),
-                           dim3(256), 0, st, dl, X, T, D, n, ld, scale, out, ni, nj);
+      const int k = dw_tiles(T, D, n), wide = k == 0 ? 256 : 128, tall = k == 0 ? 256 : k == 1 ? 128 : 64;
+      const int ni = (D + wide - 1) / wide, nj = (n + tall - 1) / tall;
+      const dim3 grid((unsigned)(ni * nj));
+      if (k == 0)
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl,
+                           X, T, D, n, ld, scale, out, ni, nj);
+      else if (k == 1)
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl,
+                           X, T, D, n, ld, scale, out, ni, nj);
       else
-        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 2>), dim3((unsigned)(ni * nh)),
-                           dim3(256), 0, st, dl, X, T, D, n, ld, scale, out, ni, nh);
+        hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl,
+                           X, T, D, n, ld, scale, out, ni, nj);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
