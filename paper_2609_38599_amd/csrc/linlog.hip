@@ -264,14 +264,33 @@ __global__ __launch_bounds__(256) void linlog_scale_kernel(const int64_t* __rest
   }
 }
 
+// What the backward pass takes of each token.
+struct Tokens {
+  const int64_t* targets;
+  const float *logprob, *lse, *rest, *dlp, *dlse;
+};
+// dl at the target, g (1 - p) + h p, from its log probability.
+__device__ __forceinline__ float at_target(float lt, float lse, float g, float h) {
+  return lse == -INFINITY ? 0.f : fmaf(h, __expf(lt), -g * expm1f(lt));
+}
+// What rounding to 16 bits leaves of it (scaled by `by`).  A token's target has most of its dl, so
+// the products add this back: dx at once, dw up to kFewTargets tokens.  (Without it both were off by
+// 1.43 times what rounding them once is, and by up to 2.4 with a few tokens, whose roundings do not
+// average.)
+template <int KIND>
+__device__ __forceinline__ float target_rest(const Tokens& k, int t, float by) {
+  const float h = k.dlse ? k.dlse[t] * by : 0.f;
+  const float d = at_target(k.logprob[t], k.lse[t], k.dlp[t] * by, h);
+  const float rest = d - from16<KIND>(to16<KIND>(d));
+  return fabsf(rest) < INFINITY ? rest : 0.f;
+}
+constexpr int kFewTargets = 512, kFewListed = 32;
+
 // dl [T][ld] of rows v0 .. v0 + n of w (ld a multiple of 8; columns n .. ld are zeros).
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
     const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V, int v0, int n,
-    int ld, const int64_t* __restrict__ targets, const float* __restrict__ logprob,
-    const float* __restrict__ lse, const float* __restrict__ rest,
-    const float* __restrict__ dlp, const float* __restrict__ dlse,
-    const float* __restrict__ scale, uint16_t* __restrict__ dl, int ni, int nj) {
+    int ld, Tokens k, const float* __restrict__ scale, uint16_t* __restrict__ dl, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef PairContig<TI, NW> LP;
   typedef PairContig<TJ, NW> LQ;
@@ -298,12 +317,12 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
 #pragma unroll
   for (int b = 0; b < BJ; ++b) {
     const int t = min(t0 + wj * 16 * BJ + 16 * b + (lane & 15), T - 1);
-    const int64_t to = targets[t];
-    const float g = to >= 0 ? dlp[t] * by : 0.f, h = dlse ? dlse[t] * by : 0.f, c = h - g;
-    const bool none = lse[t] == -INFINITY;
-    const float l = none ? 0.f : lse[t], r = -rest[t] * kLog2e;
+    const int64_t to = k.targets[t];
+    const float g = to >= 0 ? k.dlp[t] * by : 0.f, h = k.dlse ? k.dlse[t] * by : 0.f;
+    const bool none = k.lse[t] == -INFINITY;
+    const float l = none ? 0.f : k.lse[t], r = -k.rest[t] * kLog2e;
     // (a target that is none of the vocabulary's: NaN, as its log probability)
-    const float by_p = to >= V ? NAN : none ? 0.f : c;
+    const float by_p = to >= V ? NAN : none ? 0.f : h - g;
 #pragma unroll
     for (int a = 0; a < BI; ++a)
 #pragma unroll
@@ -311,8 +330,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
         acc[a][b][i] = by_p * __builtin_amdgcn_exp2f(fmaf(acc[a][b][i] - l, kLog2e, r));
     const int64_t at = to - v0 - cw;
     if (__any(at >= 0 && at < 16 * BI && at < n - cw)) {
-      const float lt = logprob[t], p = __expf(lt);
-      const float d = none ? 0.f : fmaf(h, p, -g * expm1f(lt));   // g (1 - p) + h p
+      const float d = at_target(k.logprob[t], k.lse[t], g, h);
 #pragma unroll
       for (int a = 0; a < BI; ++a)
 #pragma unroll
@@ -334,12 +352,12 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
 }
 
 // ---- backward: dx += dl w of a piece ----
-// part [splits][T][D] fp32: the sums so far (read where `add`), of the share blockIdx.y of the
-// piece's rows; without it dX gets the finished sums.  `last` with one share: both.
+// Rows v0 .. v0 + n of w.  part [splits][T][D] fp32: the sums so far of the share blockIdx.y of each
+// piece's rows; the last piece's go to dX where there is one share.
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
-    const void* __restrict__ dl, const void* __restrict__ W, int T, int D, int n, int ld, int each,
-    float* __restrict__ part, int add, const float* __restrict__ scale,
+    const void* __restrict__ dl, const void* __restrict__ W, int T, int D, int V, int v0, int n,
+    int ld, int each, Tokens k, float* __restrict__ part, const float* __restrict__ scale,
     uint16_t* __restrict__ dX, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef PairStrided<TI, NW> LP;
@@ -353,7 +371,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
   const int d0 = ti * TI, t0 = tj * TJ;
   LP lp;
   LQ lq;
-  lp.init(W, 2 * (size_t)D, d0, D, n, wave, lane);
+  lp.init((const char*)W + (size_t)v0 * 2 * D, 2 * (size_t)D, d0, D, n, wave, lane);
   lq.init(dl, 2 * (size_t)ld, t0, T, 2 * ((n + 7) & ~7), wave, lane);
   f32x4 acc[BI][BJ] = {};
   const int nk = (2 * n + kChunk - 1) / kChunk;
@@ -364,6 +382,24 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
                               __attribute__((always_inline)) {
                                 acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                               });
+  if (v0 + n == V && blockIdx.y == 0) {   // with the last piece, what the targets' roundings left
+#pragma unroll
+    for (int b = 0; b < BJ; ++b) {
+      const int t = t0 + wj * 16 * BJ + 16 * b + (lane & 15);
+      const int64_t v = t < T ? k.targets[t] : -1;
+      if (v < 0 || v >= V) continue;
+      const float rest = target_rest<KIND>(k, t, scale ? scale[0] : 1.f);
+#pragma unroll
+      for (int a = 0; a < BI; ++a) {
+        const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
+        if (d >= D) continue;
+        const u32x2 w = *(const u32x2*)((const uint16_t*)W + (size_t)v * D + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          acc[a][b][i] = fmaf(rest, from16<KIND>((uint16_t)(w[i / 2] >> (16 * (i % 2)))), acc[a][b][i]);
+      }
+    }
+  }
   if (part) {   // uniform
 #pragma unroll
     for (int b = 0; b < BJ; ++b) {
@@ -373,7 +409,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
         const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
         if (t < T && d < D) {
           f32x4* const at = (f32x4*)(part + ((size_t)blockIdx.y * T + t) * D + d);
-          if (add) acc[a][b] += *at;
+          if (v0 > 0) acc[a][b] += *at;
           if (!dX) *at = acc[a][b];
         }
       }
@@ -411,8 +447,8 @@ __global__ __launch_bounds__(256) void linlog_dx_sum_kernel(const float* __restr
 // ---- backward: dw = dl^T x of a piece ----
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
-    const void* __restrict__ dl, const void* __restrict__ X, int T, int D, int n, int ld,
-    const float* __restrict__ scale, uint16_t* __restrict__ dW, int ni, int nj) {
+    const void* __restrict__ dl, const void* __restrict__ X, int T, int D, int v0, int n, int ld,
+    Tokens k, const float* __restrict__ scale, uint16_t* __restrict__ dW, int ni, int nj) {
   constexpr int TI = 16 * WI * BI, TJ = 16 * WJ * BJ, NW = WI * WJ;
   typedef PairStrided<TI, NW> LP;
   typedef PairStrided<TJ, NW> LQ;
@@ -434,6 +470,38 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
                               __attribute__((always_inline)) {
                                 acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                               });
+  int listed = 0;   // targets among this tile's rows
+  if (T <= kFewTargets)
+    for (int t = lane; t < T + lane; t += 64) {   // (every lane in every round)
+      const int64_t v = t < T ? k.targets[t] - v0 - c0 : -1;
+      listed += __popcll(__ballot(v >= 0 && v < TJ && v < n - c0));
+    }
+  if (listed > 0 && listed <= kFewListed)   // what their roundings left, token after token
+    for (int first = 0; first < T; first += 64) {
+      const int mine = first + lane;
+      const int64_t v = mine < T ? k.targets[mine] - v0 - c0 : -1;
+      const bool here = v >= 0 && v < TJ && v < n - c0;
+      const float left = here ? target_rest<KIND>(k, mine, scale ? scale[0] : 1.f) : 0.f;
+      for (uint64_t m = __ballot(here); m != 0; m &= m - 1) {   // uniform
+        const int from = (int)__builtin_ctzll(m);
+        const int row = __builtin_amdgcn_readlane((int)v, from) - wj * 16 * BJ - (lane & 15);
+        const float rest = __uint_as_float(
+            (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(left), from));
+        const uint16_t* const x = (const uint16_t*)X + (size_t)(first + from) * D;
+#pragma unroll
+        for (int a = 0; a < BI; ++a) {
+          const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
+          const u32x2 w = d < D ? *(const u32x2*)(x + d) : u32x2{};
+#pragma unroll
+          for (int b = 0; b < BJ; ++b)
+            if (row == 16 * b)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                acc[a][b][i] = fmaf(rest, from16<KIND>((uint16_t)(w[i / 2] >> (16 * (i % 2)))),
+                                    acc[a][b][i]);
+        }
+      }
+    }
   const float by = scale ? scale[1] : 1.f;
 #pragma unroll
   for (int a = 0; a < BI; ++a)
@@ -618,14 +686,12 @@ size_t linear_logprobs_backward_workspace_bytes(int T, int D, int V) {
 
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 static void linlog_dl(hipStream_t st, int T, int D, int V, int v0, int n, int ld, const void* X,
-                      const void* W, const int64_t* targets, const float* logprob,
-                      const float* lse, const float* rest, const float* dlp, const float* dlse,
-                      const float* scale, uint16_t* dl) {
+                      const void* W, const Tokens& k, const float* scale, uint16_t* dl) {
   const int ni = (n + 16 * WI * BI - 1) / (16 * WI * BI);
   const int nj = (T + 16 * WJ * BJ - 1) / (16 * WJ * BJ);
   hipLaunchKernelGGL((linlog_dl_kernel<KIND, SP, SQ, WI, WJ, BI, BJ>), dim3((unsigned)(ni * nj)),
-                     dim3(64 * WI * WJ), 0, st, X, W, T, D, V, v0, n, ld, targets, logprob, lse,
-                     rest, dlp, dlse, scale, dl, ni, nj);
+                     dim3(64 * WI * WJ), 0, st, X, W, T, D, V, v0, n, ld, k, scale, dl, ni,
+                     nj);
 }
 
 template <int KIND>
@@ -645,6 +711,7 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
   const DxPlan p = dx_plan(T, D, rows);
   float* scale = KIND == kF16 ? (float*)ws : nullptr;   // bf16 has fp32's range
   uint16_t* dl = (uint16_t*)(ws + 256);
+  const Tokens tokens{targets, logprob, lse, rest, dlp, dlse};
   float* part = p.splits > 1 || rows < V ? (float*)(ws + 256 + pad256(2 * (size_t)T * ld)) : nullptr;
   if (scale) {
     hipLaunchKernelGGL(linlog_scale_kernel, dim3(1), dim3(256), 0, st, targets, dlp, dlse, T,
@@ -654,9 +721,8 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
   }
   for (int v0 = 0; v0 < V; v0 += rows) {
     const int n = std::min(rows, V - v0);
-#define JARQ_LINLOG_DL(...)                                                                      \
-  linlog_dl<KIND, __VA_ARGS__>(st, T, D, V, v0, n, ld, X, W, targets, logprob, lse, rest, dlp,   \
-                               dlse, scale, dl)
+#define JARQ_LINLOG_DL(...) \
+  linlog_dl<KIND, __VA_ARGS__>(st, T, D, V, v0, n, ld, X, W, tokens, scale, dl)
     switch (logit_tiles(T, D, n)) {
       case 0: JARQ_LINLOG_DL(3, 2, 2, 4, 8, 4); break;
       case 1: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 4); break;
@@ -667,20 +733,18 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (dX) {
-      const void* w = (const char*)W + (size_t)v0 * 2 * D;
       const dim3 grid((unsigned)(p.ni * p.nj), (unsigned)p.splits);
       const bool last = v0 + n == V;
       uint16_t* out = p.splits == 1 && last ? (uint16_t*)dX : nullptr;
-      const int add = v0 > 0;
       if (p.kind == 0)
-        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl, w,
-                           T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl,
+                           W, T, D, V, v0, n, ld, p.each, tokens, part, scale, out, p.ni, p.nj);
       else if (p.kind == 1)
-        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl, w,
-                           T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl,
+                           W, T, D, V, v0, n, ld, p.each, tokens, part, scale, out, p.ni, p.nj);
       else
-        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl, w,
-                           T, D, n, ld, p.each, part, add, scale, out, p.ni, p.nj);
+        hipLaunchKernelGGL((linlog_dx_kernel<KIND, 3, 2, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl,
+                           W, T, D, V, v0, n, ld, p.each, tokens, part, scale, out, p.ni, p.nj);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (last && p.splits > 1) {
         const size_t all = (size_t)T * D, b = (all / 4 + 255) / 256;
@@ -696,13 +760,13 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
       const dim3 grid((unsigned)(ni * nj));
       if (k == 0)
         hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 4, 8, 4>), grid, dim3(512), 0, st, dl,
-                           X, T, D, n, ld, scale, out, ni, nj);
+                           X, T, D, v0, n, ld, tokens, scale, out, ni, nj);
       else if (k == 1)
         hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 4>), grid, dim3(256), 0, st, dl,
-                           X, T, D, n, ld, scale, out, ni, nj);
+                           X, T, D, v0, n, ld, tokens, scale, out, ni, nj);
       else
         hipLaunchKernelGGL((linlog_dw_kernel<KIND, 3, 2, 2, 2, 4, 2>), grid, dim3(256), 0, st, dl,
-                           X, T, D, n, ld, scale, out, ni, nj);
+                           X, T, D, v0, n, ld, tokens, scale, out, ni, nj);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
