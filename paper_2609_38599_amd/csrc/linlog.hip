@@ -383,20 +383,26 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
                                 acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                               });
   if (v0 + n == V && blockIdx.y == 0) {   // with the last piece, what the targets' roundings left
+    float rest[BJ];
+    int64_t v[BJ];
 #pragma unroll
     for (int b = 0; b < BJ; ++b) {
       const int t = t0 + wj * 16 * BJ + 16 * b + (lane & 15);
-      const int64_t v = t < T ? k.targets[t] : -1;
-      if (v < 0 || v >= V) continue;
-      const float rest = target_rest<KIND>(k, t, scale ? scale[0] : 1.f);
+      v[b] = t < T ? k.targets[t] : -1;
+      if (v[b] >= V) v[b] = -1;
+      rest[b] = v[b] >= 0 ? target_rest<KIND>(k, t, scale ? scale[0] : 1.f) : 0.f;
+    }
 #pragma unroll
-      for (int a = 0; a < BI; ++a) {
-        const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
-        if (d >= D) continue;
-        const u32x2 w = *(const u32x2*)((const uint16_t*)W + (size_t)v * D + d);
+    for (int a = 0; a < BI; ++a) {
+      const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
+#pragma unroll
+      for (int b = 0; b < BJ; ++b) {
+        u32x2 w{};
+        if (v[b] >= 0 && d < D) w = *(const u32x2*)((const uint16_t*)W + (size_t)v[b] * D + d);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          acc[a][b][i] = fmaf(rest, from16<KIND>((uint16_t)(w[i / 2] >> (16 * (i % 2)))), acc[a][b][i]);
+          acc[a][b][i] = fmaf(rest[b], from16<KIND>((uint16_t)(w[i / 2] >> (16 * (i % 2)))),
+                              acc[a][b][i]);
       }
     }
   }
