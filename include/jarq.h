@@ -543,7 +543,8 @@ jarq_status jarq_token_logprobs_keep_backward(int32_t dtype, const void* logits,
  *     H = X + residual (rounded to dtype),  r = 1 / sqrt(mean H^2 + eps),
  *     Y[t][c] = H[t][c] r[t] gain[c]        (rounded once from fp32).
  * Without a residual H is X and the pointer NULL.  gain [cols] is of gain_dtype: dtype or
- * JARQ_F32.  1 <= cols <= 2^20, eps at least 2^-126 and finite.  H may be X or residual, and Y X.
+ * JARQ_F32.  1 <= cols <= 2^20, eps at least 2^-126 and finite.  H may be X or residual, and Y X,
+ * but not both the same.
  * Arrays are aligned to their type.  Sums are in fp64, so a row's squares may pass fp32's
  * range; a row with an infinity or a NaN gives NaN or 0.
  */
@@ -568,8 +569,7 @@ jarq_status jarq_rms_norm_i8(int32_t dtype, int32_t gain_dtype, int64_t tokens, 
  *     dX = r u - H r^3 mean(u H) + dH,  dgain = sum_t dY H r.
  * dX (of dtype) is the gradient of X and of the residual; dH (nullable) is what reaches H on
  * other ways, the residual stream's.  dgain is of gain_dtype.  dX and dgain are nullable (not
- * formed) and overwritten; dX may be dY or dH.  Sums over tokens are in fp32 in an order that
- * the sizes fix.  The workspace (256-byte aligned, jarq_rms_norm_workspace_bytes bytes; 0 if the sizes
+ * formed) and overwritten.  Sums over tokens are in fp32 in an order that the sizes fix.  The workspace (256-byte aligned, jarq_rms_norm_workspace_bytes bytes; 0 if the sizes
  * are invalid) is used only during the call.
  */
 size_t jarq_rms_norm_workspace_bytes(int64_t tokens, int32_t cols);

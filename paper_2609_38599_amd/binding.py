@@ -1200,6 +1200,9 @@ def adamw_step(params, grads, state: AdamWState, step, lr, beta1=0.9, beta2=0.99
                             step_at, _one_value(grad_mul, torch.float32, "grad_mul", at))
     _check(lib.jarq_adamw_step(code, bits, len(params), ctypes.addressof(table), held, to, options,
                                _queue(stream, at)), "jarq_adamw_step")
+    moved = [t for t in new_params if t.requires_grad]
+    if moved:   # a backward pass that kept the old values says so
+        torch.autograd.graph.increment_version(moved)
     return new_params, new_state
 
 

@@ -309,7 +309,7 @@ static hipError_t launch_adamw_of(hipStream_t st, int count, const jarq_adamw_te
       at += (t.numel + 127) / 128 * 128;
       continue;
     }
-    if (held == kTensors || units + most > 0x7fffffff) {
+    if (held == kTensors || units + most >= 1 << 24) {   // (fewer than 2^32 threads)
       const hipError_t e = launch();
       if (e != hipSuccess) return e;
     }

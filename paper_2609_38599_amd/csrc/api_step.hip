@@ -77,7 +77,8 @@ jarq_status jarq_rms_norm(int32_t dtype, int32_t gain_dtype, int64_t tokens, int
                           void* H, void* Y, void* stream) {
   if (!valid_norm(dtype, gain_dtype, tokens, cols, gain, eps)) return JARQ_EINVAL;
   if (tokens == 0) return JARQ_OK;
-  if (!valid_rows(dtype, X, residual, H) || !aligned(Y, bytes_of(dtype))) return JARQ_EINVAL;
+  if (!valid_rows(dtype, X, residual, H) || !aligned(Y, bytes_of(dtype)) || Y == H)
+    return JARQ_EINVAL;
   return status_of(launch_rms_norm((hipStream_t)stream, dtype, gain_dtype, X, residual, gain, eps,
                                    (int)tokens, cols, H, Y));
 }

@@ -240,13 +240,13 @@ __global__ __launch_bounds__(256) void linlog_join_kernel(
 
 // ---- backward: dl of a piece ----
 // One power of two for all tokens' gradients: scale[0], and its inverse in scale[1].
-__global__ __launch_bounds__(256) void linlog_scale_kernel(const int64_t* __restrict__ targets,
+__global__ __launch_bounds__(1024) void linlog_scale_kernel(const int64_t* __restrict__ targets,
                                                            const float* __restrict__ dlp,
                                                            const float* __restrict__ dlse, int T,
                                                            float* __restrict__ scale) {
-  __shared__ float red[4];
+  __shared__ float red[16];
   float m = 0.f;
-  for (int t = threadIdx.x; t < T; t += 256) {
+  for (int t = threadIdx.x; t < T; t += 1024) {
     const float g = targets[t] >= 0 ? dlp[t] : 0.f, h = dlse ? dlse[t] : 0.f;
     m = fmaxf(m, fmaxf(fmaxf(fabsf(g), fabsf(h)), fabsf(h - g)));
   }
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(256) void linlog_scale_kernel(const int64_t* __rest
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
   __syncthreads();
   if (threadIdx.x == 0) {
-    m = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    for (int w = 1; w < 16; ++w) m = fmaxf(m, red[w]);
     const int e = (int)(__float_as_uint(m) >> 23) - 127;
     // (the scale and its inverse are both normal)
     const int by = m > 0.f && e < 128 ? min(max(14 - e, -126), 126) : 0;
@@ -720,7 +720,7 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
   const Tokens tokens{targets, logprob, lse, rest, dlp, dlse};
   float* part = p.splits > 1 || rows < V ? (float*)(ws + 256 + pad256(2 * (size_t)T * ld)) : nullptr;
   if (scale) {
-    hipLaunchKernelGGL(linlog_scale_kernel, dim3(1), dim3(256), 0, st, targets, dlp, dlse, T,
+    hipLaunchKernelGGL(linlog_scale_kernel, dim3(1), dim3(1024), 0, st, targets, dlp, dlse, T,
                        scale);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -461,6 +461,62 @@ def test_linear_logprobs_of_many_tiles_and_pieces(T, d, V, dt, seed):
             assert off.norm() <= 1.5 * u * want.norm()
 
 
+def test_linear_logprobs_of_more_tokens_than_a_pass_takes():
+    # two passes of the forward kernel, the last a short one; two pieces of the vocabulary
+    T, d, V = 16384 + 40, 24, 9000
+    x, w, targets, g, h = _linlog_inputs(T, d, V, F16, seed=6)
+    r = jb.linear_logprobs(x, w, targets)
+    logits = x.double() @ w.double().t()
+    lse = torch.logsumexp(logits, 1)
+    has = targets >= 0
+    lp = torch.where(has, logits.gather(1, targets.clamp_min(0)[:, None])[:, 0] - lse, 0.0)
+    el = (d + 2) * E * (x.abs().double().sum(1) * w.abs().max().double() + 20)
+    assert torch.all((r.lse - lse).abs() <= 2 * el + 300 * E + 4 * E * lse.abs())
+    assert torch.all((r.logprob - lp).abs() <= 3 * el + 300 * E + 4 * E * lp.abs())
+    for a, b in ((0, 50), (16384 - 30, 16384 + 40)):
+        part = jb.linear_logprobs(x[a:b], w, targets[a:b])
+        assert torch.all((part.lse - r.lse[a:b]).abs() <= 2 * el[a:b] + 300 * E)
+    dx, dw = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    G = torch.where(has, g, 0.0).double()
+    dl = (h.double() - G)[:, None] * torch.exp(logits - lse[:, None])
+    dl.scatter_add_(1, targets.clamp_min(0)[:, None], G[:, None])
+    u = ROUND[F16][0]
+    for got, want in ((dx, dl @ w.double()), (dw, dl.t() @ x.double())):
+        assert (got.double() - want).norm() <= 1.5 * u * want.norm()
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+def test_linear_logprob_gradients_of_few_tokens_are_rounded_once(dt):
+    # rounding an entry once is off by u / sqrt(3) of it in the mean at most, over many entries, and
+    # by half the smallest subnormal number (`tiny`) each where they are subnormal: in float16 the
+    # rows of unlikely tokens are; what rounding the target's dl first would add is up to u, the same
+    # for all of a token
+    u, tiny = ROUND[dt]
+    for seed in range(30):
+        T = (1, 2, 5)[seed % 3]
+        x, w, targets, g, _ = _linlog_inputs(T, 512, 3000, dt, seed=100 + seed)
+        targets = targets.abs() % 3000
+        r = jb.linear_logprobs(x, w, targets)
+        dx, dw = jb.linear_logprobs_backward(x, w, targets, r, g)
+        logits = x.double() @ w.double().t()
+        dl = -g.double()[:, None] * torch.softmax(logits, 1)
+        dl.scatter_add_(1, targets[:, None], g.double()[:, None])
+        for got, want in ((dx, dl @ w.double()), (dw, dl.t() @ x.double())):
+            assert (got.double() - want).norm() <= 0.7 * u * want.norm() + tiny * want.numel() ** 0.5, (seed, T)
+
+
+def test_linear_logprob_gradients_of_one_target_for_all():
+    # more targets in a tile than are corrected one after the other, and as many as are
+    for T in (30, 33, 200, 513):
+        x, w, targets, g, h = _linlog_inputs(T, 136, 700, BF16, seed=50)
+        targets[:] = 77
+        r = jb.linear_logprobs(x, w, targets)
+        back = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+        _check_linlog(x, w, targets, r, back, g, h)
+        again = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+        assert torch.equal(back[0], again[0]) and torch.equal(back[1], again[1])
+
+
 def test_linear_logprob_gradient_against_differences():
     T, d, V = 12, 40, 90
     x, w, targets, g, h = _linlog_inputs(T, d, V, F16, seed=13)
@@ -764,6 +820,15 @@ def test_adamw_on_another_stream():
     jb.adamw_step(other, grads[0], b, 1, 1e-2, stream=s, **OPT)
     s.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(params, other))
+
+
+def test_adamw_is_seen_by_a_backward_pass_that_kept_the_old_values():
+    p = torch.ones(300, device="cuda", requires_grad=True)
+    x = torch.ones(300, device="cuda", requires_grad=True)
+    y = (p * x).sum()
+    jb.adamw_step([p], [torch.ones_like(p)], jb.adamw_state([p]), 1, 1e-2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
 
 
 def test_adamw_refuses_a_tensor_twice():

@@ -32,7 +32,7 @@ def test_norm_entry_points_check_arguments(lib):
         for n in ("dtype", "gt", "t", "c", "x", "res", "g", "eps", "h", "y", "st")])
     bad = (dict(dtype=3), dict(gt=1), dict(t=-1), dict(t=(1 << 22) + 1), dict(c=0), dict(c=(1 << 20) + 1),
            dict(x=None), dict(x=ctypes.c_void_p(1 << 20 | 1)), dict(g=None), dict(gt=0, g=OFF), dict(res=FAKE),
-           dict(h=FAKE), dict(y=None), dict(eps=_f(0.0)), dict(eps=_f(-1.0)), dict(eps=_f(1e-40)),
+           dict(h=FAKE), dict(res=FAKE, h=FAKE), dict(y=None), dict(eps=_f(0.0)), dict(eps=_f(-1.0)), dict(eps=_f(1e-40)),
            dict(eps=_f(float("nan"))), dict(eps=_f(float("inf"))))
     for k in bad:
         assert f(**k) == jb.JARQ_EINVAL, k
@@ -41,7 +41,7 @@ def test_norm_entry_points_check_arguments(lib):
         dtype=2, gt=2, t=4, c=64, x=FAKE, res=None, g=FAKE, eps=_f(1e-6), h=None, q=FAKE, s=FAKE, st=None), **k}[n]
         for n in ("dtype", "gt", "t", "c", "x", "res", "g", "eps", "h", "q", "s", "st")])
     for k in bad[:-1] + (dict(c=40), dict(c=131072), dict(s=None), dict(s=OFF), dict(q=None), dict(q=OFF)):
-        if "y" not in k:
+        if "y" not in k and k != dict(res=FAKE, h=FAKE):
             assert q(**k) == jb.JARQ_EINVAL, k
     assert q(t=0, x=None, q=None, s=None) == jb.JARQ_OK
     need = lib.jarq_rms_norm_workspace_bytes(4, 64)
