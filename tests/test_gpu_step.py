@@ -425,9 +425,11 @@ def test_linear_logprobs_of_tied_and_equal_logits():
 
 @pytest.mark.parametrize("dt", [BF16, F16])
 @pytest.mark.parametrize("T,d,V,seed", [(40, 1000, 9001, 0), (200, 520, 20011, 1), (1025, 264, 8200, 2),
-                                        (700, 1032, 33000, 3), (2100, 1032, 70001, 4)])
+                                        (700, 1032, 33000, 3), (2100, 1032, 70001, 4),
+                                        (611, 1000, 50257, 5), (12000, 1024, 13001, 6)])
 def test_linear_logprobs_of_many_tiles_and_pieces(T, d, V, dt, seed):
-    # on the GPU in 64 bits; the last size takes two pieces of the vocabulary
+    # on the GPU in 64 bits; 2100 and 12000 tokens take two pieces of the vocabulary, whose sums are
+    # cut into shares and not
     x, w, targets, g, h = _linlog_inputs(T, d, V, dt, seed=seed)
     say(f"[linlog] tokens {T} d {d} vocab {V} {dt}")
     if dt == F16:
