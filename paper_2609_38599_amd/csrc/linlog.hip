@@ -142,43 +142,45 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_tile_kernel
 }
 
 // ---- forward, few tokens ----
-// A work-group: 32 rows of w x up to 16 IB tokens, eight wavefronts along k.
-template <int KIND, int IB>
+// A work-group: 16 JB rows of w x up to 16 IB tokens, eight wavefronts along k.  Bound by reading w:
+// one token, 128000 x 4096 184 us, 5.7 TB/s (32 rows a work-group 198).
+template <int KIND, int IB, int JB>
 __global__ __launch_bounds__(512) void linlog_skinny_kernel(
     const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V,
     const int64_t* __restrict__ targets, float* __restrict__ target_logit,
     float2* __restrict__ part) {
   constexpr int NW = 8;
-  __shared__ __attribute__((aligned(16))) float red[NW * IB * 2 * 256];
+  __shared__ __attribute__((aligned(16))) float red[NW * IB * JB * 256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int v0 = blockIdx.x * 32;
+  const int v0 = blockIdx.x * (16 * JB);
   const int row = lane & 15;
   const size_t ld = 2 * (size_t)D;
   const char* p[IB];
 #pragma unroll
   for (int a = 0; a < IB; ++a) p[a] = (const char*)X + (size_t)min(16 * a + row, T - 1) * ld;
-  const char* const q[2] = {(const char*)W + (size_t)min(v0 + row, V - 1) * ld,
-                            (const char*)W + (size_t)min(v0 + 16 + row, V - 1) * ld};
-  f32x4 acc[IB][2] = {};
-  skinny_loop<IB, 2, 4, NW>(
+  const char* q[JB];
+#pragma unroll
+  for (int b = 0; b < JB; ++b) q[b] = (const char*)W + (size_t)min(v0 + 16 * b + row, V - 1) * ld;
+  f32x4 acc[IB][JB] = {};
+  skinny_loop<IB, JB, 4, NW>(
       p, q, 2 * D, wave, lane, [](int, int) {},
-      [&](int, int, const u32x4(&fp)[IB], const u32x4(&fq)[2]) __attribute__((always_inline)) {
+      [&](int, int, const u32x4(&fp)[IB], const u32x4(&fq)[JB]) __attribute__((always_inline)) {
 #pragma unroll
         for (int a = 0; a < IB; ++a)
 #pragma unroll
-          for (int b = 0; b < 2; ++b) acc[a][b] = Mma<KIND>::mul(fp[a], fq[b], acc[a][b]);
+          for (int b = 0; b < JB; ++b) acc[a][b] = Mma<KIND>::mul(fp[a], fq[b], acc[a][b]);
       });
 #pragma unroll
   for (int a = 0; a < IB; ++a)
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
-      *(f32x4*)(red + ((wave * IB + a) * 2 + b) * 256 + 4 * lane) = acc[a][b];
+    for (int b = 0; b < JB; ++b)
+      *(f32x4*)(red + ((wave * IB + a) * JB + b) * 256 + 4 * lane) = acc[a][b];
   __syncthreads();
-  for (int e = threadIdx.x; e < IB * 512; e += 512) {   // 32 lanes a token
-    const int j = e & 31, t = e >> 5, v = v0 + j;
+  for (int e = threadIdx.x; e < IB * JB * 256; e += 512) {   // 16 JB lanes a token
+    const int j = e & (16 * JB - 1), t = e / (16 * JB), v = v0 + j;
     if (t >= T) continue;
-    const float x = skinny_sum<NW, 2 * IB>(red, 2 * (t >> 4) + (j >> 4), t & 15, j & 15);
+    const float x = skinny_sum<NW, JB * IB>(red, JB * (t >> 4) + (j >> 4), t & 15, j & 15);
     Part s = no_part();
     if (v < V) {
       float one[1] = {x};
@@ -186,7 +188,7 @@ __global__ __launch_bounds__(512) void linlog_skinny_kernel(
       if (targets[t] == v) target_logit[t] = x;
     }
 #pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) s = join(s, of_lane(s, off));
+    for (int off = 8 * JB; off >= 1; off >>= 1) s = join(s, of_lane(s, off));
     if (j == 0) part[(size_t)blockIdx.x * T + t] = make_float2(s.m, s.more);
   }
 }
@@ -527,7 +529,6 @@ __global__ __launch_bounds__(256) void linlog_zero_kernel(u32x4* out, size_t n) 
 
 namespace {
 
-constexpr int kFewTokens = 32;       // fragments straight from memory
 constexpr int kTokensAtOnce = 16384;   // of the forward pass: bounds its parts
 
 // Tiles of l = x w^T by rows of w and tokens, the ones that cost the least.  In us with tiles of 256 x
@@ -553,9 +554,19 @@ int logit_tiles(int T, int D, int n) {
   }
   return best;
 }
+// Rows of w a work-group where fragments come straight from memory, 0: tiles.  In us with 16
+// rows, 32, and in tiles, d 4096:
+//    1 token    x 16000 23 30 36      x 128000 184 198 186
+//    8 tokens   x  1000 10 13 22      x  32001  60  58  62      x 128000 223 213 190
+//   24          x  5003 23 18 24      x  16000  44  39  37      x  32001 102  81  64
+int few_rows(int T, int V) {
+  if (T > 32) return 0;
+  if (T <= 4 || V <= 4096) return 16;
+  return V <= (T <= 16 ? 32768 : 8192) ? 32 : 0;
+}
 // Parts a token in the forward pass.
 int forward_parts(int T, int D, int V) {
-  if (T <= kFewTokens) return (V + 31) / 32;
+  if (const int rows = few_rows(T, V)) return (V + rows - 1) / rows;
   const int k = logit_tiles(T, D, V);
   return (V + kWide[k] - 1) / kWide[k];
 }
@@ -648,13 +659,15 @@ static hipError_t launch_linlog_kind(hipStream_t st, int T, int D, int V, const 
     const void* x = (const char*)X + (size_t)t0 * 2 * D;
     const int64_t* to = targets + t0;
     const int parts = forward_parts(n, D, V);
-    if (n <= kFewTokens) {
-      if (n <= 16)
-        hipLaunchKernelGGL((linlog_skinny_kernel<KIND, 1>), dim3(parts), dim3(512), 0, st, x, W, n,
-                           D, V, to, logit, part);
-      else
-        hipLaunchKernelGGL((linlog_skinny_kernel<KIND, 2>), dim3(parts), dim3(512), 0, st, x, W, n,
-                           D, V, to, logit, part);
+    if (const int rows = few_rows(n, V)) {
+#define JARQ_LINLOG_FEW(IB, JB)                                                                 \
+  hipLaunchKernelGGL((linlog_skinny_kernel<KIND, IB, JB>), dim3(parts), dim3(512), 0, st, x, W, \
+                     n, D, V, to, logit, part)
+      if (n <= 16 && rows == 16) JARQ_LINLOG_FEW(1, 1);
+      else if (n <= 16) JARQ_LINLOG_FEW(1, 2);
+      else if (rows == 16) JARQ_LINLOG_FEW(2, 1);
+      else JARQ_LINLOG_FEW(2, 2);
+#undef JARQ_LINLOG_FEW
     } else {
       switch (logit_tiles(n, D, V)) {
         case 0: linlog_tiles<KIND, 3, 2, 2, 4, 8, 4>(st, n, D, V, x, W, to, logit, part); break;

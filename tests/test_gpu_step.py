@@ -263,7 +263,8 @@ def test_norm_on_another_stream_and_in_a_graph():
 # tokens of every way through (few, the tiles, more than one), vocabularies inside a tile, at
 # its edge and past it, channels of half a chunk and of several
 LINLOG = [(1, 8, 1), (1, 72, 33), (2, 64, 7), (16, 136, 100), (17, 1000, 65), (32, 8, 300), (33, 72, 257),
-          (64, 264, 64), (65, 128, 1000), (129, 520, 513), (257, 200, 1025), (300, 64, 5003)]
+          (64, 264, 64), (65, 128, 1000), (129, 520, 513), (257, 200, 1025), (300, 64, 5003),
+          (5, 136, 4097), (20, 520, 6001), (24, 72, 8193), (3, 1000, 9001)]
 
 
 def _linlog_inputs(T, d, V, dt, seed=0, std=2.0):
