@@ -1136,18 +1136,27 @@ def _addresses(tensors, dtype, name, device, numels):
     return found
 
 
+_E4M3, _U8, _F32 = torch.float8_e4m3fn, torch.uint8, torch.float32
+_STATE_TYPES = {(32, True): (None, _F32, _F32, None, None), (32, False): (_F32, _F32, _F32, None, None),
+                (8, True): (None, _E4M3, _E4M3, _U8, _U8), (8, False): (_F32, _E4M3, _E4M3, _U8, _U8)}
+
+
 def _state_arrays(s: AdamWState, bits, wide, n, name, device):
-    held = torch.float32 if bits == 32 else torch.float8_e4m3fn
-    want = (("master", None if wide else torch.float32, n), ("m", held, n), ("v", held, n),
-            ("m_exp", None if bits == 32 else torch.uint8, n // 128),
-            ("v_exp", None if bits == 32 else torch.uint8, n // 128))
+    """The addresses of a state's arrays; wide: fp32 parameters, which have no master."""
     found = []
-    for t, (part, dt, length) in zip(s, want):
-        if (t is None) != (dt is None):
-            raise ValueError(f"{name}.{part} must be {'None' if dt is None else 'a tensor'}")
-        if t is not None and t.shape != (length,):
-            raise ValueError(f"{name}.{part} must be [{length}]")
-        found.append(_at(t, dt, f"{name}.{part}", device))
+    for part, t, dt, length in zip(AdamWState._fields, s, _STATE_TYPES[bits, wide],
+                                   (n, n, n, n // 128, n // 128)):
+        if dt is None or t is None:
+            if t is not dt:
+                raise ValueError(f"{name}.{part} must be {'None' if dt is None else 'a tensor'}")
+            found.append(None)
+        elif (t.dtype == dt and t.numel() == length and t.get_device() == device
+              and t.is_contiguous()):
+            found.append(t.data_ptr())
+        else:
+            if t.numel() != length:
+                raise ValueError(f"{name}.{part} must be [{length}]")
+            found.append(_at(t, dt, f"{name}.{part}", device))
     return _AdamWArrays(*found)
 
 
