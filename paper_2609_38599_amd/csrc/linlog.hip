@@ -88,11 +88,11 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_tile_kernel
   lq.init(X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
   f32x4 acc[BI][BJ] = {};
   mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI,
-                          wj * 16 * BJ, pslots, qslots,
-                          [&](const u32x4& p, const u32x4& q, int a, int b)
-                              __attribute__((always_inline)) {
-                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                              });
+                            wj * 16 * BJ, pslots, qslots,
+                            [&](const u32x4& p, const u32x4& q, int a, int b)
+                                __attribute__((always_inline)) {
+                                  acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                                });
   static_assert(WI <= 2 && TJ * 8 <= LP::kBytes, "the other wave's parts fit a stage");
   float2* const red = (float2*)pslot0;
   const int vw = v0 + wi * 16 * BI + 4 * (lane >> 4);   // this lane's first row of w
@@ -277,12 +277,13 @@ struct Tokens {
 };
 // dl at the target, g (1 - p) + h p, from its log probability.
 __device__ __forceinline__ float at_target(float lt, float lse, float g, float h) {
-  return lse == -INFINITY ? 0.f : fmaf(h, __expf(lt), -g * expm1f(lt));
+  return lse == -INFINITY || (g == 0.f && h == 0.f) ? 0.f : fmaf(h, __expf(lt), -g * expm1f(lt));
 }
 // What rounding to 16 bits leaves of it (scaled by `by`).  A token's target has most of its dl, so
-// the products add this back: dx at once, dw up to kFewTargets tokens.  (Without it both were off by
-// 1.43 times what rounding them once is, and by up to 2.4 with a few tokens, whose roundings do not
-// average.)
+// the products add this back: dx always; dw, which takes half a microsecond for each target, up to
+// kFewTargets tokens, in tiles that have kFewListed of their targets at most.  With it both are off
+// by 1.0 to 1.1 times what rounding them once is; without it by 1.43, and by up to 2.4 with a few
+// tokens, whose roundings do not average.
 template <int KIND>
 __device__ __forceinline__ float target_rest(const Tokens& k, int t, float by) {
   const float h = k.dlse ? k.dlse[t] * by : 0.f;
@@ -314,11 +315,11 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
   lq.init(X, 2 * (size_t)D, t0, T, 2 * D, wave, lane);
   f32x4 acc[BI][BJ] = {};
   mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * D + kChunk - 1) / kChunk, lane, wi * 16 * BI,
-                          wj * 16 * BJ, pslots, qslots,
-                          [&](const u32x4& p, const u32x4& q, int a, int b)
-                              __attribute__((always_inline)) {
-                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                              });
+                            wj * 16 * BJ, pslots, qslots,
+                            [&](const u32x4& p, const u32x4& q, int a, int b)
+                                __attribute__((always_inline)) {
+                                  acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                                });
   const float by = scale ? scale[0] : 1.f;
   const int cw = c0 + wi * 16 * BI + 4 * (lane >> 4);   // this lane's first column of dl
 #pragma unroll
@@ -335,6 +336,9 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         acc[a][b][i] = by_p * __builtin_amdgcn_exp2f(fmaf(acc[a][b][i] - l, kLog2e, r));
+    if (by_p == 0.f)   // a token without a gradient gives none, its logits NaN or not
+#pragma unroll
+      for (int a = 0; a < BI; ++a) acc[a][b] = f32x4{};
     const int64_t at = to - v0 - cw;
     if (__any(at >= 0 && at < 16 * BI && at < n - cw)) {
       const float d = at_target(k.logprob[t], k.lse[t], g, h);
@@ -387,10 +391,10 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
   const int q0 = blockIdx.y * each, q1 = min(q0 + each, nk);
   if (q0 < q1)   // (a short last piece has no rows for the last shares)
     mma_pairs<SP, SQ, BI, BJ>(lp, lq, q0, q1, lane, wi * 16 * BI, wj * 16 * BJ, pslots, qslots,
-                          [&](const u32x4& p, const u32x4& q, int a, int b)
-                              __attribute__((always_inline)) {
-                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                              });
+                              [&](const u32x4& p, const u32x4& q, int a, int b)
+                                  __attribute__((always_inline)) {
+                                    acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                                  });
   if (v0 + n == V && blockIdx.y == 0) {   // with the last piece, what the targets' roundings left
     float rest[BJ];
     int64_t v[BJ];
@@ -483,11 +487,11 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
   lq.init(dl, 2 * (size_t)ld, c0, (n + 7) & ~7, T, wave, lane);
   f32x4 acc[BI][BJ] = {};
   mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 16 * BI,
-                          wj * 16 * BJ, pslots, qslots,
-                          [&](const u32x4& p, const u32x4& q, int a, int b)
-                              __attribute__((always_inline)) {
-                                acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
-                              });
+                            wj * 16 * BJ, pslots, qslots,
+                            [&](const u32x4& p, const u32x4& q, int a, int b)
+                                __attribute__((always_inline)) {
+                                  acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
+                                });
   int listed = 0;   // targets among this tile's rows
   if (T <= kFewTargets)
     for (int t = lane; t < T + lane; t += 64) {   // (every lane in every round)
@@ -620,7 +624,7 @@ DxPlan dx_plan(int T, int D, int rows) {
   for (int kind = 0; kind < 3; ++kind) {
     const int ni = (D + wide[kind] - 1) / wide[kind], nj = (T + tall[kind] - 1) / tall[kind];
     for (int parts = 1; parts <= 32; ++parts) {
-      const int each = ((nk + parts - 1) / parts + 3) / 4 * 4;   // whole rounds of stages
+      const int each = ((nk + parts - 1) / parts + 3) / 4 * 4;   // whole pairs of chunks, two and two
       const int splits = (nk + each - 1) / each;
       if (splits != parts) continue;
       double cost = tile_cost((long long)ni * nj * splits, each, time[kind]);

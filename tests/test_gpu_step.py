@@ -413,6 +413,25 @@ def test_linear_logprobs_of_masked_broken_and_wrong_targets():
         assert torch.equal(dx[2:], want[2:]) and torch.all(torch.isnan(dx[:2]))
 
 
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T,V", [(5, 300), (90, 1000), (300, 9000)])
+def test_a_token_without_a_gradient_has_none_whatever_its_logits(T, V, dt):
+    # as the padding of a batch: no target, or one whose gradient is 0
+    x, w, targets, g, h = _linlog_inputs(T, 64, V, dt, seed=12)
+    targets.clamp_(min=0)
+    targets[0], g[1], h[0], h[1] = -1, 0, 0, 0
+    bad = x.clone()
+    bad[:3, 5] = torch.tensor([float("nan"), float("inf"), float("nan")])
+    r = jb.linear_logprobs(bad, w, targets)
+    assert torch.all(torch.isnan(r.lse[:3]))
+    for d_lse in (None, h):
+        dx = jb.linear_logprobs_backward(bad, w, targets, r, g, d_lse=d_lse, need=(True, False))[0]
+        assert torch.all(dx[:2] == 0) and torch.all(torch.isnan(dx[2]))
+        good = jb.linear_logprobs(x, w, targets)
+        want = jb.linear_logprobs_backward(x, w, targets, good, g, d_lse=d_lse, need=(True, False))[0]
+        assert torch.equal(dx[3:], want[3:])
+
+
 def test_linear_logprobs_of_tied_and_equal_logits():
     # every logit the same: the maximum's own 1 is kept apart once, not for each tie
     for T, V in ((1, 1), (3, 500), (80, 1000), (80, 1)):
