@@ -232,8 +232,8 @@ jarq_status jarq_adamw_step(int32_t dtype, int32_t bits, int32_t count,
   }
   for (int k = 0; k < 5; ++k)
     if (!same && each[k] != 0 && meets(to, span(read[k], each[k]))) return JARQ_EINVAL;
-  for (const void* p : {(const void*)o.lr_at, (const void*)o.step_at, (const void*)o.grad_mul})
-    if (p && meets(to, span(p, 4))) return JARQ_EINVAL;
+  for (const Span& s : {span(o.lr_at, 4), span(o.step_at, 8), span(o.grad_mul, 4)})
+    if (s.from != 0 && meets(to, s)) return JARQ_EINVAL;
   return status_of(launch_adamw((hipStream_t)stream, dtype, bits, count, tensors, *in, *out, o));
 } catch (...) {
   return JARQ_EHIP;   // (no host memory)

@@ -148,6 +148,14 @@ def test_adamw_refuses_arrays_that_overlap(lib):
         assert _adamw(lib, **k) == jb.JARQ_EINVAL, k
 
 
+def test_adamw_refuses_scalars_in_what_it_writes(lib):
+    # every byte of them: a step number's upper half lies where the parameters begin
+    late = 32 + 4 / MB
+    for k in (dict(step_at=32 * MB, tensors=((16, late, late, 100),)), dict(step_at=64 * MB),
+              dict(lr_at=32 * MB + 196), dict(lr_at=68 * MB), dict(grad_mul=65 * MB + 4)):
+        assert _adamw(lib, **k) == jb.JARQ_EINVAL, k
+
+
 def test_adamw_state_length(lib):
     f = lambda *n: int(lib.jarq_adamw_state_length(len(n), (ctypes.c_int64 * max(1, len(n)))(*n)))  # noqa: E731
     assert f() == 0 and f(0) == 0 and f(1) == 128 and f(128, 129) == 384
