@@ -280,10 +280,8 @@ __device__ __forceinline__ float at_target(float lt, float lse, float g, float h
   return lse == -INFINITY || (g == 0.f && h == 0.f) ? 0.f : fmaf(h, __expf(lt), -g * expm1f(lt));
 }
 // What rounding to 16 bits leaves of it (scaled by `by`).  A token's target has most of its dl, so
-// the products add this back: dx always; dw, which takes half a microsecond for each target, up to
-// kFewTargets tokens, in tiles that have kFewListed of their targets at most.  With it both are off
-// by 1.0 to 1.1 times what rounding them once is; without it by 1.43, and by up to 2.4 with a few
-// tokens, whose roundings do not average.
+// the products add this back, and both are off by 1.0 to 1.1 times what rounding them once is;
+// without it by 1.4, and by up to 2.4 with a few tokens, whose roundings do not average.
 template <int KIND>
 __device__ __forceinline__ float target_rest(const Tokens& k, int t, float by) {
   const float h = k.dlse ? k.dlse[t] * by : 0.f;
@@ -291,7 +289,6 @@ __device__ __forceinline__ float target_rest(const Tokens& k, int t, float by) {
   const float rest = d - from16<KIND>(to16<KIND>(d));
   return fabsf(rest) < INFINITY ? rest : 0.f;
 }
-constexpr int kFewTargets = 512, kFewListed = 32;
 
 // dl [T][ld] of rows v0 .. v0 + n of w (ld a multiple of 8; columns n .. n rounded up to 8 are zeros).
 // Bound as the forward pass: 4096 tokens, 32768 x 4096 810 to 840 us, 1.33 PFLOP/s.
@@ -492,38 +489,91 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
                                 __attribute__((always_inline)) {
                                   acc[a][b] = Mma<KIND>::mul(p, q, acc[a][b]);
                                 });
-  int listed = 0;   // targets among this tile's rows
-  if (T <= kFewTargets)
-    for (int t = lane; t < T + lane; t += 64) {   // (every lane in every round)
-      const int64_t v = t < T ? k.targets[t] - v0 - c0 : -1;
-      listed += __popcll(__ballot(v >= 0 && v < TJ && v < n - c0));
+  // What the roundings of dl at this tile's targets left, as further products: 64 tokens at a time,
+  // their rows of x and a row each that has its token's rest (in 16 bits) at its target and zeros.
+  // Bound by latency: 2.5 us a tile with a target or two, 5.5 for each 64 (611 tokens, 50257 x 1000
+  // 80 -> 95 us; 4096 tokens, 32768 x 4096 690 -> 730).  Looked up before the products above, the
+  // targets take registers from them (twice the cost).
+  static_assert(SP == 3 && LP::kBytes % 2048 == 0, "the list of tokens has a slot of its own");
+  constexpr int kListed = LP::kBytes / 8, IT = kListed / (64 * NW), PC = TI / 8, QC = TJ / 8;
+  static_assert(IT * 64 * NW == kListed && PC % NW == 0 && QC % NW == 0, "shares of a wave");
+  uint32_t* const list = (uint32_t*)pslot2;               // a token's place and its row of w in the tile
+  int* const counts = (int*)(pslot2 + 4 * kListed);
+  const typename LP::template Lane<BI> pl(wi * 16 * BI, lane);
+  const typename LQ::template Lane<BJ> ql(wj * 16 * BJ, lane);
+  for (int t0 = 0; t0 < T; t0 += kListed) {
+    if (t0 > 0) __syncthreads();   // (the last list is read)
+    int at[IT], mine = 0;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+      const int t = t0 + 64 * (wave * IT + i) + lane;
+      const int64_t v = k.targets[min(t, T - 1)] - v0 - c0;   // (no branch: all loads at once)
+      at[i] = t < T && v >= 0 && v < min(TJ, n - c0) ? (int)v : -1;
     }
-  if (listed > 0 && listed <= kFewListed)   // what their roundings left, token after token
-    for (int first = 0; first < T; first += 64) {
-      const int mine = first + lane;
-      const int64_t v = mine < T ? k.targets[mine] - v0 - c0 : -1;
-      const bool here = v >= 0 && v < TJ && v < n - c0;
-      const float left = here ? target_rest<KIND>(k, mine, scale ? scale[0] : 1.f) : 0.f;
-      for (uint64_t m = __ballot(here); m != 0; m &= m - 1) {   // uniform
-        const int from = (int)__builtin_ctzll(m);
-        const int row = __builtin_amdgcn_readlane((int)v, from) - wj * 16 * BJ - (lane & 15);
-        const float rest = __uint_as_float(
-            (uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(left), from));
-        const uint16_t* const x = (const uint16_t*)X + (size_t)(first + from) * D;
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {   // each wave's from a place of its own on
+      const uint64_t found = __ballot(at[i] >= 0);
+      if (at[i] >= 0)
+        list[64 * IT * wave + mine + __popcll(found & (((uint64_t)1 << lane) - 1))] =
+            (uint32_t)(64 * (wave * IT + i) + lane) << 8 | (uint32_t)at[i];
+      mine += __popcll(found);
+    }
+    if (lane == 0) counts[wave] = mine;
+    __syncthreads();
+    int begin[NW], listed = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      begin[w] = listed;
+      listed += counts[w];
+    }
+    auto entry = [&](int e) __attribute__((always_inline)) {
+      int place = e;
+#pragma unroll
+      for (int w = 1; w < NW; ++w) place = e >= begin[w] ? 64 * IT * w + e - begin[w] : place;
+      return list[place];
+    };
+    for (int first = 0; first < listed; first += 64) {
+      const int rows = min(listed - first, 64), halves = rows > 32 ? 2 : 1;
+      u32x4 w[PC / NW];
+#pragma unroll
+      for (int i = 0; i < PC / NW; ++i) {   // (no branch here either; what is past the last row is not kept)
+        const int e = threadIdx.x + 64 * NW * i, r = e / PC, d = d0 + 8 * LP::piece(r, e % PC);
+        const int t = t0 + (int)(entry(first + min(r, rows - 1)) >> 8);
+        w[i] = *(const u32x4*)((const uint16_t*)X + (size_t)t * D + min(d, D - 8));
+      }
+      float rest = 0.f;
+      uint32_t one = 0;
+      if ((int)threadIdx.x < rows) {
+        one = entry(first + threadIdx.x);
+        rest = target_rest<KIND>(k, t0 + (int)(one >> 8), scale ? scale[0] : 1.f);
+      }
+#pragma unroll
+      for (int i = 0; i < QC / NW; ++i) *(u32x4*)(qslot0 + 16 * (threadIdx.x + 64 * NW * i)) = u32x4{};
+#pragma unroll
+      for (int i = 0; i < PC / NW; ++i) {
+        const int e = threadIdx.x + 64 * NW * i;
+        *(u32x4*)(pslot0 + 16 * e) = e / PC < rows ? w[i] : u32x4{};
+      }
+      __syncthreads();
+      if ((int)threadIdx.x < rows) {
+        const int r = threadIdx.x, v = (int)(one & 255);
+        *(uint16_t*)(qslot0 + 2 * (r * TJ + 8 * LQ::piece(r, v / 8) + v % 8)) = to16<KIND>(rest);
+      }
+      __syncthreads();
+      for (int half = 0; half < halves; ++half) {
+        u32x4 q[BJ];
+#pragma unroll
+        for (int b = 0; b < BJ; ++b) q[b] = ql.frag(qslot0, half, b);
 #pragma unroll
         for (int a = 0; a < BI; ++a) {
-          const int d = d0 + wi * 16 * BI + 16 * a + 4 * (lane >> 4);
-          const u32x2 w = d < D ? *(const u32x2*)(x + d) : u32x2{};
+          const u32x4 p = pl.frag(pslot0, half, a);
 #pragma unroll
-          for (int b = 0; b < BJ; ++b)
-            if (row == 16 * b)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                acc[a][b][i] = fmaf(rest, from16<KIND>((uint16_t)(w[i / 2] >> (16 * (i % 2)))),
-                                    acc[a][b][i]);
+          for (int b = 0; b < BJ; ++b) acc[a][b] = Mma<KIND>::mul(p, q[b], acc[a][b]);
         }
       }
+      __syncthreads();
     }
+  }
   const float by = scale ? scale[1] : 1.f;
 #pragma unroll
   for (int a = 0; a < BI; ++a)

@@ -81,6 +81,11 @@ struct PairStrided {
   uint32_t off[N];
   int rows, wave, lt;
 
+  // Which piece (eight columns) of row t of a pair lies in place x of the row; the other way round
+  // the same.
+  static __device__ __forceinline__ int piece(int t, int x) {
+    return x ^ (One::swz(t) << 2) ^ ((t >> 2) & 2);
+  }
   // As KStrided::init.
   __device__ __forceinline__ void init(const void* p, size_t ld_, int c0, int cols, int rows_,
                                        int w, int lane) {
@@ -92,8 +97,8 @@ struct PairStrided {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int t = lt + NW * One::RPI * n;
-      const int pc = (lane % One::CPR) ^ (One::swz(t) << 2) ^ ((t >> 2) & 2);
-      off[n] = (uint32_t)t * (uint32_t)ld + 2u * (uint32_t)min(c0 + 8 * pc, cols - 8);
+      off[n] = (uint32_t)t * (uint32_t)ld +
+               2u * (uint32_t)min(c0 + 8 * piece(t, lane % One::CPR), cols - 8);
     }
   }
   struct Pair {

@@ -1,0 +1,82 @@
+"""The operators around a block on the GPU where numbers, tokens and arrays are at their limits:
+gradients against what one rounding leaves, logits far from 0, targets and gradients that are none,
+arrays that are written in place."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_38599_amd import binding as jb
+from tests._gpu_common import say
+from tests.test_gpu_step import BF16, F16, _linlog_inputs
+
+pytestmark = [pytest.mark.gpu,
+              pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
+
+
+# ---- log probabilities: one rounding ----
+
+def _gradients(x, w, targets, g, h):
+    """(dl, dX, dW) in 64 bits on the GPU."""
+    X, W = x.double(), w.double()
+    logits = X @ W.t()
+    has = targets >= 0
+    G = torch.where(has, g, 0.0).double()
+    dl = (h.double() - G)[:, None] * torch.softmax(logits, 1)
+    dl.scatter_add_(1, targets.clamp_min(0)[:, None], G[:, None])
+    return dl, dl @ W, dl.t() @ X
+
+
+def _check_rounded_once(x, w, targets, g, h, say_at):
+    # An output's rounding and those of dl's entries other than the targets, which are taken as
+    # they are, are independent, so their squares add up over many entries.  Sums in fp32 are off
+    # by sqrt(n) 2^-24 of the partial sums, far below; 15 % of margin.  With the targets' entries
+    # rounded too the norm is 1.4 times one rounding's.
+    dt = x.dtype
+    r = jb.linear_logprobs(x, w, targets)
+    back = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    dl, dX, dW = _gradients(x, w, targets, g, h)
+    G = torch.where(targets >= 0, g, 0.0)
+    most = torch.stack([G.abs().max(), h.abs().max(), (h - G).abs().max()]).max().item()
+    by = 2.0 ** (14 - np.floor(np.log2(most))) if dt == F16 else 1.0
+    e = (dl * by).to(dt).double() / by - dl
+    rows = torch.nonzero(targets >= 0)[:, 0]
+    e[rows, targets[rows]] = 0
+    for got, want, left in ((back[0], dX, e @ w.double()), (back[1], dW, e.t() @ x.double())):
+        once = want.to(dt).double() - want
+        bound = (once.norm() ** 2 + left.norm() ** 2).sqrt()
+        off = (got.double() - want).norm()
+        say(f"  {say_at}: {(off / once.norm()).item():.3f} of one rounding, bound {(1.15 * bound / once.norm()).item():.3f}")
+        assert off <= 1.15 * bound, say_at
+    again = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    assert torch.equal(back[0], again[0]) and torch.equal(back[1], again[1])
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T,d,V", [(40, 136, 3000), (513, 136, 2000), (700, 1032, 33000), (1500, 264, 5003),
+                                   (4096, 72, 700), (9000, 520, 300), (4200, 1024, 40000)])
+def test_linear_logprob_gradients_are_rounded_once_at_any_number_of_tokens(T, d, V, dt):
+    x, w, targets, g, h = _linlog_inputs(T, d, V, dt, seed=70)
+    h *= 0.1
+    _check_rounded_once(x, w, targets, g, h, (T, d, V, dt))
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T", [33, 64, 65, 600, 5000])
+def test_linear_logprob_gradients_of_targets_in_one_tile_are_rounded_once(T, dt):
+    x, w, targets, g, h = _linlog_inputs(T, 200, 3000, dt, seed=71)
+    targets = torch.where(targets >= 0, 1290 + targets % 30, -1)
+    _check_rounded_once(x, w, targets, g, h * 0.1, (T, dt, "thirty targets"))
+    targets = torch.where(targets >= 0, 2999, -1)
+    _check_rounded_once(x, w, targets, g, h * 0.1, (T, dt, "one target"))
+
+
+# ---- log probabilities: targets and gradients that are none ----
+
+def test_float16_gradients_far_below_its_range():
+    # normal outputs from gradients below float16's smallest number: channels that x has large where
+    # w is 0 and the other way round
+    x, w, targets, g, h = _linlog_inputs(700, 264, 9000, F16, seed=93)
+    x[:, :64], w[:, :64] = x[:, :64] * 4096, 0
+    w[:, 64:128], x[:, 64:128] = w[:, 64:128] * 30000, 0
+    _check_rounded_once(x, w, targets, g * 1e-8, h * 1e-9, "small gradients")
