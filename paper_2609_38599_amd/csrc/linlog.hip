@@ -38,8 +38,9 @@ __device__ __forceinline__ Part of_lane(const Part& s, int off) {
 constexpr float kLog2e = 1.44269504088896340736f;
 // N entries (a power of two); -infinity has no part, +infinity and NaN make it NaN.  The largest
 // by a tournament: every other entry loses once, and the losers' exponentials are the sum beside
-// the largest's own 1, ties included.  (Eight issue slots an entry, four of them the exponential;
-// twelve with a maximum first and the entries that equal it counted.)
+// the largest's own 1, ties included.  Differences from it are taken before they are scaled: exact
+// near it however far it is from 0.  (Nine issue slots an entry, four of them the exponential;
+// thirteen with a maximum first and the entries that equal it counted.)
 template <int N>
 __device__ __forceinline__ Part part_of(float (&x)[N]) {
 #pragma unroll
@@ -51,12 +52,12 @@ __device__ __forceinline__ Part part_of(float (&x)[N]) {
       x[i] = hi;
     }
   const bool none = x[0] == -INFINITY;
-  const float m = none ? 0.f : x[0], ml = m * kLog2e;
+  const float m = none ? 0.f : x[0];
   float more = 0.f;
 #pragma unroll
-  for (int i = 1; i < N; ++i) more += __builtin_amdgcn_exp2f(fmaf(x[i], kLog2e, -ml));
-  more *= __builtin_amdgcn_exp2f(-fmaf(m, kLog2e, -ml));   // what rounding left of ml
-  return Part{none ? -FLT_MAX : m, none ? -1.f : m == INFINITY ? NAN : more};
+  for (int i = 1; i < N; ++i) more += __builtin_amdgcn_exp2f((x[i] - m) * kLog2e);
+  // (one entry has no losers to carry a NaN)
+  return Part{none ? -FLT_MAX : m, none ? -1.f : fabsf(m) < INFINITY ? more : NAN};
 }
 
 }  // namespace

@@ -8,6 +8,7 @@ import torch
 
 from paper_2609_38599_amd import binding as jb
 from tests._gpu_common import say
+from tests.test_gpu_blocks import E, ROUND, _np
 from tests.test_gpu_step import BF16, F16, _linlog_inputs
 
 pytestmark = [pytest.mark.gpu,
@@ -69,6 +70,60 @@ def test_linear_logprob_gradients_of_targets_in_one_tile_are_rounded_once(T, dt)
     _check_rounded_once(x, w, targets, g, h * 0.1, (T, dt, "thirty targets"))
     targets = torch.where(targets >= 0, 2999, -1)
     _check_rounded_once(x, w, targets, g, h * 0.1, (T, dt, "one target"))
+
+
+# ---- log probabilities: logits far from 0 ----
+
+def _far(dt, T, logits):
+    """x [T][16] and w [V][16] whose logits are exactly these: the same product in four channels."""
+    scale = 2.0 ** 64 if dt == BF16 else 2.0 ** 15
+    w = torch.zeros(len(logits), 16, dtype=torch.float64)
+    w[:, 3:7] = torch.tensor(logits, dtype=torch.float64)[:, None] / scale / 4
+    x = torch.zeros(T, 16, dtype=torch.float64)
+    x[:, 3:7] = scale
+    assert torch.equal(w.to(dt).double(), w)
+    return x.to(dt).cuda(), w.to(dt).cuda()
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("V", [1, 40, 700])
+@pytest.mark.parametrize("T", [3, 90])
+def test_linear_logprobs_of_finite_logits_far_from_0(T, V, dt):
+    far = [1.5 * 2.0 ** 30, 1.3125 * 2.0 ** 32, 1.9375 * 2.0 ** 32] if dt == F16 else [1.25 * 2.0 ** 33, 1.625 * 2.0 ** 99, 1.9375 * 2.0 ** 127]
+    for top in [s * f for f in far for s in (1, -1)]:
+        for name in ("tied", "leads", "two lead"):
+            low = top * (0.5 if top > 0 else 1) if name != "tied" else top
+            high = top * (1 if top > 0 else 0.5) if name != "tied" else top
+            logits = [low] * V
+            lead = range(V) if name == "tied" else [V // 2] if name == "leads" else [0, V - 1]
+            for v in lead:
+                logits[v] = high
+            n = len(set(lead))
+            x, w = _far(dt, T, logits)
+            targets = torch.arange(T, device="cuda") % V
+            targets[0] = lead[0]
+            g = torch.linspace(0.25, 0.5, T, device="cuda") / 64
+            h = torch.linspace(-0.125, 0.125, T, device="cuda") / 64
+            r = jb.linear_logprobs(x, w, targets)
+            to, L = targets.cpu().numpy(), np.array(logits)
+            p = np.where(L == high, 1 / n, 0.0)
+            want = L[to] - high - np.log(n)
+            with np.errstate(over="ignore"):
+                want = want.astype(np.float32).astype(np.float64)
+            assert np.all(np.abs(_np(r.logprob) - want) <= 4 * E * (np.abs(want) + 8)), (top, name)
+            assert np.all(np.abs(_np(r.lse) - high) <= 4 * E * abs(high)), (top, name)
+            dX, dW = (_np(t) for t in jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h))
+            G, H = _np(g), _np(h)
+            dl = (H - G)[:, None] * p[None]
+            dl[np.arange(T), to] += G
+            u, tiny = ROUND[dt]
+            W, X = _np(w), _np(x)
+            # p to 700 terms' sums, dl's rounding, the output's
+            rel = 3 * u + (V + T + 20) * E
+            for got, size, exact in ((dX, np.abs(dl) @ np.abs(W), dl @ W), (dW, np.abs(dl).T @ np.abs(X), dl.T @ X)):
+                # (1 - p of a leader alone is 0, of n a difference of halves)
+                bound = rel * size + 8 * E * (np.abs(W).max() if got is dX else np.abs(X).sum()) + tiny
+                assert np.all(np.abs(got - exact) <= bound), (top, name)
 
 
 # ---- log probabilities: targets and gradients that are none ----
