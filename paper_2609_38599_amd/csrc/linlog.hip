@@ -147,18 +147,15 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_tile_kernel
 }
 
 // ---- forward, few tokens ----
-// A work-group: 16 JB rows of w x up to 16 IB tokens, eight wavefronts along k.  Bound by reading w:
-// one token, 128000 x 4096 184 us, 5.7 TB/s (32 rows a work-group 198).
+// The parts of logits of 16 JB rows of w (of `rows`, from r0 on) and up to 16 IB tokens by eight
+// wavefronts along k, for skinny_sum.  The backward pass takes its logits from the same sums: those
+// of the tiles above are off by other roundings, which large logits turn into other probabilities.
 template <int KIND, int IB, int JB>
-__global__ __launch_bounds__(512) void linlog_skinny_kernel(
-    const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V,
-    const int64_t* __restrict__ targets, float* __restrict__ target_logit,
-    float2* __restrict__ part) {
+__device__ __forceinline__ void few_logits(const void* X, const void* W, int T, int D, int rows,
+                                           int r0, float* red) {
   constexpr int NW = 8;
-  __shared__ __attribute__((aligned(16))) float red[NW * IB * JB * 256];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int v0 = blockIdx.x * (16 * JB);
   const int row = lane & 15;
   const size_t ld = 2 * (size_t)D;
   const char* p[IB];
@@ -166,7 +163,7 @@ __global__ __launch_bounds__(512) void linlog_skinny_kernel(
   for (int a = 0; a < IB; ++a) p[a] = (const char*)X + (size_t)min(16 * a + row, T - 1) * ld;
   const char* q[JB];
 #pragma unroll
-  for (int b = 0; b < JB; ++b) q[b] = (const char*)W + (size_t)min(v0 + 16 * b + row, V - 1) * ld;
+  for (int b = 0; b < JB; ++b) q[b] = (const char*)W + (size_t)min(r0 + 16 * b + row, rows - 1) * ld;
   f32x4 acc[IB][JB] = {};
   skinny_loop<IB, JB, 4, NW>(
       p, q, 2 * D, wave, lane, [](int, int) {},
@@ -182,6 +179,19 @@ __global__ __launch_bounds__(512) void linlog_skinny_kernel(
     for (int b = 0; b < JB; ++b)
       *(f32x4*)(red + ((wave * IB + a) * JB + b) * 256 + 4 * lane) = acc[a][b];
   __syncthreads();
+}
+
+// Bound by reading w: one token, 128000 x 4096 166 us, 6.3 TB/s; 181 among other kernels, which
+// leave less of w in the last cache (32 rows a work-group 8 % longer).
+template <int KIND, int IB, int JB>
+__global__ __launch_bounds__(512) void linlog_skinny_kernel(
+    const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V,
+    const int64_t* __restrict__ targets, float* __restrict__ target_logit,
+    float2* __restrict__ part) {
+  constexpr int NW = 8;
+  __shared__ __attribute__((aligned(16))) float red[NW * IB * JB * 256];
+  const int v0 = blockIdx.x * (16 * JB);
+  few_logits<KIND, IB, JB>(X, W, T, D, V, v0, red);
   for (int e = threadIdx.x; e < IB * JB * 256; e += 512) {   // 16 JB lanes a token
     const int j = e & (16 * JB - 1), t = e / (16 * JB), v = v0 + j;
     if (t >= T) continue;
@@ -280,6 +290,26 @@ struct Tokens {
 __device__ __forceinline__ float at_target(float lt, float lse, float g, float h) {
   return lse == -INFINITY || (g == 0.f && h == 0.f) ? 0.f : fmaf(h, __expf(lt), -g * expm1f(lt));
 }
+// Token t's row of dl, scaled by `by`.
+struct TokenGrad {
+  int64_t to;
+  float g, h, by_p, l, r;
+  __device__ __forceinline__ TokenGrad(const Tokens& k, int t, int V, float by) {
+    to = k.targets[t];
+    g = to >= 0 ? k.dlp[t] * by : 0.f;
+    h = k.dlse ? k.dlse[t] * by : 0.f;
+    const bool none = k.lse[t] == -INFINITY;
+    l = none ? 0.f : k.lse[t];
+    r = -k.rest[t] * kLog2e;
+    // (a target that is none of the vocabulary's: NaN, as its log probability)
+    by_p = to >= V ? NAN : none ? 0.f : h - g;
+  }
+  // From a logit, beside the target; 0 is for the caller where by_p is: a token without a gradient
+  // gives none, its logits NaN or not.
+  __device__ __forceinline__ float other(float logit) const {
+    return by_p * __builtin_amdgcn_exp2f(fmaf(logit - l, kLog2e, r));
+  }
+};
 // What rounding to 16 bits leaves of it (scaled by `by`).  A token's target has most of its dl, so
 // the products add this back, and both are off by 1.0 to 1.1 times what rounding them once is;
 // without it by 1.4, and by up to 2.4 with a few tokens, whose roundings do not average.
@@ -323,23 +353,17 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
 #pragma unroll
   for (int b = 0; b < BJ; ++b) {
     const int t = min(t0 + wj * 16 * BJ + 16 * b + (lane & 15), T - 1);
-    const int64_t to = k.targets[t];
-    const float g = to >= 0 ? k.dlp[t] * by : 0.f, h = k.dlse ? k.dlse[t] * by : 0.f;
-    const bool none = k.lse[t] == -INFINITY;
-    const float l = none ? 0.f : k.lse[t], r = -k.rest[t] * kLog2e;
-    // (a target that is none of the vocabulary's: NaN, as its log probability)
-    const float by_p = to >= V ? NAN : none ? 0.f : h - g;
+    const TokenGrad of(k, t, V, by);
 #pragma unroll
     for (int a = 0; a < BI; ++a)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        acc[a][b][i] = by_p * __builtin_amdgcn_exp2f(fmaf(acc[a][b][i] - l, kLog2e, r));
-    if (by_p == 0.f)   // a token without a gradient gives none, its logits NaN or not
+      for (int i = 0; i < 4; ++i) acc[a][b][i] = of.other(acc[a][b][i]);
+    if (of.by_p == 0.f)
 #pragma unroll
       for (int a = 0; a < BI; ++a) acc[a][b] = f32x4{};
-    const int64_t at = to - v0 - cw;
+    const int64_t at = of.to - v0 - cw;
     if (__any(at >= 0 && at < 16 * BI && at < n - cw)) {
-      const float d = at_target(k.logprob[t], k.lse[t], g, h);
+      const float d = at_target(k.logprob[t], k.lse[t], of.g, of.h);
 #pragma unroll
       for (int a = 0; a < BI; ++a)
 #pragma unroll
@@ -358,6 +382,28 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
   store_tile16<KIND, WI, BI, BJ>(acc, stage, wi, lane, [&](int t, int i, const u32x4& w) {
     if (tw + t < T && c0 + i < ld) *(u32x4*)(dl + (size_t)(tw + t) * ld + c0 + i) = w;
   });
+}
+
+// The same of few tokens, from the forward pass's sums.  Bound by reading w, as they are: one token,
+// 128000 x 4096 217 us behind a gradient of w of the same size (in tiles 229), 8 x 32001 78 (90).
+template <int KIND, int IB, int JB>
+__global__ __launch_bounds__(512) void linlog_few_dl_kernel(
+    const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V, int v0, int n,
+    int ld, Tokens k, const float* __restrict__ scale, uint16_t* __restrict__ dl) {
+  constexpr int NW = 8;
+  __shared__ __attribute__((aligned(16))) float red[NW * IB * JB * 256];
+  const int c0 = blockIdx.x * (16 * JB);
+  few_logits<KIND, IB, JB>(X, (const char*)W + (size_t)v0 * 2 * D, T, D, n, c0, red);
+  const float by = scale ? scale[0] : 1.f;
+  for (int e = threadIdx.x; e < IB * JB * 256; e += 512) {
+    const int j = e & (16 * JB - 1), t = e / (16 * JB), c = c0 + j;
+    if (t >= T) continue;
+    const TokenGrad of(k, t, V, by);
+    const float x = skinny_sum<NW, JB * IB>(red, JB * (t >> 4) + (j >> 4), t & 15, j & 15);
+    float d = of.by_p == 0.f ? 0.f : of.other(x);
+    if (of.to - v0 == c) d = at_target(k.logprob[t], k.lse[t], of.g, of.h);
+    if (c < ld) dl[(size_t)t * ld + c] = to16<KIND>(c < n ? d : 0.f);
+  }
 }
 
 // ---- backward: dx += dl w of a piece ----
@@ -483,6 +529,7 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
   LQ lq;
   lp.init(X, 2 * (size_t)D, d0, D, T, wave, lane);
   lq.init(dl, 2 * (size_t)ld, c0, (n + 7) & ~7, T, wave, lane);
+  const int64_t ahead = k.targets[min(lane, T - 1)];
   f32x4 acc[BI][BJ] = {};
   mma_pairs<SP, SQ, BI, BJ>(lp, lq, 0, (2 * T + kChunk - 1) / kChunk, lane, wi * 16 * BI,
                             wj * 16 * BJ, pslots, qslots,
@@ -502,7 +549,9 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
   int* const counts = (int*)(pslot2 + 4 * kListed);
   const typename LP::template Lane<BI> pl(wi * 16 * BI, lane);
   const typename LQ::template Lane<BJ> ql(wj * 16 * BJ, lane);
-  for (int t0 = 0; t0 < T; t0 += kListed) {
+  // (up to 64 tokens a wave knows by itself whether the tile has any, without a wait)
+  const int end = T > 64 || __any(ahead - v0 - c0 >= 0 && ahead - v0 - c0 < min(TJ, n - c0)) ? T : 0;
+  for (int t0 = 0; t0 < end; t0 += kListed) {
     if (t0 > 0) __syncthreads();   // (the last list is read)
     int at[IT], mine = 0;
 #pragma unroll
@@ -629,10 +678,10 @@ int few_rows(int T, int V) {
   if (T <= 4 || V <= 4096) return 16;
   return V <= (T <= 16 ? 32768 : 8192) ? 32 : 0;
 }
-// Parts a token in the forward pass.
-int forward_parts(int T, int D, int V) {
+// Parts a token of n that the forward pass takes at once, of T.
+int forward_parts(int T, int n, int D, int V) {
   if (const int rows = few_rows(T, V)) return (V + rows - 1) / rows;
-  const int k = logit_tiles(T, D, V);
+  const int k = logit_tiles(n, D, V);
   return (V + kWide[k] - 1) / kWide[k];
 }
 
@@ -698,9 +747,9 @@ int dl_stride(int rows) { return ((rows + 63) / 64 | 1) * 64; }
 size_t linear_logprobs_workspace_bytes(int T, int D, int V) {
   const int most = std::min(T, kTokensAtOnce);
   // (a shorter last share of the tokens may take smaller tiles)
-  size_t parts = (size_t)forward_parts(most, D, V) * most;
-  if (T > kTokensAtOnce && T % kTokensAtOnce)
-    parts = std::max(parts, (size_t)forward_parts(T % kTokensAtOnce, D, V) * (T % kTokensAtOnce));
+  size_t parts = (size_t)forward_parts(T, most, D, V) * most;
+  if (const int last = T % kTokensAtOnce; T > kTokensAtOnce && last)
+    parts = std::max(parts, (size_t)forward_parts(T, last, D, V) * last);
   return pad256(4 * (size_t)most) + 8 * parts;
 }
 
@@ -723,8 +772,8 @@ static hipError_t launch_linlog_kind(hipStream_t st, int T, int D, int V, const 
     const int n = std::min(T - t0, kTokensAtOnce);
     const void* x = (const char*)X + (size_t)t0 * 2 * D;
     const int64_t* to = targets + t0;
-    const int parts = forward_parts(n, D, V);
-    if (const int rows = few_rows(n, V)) {
+    const int parts = forward_parts(T, n, D, V);
+    if (const int rows = few_rows(T, V)) {   // (not a last share alone: the backward pass's rule)
 #define JARQ_LINLOG_FEW(IB, JB)                                                                 \
   hipLaunchKernelGGL((linlog_skinny_kernel<KIND, IB, JB>), dim3(parts), dim3(512), 0, st, x, W, \
                      n, D, V, to, logit, part)
@@ -807,12 +856,23 @@ static hipError_t launch_linlog_backward_kind(hipStream_t st, int T, int D, int 
     const int n = std::min(rows, V - v0);
 #define JARQ_LINLOG_DL(...) \
   linlog_dl<KIND, __VA_ARGS__>(st, T, D, V, v0, n, ld, X, W, tokens, scale, dl)
-    switch (logit_tiles(T, D, n)) {
-      case 0: JARQ_LINLOG_DL(3, 2, 2, 4, 8, 4); break;
-      case 1: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 4); break;
-      case 2: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 2); break;
-      default: JARQ_LINLOG_DL(3, 3, 1, 2, 4, 2);
+#define JARQ_LINLOG_FEW(IB, JB)                                                              \
+  hipLaunchKernelGGL((linlog_few_dl_kernel<KIND, IB, JB>), dim3((n + few - 1) / few), dim3(512), 0, \
+                     st, X, W, T, D, V, v0, n, ld, tokens, scale, dl)
+    if (const int few = few_rows(T, V)) {   // the forward pass's rule
+      if (T <= 16 && few == 16) JARQ_LINLOG_FEW(1, 1);
+      else if (T <= 16) JARQ_LINLOG_FEW(1, 2);
+      else if (few == 16) JARQ_LINLOG_FEW(2, 1);
+      else JARQ_LINLOG_FEW(2, 2);
+    } else {
+      switch (logit_tiles(T, D, n)) {
+        case 0: JARQ_LINLOG_DL(3, 2, 2, 4, 8, 4); break;
+        case 1: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 4); break;
+        case 2: JARQ_LINLOG_DL(3, 2, 2, 2, 4, 2); break;
+        default: JARQ_LINLOG_DL(3, 3, 1, 2, 4, 2);
+      }
     }
+#undef JARQ_LINLOG_FEW
 #undef JARQ_LINLOG_DL
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

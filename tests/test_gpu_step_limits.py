@@ -8,7 +8,7 @@ import torch
 
 from paper_2609_38599_amd import binding as jb
 from tests._gpu_common import say
-from tests.test_gpu_blocks import E, ROUND, _np
+from tests.test_gpu_blocks import E, ROUND, _np, _randn
 from tests.test_gpu_step import BF16, F16, _linlog_inputs
 
 pytestmark = [pytest.mark.gpu,
@@ -124,6 +124,31 @@ def test_linear_logprobs_of_finite_logits_far_from_0(T, V, dt):
                 # (1 - p of a leader alone is 0, of n a difference of halves)
                 bound = rel * size + 8 * E * (np.abs(W).max() if got is dX else np.abs(X).sum()) + tiny
                 assert np.all(np.abs(got - exact) <= bound), (top, name)
+
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T,d,V", [(1, 4096, 3000), (3, 4096, 3001), (20, 4096, 700), (32, 2056, 4100), (40, 4096, 700),
+                                   (16384 + 20, 1024, 600)])
+def test_gradients_of_large_logits_take_the_forward_pass_sums(T, d, V, dt):
+    # Logits of several 10^8, whose sums in fp32 are off by 100 and more: the leading token takes
+    # all in either order of the sum, but its probability is exp of the difference of two sums.
+    x, w = (_randn(80, T, d) * 3000).to(dt).cuda(), (_randn(81, V, d) * 3000).to(dt).cuda()
+    gen = torch.Generator().manual_seed(82)
+    targets = torch.randint(0, V, (T,), generator=gen).cuda()
+    g, h = _randn(83, T).cuda(), _randn(84, T, std=0.1).cuda()
+    g, h = g * 2.0 ** -8, h * 2.0 ** -8       # (dX within float16)
+    W = w.double()
+    value, index = (x.double() @ W.t()).topk(2, dim=1)
+    lead, clear = index[:, 0], value[:, 0] - value[:, 1] > 1e5
+    r = jb.linear_logprobs(x, w, targets)
+    dX, dW = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    assert clear.float().mean() > 0.9 and torch.all(torch.isfinite(dX)) and torch.all(torch.isfinite(dW))
+    G, H = g.double()[:, None], h.double()[:, None]
+    want = G * W[targets] + (H - G) * W[lead]
+    size = G.abs() * W[targets].abs() + (H - G).abs() * W[lead].abs()
+    u, tiny = ROUND[dt]
+    off = (dX.double() - want).abs()
+    assert torch.all((off <= 2.1 * u * size + tiny)[clear])
 
 
 # ---- log probabilities: targets and gradients that are none ----
