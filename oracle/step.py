@@ -66,7 +66,9 @@ def linear_logprobs_grad(X, W, targets, d_logprob, d_lse):
     g = np.where(np.asarray(targets) >= 0, d_logprob, 0.0)
     dl = (d_lse - g)[:, None] * p
     for t, v in enumerate(targets):
-        if v >= 0:
+        if v >= len(W):
+            dl[t] = np.nan if g[t] != 0 or d_lse[t] != 0 else 0.0
+        elif v >= 0:
             dl[t, v] += g[t]
     return dl @ W, dl.T @ X, dl
 

@@ -302,7 +302,7 @@ struct TokenGrad {
     l = none ? 0.f : k.lse[t];
     r = -k.rest[t] * kLog2e;
     // (a target that is none of the vocabulary's: NaN, as its log probability)
-    by_p = to >= V ? NAN : none ? 0.f : h - g;
+    by_p = g == 0.f && h == 0.f ? 0.f : to >= V ? NAN : none ? 0.f : h - g;
   }
   // From a logit, beside the target; 0 is for the caller where by_p is: a token without a gradient
   // gives none, its logits NaN or not.

@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import step
 from paper_2609_38599_amd import binding as jb
 from tests._gpu_common import say
 from tests.test_gpu_blocks import E, ROUND, _np, _randn
@@ -152,6 +153,33 @@ def test_gradients_of_large_logits_take_the_forward_pass_sums(T, d, V, dt):
 
 
 # ---- log probabilities: targets and gradients that are none ----
+
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T,V", [(3, 300), (90, 1000), (600, 2000)])
+def test_targets_outside_the_vocabulary(T, V, dt):
+    x, w, targets, g, h = _linlog_inputs(T, 64, V, dt, seed=90)
+    wrong = targets.clone()
+    wrong[0], wrong[1] = V, 2 ** 40
+    targets[0] = targets[1] = -1
+    g[:2] = 0
+    h[:2] = 0
+    g[2] = 1
+    r, s = jb.linear_logprobs(x, w, targets), jb.linear_logprobs(x, w, wrong)
+    assert torch.all(torch.isnan(s.logprob[:2])) and torch.equal(r.lse, s.lse)
+    for d_lse in (None, h):   # without a gradient: as no target
+        want = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=d_lse)
+        got = jb.linear_logprobs_backward(x, w, wrong, s, g, d_lse=d_lse)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.all(got[0][:2] == 0)
+    for name in ("g", "h"):   # with one: NaN, as the log probability
+        a, b = g.clone(), h.clone()
+        (a if name == "g" else b)[1] = 0.5
+        got = jb.linear_logprobs_backward(x, w, wrong, s, a, d_lse=b)
+        assert torch.all(torch.isnan(got[0][1])) and torch.all(torch.isnan(got[1]))
+        assert torch.equal(got[0][2:], want[0][2:]) and torch.all(got[0][0] == 0)
+        for t, e in zip(got, step.linear_logprobs_grad(_np(x), _np(w), wrong.cpu().numpy(), _np(a), _np(b))):
+            assert np.array_equal(np.isnan(_np(t)), np.isnan(e))
+
 
 def test_float16_gradients_far_below_its_range():
     # normal outputs from gradients below float16's smallest number: channels that x has large where
