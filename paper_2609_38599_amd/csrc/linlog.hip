@@ -10,8 +10,8 @@
 //     dl = g 1{v = target} + (h - g) exp(l - lse)
 // in 16 bits as the matrix cores take them, then dx += dl w (fp32 sums between the pieces) and
 // dw = dl^T x.  Forming the logits twice is a quarter of the work; kept, they would be T V
-// values in memory.  In fp16 dl is scaled by a power of two, the largest |g|, |h| and |h - g| to
-// 2^14, so that a probability of 2^-38 is not lost; the sums are scaled back in fp32.
+// values in memory.  In fp16 dl is scaled by a power of two, the largest finite |g|, |h| and
+// |h - g| to 2^14, so that what is 2^-38 of it is not lost; the sums are scaled back in fp32.
 #include <float.h>
 
 #include "mma_pairs.h"
@@ -256,7 +256,8 @@ __global__ __launch_bounds__(256) void linlog_join_kernel(
 }
 
 // ---- backward: dl of a piece ----
-// One power of two for all tokens' gradients: scale[0], and its inverse in scale[1].
+// One power of two for all tokens' gradients: scale[0], and its inverse in scale[1].  The largest of
+// halves, whose differences stay in range; what is infinite or NaN is its own token's alone.
 __global__ __launch_bounds__(1024) void linlog_scale_kernel(const int64_t* __restrict__ targets,
                                                            const float* __restrict__ dlp,
                                                            const float* __restrict__ dlse, int T,
@@ -264,8 +265,9 @@ __global__ __launch_bounds__(1024) void linlog_scale_kernel(const int64_t* __res
   __shared__ float red[16];
   float m = 0.f;
   for (int t = threadIdx.x; t < T; t += 1024) {
-    const float g = targets[t] >= 0 ? dlp[t] : 0.f, h = dlse ? dlse[t] : 0.f;
-    m = fmaxf(m, fmaxf(fmaxf(fabsf(g), fabsf(h)), fabsf(h - g)));
+    const float g = targets[t] >= 0 ? 0.5f * dlp[t] : 0.f, h = dlse ? 0.5f * dlse[t] : 0.f;
+    for (const float x : {fabsf(g), fabsf(h), fabsf(h - g)})
+      if (x < INFINITY) m = fmaxf(m, x);
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(1024) void linlog_scale_kernel(const int64_t* __res
     for (int w = 1; w < 16; ++w) m = fmaxf(m, red[w]);
     const int e = (int)(__float_as_uint(m) >> 23) - 127;
     // (the scale and its inverse are both normal)
-    const int by = m > 0.f && e < 128 ? min(max(14 - e, -126), 126) : 0;
+    const int by = m > 0.f ? min(13 - e, 126) : 0;
     scale[0] = ldexpf(1.f, by);
     scale[1] = ldexpf(1.f, -by);
   }

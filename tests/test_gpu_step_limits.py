@@ -181,6 +181,35 @@ def test_targets_outside_the_vocabulary(T, V, dt):
             assert np.array_equal(np.isnan(_np(t)), np.isnan(e))
 
 
+@pytest.mark.parametrize("T", [5, 90])
+@pytest.mark.parametrize("bad", [float("inf"), float("-inf"), float("nan")])
+def test_a_broken_gradient_is_its_tokens_alone(T, bad):
+    # (float16 scales all tokens' gradients by one power of two)
+    x, w, targets, g, h = _linlog_inputs(T, 64, 500, F16, seed=91)
+    x, w, g, h = x / 64, w * 64, g * 1e-7, h * 1e-7
+    targets = targets.clamp_min(0)
+    r = jb.linear_logprobs(x, w, targets)
+    g[2] = h[2] = 0
+    want = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h, need=(True, False))[0]
+    assert (want != 0).float().mean() > 0.5
+    for name in ("g", "h"):
+        a, b = g.clone(), h.clone()
+        (a if name == "g" else b)[2] = bad
+        got = jb.linear_logprobs_backward(x, w, targets, r, a, d_lse=b, need=(True, False))[0]
+        keep = torch.arange(T, device="cuda") != 2
+        assert torch.equal(got[keep], want[keep]) and not torch.all(torch.isfinite(got[2]))
+
+
+@pytest.mark.parametrize("T", [5, 90])
+def test_gradients_whose_difference_passes_the_range(T):
+    x, w, targets, g, h = _linlog_inputs(T, 64, 500, F16, seed=92)
+    targets = targets.clamp_min(0)
+    r = jb.linear_logprobs(x, w, targets)
+    g[1], h[1] = 3e38, -2e38
+    dX, dW = jb.linear_logprobs_backward(x, w, targets, r, g, d_lse=h)
+    assert not torch.any(torch.isnan(dX)) and not torch.any(torch.isnan(dW))
+
+
 def test_float16_gradients_far_below_its_range():
     # normal outputs from gradients below float16's smallest number: channels that x has large where
     # w is 0 and the other way round
