@@ -543,8 +543,8 @@ jarq_status jarq_token_logprobs_keep_backward(int32_t dtype, const void* logits,
  *     H = X + residual (rounded to dtype),  r = 1 / sqrt(mean H^2 + eps),
  *     Y[t][c] = H[t][c] r[t] gain[c]        (rounded once from fp32).
  * Without a residual H is X and the pointer NULL.  gain [cols] is of gain_dtype: dtype or
- * JARQ_F32.  1 <= cols <= 2^20, eps at least 2^-126 and finite.  H may be X or residual, and Y X,
- * but not both the same.
+ * JARQ_F32.  1 <= cols <= 2^20, eps at least 2^-126 and finite.  H and Y may each be X or residual,
+ * but not both the same; arrays that overlap otherwise give JARQ_EINVAL.
  * Arrays are aligned to their type.  Sums are in fp64, so a row's squares may pass fp32's
  * range; a row with an infinity or a NaN gives NaN or 0.
  */
@@ -556,7 +556,8 @@ jarq_status jarq_rms_norm(int32_t dtype, int32_t gain_dtype, int64_t tokens, int
  * The same norm on 8 bits, for jarq_matmul_i8 (cols a multiple of 16, at most 131056; Q 16-byte
  * aligned): with w = H gain in fp32 and amax = max |w| of the row,
  *     Q = rint(w (127 / amax)),  scale[t] = (amax / 127) r[t],
- * so that the integers depend on no sum.  Y itself is not rounded to dtype first.  Rows with amax <
+ * so that the integers depend on no sum.  H may be X or residual; Q and scale overlap nothing.  Y
+ * itself is not rounded to dtype first.  Rows with amax <
  * 2^-100 get zeros and scale 0, rows with an infinity or a NaN zeros and scale NaN.
  */
 jarq_status jarq_rms_norm_i8(int32_t dtype, int32_t gain_dtype, int64_t tokens, int32_t cols,
@@ -569,8 +570,9 @@ jarq_status jarq_rms_norm_i8(int32_t dtype, int32_t gain_dtype, int64_t tokens, 
  *     dX = r u - H r^3 mean(u H) + dH,  dgain = sum_t dY H r.
  * dX (of dtype) is the gradient of X and of the residual; dH (nullable) is what reaches H on
  * other ways, the residual stream's.  dgain is of gain_dtype.  dX and dgain are nullable (not
- * formed) and overwritten.  Sums over tokens are in fp32 in an order that the sizes fix.  The workspace (256-byte aligned, jarq_rms_norm_workspace_bytes bytes; 0 if the sizes
- * are invalid) is used only during the call.
+ * formed) and overwritten.  dX may be dY or dH; arrays that overlap otherwise give JARQ_EINVAL.  Sums
+ * over tokens are in fp32 in an order that the sizes fix.  The workspace (256-byte aligned,
+ * jarq_rms_norm_workspace_bytes bytes; 0 if the sizes are invalid) is used only during the call.
  */
 size_t jarq_rms_norm_workspace_bytes(int64_t tokens, int32_t cols);
 jarq_status jarq_rms_norm_backward(int32_t dtype, int32_t gain_dtype, int64_t tokens,

@@ -910,7 +910,7 @@ def rms_norm(X, gain, residual=None, eps=1e-6, out=None, sum_out=None, stream=No
     """The root-mean-square norm of X [tokens, cols] times gain [cols] (X's type or float32).
 
     With a residual the norm is of H = X + residual, rounded to X's type, and (Y, H) is returned;
-    sum_out may be X or the residual, and out X.  rms_norm_backward gives the gradients; autograd
+    out and sum_out may each be X or the residual.  rms_norm_backward gives the gradients; autograd
     records none.
     """
     lib = load_library()

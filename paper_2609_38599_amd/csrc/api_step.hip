@@ -2,6 +2,7 @@
 // include/jarq.h): argument checks and dispatch to the kernels' launchers.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <vector>
 
 #include "jarq.h"
@@ -68,6 +69,20 @@ bool meets(const std::vector<Span>& s, const Span& r) {
   return (at != s.end() && at->from < r.to) || (at != s.begin() && (at - 1)->to > r.from);
 }
 
+// Whether two arrays share bytes (an empty one and a null pointer share none).
+bool overlap(const Span& a, const Span& b) {
+  return a.from != 0 && b.from != 0 && std::max(a.from, b.from) < std::min(a.to, b.to);
+}
+// Whether what is written lies where it may: over one of `over` as a whole or apart from it (row by
+// row the same), and apart from `others`.
+bool fits(const Span& out, std::initializer_list<Span> over, std::initializer_list<Span> others) {
+  for (const Span& s : over)
+    if (s.from != out.from && overlap(out, s)) return false;
+  for (const Span& s : others)
+    if (overlap(out, s)) return false;
+  return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -77,8 +92,12 @@ jarq_status jarq_rms_norm(int32_t dtype, int32_t gain_dtype, int64_t tokens, int
                           void* H, void* Y, void* stream) {
   if (!valid_norm(dtype, gain_dtype, tokens, cols, gain, eps)) return JARQ_EINVAL;
   if (tokens == 0) return JARQ_OK;
-  if (!valid_rows(dtype, X, residual, H) || !aligned(Y, bytes_of(dtype)) || Y == H)
-    return JARQ_EINVAL;
+  if (!valid_rows(dtype, X, residual, H) || !aligned(Y, bytes_of(dtype))) return JARQ_EINVAL;
+  // (a row is read before it is written)
+  const size_t rows = bytes_of(dtype) * (size_t)tokens * cols;
+  const Span x = span(X, rows), r = span(residual, rows), h = span(H, rows), y = span(Y, rows);
+  const Span g = span(gain, bytes_of(gain_dtype) * (size_t)cols);
+  if (!fits(h, {x, r}, {g, y}) || !fits(y, {x, r}, {g})) return JARQ_EINVAL;
   return status_of(launch_rms_norm((hipStream_t)stream, dtype, gain_dtype, X, residual, gain, eps,
                                    (int)tokens, cols, H, Y));
 }
@@ -90,6 +109,12 @@ jarq_status jarq_rms_norm_i8(int32_t dtype, int32_t gain_dtype, int64_t tokens, 
     return JARQ_EINVAL;
   if (tokens == 0) return JARQ_OK;
   if (!valid_rows(dtype, X, residual, H) || !aligned(Q, 16) || !aligned(scale, 4))
+    return JARQ_EINVAL;
+  const size_t rows = bytes_of(dtype) * (size_t)tokens * cols;
+  const Span x = span(X, rows), r = span(residual, rows), h = span(H, rows);
+  const Span q = span(Q, (size_t)tokens * cols), s = span(scale, 4 * (size_t)tokens);
+  const Span g = span(gain, bytes_of(gain_dtype) * (size_t)cols);
+  if (!fits(h, {x, r}, {g, q, s}) || !fits(q, {}, {x, r, g, s}) || !fits(s, {}, {x, r, g}))
     return JARQ_EINVAL;
   return status_of(launch_rms_norm_i8((hipStream_t)stream, dtype, gain_dtype, X, residual, gain,
                                       eps, (int)tokens, cols, H, Q, scale));
@@ -113,6 +138,14 @@ jarq_status jarq_rms_norm_backward(int32_t dtype, int32_t gain_dtype, int64_t to
   const jarq_status s =
       check(workspace, workspace_bytes, jarq_rms_norm_workspace_bytes(tokens, cols));
   if (s != JARQ_OK) return s;
+  const size_t rows = a * (size_t)tokens * cols;
+  const Span h = span(H, rows), y = span(dY, rows), d = span(dH, rows);
+  const Span g = span(gain, bytes_of(gain_dtype) * (size_t)cols), x = span(dX, rows);
+  const Span dg = span(dgain, bytes_of(gain_dtype) * (size_t)cols);
+  const Span ws = span(workspace, jarq_rms_norm_workspace_bytes(tokens, cols));
+  if (!fits(x, {y, d}, {h, g, dg, ws}) || !fits(dg, {}, {h, y, d, g, ws}) ||
+      !fits(ws, {}, {h, y, d, g}))
+    return JARQ_EINVAL;
   return status_of(launch_rms_norm_backward((hipStream_t)stream, dtype, gain_dtype, H, gain, dY,
                                             dH, eps, (int)tokens, cols, dX, dgain,
                                             (char*)workspace));

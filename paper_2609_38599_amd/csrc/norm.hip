@@ -18,7 +18,6 @@ namespace {
 
 // Eight values from element 8 v of a row at any element's alignment, as they are stored.
 typedef u32x4 AnyVec __attribute__((aligned(2)));
-typedef u32x2 AnyHalf __attribute__((aligned(1)));
 template <int DT> struct Elem { typedef uint16_t T; };
 template <> struct Elem<0> { typedef float T; };
 template <int DT> struct Eight { u32x4 w[DT == 0 ? 2 : 1]; };
@@ -490,15 +489,20 @@ static hipError_t launch_norm_grad(hipStream_t st, const void* H, const void* ga
   float* part = dgain ? (float*)ws : nullptr;
   if (cols > kMostCols) {
     float* rs = dgain ? (float*)ws : nullptr;
+    // dgain reads dY once more: where dX lies over it, before dX is formed
+    const bool over = dgain && dX == dY;
     if (T > 0)
       hipLaunchKernelGGL((norm_grad_long_kernel<DT, GAIN32>), dim3(T), dim3(256), 0, st, H, gain,
-                         dY, dH, eps, cols, dX, rs);
+                         dY, dH, eps, cols, over ? nullptr : dX, rs);
     if (dgain) {
       parts = norm_long_parts(T);
       part = (float*)(ws + pad256(4 * (size_t)T));
       hipLaunchKernelGGL((norm_gain_long_kernel<DT>), dim3((cols + 2047) / 2048, parts), dim3(256),
                          0, st, H, dY, rs, T, cols, part);
     }
+    if (T > 0 && over)
+      hipLaunchKernelGGL((norm_grad_long_kernel<DT, GAIN32>), dim3(T), dim3(256), 0, st, H, gain,
+                         dY, dH, eps, cols, dX, nullptr);
   } else {
 #define JARQ_NORM_GRAD(NW, R)                                                                   \
   hipLaunchKernelGGL((norm_grad_kernel<DT, GAIN32, NW, R>), dim3(parts),                        \

@@ -2,6 +2,8 @@
 gradients against what one rounding leaves, logits far from 0, targets and gradients that are none,
 arrays that are written in place."""
 
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -10,7 +12,7 @@ from oracle import step
 from paper_2609_38599_amd import binding as jb
 from tests._gpu_common import say
 from tests.test_gpu_blocks import E, ROUND, _np, _randn
-from tests.test_gpu_step import BF16, F16, _linlog_inputs
+from tests.test_gpu_step import BF16, F16, F32, _linlog_inputs, _norm_inputs
 
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
@@ -217,3 +219,44 @@ def test_float16_gradients_far_below_its_range():
     x[:, :64], w[:, :64] = x[:, :64] * 4096, 0
     w[:, 64:128], x[:, 64:128] = w[:, 64:128] * 30000, 0
     _check_rounded_once(x, w, targets, g * 1e-8, h * 1e-9, "small gradients")
+
+
+# ---- the norm's gradient in place ----
+
+@pytest.mark.parametrize("dt", [F32, BF16])
+@pytest.mark.parametrize("cols", [64, 1024, 4096, 16384, 16392, 20011])
+def test_norm_gradient_in_place(cols, dt):
+    T, lib = 70, jb.load_library()
+    x, _, gain, dy, dh = _norm_inputs(T, cols, dt, dt, seed=60)
+    n = int(lib.jarq_rms_norm_workspace_bytes(T, cols))
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    for a in (None, dh):
+        want = jb.rms_norm_backward(x, gain, dy, dH=a)
+        for over in ("dy", "dh"):
+            for wanted in (True, False):
+                y, b = dy.clone(), None if a is None else a.clone()
+                if over == "dh" and a is None:
+                    continue
+                dx, dgain = y if over == "dy" else b, torch.empty_like(gain)
+                assert lib.jarq_rms_norm_backward(
+                    jb.DTYPES[dt], jb.DTYPES[dt], T, cols, x.data_ptr(), gain.data_ptr(), y.data_ptr(),
+                    None if b is None else b.data_ptr(), ctypes.c_float(1e-6), dx.data_ptr(),
+                    dgain.data_ptr() if wanted else None, ws.data_ptr(), n,
+                    torch.cuda.current_stream().cuda_stream) == jb.JARQ_OK
+                assert torch.equal(dx, want[0]) and (not wanted or torch.equal(dgain, want[1]))
+
+
+def test_norm_into_what_it_reads():
+    for cols in (64, 4096, 20000):
+        x, res, gain, _, _ = _norm_inputs(9, cols, BF16, BF16, seed=61)
+        y, h = jb.rms_norm(x, gain, residual=res)
+        for out, sum_out in ((0, 1), (1, 0), (1, None), (None, 1)):
+            at = [x.clone(), res.clone()]
+            got = jb.rms_norm(at[0], gain, residual=at[1], out=None if out is None else at[out],
+                              sum_out=None if sum_out is None else at[sum_out])
+            assert torch.equal(got[0], y) and torch.equal(got[1], h)
+        with pytest.raises(jb.JarqError):
+            jb.rms_norm(x, gain, residual=res, out=x, sum_out=x)
+        flat = torch.cat([x.view(-1), x.view(-1)[:2]])
+        with pytest.raises(jb.JarqError):
+            jb.rms_norm(flat[:-2].view(9, cols), gain, out=flat[2:].view(9, cols))
