@@ -590,6 +590,17 @@ def _work(n, like):
     return ws if ws.data_ptr() % 256 == 0 else _scratch(n, like.device)
 
 
+_written = torch.autograd.graph.increment_version
+
+
+def _wrote(*tensors):
+    """Tells autograd that a call has written into these tensors (or None).
+
+    A backward pass that kept one of them then says that it is no longer what it was.
+    """
+    _written([t for t in tensors if t is not None])
+
+
 def _outside(call, gradient):
     """Says that the result of an input that requires a gradient is none of autograd's."""
     if torch.is_grad_enabled():
@@ -627,7 +638,7 @@ def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
     at = _device(X, "X")
     if _rows(Wu, "Wu", d)[0] != f:
         raise ValueError("Wg and Wu must have the same shape")
-    pre = None
+    pre, given = None, out is not None
     if not save and (X.requires_grad or Wg.requires_grad or Wu.requires_grad):
         _outside("gated_forward", "gated_backward gives its gradients, from save=True")
     with _on(stream):
@@ -643,6 +654,8 @@ def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
                                   _at(out, dt, "out", at), _own(pre),
                                   _queue(stream, at)),
            "jarq_gated_forward")
+    if given:
+        _wrote(out)
     return (out, pre) if save else out
 
 
@@ -681,6 +694,7 @@ def quant_rows_i8(X, out=None, scale=None, stream=None):
     lib = load_library()
     rows, cols = _rows(X, "X")
     at = _device(X, "X")
+    given = out is not None or scale is not None
     with _on(stream):
         if out is None:
             out = torch.empty(rows, cols, dtype=torch.int8, device=X.device)
@@ -692,6 +706,8 @@ def quant_rows_i8(X, out=None, scale=None, stream=None):
                                   _at(out, torch.int8, "out", at),
                                   _at(scale, torch.float32, "scale", at), _queue(stream, at)),
            "jarq_quant_rows_i8")
+    if given:
+        _wrote(out, scale)
     return out, scale
 
 
@@ -699,6 +715,7 @@ def codes_i8(p: Params, codes, zeros, out=None, stream=None):
     """q - z as int8: a quantized layer's weights for matmul_i8 and linear_i8."""
     lib = load_library()
     at = _device(codes, "codes")
+    given = out is not None
     with _on(stream):
         if out is None:
             out = torch.empty(p.rows, p.cols, dtype=torch.int8, device=codes.device)
@@ -710,6 +727,8 @@ def codes_i8(p: Params, codes, zeros, out=None, stream=None):
                              _at(zeros, torch.int32, "zeros", at), _at(out, torch.int8, "out", at),
                              _own(flag), _queue(stream, at)),
            "jarq_codes_i8")
+    if given:
+        _wrote(out)
     return out
 
 
@@ -732,6 +751,7 @@ def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
         raise ValueError("sx must hold one scale a token")
     if sx.requires_grad or sw.requires_grad:
         _outside("matmul_i8", "it has no gradient")
+    given = out is not None
     with _on(stream):
         if out is None:
             out = torch.empty(T, n, dtype=dtype, device=Xq.device)
@@ -741,6 +761,8 @@ def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
                               _at(sx, torch.float32, "sx", at), _at(Wq, torch.int8, "Wq", at),
                               _at(sw, torch.float32, "sw", at), _at(out, out.dtype, "out", at),
                               _queue(stream, at)), "jarq_matmul_i8")
+    if given:
+        _wrote(out)
     return out
 
 
@@ -758,7 +780,7 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
         raise JarqError(JARQ_EINVAL, "jarq_linear_i8_workspace_bytes")
     if X.requires_grad or sw.requires_grad:
         _outside("linear_i8", "it has no gradient")
-    dt = X.dtype
+    dt, given = X.dtype, out is not None
     with _on(stream):
         if out is None:
             out = torch.empty(T, n, dtype=dt, device=X.device)
@@ -770,6 +792,8 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
                               _at(Wq, torch.int8, "Wq", at), _at(sw, torch.float32, "sw", at),
                               _at(out, dt, "out", at), _at(ws, torch.uint8, "workspace", at),
                               ws.numel(), _queue(stream, at)), "jarq_linear_i8")
+    if given:
+        _wrote(out)
     return out
 
 
@@ -846,6 +870,7 @@ def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, 
                     (d_entropy, "d_entropy")):
         if t is not None and t.shape != (T,):
             raise ValueError(f"{name} must be [tokens]")
+    given = out is not None
     if out is None:
         with _on(stream):
             out = torch.empty(T, V, dtype=logits.dtype, device=logits.device)
@@ -868,6 +893,8 @@ def token_logprobs_backward(logits, targets, forward: TokenLogprobs, d_logprob, 
         _check(lib.jarq_token_logprobs_keep_backward(
             *head, _at(rest, torch.float32, "lse_rest", at), *tail),
             "jarq_token_logprobs_keep_backward")
+    if given:
+        _wrote(out)
     return out
 
 
@@ -917,6 +944,7 @@ def rms_norm(X, gain, residual=None, eps=1e-6, out=None, sum_out=None, stream=No
     at = _device(X, "X")
     code, gcode, T, cols, x, res, g = _norm_args(X, gain, residual, at)
     _no_norm_graph("rms_norm", X, gain, residual, "rms_norm_backward gives its gradients")
+    given = out is not None or sum_out is not None
     with _on(stream):
         if out is None:
             out = torch.empty_like(X)
@@ -925,6 +953,8 @@ def rms_norm(X, gain, residual=None, eps=1e-6, out=None, sum_out=None, stream=No
         H = _sum_out(sum_out, X, residual)
     _check(lib.jarq_rms_norm(code, gcode, T, cols, x, res, g, eps, _at(H, X.dtype, "sum_out", at),
                              _at(out, X.dtype, "out", at), _queue(stream, at)), "jarq_rms_norm")
+    if given:
+        _wrote(out, H)
     return out if residual is None else (out, H)
 
 
@@ -937,6 +967,7 @@ def rms_norm_i8(X, gain, residual=None, eps=1e-6, out=None, scale=None, sum_out=
     at = _device(X, "X")
     code, gcode, T, cols, x, res, g = _norm_args(X, gain, residual, at)
     _no_norm_graph("rms_norm_i8", X, gain, residual, "it has no gradient")
+    given = out is not None or scale is not None or sum_out is not None
     with _on(stream):
         if out is None:
             out = torch.empty(T, cols, dtype=torch.int8, device=X.device)
@@ -949,6 +980,8 @@ def rms_norm_i8(X, gain, residual=None, eps=1e-6, out=None, scale=None, sum_out=
                                 _at(H, X.dtype, "sum_out", at), _at(out, torch.int8, "out", at),
                                 _at(scale, torch.float32, "scale", at), _queue(stream, at)),
            "jarq_rms_norm_i8")
+    if given:
+        _wrote(out, scale, H)
     return (out, scale) if residual is None else (out, scale, H)
 
 
@@ -1209,9 +1242,7 @@ def adamw_step(params, grads, state: AdamWState, step, lr, beta1=0.9, beta2=0.99
                             step_at, _one_value(grad_mul, torch.float32, "grad_mul", at))
     _check(lib.jarq_adamw_step(code, bits, len(params), ctypes.addressof(table), held, to, options,
                                _queue(stream, at)), "jarq_adamw_step")
-    moved = [t for t in new_params if t.requires_grad]
-    if moved:   # a backward pass that kept the old values says so
-        torch.autograd.graph.increment_version(moved)
+    _written(new_params + [t for t in new_state if t is not None])
     return new_params, new_state
 
 

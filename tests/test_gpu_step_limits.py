@@ -260,3 +260,62 @@ def test_norm_into_what_it_reads():
         flat = torch.cat([x.view(-1), x.view(-1)[:2]])
         with pytest.raises(jb.JarqError):
             jb.rms_norm(flat[:-2].view(9, cols), gain, out=flat[2:].view(9, cols))
+
+
+# ---- autograd: what a call writes into, and what it loses ----
+
+def _calls_into():
+    """(name, call, the tensors that it writes into): every call with tensors of the caller's."""
+    def t(*shape, dtype=BF16):
+        return torch.ones(*shape, dtype=dtype, device="cuda")
+
+    x, y, h, gain, w = t(4, 64), t(4, 64), t(4, 64), t(64), t(8, 64)
+    q, s = t(4, 64, dtype=torch.int8), t(4, 1, dtype=F32)
+    wq, sw = t(8, 64, dtype=torch.int8), t(8, 1, dtype=F32)
+    to, g = torch.zeros(4, dtype=torch.int64, device="cuda"), t(4, dtype=F32)
+    o8, o64 = t(4, 8), t(4, 64)
+    p, new = t(300), t(300)
+    state, other = jb.adamw_state([p], bits=8), jb.adamw_state([p], bits=8)
+    prm = jb.make_params(8, 64, 32, 3)
+    codes, zeros = t(8, 64, dtype=torch.uint8), t(8, 2, dtype=torch.int32)
+    return [
+        ("rms_norm", lambda: jb.rms_norm(x, gain, residual=y, out=h, sum_out=y), [h, y]),
+        ("rms_norm out", lambda: jb.rms_norm(x, gain, out=x), [x]),
+        ("rms_norm_i8", lambda: jb.rms_norm_i8(y, gain, residual=h, out=q, scale=s, sum_out=y), [q, s, y]),
+        ("adamw_step", lambda: jb.adamw_step([p], [t(300)], state, 1, 1e-3),
+         [p, state.master, state.m, state.v, state.m_exp, state.v_exp]),
+        ("adamw_step out", lambda: jb.adamw_step([p], [t(300)], state, 1, 1e-3, out=([new], other)),
+         [new, other.master, other.m, other.v, other.m_exp, other.v_exp]),
+        ("gated_forward", lambda: jb.gated_forward(x, w, w, out=o8), [o8]),
+        ("quant_rows_i8", lambda: jb.quant_rows_i8(x, out=q, scale=s), [q, s]),
+        ("codes_i8", lambda: jb.codes_i8(prm, codes, zeros, out=wq), [wq]),
+        ("matmul_i8", lambda: jb.matmul_i8(q, s, wq, sw, out=o8), [o8]),
+        ("linear_i8", lambda: jb.linear_i8(x, wq, sw, out=o8), [o8]),
+        ("token_logprobs_backward", lambda: jb.token_logprobs_backward(
+            o64, to, jb.token_logprobs(o64, to), g, out=h), [h]),
+    ]
+
+
+def test_what_a_call_writes_into_has_another_version():
+    for name, call, into in _calls_into():
+        before = [t._version for t in into]
+        call()
+        assert all(t._version > v for t, v in zip(into, before)), name
+    with torch.inference_mode():   # whose tensors have none
+        for name, call, into in _calls_into():
+            call()
+
+
+def test_a_backward_pass_that_kept_what_is_overwritten_says_so():
+    x = torch.ones(300, device="cuda", requires_grad=True)
+    p = torch.ones(300, device="cuda")
+    y = (p * x).sum()      # keeps p, which needs no gradient itself
+    jb.adamw_step([p], [torch.ones_like(p)], jb.adamw_state([p]), 1, 1e-2)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    stream = torch.ones(4, 64, device="cuda")
+    a = torch.ones(4, 64, device="cuda", requires_grad=True)
+    y = (stream * a).sum()
+    jb.rms_norm(torch.ones(4, 64, device="cuda"), torch.ones(64, device="cuda"), residual=stream, sum_out=stream)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
