@@ -14,6 +14,7 @@ import warnings
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libjarq.so")
@@ -601,8 +602,14 @@ def _wrote(*tensors):
     _written([t for t in tensors if t is not None])
 
 
+def _dual(*tensors):
+    """Whether one of them (or None) carries a tangent of forward-mode differentiation."""
+    return forward_ad._current_level >= 0 and any(
+        t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
+
+
 def _outside(call, gradient):
-    """Says that the result of an input that requires a gradient is none of autograd's."""
+    """Says that the result of an input that requires a gradient or has a tangent is none of autograd's."""
     if torch.is_grad_enabled():
         warnings.warn(f"{call}: the result is outside autograd's graph; {gradient} "
                       "(this is not said under torch.no_grad())", stacklevel=3)
@@ -639,7 +646,8 @@ def gated_forward(X, Wg, Wu, act="silu", out=None, save=False, stream=None):
     if _rows(Wu, "Wu", d)[0] != f:
         raise ValueError("Wg and Wu must have the same shape")
     pre, given = None, out is not None
-    if not save and (X.requires_grad or Wg.requires_grad or Wu.requires_grad):
+    if (not save and (X.requires_grad or Wg.requires_grad or Wu.requires_grad)
+            or _dual(X, Wg, Wu)):
         _outside("gated_forward", "gated_backward gives its gradients, from save=True")
     with _on(stream):
         if out is None:
@@ -749,7 +757,7 @@ def matmul_i8(Xq, sx, Wq, sw, dtype=torch.bfloat16, out=None, stream=None):
     at = _device(Xq, "Xq")
     if sx.numel() != T:
         raise ValueError("sx must hold one scale a token")
-    if sx.requires_grad or sw.requires_grad:
+    if sx.requires_grad or sw.requires_grad or _dual(sx, sw):
         _outside("matmul_i8", "it has no gradient")
     given = out is not None
     with _on(stream):
@@ -778,7 +786,7 @@ def linear_i8(X, Wq, sw, out=None, ws=None, stream=None):
     need = int(lib.jarq_linear_i8_workspace_bytes(T, k))
     if need == 0:
         raise JarqError(JARQ_EINVAL, "jarq_linear_i8_workspace_bytes")
-    if X.requires_grad or sw.requires_grad:
+    if X.requires_grad or sw.requires_grad or _dual(X, sw):
         _outside("linear_i8", "it has no gradient")
     dt, given = X.dtype, out is not None
     with _on(stream):
@@ -838,7 +846,7 @@ def token_logprobs(logits, targets, top=0, ws=None, stream=None) -> TokenLogprob
     n = int(lib.jarq_token_logprobs_workspace_bytes(T, V, top))
     if n == 0:
         raise JarqError(JARQ_EINVAL, "jarq_token_logprobs_workspace_bytes")
-    if logits.requires_grad:
+    if logits.requires_grad or _dual(logits):
         _outside("token_logprobs", "token_logprobs_backward gives the logits' gradient")
     dev = logits.device
     with _on(stream):
@@ -916,7 +924,8 @@ def _norm_args(X, gain, residual, at):
 
 
 def _no_norm_graph(call, X, gain, residual, says):
-    if X.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad):
+    if (X.requires_grad or gain.requires_grad or (residual is not None and residual.requires_grad)
+            or _dual(X, gain, residual)):
         _outside(call, says)
 
 
@@ -1035,7 +1044,7 @@ def linear_logprobs(X, W, targets, ws=None, stream=None) -> LinearLogprobs:
     n = int(lib.jarq_linear_logprobs_workspace_bytes(T, d, V))
     if n == 0:
         raise JarqError(JARQ_EINVAL, "jarq_linear_logprobs_workspace_bytes")
-    if X.requires_grad or W.requires_grad:
+    if X.requires_grad or W.requires_grad or _dual(X, W):
         _outside("linear_logprobs", "linear_logprobs_backward gives its gradients")
     dt = X.dtype
     with _on(stream):

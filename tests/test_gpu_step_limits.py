@@ -3,10 +3,12 @@ gradients against what one rounding leaves, logits far from 0, targets and gradi
 arrays that are written in place."""
 
 import ctypes
+import warnings
 
 import numpy as np
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from oracle import step
 from paper_2609_38599_amd import binding as jb
@@ -319,3 +321,27 @@ def test_a_backward_pass_that_kept_what_is_overwritten_says_so():
     jb.rms_norm(torch.ones(4, 64, device="cuda"), torch.ones(64, device="cuda"), residual=stream, sum_out=stream)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         y.backward()
+
+
+def test_tangents_that_are_lost_are_said_to_be():
+    def t(*shape, dtype=BF16):
+        return torch.ones(*shape, dtype=dtype, device="cuda")
+
+    gain, w = t(64), t(8, 64)
+    wq, sw = t(8, 64, dtype=torch.int8), t(8, 1, dtype=F32)
+    to = torch.zeros(4, dtype=torch.int64, device="cuda")
+    with forward_ad.dual_level():
+        x = forward_ad.make_dual(t(4, 64), t(4, 64))
+        dual = forward_ad.make_dual(gain, t(64))
+        calls = (lambda: jb.rms_norm(x, gain), lambda: jb.rms_norm(t(4, 64), dual),
+                 lambda: jb.rms_norm(t(4, 64), gain, residual=x), lambda: jb.rms_norm_i8(x, gain),
+                 lambda: jb.linear_logprobs(x, w, to), lambda: jb.gated_forward(x, w, w),
+                 lambda: jb.linear_i8(x, wq, sw), lambda: jb.token_logprobs(x, to))
+        for k, call in enumerate(calls):
+            with pytest.warns(UserWarning, match="autograd"):
+                call()
+        with warnings.catch_warnings():
+            warnings.simplefilter("error")
+            jb.rms_norm(t(4, 64), gain)
+            with torch.no_grad():
+                jb.linear_logprobs(x, w, to)
