@@ -631,8 +631,8 @@ jarq_status jarq_linear_logprobs_backward(int32_t dtype, int64_t tokens, int32_t
  * to their type.  Parameters of 16 bits are the rounded ones of fp32 in `master`.
  *
  * The state is flat: a tensor's values begin at the sum of the lengths before it, each rounded up to
- * a multiple of 128 (jarq_adamw_state_length is the total).  What lies between is not read, and
- * zero or left as it was.
+ * a multiple of 128 (jarq_adamw_state_length is the total).  What lies between has no part in the
+ * step and becomes zero or stays (a step that changes nothing may copy it to `out`).
  *   master [n] fp32 (NULL for fp32 parameters);
  *   bits = 32: m, v [n] fp32;
  *   bits = 8: m and sqrt(v) [n] in e4m3 (bias 7, no infinities), m_exp, v_exp [n / 128]: a value

@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamScalars s, j
   float root[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if (i + j >= n) m[j] = v[j] = 0.f;   // the padding has no part in its block's largest
+    if (i + j >= n) p[j] = m[j] = v[j] = 0.f;   // the padding has no part in its block's largest
     if constexpr (BITS == 8) v[j] *= v[j];
     advance(s, s.grad_mul ? g[j] * mul : g[j], p[j], m[j], v[j], root[j]);
   }

@@ -14,7 +14,7 @@ from oracle import step
 from paper_2609_38599_amd import binding as jb
 from tests._gpu_common import say
 from tests.test_gpu_blocks import E, ROUND, _np, _randn
-from tests.test_gpu_step import BF16, F16, F32, _linlog_inputs, _norm_inputs
+from tests.test_gpu_step import BF16, F16, F32, OPT, _linlog_inputs, _norm_inputs
 
 pytestmark = [pytest.mark.gpu,
               pytest.mark.skipif(not torch.cuda.is_available(), reason="needs a GPU")]
@@ -345,3 +345,38 @@ def test_tangents_that_are_lost_are_said_to_be():
             jb.rms_norm(t(4, 64), gain)
             with torch.no_grad():
                 jb.linear_logprobs(x, w, to)
+
+
+# ---- AdamW: what lies between the tensors ----
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("dt", [F32, BF16])
+def test_adamw_leaves_or_clears_what_lies_between_the_tensors(dt, bits):
+    # lengths that end inside eight values, inside a block, inside a work-group's share
+    sizes = [1, 5, 127, 300, 2049]
+    params = [_randn(k, n).to(dt).cuda() for k, n in enumerate(sizes)]
+    grads = [_randn(9 + k, n).to(dt).cuda() for k, n in enumerate(sizes)]
+    state = jb.adamw_state(params, bits=bits)
+    between = torch.ones(len(state.m), dtype=torch.bool, device="cuda")
+    at = step.offsets(sizes)[0]
+    for first, n in zip(at, sizes):
+        between[first:first + n] = False
+    held = [a for a in (state.master, state.m, state.v) if a is not None]
+    for a in held:
+        raw = a.view(torch.uint8) if a.dtype != F32 else a
+        raw[between] = 57
+    clean = [p.clone() for p in params]
+    same = jb.adamw_state(clean, bits=bits)
+    jb.adamw_step(params, grads, state, 1, 1e-2, seed=4, **OPT)
+    jb.adamw_step(clean, grads, same, 1, 1e-2, seed=4, **OPT)
+    assert all(torch.equal(a, b) for a, b in zip(params, clean))     # it has no part in the step
+    for a, b in zip(state, same):
+        if a is None:
+            continue
+        if a.dtype == torch.uint8:
+            assert torch.equal(a, b)
+            continue
+        a, b = (t.view(torch.uint8) if t.dtype != F32 else t for t in (a, b))
+        assert torch.equal(a[~between], b[~between])
+        left = a[between]
+        assert torch.all((left == 0) | (left == 57))
