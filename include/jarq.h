@@ -570,8 +570,8 @@ jarq_status jarq_rms_norm_i8(int32_t dtype, int32_t gain_dtype, int64_t tokens, 
  *     dX = r u - H r^3 mean(u H) + dH,  dgain = sum_t dY H r.
  * dX (of dtype) is the gradient of X and of the residual; dH (nullable) is what reaches H on
  * other ways, the residual stream's.  dgain is of gain_dtype.  dX and dgain are nullable (not
- * formed) and overwritten.  dX may be dY or dH; arrays that overlap otherwise give JARQ_EINVAL.  Sums
- * over tokens are in fp32 in an order that the sizes fix.  The workspace (256-byte aligned,
+ * formed) and overwritten.  dX may be dY or dH; arrays that overlap otherwise give JARQ_EINVAL.
+ * Sums over tokens are in fp32 in an order that the sizes fix.  The workspace (256-byte aligned,
  * jarq_rms_norm_workspace_bytes bytes; 0 if the sizes are invalid) is used only during the call.
  */
 size_t jarq_rms_norm_workspace_bytes(int64_t tokens, int32_t cols);
@@ -609,9 +609,10 @@ jarq_status jarq_linear_logprobs(int32_t dtype, int64_t tokens, int32_t d, int32
  * 2^14..2^15: entries below 2^-39 of it become 0); what that leaves at a
  * token's target is added to dX and dW.  A token of g = h = 0 has dX = 0 whatever its logits and
  * target (W being finite); to dW it adds products with 0, so an infinity or a NaN in its X makes dW
- * NaN.  With a gradient, a target that is not below vocab makes its token's dX and all of dW NaN.  logprob, lse and lse_rest as the forward pass left them.  The workspace (256-byte aligned,
+ * NaN.  With a gradient, a target that is not below vocab makes its token's dX and all of dW NaN.
+ * logprob, lse and lse_rest as the forward pass left them.  The workspace (256-byte aligned,
  * jarq_linear_logprobs_backward_workspace_bytes bytes, 0 if the sizes are invalid: up to 2^17
- * tokens 256 MiB at most, and 4 bytes a value of dX times the shares that its sums are cut into,
+ * tokens 272 MiB at most, and 4 bytes a value of dX times the shares that its sums are cut into,
  * 32 at most) is used only during the call.
  */
 size_t jarq_linear_logprobs_backward_workspace_bytes(int64_t tokens, int32_t d, int32_t vocab);

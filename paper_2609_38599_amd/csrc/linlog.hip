@@ -163,7 +163,8 @@ __device__ __forceinline__ void few_logits(const void* X, const void* W, int T, 
   for (int a = 0; a < IB; ++a) p[a] = (const char*)X + (size_t)min(16 * a + row, T - 1) * ld;
   const char* q[JB];
 #pragma unroll
-  for (int b = 0; b < JB; ++b) q[b] = (const char*)W + (size_t)min(r0 + 16 * b + row, rows - 1) * ld;
+  for (int b = 0; b < JB; ++b)
+    q[b] = (const char*)W + (size_t)min(r0 + 16 * b + row, rows - 1) * ld;
   f32x4 acc[IB][JB] = {};
   skinny_loop<IB, JB, 4, NW>(
       p, q, 2 * D, wave, lane, [](int, int) {},
@@ -256,8 +257,9 @@ __global__ __launch_bounds__(256) void linlog_join_kernel(
 }
 
 // ---- backward: dl of a piece ----
-// One power of two for all tokens' gradients: scale[0], and its inverse in scale[1].  The largest of
-// halves, whose differences stay in range; what is infinite or NaN is its own token's alone.
+// One power of two for all tokens' gradients: scale[0], and its inverse in scale[1].  From the
+// largest of their halves, whose differences stay in range; what is infinite or NaN is its own
+// token's alone.
 __global__ __launch_bounds__(1024) void linlog_scale_kernel(const int64_t* __restrict__ targets,
                                                            const float* __restrict__ dlp,
                                                            const float* __restrict__ dlse, int T,
@@ -687,7 +689,8 @@ int forward_parts(int T, int n, int D, int V) {
   return (V + kWide[k] - 1) / kWide[k];
 }
 
-// Rows of w a piece: dl of a piece at most 256 MiB (at least 1024 rows).
+// Rows of w a piece: 256 MiB of dl (at least 1024 rows).  Its stride, up to 64 values longer, adds 128
+// bytes a token: 272 MiB at 2^17 tokens.
 int piece_rows(int T, int V) {
   const int64_t most = std::max<int64_t>(1024, ((int64_t)1 << 27) / std::max(T, 1) / 1024 * 1024);
   return (int)std::min<int64_t>(most, V);

@@ -1,6 +1,9 @@
-"""What the norm's entry points refuse of arrays that overlap (CPU only: every call fails its checks)."""
+"""What the norm's entry points refuse of arrays that overlap, and what the backward passes' workspaces
+take (CPU only: every call fails its checks)."""
 
 import ctypes
+import os
+import re
 
 import pytest
 import torch
@@ -63,3 +66,19 @@ def test_norm_gradient_refuses_arrays_that_overlap(lib):
                   dict(dg=5 * MB + rows - 2), dict(ws=1 * MB), dict(ws=2 * MB), dict(ws=3 * MB), dict(ws=4 * MB),
                   dict(ws=5 * MB), dict(ws=6 * MB)):
             assert _backward(lib, cols=cols, **k) == jb.JARQ_EINVAL, (cols, k)
+
+
+def test_workspace_of_the_log_probabilities_gradient_is_what_the_header_says(lib):
+    with open(os.path.join(os.path.dirname(jb.LIB_PATH), "..", "include", "jarq.h")) as f:
+        said = int(re.search(r"tokens (\d+) MiB at most", f.read()).group(1)) * MB
+    most = 0
+    for t in (1, 5, 300, 511, 1000, 4095, 4096, 4097, 10000, 65536, 100003, 131071, 131072):
+        for v in (1, 1000, 8191, 8192, 32001, 128000, 1 << 20, 1 << 22):
+            for d in (8, 1024, 4096):
+                n = int(lib.jarq_linear_logprobs_backward_workspace_bytes(t, d, v))
+                assert 256 <= n <= said + 32 * 4 * t * d + 1024, (t, v, d)
+            # (narrow rows: their sums are 4 MiB a share)
+            n = int(lib.jarq_linear_logprobs_backward_workspace_bytes(t, 8, v))
+            most = max(most, n)
+            assert n - 4 * t * 8 <= said + 512
+    assert most > said - 8 * MB
