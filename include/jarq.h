@@ -546,7 +546,7 @@ jarq_status jarq_token_logprobs_keep_backward(int32_t dtype, const void* logits,
  * JARQ_F32.  1 <= cols <= 2^20, eps at least 2^-126 and finite.  H and Y may each be X or residual,
  * but not both the same; arrays that overlap otherwise give JARQ_EINVAL.
  * Arrays are aligned to their type.  Sums are in fp64, so a row's squares may pass fp32's
- * range; a row with an infinity or a NaN gives NaN or 0.
+ * range (r is fp32: to 2^-22 where it is below 2^-126); a row with an infinity or a NaN gives NaN or 0.
  */
 jarq_status jarq_rms_norm(int32_t dtype, int32_t gain_dtype, int64_t tokens, int32_t cols,
                           const void* X, const void* residual, const void* gain, float eps,

@@ -198,7 +198,7 @@ __device__ __forceinline__ void advance(const AdamScalars& s, float g, float& p,
 // dtype of the parameters and gradients; BITS of the moments.  A work-group takes 2048 values, a
 // lane eight of each array, all loaded at once; sixteen lanes are a block on 8 bits, whose largest
 // comes by four exchanges in a row of lanes.  Bound by memory: 135 M values in bf16, moments in
-// 32 bits (28 bytes a value) 686 us, 5.5 TB/s, in 8 (16.03 bytes) 371 us, 5.8 TB/s; the noise, the
+// 32 bits (28 bytes a value) 686 us, 5.5 TB/s, in 8 (16.03 bytes) 371 to 378 us, 5.8 TB/s; the noise, the
 // roundings and a correctly rounded root are hidden behind it.
 template <int DT, int BITS>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamArgs a, AdamScalars s, jarq_adamw_state in,

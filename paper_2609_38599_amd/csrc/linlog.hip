@@ -65,7 +65,7 @@ __device__ __forceinline__ Part part_of(float (&x)[N]) {
 // ---- forward, many tokens ----
 // WI x WJ wavefronts, each BI blocks of 16 rows of w x BJ blocks of 16 tokens.  Bound by the matrix
 // cores at the clock that the card's power allows: 4096 tokens, 128000 x 4096 in bf16 3.0 ms,
-// 1.43 PFLOP/s (a large library product with the logits stored: 1.45 to 1.52); 2047 x 32001 400 us.
+// 1.43 PFLOP/s (a large library product with the logits stored: 1.45 to 1.52); 2047 x 32001 400 to 420 us.
 // On zeros, at the full clock, 1.88 PFLOP/s.  Tiles that go on with the next while they finish one
 // (256 work-groups that stay) took as long.
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
@@ -326,7 +326,7 @@ __device__ __forceinline__ float target_rest(const Tokens& k, int t, float by) {
 }
 
 // dl [T][ld] of rows v0 .. v0 + n of w (ld a multiple of 8; columns n .. n rounded up to 8 are zeros).
-// Bound as the forward pass: 4096 tokens, 32768 x 4096 810 to 840 us, 1.33 PFLOP/s.
+// Bound as the forward pass: 4096 tokens, 32768 x 4096 805 to 830 us, 1.32 to 1.37 PFLOP/s.
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dl_kernel(
     const void* __restrict__ X, const void* __restrict__ W, int T, int D, int V, int v0, int n,
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(512) void linlog_few_dl_kernel(
 // ---- backward: dx += dl w of a piece ----
 // Rows v0 .. v0 + n of w.  part [splits][T][D] fp32: the sums so far of the share blockIdx.y of each
 // piece's rows; the last piece's go to dX where there is one share.  Bound by the matrix cores: 4096
-// tokens, 32768 x 4096 750 to 780 us, 1.44 PFLOP/s; with four by two wavefronts of 64 x 128 each, which
+// tokens, 32768 x 4096 750 to 770 us, 1.45 PFLOP/s; with four by two wavefronts of 64 x 128 each, which
 // take a fifth less of LDS, as long.
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dx_kernel(
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(256) void linlog_dx_sum_kernel(const float* __restr
 
 // ---- backward: dw = dl^T x of a piece ----
 // Bound by the matrix cores and the transposing reads of LDS, which take twice as long as plain ones:
-// 4096 tokens, 32768 x 4096 820 to 840 us, 1.32 PFLOP/s.  With x transposed beforehand, so that plain
+// 4096 tokens, 32768 x 4096 840 to 870 us, 1.28 PFLOP/s.  With x transposed beforehand, so that plain
 // reads do for eight fragments of twelve, 1 % less.
 template <int KIND, int SP, int SQ, int WI, int WJ, int BI, int BJ>
 __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
@@ -673,10 +673,14 @@ int logit_tiles(int T, int D, int n) {
   return best;
 }
 // Rows of w a work-group where fragments come straight from memory, 0: tiles.  In us with 16
-// rows, 32, and in tiles, d 4096:
-//    1 token    x 16000 23 30 36      x 128000 184 198 186
-//    8 tokens   x  1000 10 13 22      x  32001  60  58  62      x 128000 223 213 190
-//   24          x  5003 23 18 24      x  16000  44  39  37      x  32001 102  81  64
+// rows, 32, and in tiles, the weights from memory (several copies in turn):
+//    d 4096    1 token  x 16000 28 34 40      x 128000 172 197 176
+//              8 tokens x  5003 19 17 36      x  32001  59  61  64     x 128000 223 212 180
+//             24        x  5003 28 21 36      x  16000  54  46  42     x  32001 102  85  65
+//    d  512    4        x 16000 14 14 14      x  32001  19  14  14     x 128000  56  41  33
+// The rule looks at tokens and vocabulary alone: 3 % off the best over 175 sizes in the mean, up to
+// 17 % from 4096 channels on, and up to 1.7 times with few channels and a large vocabulary (the last
+// row).  With the weights in the last cache tiles gain up to a third.
 int few_rows(int T, int V) {
   if (T > 32) return 0;
   if (T <= 4 || V <= 4096) return 16;
@@ -715,6 +719,13 @@ int dw_tiles(int T, int D, int n) {
   return best;
 }
 
+// Tiles and shares of dx, the ones that cost the least; each further share adds its sums' way through
+// memory and the launch that joins them.  dl and dx in us by tiles (channels x tokens) / shares:
+//    8 x 32001, d 4096       128 x 64 / 8   97     128 x 128 / 8  99    256 x 256 / 16 111
+//    200 x 5003, d 1000      128 x 64 / 8   28     128 x 128 / 8  31    256 x 256 /  8  43
+//    611 x 50257, d 1000     128 x 128 / 6 187     256 x 256 / 12 185   128 x  64 /  6 205
+//    2047 x 32001, d 4096    256 x 256 / 2 833     / 4 860   / 3 899    128 x 128 /  1 932
+// 1.7 % off the best of ten sizes in the mean; the most, 6 %, at 611 x 17000, d 4096 (191, 180).
 struct DxPlan {
   int kind;   // tiles of 256 x 256 (channels x tokens), 128 x 128, 128 x 64
   int ni, nj, splits, each;

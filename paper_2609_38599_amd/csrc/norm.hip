@@ -120,7 +120,7 @@ __device__ __forceinline__ float inverse_rms(double squares, int cols, float eps
 // NW wavefronts a row, which stays in registers (R pieces of eight values a lane) between
 // its sum and its outputs; what is beyond 512 NW R columns is read again, from H where there
 // is a residual (H may be X or the residual: each lane reads an element before it writes it).
-// Bound by memory: 8192 x 4096 in bf16 with a residual 47 us, 5.7 TB/s; 4096 x 4096 on 8 bits
+// Bound by memory: 8192 x 4096 in bf16 with a residual 47 to 49 us, 5.6 TB/s; 4096 x 4096 on 8 bits
 // 23.5 us, 5.0 TB/s.  A row of 4096 by four wavefronts: one row's loads are all in flight at once and
 // eight rows share a unit; up to 1024 columns a wavefront has a row to itself and needs no barrier.
 template <int DT, bool GAIN32, bool I8, int NW, int R>
