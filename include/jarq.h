@@ -604,13 +604,14 @@ jarq_status jarq_linear_logprobs(int32_t dtype, int64_t tokens, int32_t d, int32
  * without a target) and h = d_lse[t] (d_lse nullable: 0),
  *     dl = g 1{v = target} + (h - g) exp(l - lse),  dX = dl W,  dW = dl^T X,
  * dX [tokens][d] and dW [vocab][d] of dtype, each nullable (not formed) and overwritten.  dl is
- * formed in pieces of the vocabulary and rounded to dtype before its products (in float16
- * scaled by one power of two for all tokens that puts the largest finite |g|, |h| and |h - g| in
- * 2^14..2^15: entries below 2^-39 of it become 0); what that leaves at a
- * token's target is added to dX and dW.  A token of g = h = 0 has dX = 0 whatever its logits and
- * target (W being finite); to dW it adds products with 0, so an infinity or a NaN in its X makes dW
- * NaN.  With a gradient, a target that is not below vocab makes its token's dX and all of dW NaN.
- * logprob, lse and lse_rest as the forward pass left them.  The workspace (256-byte aligned,
+ * formed in pieces of the vocabulary and rounded to dtype before its products (in float16 scaled
+ * by one power of two for all tokens that puts the largest finite |g|, |h| and |h - g| in
+ * 2^14..2^15: entries below 2^-39 of it become 0); what that leaves at a token's target is added
+ * to dX and dW.  A token of g = h = 0 has dX = 0 whatever its logits and target (W being finite);
+ * to dW it adds products with 0, so an infinity or a NaN in its X makes dW NaN.  With a gradient,
+ * a target that is not below vocab makes its token's dX and all of dW NaN. logprob, lse and
+ * lse_rest as the forward pass left them (of as many tokens: the sums of a logit depend on it,
+ * which shows in probabilities from logits of about 10^5 on).  The workspace (256-byte aligned,
  * jarq_linear_logprobs_backward_workspace_bytes bytes, 0 if the sizes are invalid: up to 2^17
  * tokens 272 MiB at most, and 4 bytes a value of dX times the shares that its sums are cut into,
  * 32 at most) is used only during the call.

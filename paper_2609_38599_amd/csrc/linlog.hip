@@ -557,28 +557,40 @@ __global__ __launch_bounds__(64 * WI * WJ) JARQ_WAVES(2) void linlog_dw_kernel(
   const int end = T > 64 || __any(ahead - v0 - c0 >= 0 && ahead - v0 - c0 < min(TJ, n - c0)) ? T : 0;
   for (int t0 = 0; t0 < end; t0 += kListed) {
     if (t0 > 0) __syncthreads();   // (the last list is read)
-    int at[IT], mine = 0;
+    int at[IT], mine;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
       const int t = t0 + 64 * (wave * IT + i) + lane;
       const int64_t v = k.targets[min(t, T - 1)] - v0 - c0;   // (no branch: all loads at once)
       at[i] = t < T && v >= 0 && v < min(TJ, n - c0) ? (int)v : -1;
     }
+    int begin[NW], listed;
+    for (bool all = true;; all = false) {
+      mine = 0;
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {   // each wave's from a place of its own on
-      const uint64_t found = __ballot(at[i] >= 0);
-      if (at[i] >= 0)
-        list[64 * IT * wave + mine + __popcll(found & (((uint64_t)1 << lane) - 1))] =
-            (uint32_t)(64 * (wave * IT + i) + lane) << 8 | (uint32_t)at[i];
-      mine += __popcll(found);
-    }
-    if (lane == 0) counts[wave] = mine;
-    __syncthreads();
-    int begin[NW], listed = 0;
+      for (int i = 0; i < IT; ++i) {   // each wave's from a place of its own on
+        const uint64_t found = __ballot(at[i] >= 0);
+        if (at[i] >= 0)
+          list[64 * IT * wave + mine + __popcll(found & (((uint64_t)1 << lane) - 1))] =
+              (uint32_t)(64 * (wave * IT + i) + lane) << 8 | (uint32_t)at[i];
+        mine += __popcll(found);
+      }
+      if (lane == 0) counts[wave] = mine;
+      __syncthreads();
+      listed = 0;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      begin[w] = listed;
-      listed += counts[w];
+      for (int w = 0; w < NW; ++w) {
+        begin[w] = listed;
+        listed += counts[w];
+      }
+      if (!all || listed <= 64) break;   // uniform
+      // many: masked tokens may share a target, and those without a gradient have no rest
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const int t = min(t0 + 64 * (wave * IT + i) + lane, T - 1);
+        if (k.dlp[t] == 0.f && (!k.dlse || k.dlse[t] == 0.f)) at[i] = -1;
+      }
+      __syncthreads();   // (the counts are read)
     }
     auto entry = [&](int e) __attribute__((always_inline)) {
       int place = e;

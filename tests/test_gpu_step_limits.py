@@ -77,6 +77,21 @@ def test_linear_logprob_gradients_of_targets_in_one_tile_are_rounded_once(T, dt)
     _check_rounded_once(x, w, targets, g, h * 0.1, (T, dt, "one target"))
 
 
+@pytest.mark.parametrize("dt", [BF16, F16])
+@pytest.mark.parametrize("T", [300, 5000])
+def test_masked_tokens_that_share_a_target_are_as_without_one(T, dt):
+    # padding by gradients of 0 instead of targets below 0
+    x, w, targets, g, h = _linlog_inputs(T, 200, 3000, dt, seed=72)
+    pad = torch.arange(T, device="cuda") % 2 == 0
+    g[pad], h[pad] = 0, 0
+    targets = targets.clamp_min(0)
+    shared, none = targets.clone(), targets.clone()
+    shared[pad], none[pad] = 1777, -1
+    _check_rounded_once(x, w, shared, g, h * 0.1, (T, dt, "padding"))
+    got, want = (jb.linear_logprobs_backward(x, w, t, jb.linear_logprobs(x, w, t), g, d_lse=h) for t in (shared, none))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 # ---- log probabilities: logits far from 0 ----
 
 def _far(dt, T, logits):
