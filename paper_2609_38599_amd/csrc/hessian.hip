@@ -338,8 +338,8 @@ __global__ __launch_bounds__(256, WHOLE ? 2 : 4) void syrk_bf16_kernel(
 // 4096 tokens x 2048 channels, 120 of them: 46 us, whole 79, cut but with the
 // stages of the whole ones 75; x 2816, 231 of them: 64, 81 and 81); beyond, the last
 // round of 128-wide ones (512 at a time, two on a CU) is cut where it would leave
-// more than half of the chip idle (x 6144, 104 left over: 320, whole 326; x 3072,
-// 276 of them: 91, all cut 115).
+// more than half of the chip idle (x 6144, 104 left over: 320, whole 326; 276
+// of them alone: 91, all cut 115).
 hipError_t launch_hessian_update_bf16(hipStream_t st, const void* X, int m, int d, double alpha,
                                       double* Hacc) {
   Split s = split_of(d, true);
@@ -584,7 +584,7 @@ static hipError_t launch_syrk_f32(hipStream_t st, const float* Xq, const float* 
   // quarters: a round of whole tiles takes 2.2 times, one of halves 1.7 times as
   // long as one of quarters (4096 tokens: 221, 168 and 98 us; cross term 262, 202 and
   // 127).  66 whole tiles (1536 channels) 220, 168 and 197 us, 120 of them (2048) 221 in
-  // one round, 293 in three of quarters, 20 left over (3072) 446 whole and 328.
+  // one round, 293 in three of quarters, 20 left over 446 whole and 328.
   Split s = split_of(d, !CROSS);
   const int last = s.big % 256;
   auto rounds = [&](int parts) { return (parts * last + s.small + 255) / 256; };
